@@ -20,7 +20,7 @@ import torch
 own = False
 
 PAGE = 16
-WORKSPACE_BYTES = 16 << 20     # what the operators' header asks for, whatever the sizes
+WORKSPACE_BYTES = 32 << 20     # what the operators' header asks for, whatever the sizes
 TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 
 
