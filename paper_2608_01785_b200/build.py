@@ -8,11 +8,14 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libhorizonserve.so")
-SOURCES = ["api.cu", "gemm.cu", "gemm_skinny.cu", "small_step.cu", "metadata.cu", "attention.cu", "attention_prefill.cu", "norm.cu", "noalloc.cu", "diag.cu", "head.cu", "plan.cc", "control.cc"]
-HEADERS = ["hs_internal.h", "kernels.h", "ptx.cuh", "attention_decode.cuh", "weight_stream.cuh", os.path.join("..", "..", "include", "horizonserve.h"),
+SOURCES = ["api.cu", "gemm.cu", "gemm_skinny.cu", "small_step.cu", "metadata.cu", "attention.cu", "attention_prefill.cu", "norm.cu", "noalloc.cu", "diag.cu", "head.cu", "step_tables.cu", "rope_cache.cu", "paged_decode.cu",
+           "paged_chunk.cu", "token_logprobs.cu", "device_api.cu", "plan.cc", "control.cc"]
+HEADERS = ["hs_internal.h", "kernels.h", "ptx.cuh", "attention_decode.cuh", "weight_stream.cuh", "device_ops.h", "paged_scores.cuh",
+           os.path.join("..", "..", "include", "horizonserve.h"),
            os.path.join("..", "..", "include", "horizonserve_ops.h"),
            os.path.join("..", "..", "include", "horizonserve_control.h"),
-           os.path.join("..", "..", "include", "horizonserve_head.h")]
+           os.path.join("..", "..", "include", "horizonserve_head.h"),
+           os.path.join("..", "..", "include", "horizonserve_device.h")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
 

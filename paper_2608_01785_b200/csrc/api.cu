@@ -224,6 +224,8 @@ hs_status_t ensure_attributes(int device) {
 }
 
 }  // namespace
+
+hs_status_t report_cuda_error(const char* where, int cuda_error) { return cuda_fail(where, static_cast<cudaError_t>(cuda_error)); }
 }  // namespace hs
 
 using namespace hs;

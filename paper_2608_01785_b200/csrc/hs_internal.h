@@ -91,4 +91,7 @@ hs_status_t plan_step(const hs_stage_config_t& c, const MetaLayout& ml, const hs
 
 hs_status_t validate_config(const hs_stage_config_t& c);
 
+// Records the CUDA error behind the calling thread's next hs_last_error; returns HS_ERR_CUDA (api.cu).
+hs_status_t report_cuda_error(const char* where, int cuda_error);
+
 }  // namespace hs
