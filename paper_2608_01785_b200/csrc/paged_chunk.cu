@@ -96,6 +96,9 @@ __host__ __device__ constexpr uint32_t idesc_16(int M, int N) {
   return F16 ? bf16 & ~((1u << 7) | (1u << 10)) : bf16;
 }
 
+// The n lowest bits (all for n >= 32, none for n <= 0).
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 __device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* item_begin, int idx) {
   ItemView v{};
   const hs_paged_attention_t& a = p.a;
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
     const int r = threadIdx.x & 127;              // row of the tile = TMEM lane
     const uint32_t lane_base = uint32_t((warp & 3) * 32) << 16;
     const uint32_t s_col = G_::S0 + t * 128, o_col = G_::O0 + t * DH;
-    const float in = p.score.in, out = p.score.out;
+    const ScoreScale& sc = p.score;
     uint32_t g = 0;                               // blocks this tile has processed, over all items
     for (;;) {
       bool ok = mbar_wait(&bar->ring_full[rs], rph, abort_flag, a.status);
@@ -417,51 +420,92 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         tmem_ld32(tmem + lane_base + s_col + buf * PC_KEYS, sreg);
         tmem_ld32(tmem + lane_base + s_col + buf * PC_KEYS + 32, sreg2);
         tmem_ld_wait();
+        // whether this row does not see every key of the block
+        const bool masked = key0 + PC_KEYS - 1 > hi || (key0 < lo && key0 + PC_KEYS > v.prefix);
+        uint32_t seen1 = 0xffffffffu, seen2 = 0xffffffffu;       // bit e: key key0 + e, key0 + 32 + e
+        if (masked) {
+          seen1 = first_bits(hi + 1 - key0) & (~first_bits(lo - key0) | first_bits(v.prefix - key0));
+          seen2 = first_bits(hi - 31 - key0) & (~first_bits(lo - 32 - key0) | first_bits(v.prefix - 32 - key0));
+        }
+        auto mask = [&](uint32_t to) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            if (!(seen1 & (1u << e))) sreg[e] = to;
+            if (!(seen2 & (1u << e))) sreg2[e] = to;
+          }
+        };
+        auto largest = [&](float sign) {              // of sign * score; four chains
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            mx[(e >> 1) & 1] = fmaxf(mx[(e >> 1) & 1], fmaxf(sign * __uint_as_float(sreg[e]), sign * __uint_as_float(sreg[e + 1])));
+            mx[2 + ((e >> 1) & 1)] = fmaxf(mx[2 + ((e >> 1) & 1)], fmaxf(sign * __uint_as_float(sreg2[e]), sign * __uint_as_float(sreg2[e + 1])));
+          }
+          return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        };
+        // Of a capped block that the whole warp sees, the polynomial of the largest score is the largest polynomial, and the reference is part of its
+        // last multiply-add: nothing is written back in between.  A mask or a bias has to be applied in between.
+        float mx;
+        int direct = 0;                               // 3, 5: such a block, by the polynomial's degree; 0: the registers hold finished scores
         if (MOD) {
-          float biggest = 0.f;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            sreg[e] = __float_as_uint(__uint_as_float(sreg[e]) * in);
-            sreg2[e] = __float_as_uint(__uint_as_float(sreg2[e]) * in);
-            biggest = fmaxf(biggest, fmaxf(fabsf(__uint_as_float(sreg[e])), fabsf(__uint_as_float(sreg2[e]))));
+          int degree = 0;
+          float top = 0.f;
+          if (sc.out != 0.f) {
+            if (masked) mask(0u);                     // (what is not seen must not decide which polynomial the others take)
+            top = largest(1.f);
+            const float low = largest(-1.f), u = row_valid ? fmaxf(top * top, low * low) : 0.f;         // (rows of padding hold anything)
+            if (__all_sync(0xffffffffu, u <= sc.limit5)) degree = __all_sync(0xffffffffu, u <= sc.limit3) ? 3 : 5;
           }
-          if (out != 0.f) {
-            if (__all_sync(0xffffffffu, biggest <= kTanhPoly)) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                sreg[e] = __float_as_uint(out * tanh_small(__uint_as_float(sreg[e])));
-                sreg2[e] = __float_as_uint(out * tanh_small(__uint_as_float(sreg2[e])));
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                sreg[e] = __float_as_uint(out * tanh_any(__uint_as_float(sreg[e])));
-                sreg2[e] = __float_as_uint(out * tanh_any(__uint_as_float(sreg2[e])));
-              }
-            }
-          }
-          if (a.slopes) {
+          if (degree != 0 && a.slopes == nullptr && __all_sync(0xffffffffu, !masked)) {
+            direct = degree;
+            float unused;
+            if (degree == 3) split(odd_poly(f2(top, top), sc.c3, f2(0.f, 0.f)), mx, unused);
+            else split(odd_poly(f2(top, top), sc.c5, f2(0.f, 0.f)), mx, unused);
+          } else {
+            // (the distance of a key in front of the row needs its sign only where there is one)
             const float dist = float(pos - key0);
+            const bool ahead = pos - key0 < PC_KEYS - 1;
+            const F2 base2 = f2(-slope * dist, -slope * dist), slope2 = f2(slope, slope), in2 = f2(sc.in, sc.in);
+            auto finish = [&](auto score) {           // score(pair of raw scores, what to add)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              sreg[e] = __float_as_uint(fmaf(-slope, fabsf(dist - float(e)), __uint_as_float(sreg[e])));
-              sreg2[e] = __float_as_uint(fmaf(-slope, fabsf(dist - float(e + 32)), __uint_as_float(sreg2[e])));
+              for (int e = 0; e < 32; e += 2) {
+                float x0, x1;
+                const F2 p1 = fma2(slope2, f2(float(e), float(e + 1)), base2), p2 = fma2(slope2, f2(float(e + 32), float(e + 33)), base2);
+                split(score(f2(__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1])), p1), x0, x1);
+                sreg[e] = __float_as_uint(x0);
+                sreg[e + 1] = __float_as_uint(x1);
+                split(score(f2(__uint_as_float(sreg2[e]), __uint_as_float(sreg2[e + 1])), p2), x0, x1);
+                sreg2[e] = __float_as_uint(x0);
+                sreg2[e + 1] = __float_as_uint(x1);
+              }
+            };
+            if (degree == 3) finish([&](F2 s, F2 plus) { return odd_poly(s, sc.c3, plus); });
+            else if (degree == 5) finish([&](F2 s, F2 plus) { return odd_poly(s, sc.c5, plus); });
+            else if (sc.out == 0.f) finish([&](F2 s, F2 plus) { return fma2(s, in2, plus); });
+            else {
+              finish([&](F2 s, F2 plus) {
+                float s0, s1;
+                split(s, s0, s1);
+                return fma2(f2(tanh_any(s0 * sc.in), tanh_any(s1 * sc.in)), f2(sc.out, sc.out), plus);
+              });
             }
-          }
-        }
-        if (key0 + PC_KEYS - 1 > hi || (key0 < lo && key0 + PC_KEYS > v.prefix)) {       // this row does not see every key of the block
+            if (ahead && slope != 0.f) {              // keys behind the row's position (a prefix): their distance counts the other way
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const int k1 = key0 + e, k2 = key0 + 32 + e;
-            if (k1 > hi || (k1 < lo && k1 >= v.prefix)) sreg[e] = 0xff800000u;          // -inf
-            if (k2 > hi || (k2 < lo && k2 >= v.prefix)) sreg2[e] = 0xff800000u;
+              for (int e = 0; e < 32; ++e) {
+                const float f1 = fmaxf(float(e) - dist, 0.f), f3 = fmaxf(float(e + 32) - dist, 0.f);
+                sreg[e] = __float_as_uint(fmaf(-2.f * slope, f1, __uint_as_float(sreg[e])));
+                sreg2[e] = __float_as_uint(fmaf(-2.f * slope, f3, __uint_as_float(sreg2[e])));
+              }
+            }
+            if (masked) mask(0xff800000u);          // -infinity
+            mx = largest(1.f);
           }
+        } else {
+          if (masked) mask(0xff800000u);          // -infinity
+          mx = largest(1.f);
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, fmaxf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e])));
         // the reference maximum moves only when the block's maximum is far above it
-        const float unit = MOD ? 1.f : in;
+        const float unit = MOD ? 1.f : sc.in;
         float alpha = 1.f;
         const bool move = row_valid && mx > -INFINITY && (m_ref == -INFINITY || (mx - m_ref) * unit > kRefSlack);
         if (move) {
@@ -470,17 +514,32 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         }
         const bool rescale = j > 0 && __any_sync(0xffffffffu, move);
         const float neg_ms = m_ref == -INFINITY ? 0.f : -m_ref * unit;
-        float sum = 0.f;
+        const F2 neg2 = f2(neg_ms, neg_ms), unit2 = f2(unit, unit);
+        F2 sums[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
         uint32_t pk[32];
+        auto weights = [&](auto score) {              // score(pair of raw or finished scores) = log2 of their weights
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float x[4] = {__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1]), __uint_as_float(sreg2[e]), __uint_as_float(sreg2[e + 1])};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = fast_exp2(MOD ? x[i] + neg_ms : fmaf(x[i], unit, neg_ms));
-          sum += (x[0] + x[1]) + (x[2] + x[3]);
-          pk[e >> 1] = pack_16<F16>(x[0], x[1]);
-          pk[16 + (e >> 1)] = pack_16<F16>(x[2], x[3]);
-        }
+          for (int e = 0; e < 32; e += 2) {
+            float x0, x1, y0, y1;
+            split(score(f2(__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1]))), x0, x1);
+            split(score(f2(__uint_as_float(sreg2[e]), __uint_as_float(sreg2[e + 1]))), y0, y1);
+            x0 = fast_exp2(x0);
+            x1 = fast_exp2(x1);
+            y0 = fast_exp2(y0);
+            y1 = fast_exp2(y1);
+            sums[0] = add2(sums[0], f2(x0, x1));
+            sums[1] = add2(sums[1], f2(y0, y1));
+            pk[e >> 1] = pack_16<F16>(x0, x1);
+            pk[16 + (e >> 1)] = pack_16<F16>(y0, y1);
+          }
+        };
+        if (!MOD) weights([&](F2 s) { return fma2(s, unit2, neg2); });
+        else if (direct == 3) weights([&](F2 s) { return odd_poly(s, sc.c3, neg2); });
+        else if (direct == 5) weights([&](F2 s) { return odd_poly(s, sc.c5, neg2); });
+        else weights([&](F2 s) { return add2(s, neg2); });
+        float sum_a, sum_b;
+        split(add2(sums[0], sums[1]), sum_a, sum_b);
+        const float sum = sum_a + sum_b;
         l_run = l_run * alpha + sum;
         if (rescale) {
           // O must be at rest: the P V product of the previous block has completed (its successor cannot be issued
@@ -526,7 +585,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       const int64_t row = v.row0 + t * Mt + tok;
       uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
       if (row_valid && a.lse)
-        a.lse[row * a.n_q_heads + v.head0 + hg] = l_run == 0.f ? -INFINITY : kLn2 * (m_ref * (MOD ? 1.f : in) + log2f(l_run));
+        a.lse[row * a.n_q_heads + v.head0 + hg] = l_run == 0.f ? -INFINITY : kLn2 * (m_ref * (MOD ? 1.f : sc.in) + log2f(l_run));
 #pragma unroll
       for (int c = 0; c < DH / 32; ++c) {
         tmem_ld32(tmem + lane_base + o_col + c * 32, sreg);

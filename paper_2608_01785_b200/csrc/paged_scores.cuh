@@ -7,35 +7,82 @@ namespace hs {
 namespace {
 
 // Scores become x in log2 units: x = log2(e) (cap tanh(scale s / cap) - slope |p - j|), or without a cap log2(e) (scale s - ...).
+// tanh(y) is y P(y^2) while |y| <= 0.7, with P of degree five fitted to tanh(y) / y for the least largest error of y P (4e-9), or of degree three
+// while |y| <= 0.35 (6e-9): multiply-adds only, as the unit that takes exponentials has the softmax's to do.  Scores that a cap is
+// meant for lie there.  Beyond, 1 - 2 / (1 + e^2y).  The polynomials stand ready in powers of the raw score, its scale and the cap folded in.
+constexpr float kTanhPoly = 0.7f;
 struct ScoreScale {
-  float in;        // cap > 0: scale / cap; else scale * log2(e)
-  float out;       // cap > 0: cap * log2(e); else 0: not capped
+  float in;                // cap > 0: scale / cap; else scale * log2(e)
+  float out;               // cap > 0: cap * log2(e); else 0: not capped
+  float limit3, limit5;    // largest s^2 of either polynomial; below 0: neither is to be used
+  float c3[4], c5[6];      // x = s (c[0] + c[1] s^2 + ..)
 };
 inline ScoreScale score_scale(float scale, float cap) {
   const double l2e = 1.4426950408889634074;
-  ScoreScale r;
+  const double p3[4] = {0.9999998477158822, -0.3333165701286625, 0.13283323562153154, -0.048376919236770864};
+  const double p5[6] = {0.9999999197418465, -0.3333286097994273, 0.13325353247878916, -0.05338380790998526, 0.019735207866603637, -0.00487424220323607};
+  ScoreScale r{};
   r.in = cap > 0.f ? float(double(scale) / cap) : float(scale * l2e);
   r.out = cap > 0.f ? float(cap * l2e) : 0.f;
+  r.limit3 = r.limit5 = -1.f;
+  const double in = double(scale) / cap, out = double(cap) * l2e;
+  if (cap > 0.f && cap < 1e6f && in > 1e-3 / 64 && in < 1e2) {       // (the powers stay far inside fp32)
+    r.limit3 = float(0.35 * 0.35 / (in * in));
+    r.limit5 = float(0.7 * 0.7 / (in * in));
+    double f = out * in;
+    for (int i = 0; i < 6; ++i, f *= in * in) {
+      if (i < 4) r.c3[i] = float(f * p3[i]);
+      r.c5[i] = float(f * p5[i]);
+    }
+  }
   return r;
 }
 
-// tanh to about 1e-7 absolute.  Up to 0.7 in magnitude, where scores that a cap is meant for lie, y P(y^2) with P of degree five fitted to
-// tanh(y) / y for the least largest error of y P (4e-9): multiply-adds only, as the unit that takes exponentials has the
-// softmax's to do.  Beyond, 1 - 2 / (1 + e^2y).
-constexpr float kTanhPoly = 0.7f;
-__device__ __forceinline__ float tanh_small(float y) {
-  const float u = y * y;
-  float p = -0.004874242004007101f;
-  p = fmaf(p, u, 0.01973520778119564f);
-  p = fmaf(p, u, -0.053383808583021164f);
-  p = fmaf(p, u, 0.1332535296678543f);
-  p = fmaf(p, u, -0.33332860469818115f);
-  p = fmaf(p, u, 0.9999999403953552f);
-  return p * y;
-}
 __device__ __forceinline__ float tanh_any(float y) {
   const float e = fast_exp2(y * 2.8853900817779268f);          // e^2y; infinity gives 1, 0 gives -1
-  return fabsf(y) <= kTanhPoly ? tanh_small(y) : 1.f - __fdividef(2.f, 1.f + e);
+  const float u = y * y;
+  float p = -0.00487424220323607f;
+  p = fmaf(p, u, 0.019735207866603637f);
+  p = fmaf(p, u, -0.05338380790998526f);
+  p = fmaf(p, u, 0.13325353247878916f);
+  p = fmaf(p, u, -0.3333286097994273f);
+  p = fmaf(p, u, 0.9999999197418465f);
+  return fabsf(y) <= kTanhPoly ? p * y : 1.f - __fdividef(2.f, 1.f + e);
+}
+
+// Two fp32 at a time.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+// s (c[0] + c[1] s^2 + ..) + plus
+template <int N>
+__device__ __forceinline__ F2 odd_poly(F2 s, const float (&c)[N], F2 plus) {
+  const F2 u = mul2(s, s);
+  F2 p = f2(c[N - 1], c[N - 1]);
+#pragma unroll
+  for (int i = N - 2; i >= 0; --i) p = fma2(p, u, f2(c[i], c[i]));
+  return fma2(p, s, plus);
 }
 
 // 16-bit operands of the products: bf16 or fp16.
