@@ -438,10 +438,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            mx[(e >> 1) & 1] = fmaxf(mx[(e >> 1) & 1], fmaxf(sign * __uint_as_float(sreg[e]), sign * __uint_as_float(sreg[e + 1])));
-            mx[2 + ((e >> 1) & 1)] = fmaxf(mx[2 + ((e >> 1) & 1)], fmaxf(sign * __uint_as_float(sreg2[e]), sign * __uint_as_float(sreg2[e + 1])));
+            mx[(e >> 1) & 1] = max_nan(mx[(e >> 1) & 1], max_nan(sign * __uint_as_float(sreg[e]), sign * __uint_as_float(sreg[e + 1])));
+            mx[2 + ((e >> 1) & 1)] = max_nan(mx[2 + ((e >> 1) & 1)], max_nan(sign * __uint_as_float(sreg2[e]), sign * __uint_as_float(sreg2[e + 1])));
           }
-          return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          return max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3]));
         };
         // Of a capped block that the whole warp sees, the polynomial of the largest score is the largest polynomial, and the reference is part of its
         // last multiply-add: nothing is written back in between.  A mask or a bias has to be applied in between.

@@ -50,6 +50,12 @@ __device__ __forceinline__ float tanh_any(float y) {
   return fabsf(y) <= kTanhPoly ? p * y : 1.f - __fdividef(2.f, 1.f + e);
 }
 
+// The larger one, or NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // Two fp32 at a time.
 struct F2 {
   uint64_t v;

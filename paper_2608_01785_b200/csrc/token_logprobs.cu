@@ -1,72 +1,145 @@
 // Log probabilities of given tokens, entropy, rank and top alternatives of logit rows, in one pass over the logits.
 //
-// With k = scale * log2(e), M = max x and d_v = k x_v - k M (log2 units, at most 0):
+// With k = scale * log2(e), any reference M near max x and d_v = k (x_v - M) (log2 units):
 //     s = sum 2^d_v,   t = sum 2^d_v d_v,   logprob_v = ln2 (d_v - log2 s),   entropy = ln2 (log2 s - t / s).
-// Every thread keeps (M, s, t) of its own elements and rescales when its maximum moves; they are joined once per row.
+// Every thread keeps (M, s, t) of its own elements and rescales when an element lies 2^10 above its reference; they are joined once per row.
 //
-// Alternatives.  Each lane index keeps the largest value that any of the block's sixteen warps has seen in that lane; the n_top-th
-// largest of these 32 values is a value that n_top elements reach at least, so an element below it cannot be an alternative.  Only what reaches it is
-// written to a list (about 32 ln(32 / (32 - n_top)) elements of the row reach the final bound, 31 at n_top = 20) and the list is
-// sorted by counting at the row's end.  A list that overflows (rows of many equal values) is made again by n_top passes over the row.
+// Alternatives.  An element's key orders by value, then by the lower index.  Every thread keeps (a lower bound of) its largest key; the largest
+// of them over the sixteen warps, lane by lane, are 32 keys of distinct elements, and the n_top-th largest of those is a bound that no
+// alternative lies below.  What reaches the bound is written to a list: about 32 ln(32 / (32 - n_top)) elements of the row reach the final
+// one (31 at n_top = 20), and its logarithm of them come while it rises.  The list becomes the alternatives by running top 32 of a warp,
+// 32 keys at a time, sorted and merged in the lanes.  A list that overflows is made again from the row itself.
 //
 // Work.  The rows' elements, in units of 1024, are cut into one share per SM of the device, equal and contiguous, whatever the number
 // of rows: a share is the end of a row, whole rows and the beginning of one.  The block that delivers a divided row's last
 // part joins the parts in order.  A share streams through a ring of tiles in shared memory by bulk copies of 16-byte pieces; the
 // few elements of a row outside 16-byte boundaries are fetched one by one.
+//
+// Roles.  Beside the readers one warp requests tiles, one keeps the bound and one ends the rows: a reader that has its part of a row leaves it in shared
+// memory, where rows take turns with two places, and goes on with the next row.  The readers wait for one another once in a row, behind its first
+// tile, for the first bound.
 #include <algorithm>
 
-#include "device_ops.h"
-#include "ptx.cuh"
+#include "paged_scores.cuh"
 
 namespace hs {
 namespace {
 
-constexpr int LP_WARPS = 16, LP_READERS = LP_WARPS * 32, LP_THREADS = LP_READERS + 32;     // and a warp that requests the tiles
-constexpr int LP_UNIT = 1024, LP_TILE = 8 * LP_UNIT, LP_MINE = LP_TILE / LP_READERS;       // elements
-constexpr int LP_LIST = kMaxShares * HS_MAX_ALTERNATIVES;                                  // room for a join of all shares' alternatives
-constexpr int LP_RING_BYTES = 160 * 1024;
+constexpr int LP_WARPS = 16, LP_READERS = LP_WARPS * 32, LP_THREADS = LP_READERS + 96;     // and warps that request tiles, keep the bound, end the rows
+constexpr int LP_UNIT = 1024;                                                              // elements
+constexpr int LP_PIECES = 8, LP_SLOTS = 3;                                                 // 16-byte pieces of a tile per thread; tiles of the ring
+constexpr int LP_TILE_BYTES = LP_READERS * LP_PIECES * 16;
+constexpr int LP_LIST = 1472;                                                              // candidates of a row
 constexpr int LP_MIN_UNITS = 2;                                                            // of a share
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 10.f;                                                             // log2 units that a logit may lie above its thread's reference
 
+// 16-byte pieces of logits as 32-bit words.  kFloor: what stands for -infinity where its weight is to be 0 and its distance finite; right
+// for rows whose maximum is above kLow.
 template <int TYPE>
-struct Logit;                                            // one 16-byte piece
+struct Logit;
 template <>
 struct Logit<HS_TYPE_F32> {
   static constexpr int kSize = 4;
-  static __device__ __forceinline__ float one(const void* p, int64_t at) { return static_cast<const float*>(p)[at]; }
-  static __device__ __forceinline__ void get(const uint4& v, float* x) {
-    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-  }
   static constexpr uint32_t kEmpty = 0xff800000u;        // -infinity
+  static constexpr float kFloor = -1e36f, kLow = -1e35f;
+  static __device__ __forceinline__ void get_above_floor(const uint32_t* w, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = max_nan(__uint_as_float(w[i]), kFloor);
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t at) { return static_cast<const float*>(p)[at]; }
+  static __device__ __forceinline__ void get(const uint32_t* w, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+  }
+  static __device__ __forceinline__ float largest(const uint32_t* w) {
+    return max_nan(max_nan(__uint_as_float(w[0]), __uint_as_float(w[1])), max_nan(__uint_as_float(w[2]), __uint_as_float(w[3])));
+  }
+  static __device__ __forceinline__ float largest_of_all(const uint32_t (&w)[LP_PIECES * 4]) {
+    float m[4] = {__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+#pragma unroll
+    for (int i = 4; i < LP_PIECES * 4; ++i) m[i & 3] = max_nan(m[i & 3], __uint_as_float(w[i]));
+    return max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3]));
+  }
+  static __device__ __forceinline__ int above(const uint32_t (&w)[LP_PIECES * 4], float x) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < LP_PIECES * 4; ++i) n += __uint_as_float(w[i]) > x ? 1 : 0;
+    return n;
+  }
+};
+template <typename T2>
+struct Logit16 {
+  static constexpr int kSize = 2;
+  static __device__ __forceinline__ T2 two(uint32_t w) { return *reinterpret_cast<const T2*>(&w); }
+  static __device__ __forceinline__ float largest(const uint32_t* w) {
+    const T2 m = __hmax2_nan(__hmax2_nan(two(w[0]), two(w[1])), __hmax2_nan(two(w[2]), two(w[3])));
+    return max_nan(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ float largest_of_all(const uint32_t (&w)[LP_PIECES * 4]) {
+    T2 m[4] = {two(w[0]), two(w[1]), two(w[2]), two(w[3])};
+#pragma unroll
+    for (int i = 4; i < LP_PIECES * 4; ++i) m[i & 3] = __hmax2_nan(m[i & 3], two(w[i]));
+    const T2 r = __hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3]));
+    return max_nan(__low2float(r), __high2float(r));
+  }
+  // (whole numbers up to LP_PIECES * 4 per half: exact)
+  static __device__ __forceinline__ int count(const uint32_t (&w)[LP_PIECES * 4], T2 t) {
+    T2 n[2] = {__hgt2(two(w[0]), t), __hgt2(two(w[1]), t)};
+#pragma unroll
+    for (int i = 2; i < LP_PIECES * 4; ++i) n[i & 1] = __hadd2(n[i & 1], __hgt2(two(w[i]), t));
+    const T2 m = __hadd2(n[0], n[1]);
+    return int(__low2float(m) + __high2float(m));
+  }
 };
 template <>
-struct Logit<HS_TYPE_BF16> {
-  static constexpr int kSize = 2;
+struct Logit<HS_TYPE_BF16> : Logit16<__nv_bfloat162> {
+  static constexpr uint32_t kEmpty = 0xff80ff80u;
+  static constexpr float kFloor = -1e36f, kLow = -1e35f;
+  static __device__ __forceinline__ __nv_bfloat162 floor2() { return __float2bfloat162_rn(kFloor); }
   static __device__ __forceinline__ float one(const void* p, int64_t at) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]); }
-  static __device__ __forceinline__ void get(const uint4& v, float* x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  static __device__ __forceinline__ void get(const uint32_t* w, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[2 * i] = __uint_as_float(w[i] << 16);
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
-  static constexpr uint32_t kEmpty = 0xff80ff80u;
-};
-template <>
-struct Logit<HS_TYPE_F16> {
-  static constexpr int kSize = 2;
-  static __device__ __forceinline__ float one(const void* p, int64_t at) { return __half2float(static_cast<const __half*>(p)[at]); }
-  static __device__ __forceinline__ void get(const uint4& v, float* x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  static __device__ __forceinline__ void get_above_floor(const uint32_t* w, float (&x)[8]) {
+    uint32_t q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      const auto m = __hmax2_nan(two(w[i]), floor2());
+      q[i] = *reinterpret_cast<const uint32_t*>(&m);
+    }
+    get(q, x);
+  }
+  static __device__ __forceinline__ int above(const uint32_t (&w)[LP_PIECES * 4], float x) { return count(w, __float2bfloat162_rn(x)); }
+};
+template <>
+struct Logit<HS_TYPE_F16> : Logit16<__half2> {
+  static constexpr uint32_t kEmpty = 0xfc00fc00u;
+  static constexpr float kFloor = -65504.f, kLow = -60000.f;
+  static __device__ __forceinline__ __half2 floor2() { return __float2half2_rn(kFloor); }
+  static __device__ __forceinline__ float one(const void* p, int64_t at) { return __half2float(static_cast<const __half*>(p)[at]); }
+  static __device__ __forceinline__ void get(const uint32_t* w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(two(w[i]));
       x[2 * i] = f.x;
       x[2 * i + 1] = f.y;
     }
   }
-  static constexpr uint32_t kEmpty = 0xfc00fc00u;
+  static __device__ __forceinline__ void get_above_floor(const uint32_t* w, float (&x)[8]) {
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto m = __hmax2_nan(two(w[i]), floor2());
+      q[i] = *reinterpret_cast<const uint32_t*>(&m);
+    }
+    get(q, x);
+  }
+  static __device__ __forceinline__ int above(const uint32_t (&w)[LP_PIECES * 4], float x) { return count(w, __float2half2_rn(x)); }
 };
 
 // Whole numbers in the order of the floats (and NaN above or below all).
@@ -79,63 +152,93 @@ __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(
 __device__ __forceinline__ unsigned long long make_key(float x, int v) {
   return (static_cast<unsigned long long>(ordered(x + 0.f)) << 32) | (0xffffffffu - unsigned(v));       // (-0 counts as 0)
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes),
                "r"(smem_u32(bar))
                : "memory");
 }
-// The n-th largest (n = 1 .. 32) of the 32 lanes' values, in every lane.
-__device__ __forceinline__ uint32_t nth_largest(uint32_t v, int n) {
+using Key = unsigned long long;
+__device__ __forceinline__ Key larger(Key a, Key b) { return a > b ? a : b; }
+__device__ __forceinline__ Key smaller(Key a, Key b) { return a > b ? b : a; }
+// Lanes 0 .. 31 in falling order: a bitonic sequence (stages 16 .. 1), or any keys.
+__device__ __forceinline__ Key merge_lanes(Key v) {
   const int lane = threadIdx.x & 31;
-  int above = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const uint32_t w = __shfl_sync(0xffffffffu, v, i);
-    above += w > v || (w == v && i < lane) ? 1 : 0;
+  for (int o = 16; o > 0; o >>= 1) {
+    const Key w = __shfl_xor_sync(0xffffffffu, v, o);
+    v = (lane & o) == 0 ? larger(v, w) : smaller(v, w);
   }
-  const unsigned at = __ballot_sync(0xffffffffu, above == n - 1);
-  return __shfl_sync(0xffffffffu, v, __ffs(at) - 1);
+  return v;
+}
+__device__ __forceinline__ Key sort_lanes(Key v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int size = 2; size < 32; size <<= 1) {
+#pragma unroll
+    for (int o = size >> 1; o > 0; o >>= 1) {
+      const Key w = __shfl_xor_sync(0xffffffffu, v, o);
+      v = ((lane & o) == 0) == ((lane & size) == 0) ? larger(v, w) : smaller(v, w);
+    }
+  }
+  return merge_lanes(v);
+}
+// The n-th largest (n = 1 .. 32) of the lanes' keys, in every lane.  The values alone are sorted; where more of them are equal to the n-th than
+// are needed, the whole keys.
+__device__ __forceinline__ Key nth_largest(Key k, int n) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t mine = uint32_t(k >> 32);
+  uint32_t v = mine;
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll
+    for (int o = size >> 1; o > 0; o >>= 1) {
+      const uint32_t w = __shfl_xor_sync(0xffffffffu, v, o);
+      v = ((lane & o) == 0) == (size == 32 || (lane & size) == 0) ? max(v, w) : min(v, w);
+    }
+  }
+  const uint32_t at = __shfl_sync(0xffffffffu, v, n - 1);
+  const int above = __popc(__ballot_sync(0xffffffffu, mine > at)), equal = __popc(__ballot_sync(0xffffffffu, mine == at));
+  if (above + equal > n) return __shfl_sync(0xffffffffu, sort_lanes(k), n - 1);
+  const uint32_t low = __reduce_min_sync(0xffffffffu, mine == at ? uint32_t(k) : 0xffffffffu);
+  return (Key(at) << 32) | low;
+}
+// The 32 largest of two sets in falling order.
+__device__ __forceinline__ Key merge_sorted(Key a, Key b) { return merge_lanes(larger(a, __shfl_sync(0xffffffffu, b, 31 - (threadIdx.x & 31)))); }
+// The same with 32 keys in any order, of which a later one than `last` in `a` does not count.
+__device__ __forceinline__ void take(Key& a, Key key, int last) {
+  const Key least = __shfl_sync(0xffffffffu, a, last);
+  if (__any_sync(0xffffffffu, key > least)) a = merge_sorted(a, sort_lanes(key));
 }
 
-// What is known of a run of elements: maximum (k x, log2 units; -infinity: none), sum, weighted sum, elements above the target.
+// What is known of a run of elements: reference M (about the maximum; -infinity: no element above it), s = sum 2^d, t = sum 2^d d with d = k (x - M), elements above the target.
 struct Sums {
   float m, s, t;
   int above;
 };
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
-  Sums r;
-  r.m = max_nan(a.m, b.m);
-  r.above = a.above + b.above;
-  if (r.m == -INFINITY) {
-    r.s = r.t = 0.f;
-    return r;
+// The sums relative to a larger maximum.
+__device__ __forceinline__ void raise(Sums& v, float m, float k) {
+  if (v.m != m && v.s != 0.f) {                          // (nothing, or weights that are all 0, have no distance)
+    const float d = max_nan(k * (v.m - m), -200.f), f = exp2f(d);        // (0 from far below: its product with the distance has to be 0)
+    v.t = f * fmaf(v.s, d, v.t);
+    v.s *= f;
   }
-  // (a part without elements has s = t = 0, and its distance, which is infinite, must not meet them)
-  const float da = a.s == 0.f ? 0.f : a.m - r.m, db = b.s == 0.f ? 0.f : b.m - r.m;
-  const float fa = exp2f(da), fb = exp2f(db);
-  r.s = fa * a.s + fb * b.s;
-  r.t = fa * fmaf(a.s, da, a.t) + fb * fmaf(b.s, db, b.t);
-  return r;
+  v.m = m;
 }
-__device__ __forceinline__ Sums warp_join(Sums v) {
+// Over the 32 lanes, the same bits in every lane.
+__device__ __forceinline__ Sums warp_join(Sums v, float k) {
+  raise(v, unordered(__reduce_max_sync(0xffffffffu, ordered(v.m))), k);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Sums w = {__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o), __shfl_xor_sync(0xffffffffu, v.t, o),
-                    __shfl_xor_sync(0xffffffffu, v.above, o)};
-    const bool low = (threadIdx.x & o) == 0;             // the lower lanes' sums come first in both partners: the same bits
-    v = low ? join(v, w) : join(w, v);
+    v.s += __shfl_xor_sync(0xffffffffu, v.s, o);
+    v.t += __shfl_xor_sync(0xffffffffu, v.t, o);
   }
+  v.above = __reduce_add_sync(0xffffffffu, v.above);
   return v;
 }
 
 struct Part {                                            // of a divided row, in the workspace
   Sums sums;
-  unsigned long long keys[HS_MAX_ALTERNATIVES];
+  Key keys[HS_MAX_ALTERNATIVES];
 };
 
 struct LogprobsParams {
@@ -144,315 +247,454 @@ struct LogprobsParams {
   float k;                                               // scale * log2(e)
 };
 
-template <int TYPE>
+// What the readers leave of a row for the warp that ends it.
+struct RowPlace {
+  Key list[LP_LIST];
+  Key best[LP_WARPS][32];                                // of each thread; 0: none
+  Key bound;
+  Sums sums[LP_WARPS];
+  float x_t;
+  int target, n_list, news;                              // news: best[] has changed since the bound was worked out
+};
 struct LpSmem {
-  static constexpr int kTileBytes = LP_TILE * Logit<TYPE>::kSize, kSlots = LP_RING_BYTES / kTileBytes;
-  uint8_t ring[kSlots][kTileBytes];
-  unsigned long long list[LP_LIST];
-  unsigned long long top[HS_MAX_ALTERNATIVES];
-  uint64_t full[kSlots], empty[kSlots];
-  Sums warp_sums[LP_WARPS];
-  uint32_t lane_max[2][32];
-  Sums row;
-  int n_list, abort_flag, flag;
+  uint8_t ring[LP_SLOTS][LP_TILE_BYTES];
+  RowPlace place[2];
+  uint64_t full[LP_SLOTS], empty[LP_SLOTS], row_full[2], row_empty[2], best_full[2], bound_full[2];
+  int abort_flag;
 };
 
 template <int TYPE>
 __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __grid_constant__ LogprobsParams p) {
   using L = Logit<TYPE>;
-  using S = LpSmem<TYPE>;
   constexpr int kPer = 16 / L::kSize;                    // elements of a 16-byte piece
+  constexpr int kTile = LP_TILE_BYTES / L::kSize;        // and of a tile
+  static_assert(kTile % LP_UNIT == 0, "a tile is whole units");
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  S& sm = *reinterpret_cast<S*>(smem_raw);
+  LpSmem& sm = *reinterpret_cast<LpSmem*>(smem_raw);
   volatile int* abort_flag = &sm.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int vocab = p.a.vocab, n_top = p.a.n_top, upr = p.units_per_row;
   if (tid == 0) {
-    for (int i = 0; i < S::kSlots; ++i) {
+    for (int i = 0; i < LP_SLOTS; ++i) {
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], LP_WARPS);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.row_full[i], LP_WARPS);
+      mbar_init(&sm.row_empty[i], 1);
+      mbar_init(&sm.best_full[i], LP_WARPS);
+      mbar_init(&sm.bound_full[i], 1);
+      sm.place[i].news = 0;
+      sm.place[i].n_list = 0;
     }
     sm.abort_flag = 0;
     fence_barrier_init();
   }
-  if (tid < 64) sm.lane_max[tid >> 5][lane] = 0;
-  if (tid == 0) sm.n_list = 0;
+  if (tid < LP_READERS) sm.place[0].best[warp][lane] = sm.place[1].best[warp][lane] = 0;
   __syncthreads();
   griddep_wait();
 
   const int64_t units = int64_t(p.a.n_rows) * upr;
-  int* done_words = reinterpret_cast<int*>(static_cast<char*>(p.a.workspace) + kWsLogprobsDone);
-  Part* parts = reinterpret_cast<Part*>(static_cast<char*>(p.a.workspace) + kWsScratch);
   // A share is a run of segments: units u0 .. u1 - 1 of a row.  Elements are counted from the 16-byte boundary at or below the row's
-  // beginning ("virtual" indices).
+  // beginning ("virtual" indices); whole pieces of the row are first .. last - 1.
   auto share_begin = [&](int b) { return units * b / p.shares; };
   auto share_of = [&](int64_t u) { return int(((u + 1) * p.shares - 1) / units); };
-  auto misaligned = [&](int row) -> int {
-    return int((reinterpret_cast<uintptr_t>(p.a.logits) / L::kSize + uint64_t(row) * uint64_t(p.a.row_stride)) % kPer);
+  struct Segment {
+    int row, u0, u1, mis, first, last;
+    const char* row_p;
   };
-  auto row_at = [&](int row) { return static_cast<const char*>(p.a.logits) + int64_t(row) * p.a.row_stride * L::kSize; };
+  auto segment_at = [&](int row, int u0, int64_t end) {               // the one that begins with unit u0 of a row, in a share that ends at `end`
+    Segment g;
+    g.row = row;
+    g.u0 = u0;
+    g.u1 = int(std::min<int64_t>(upr, end - int64_t(row) * upr));
+    g.mis = int((reinterpret_cast<uintptr_t>(p.a.logits) / L::kSize + uint64_t(g.row) * uint64_t(p.a.row_stride)) % kPer);
+    g.first = g.mis ? kPer : 0;
+    g.last = (g.mis + vocab) / kPer * kPer;
+    g.row_p = static_cast<const char*>(p.a.logits) + int64_t(g.row) * p.a.row_stride * L::kSize;
+    return g;
+  };
 
-  int slot = 0;
-  uint32_t phase = 0;
-  if (warp == LP_WARPS) {
+  // (a wait that gives up lets every role go on to its end, past the waits that follow, without what it waited for)
+  bool ok = true;
+  if (warp < LP_WARPS) {
+    // ------------------------------------------------------------------- the readers
+    int slot = 0, at = 0;
+    uint32_t phase = 0, row_phase = 0;
+    auto target_of = [&](int row) { return row < p.a.n_rows ? p.a.targets[row] : -1; };
+    auto target_logit = [&](const char* row_p, int target) { return target >= 0 && target < vocab ? L::one(row_p, target) : INFINITY; };
+    for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
+      const int64_t begin = share_begin(share), end = share_begin(share + 1);
+      if (begin >= end) continue;
+      int row = int(begin / upr), u0 = int(begin % upr), target = target_of(row);
+      float x_t = target_logit(segment_at(row, u0, end).row_p, target);
+      for (; int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+        const Segment g = segment_at(row, u0, end);
+        const bool more = int64_t(row + 1) * upr < end;  // the share goes on with the next row
+        const int next_target = more ? target_of(row + 1) : -1;
+        float next_x_t = INFINITY;                       // (asked for behind the first tile: a round trip to memory)
+        auto ask_target = [&]() { if (more) next_x_t = target_logit(g.row_p + p.a.row_stride * L::kSize, next_target); };
+        const bool count = p.a.rank != nullptr && target >= 0 && target < vocab;
+        RowPlace& place = sm.place[at];
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_empty[at], row_phase ^ 1, abort_flag, p.a.status));
+        float m = -INFINITY;                             // the thread's reference: its maximum, or up to kSlack below it
+        float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};      // its sums, even and odd elements
+        int above = 0;
+        auto push = [&](float x, int v) {
+          const int i = atomicAdd(&place.n_list, 1);
+          if (i < LP_LIST) place.list[i] = make_key(x, v);
+        };
+        // the elements outside whole pieces: in front of the first one (with unit 0), behind the last one
+        {
+          const int n_front = g.mis && g.u0 == 0 ? min(g.first - g.mis, vocab) : 0;                     // virtual mis .. first - 1
+          const int tail = max(g.last, min(g.first, g.mis + vocab)), n_back = g.mis + vocab - tail;      // virtual tail .. mis + vocab - 1
+          int v = -1;
+          if (tid < n_front) v = tid;
+          else if (tid >= 32 && tid - 32 < n_back && (tail + tid - 32) / LP_UNIT >= g.u0 && (tail + tid - 32) / LP_UNIT < g.u1) v = tail - g.mis + tid - 32;
+          if (v >= 0) {
+            const float x = L::one(g.row_p, v);
+            m = x;
+            if (x != -INFINITY) s[0] = x - x + 1.f;                    // (NaN of NaN and of infinity)
+            above = x > x_t ? 1 : 0;
+            if (n_top > 0 && x > -INFINITY) push(x, v);
+          }
+        }
+        for (int v0 = g.u0 * LP_UNIT; v0 < g.u1 * LP_UNIT; v0 += kTile) {
+          const bool first = v0 == g.u0 * LP_UNIT;
+          const int lo = max(v0, g.first), hi = min(min(v0 + kTile, g.u1 * LP_UNIT), g.last);
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status));
+          const int pieces = ok ? max(hi - lo, 0) / kPer : 0;
+          const uint8_t* tile = sm.ring[slot];
+          uint32_t w[LP_PIECES * 4];
+          auto fetch = [&](int i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(tile + (i * LP_READERS + tid) * 16);
+            w[4 * i] = x.x;
+            w[4 * i + 1] = x.y;
+            w[4 * i + 2] = x.z;
+            w[4 * i + 3] = x.w;
+          };
+          const bool full = pieces == LP_PIECES * LP_READERS;
+          if (full) {
+#pragma unroll
+            for (int i = 0; i < LP_PIECES; ++i) fetch(i);
+          } else {
+#pragma unroll
+            for (int i = 0; i < LP_PIECES; ++i) {
+              w[4 * i] = w[4 * i + 1] = w[4 * i + 2] = w[4 * i + 3] = L::kEmpty;
+              if (i * LP_READERS + tid < pieces) fetch(i);
+            }
+          }
+          const float mx = L::largest_of_all(w);
+          auto look_for_candidates = [&]() {
+            const Key bound = *reinterpret_cast<volatile Key*>(&place.bound);
+            const float b_x = bound ? unordered(uint32_t(bound >> 32)) : -INFINITY;
+            const int b_v = int(0xffffffffu - unsigned(bound));          // (-1 without a bound: everything above -infinity)
+            auto reaches = [&](float x, int v) { return x > b_x || (x == b_x && v <= b_v); };
+            // A thread whose largest element reaches the bound has all of its elements looked at by the warp, 32 at a time.  (By itself, in a
+            // loop, it held its warp up for 3300 cycles, longer than two tiles take.)
+            for (unsigned who = __ballot_sync(0xffffffffu, reaches(mx, lo - g.mis)); who; who &= who - 1) {
+              const int of = __ffs(who) - 1;
+#pragma unroll 1
+              for (int e0 = 0; e0 < LP_PIECES * kPer; e0 += 32) {
+                const int e = e0 + lane, i = (e / kPer * LP_READERS + warp * 32 + of) * kPer + e % kPer, v = lo - g.mis + i;
+                const float x = e < LP_PIECES * kPer && i < pieces * kPer ? L::one(tile, i) : -INFINITY;
+                const bool hit = x > -INFINITY && reaches(x, v);
+                const unsigned hits = __ballot_sync(0xffffffffu, hit);
+                if (hits == 0) continue;
+                const uint32_t top = __reduce_max_sync(0xffffffffu, hit ? ordered(x) : 0u);
+                const int at_v = int(__reduce_min_sync(0xffffffffu, hit && ordered(x) == top ? unsigned(v) : 0xffffffffu));
+                int i_list = 0;
+                if (lane == 0) {
+                  i_list = atomicAdd(&place.n_list, __popc(hits));
+                  const Key k = make_key(unordered(top), at_v);
+                  if (k > place.best[warp][of]) place.best[warp][of] = k;
+                  place.news = 1;
+                }
+                i_list = __shfl_sync(0xffffffffu, i_list, 0) + __popc(hits & ((1u << lane) - 1u));
+                if (hit && i_list < LP_LIST) place.list[i_list] = make_key(x, v);
+              }
+            }
+          };
+          auto give_back = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.empty[slot]);
+          };
+          if (first && n_top > 0) {                      // the first bound is that of all warps: what it needs goes out before the sums
+            // (the last index of the thread's first piece, or of its last one, stands for the place of its largest element)
+            const int i = L::largest(w) == mx ? 0 : LP_PIECES - 1;
+            if (pieces > 0 && mx > -INFINITY) place.best[warp][lane] = make_key(mx, lo - g.mis + (i * LP_READERS + tid) * kPer + kPer - 1);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.best_full[at]);
+          }
+          const bool early = !first && full;             // the tile goes back at once, but for the first one, whose bound is on its way, and ragged ones
+          if (early) {
+            if (n_top > 0) look_for_candidates();
+            give_back();
+          }
+          if (first) ask_target();
+          const bool higher = !(mx <= m) && !((mx - m) * p.k <= kSlack);          // (true of the first element above -infinity, and of NaN)
+          if (higher) {
+            const float to = max_nan(mx, m), d = max_nan(p.k * (m - to), -200.f), f = exp2f(d);      // (nothing so far: d = -infinity, s = t = 0)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              t[i] = f * fmaf(s[i], d, t[i]);
+              s[i] *= f;
+            }
+            m = to;
+            if (to == INFINITY) s[0] = to - to;          // (a row with infinity has no sum)
+          }
+          const float from = m == -INFINITY ? 0.f : m, c = -from * p.k;
+          const bool apart = !full || !(from > L::kLow) || p.k > 100.f;         // one piece after the other: a ragged chunk, or logits near the type's lowest (or NaN)
+          if (!apart) {
+#pragma unroll
+            for (int i = 0; i < LP_PIECES; ++i) {
+              float x[kPer];
+              L::get_above_floor(w + 4 * i, x);
+#pragma unroll
+              for (int e = 0; e < kPer; e += 2) {
+                const F2 d = fma2(f2(x[e], x[e + 1]), f2(p.k, p.k), f2(c, c));
+                float d0, d1;
+                split(d, d0, d1);
+                const F2 weight = f2(fast_exp2(d0), fast_exp2(d1));
+                split(add2(f2(s[0], s[1]), weight), s[0], s[1]);
+                split(fma2(weight, d, f2(t[0], t[1])), t[0], t[1]);
+              }
+            }
+          }
+          if (apart) {
+#pragma unroll 1
+            for (int i = 0; i < LP_PIECES && i * LP_READERS + tid < pieces; ++i) {
+              // (from memory once more where the tile has gone back)
+              const uint4 y = *reinterpret_cast<const uint4*>(early ? reinterpret_cast<const uint8_t*>(g.row_p) + int64_t(lo - g.mis + (i * LP_READERS + tid) * kPer) * L::kSize
+                                                                    : tile + (i * LP_READERS + tid) * 16);
+              const uint32_t q[4] = {y.x, y.y, y.z, y.w};
+              float x[kPer];
+              L::get(q, x);
+#pragma unroll
+              for (int e = 0; e < kPer; ++e) {
+                const float d = max_nan((x[e] - from) * p.k, -126.f), weight = fast_exp2(d);
+                s[0] += weight;
+                t[0] = fmaf(weight, d, t[0]);
+              }
+            }
+          }
+          if (count && mx > x_t) above += L::above(w, x_t);
+          if (!early) {
+            if (n_top > 0) {
+              if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status));
+              look_for_candidates();
+            }
+            give_back();
+          }
+          if (++slot == LP_SLOTS) { slot = 0; phase ^= 1; }
+        }
+        const Sums mine = warp_join(Sums{m, s[0] + s[1], t[0] + t[1], above}, p.k);
+        if (lane == 0) {
+          place.sums[warp] = mine;
+          if (warp == 0) {
+            place.target = target;
+            place.x_t = x_t;
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.row_full[at]);
+        if (++at == 2) { at = 0; row_phase ^= 1; }
+        x_t = next_x_t;
+        target = next_target;
+      }
+    }
+  } else if (warp == LP_WARPS + 2) {
     // ------------------------------------------------------------ the tiles' requests
     if (lane == 0) {
-      bool ok = true;
+      int slot = 0;
+      uint32_t phase = 0;
       for (int share = blockIdx.x; share < p.shares && ok; share += gridDim.x) {
-        const int64_t end = share_begin(share + 1);
-        for (int64_t u = share_begin(share); u < end && ok;) {
-          const int row = int(u / upr), u0 = int(u - int64_t(row) * upr), u1 = int(std::min<int64_t>(upr, u0 + (end - u)));
-          const int mis = misaligned(row);
-          // whole pieces of the row: [first, last) in virtual elements
-          const int first = mis ? kPer : 0, last = (mis + vocab) / kPer * kPer;
-          const char* base = row_at(row) - mis * L::kSize;
-          for (int v = u0 * LP_UNIT; v < u1 * LP_UNIT; v += LP_TILE) {
-            const int lo = max(v, first), hi = min(min(v + LP_TILE, u1 * LP_UNIT), last);
+        const int64_t begin = share_begin(share), end = share_begin(share + 1);
+        for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end && ok; ++row, u0 = 0) {
+          const Segment g = segment_at(row, u0, end);
+          for (int v = g.u0 * LP_UNIT; v < g.u1 * LP_UNIT; v += kTile) {
+            const int lo = max(v, g.first), hi = min(min(v + kTile, g.u1 * LP_UNIT), g.last);
             ok = mbar_wait(&sm.empty[slot], phase ^ 1, abort_flag, p.a.status);
             if (!ok) break;
             if (hi > lo) {
               mbar_expect_tx(&sm.full[slot], (hi - lo) * L::kSize);
-              bulk_load(sm.ring[slot], base + int64_t(lo) * L::kSize, (hi - lo) * L::kSize, &sm.full[slot]);
+              bulk_load(sm.ring[slot], g.row_p + int64_t(lo - g.mis) * L::kSize, (hi - lo) * L::kSize, &sm.full[slot]);
             } else {
               mbar_arrive(&sm.full[slot]);
             }
-            if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
+            if (++slot == LP_SLOTS) { slot = 0; phase ^= 1; }
           }
-          u += u1 - u0;
         }
       }
     }
     __syncwarp();
+  } else if (warp == LP_WARPS) {
+    // --------------------------------------------------------------- the bounds of rows
+    // The first one of a segment from the first tile's largest keys; then again whenever a reader has found a candidate, until the next segment's
+    // largest keys are there.  (This warp alone writes the word, and a bound that comes late finds nobody who reads it.)
+    if (n_top > 0) {
+      int at = 0;
+      uint32_t row_phase = 0;
+      for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
+        const int64_t begin = share_begin(share), end = share_begin(share + 1);
+        for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.best_full[at], row_phase, abort_flag, p.a.status));
+          RowPlace& place = sm.place[at];
+          const int next = at ^ 1;
+          const uint32_t next_phase = at ? row_phase ^ 1 : row_phase;
+          const bool more = int64_t(row + 1) * upr < end || share + int(gridDim.x) < p.shares;
+          Key known = 0;
+          for (bool first = true;; first = false) {
+            if (lane == 0) place.news = 0;
+            __syncwarp();
+            Key k = 0;
+#pragma unroll
+            for (int q = 0; q < LP_WARPS; ++q) k = larger(k, reinterpret_cast<volatile Key*>(place.best[q])[lane]);
+            const Key bound = nth_largest(k, n_top);
+            if (first || bound > known) {
+              known = bound;
+              if (lane == 0) *reinterpret_cast<volatile Key*>(&place.bound) = bound;
+            }
+            __syncwarp();
+            if (first && lane == 0) mbar_arrive(&sm.bound_full[at]);
+            bool news = false;
+            const unsigned long long t0 = globaltimer_ns();
+            while (ok && !news && !*abort_flag) {
+              if (globaltimer_ns() - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                atomicExch(p.a.status, kErrTimeout);
+              }
+              __nanosleep(64);
+              if (__any_sync(0xffffffffu, more ? mbar_try_wait(&sm.best_full[next], next_phase) : mbar_try_wait(&sm.row_full[at], row_phase))) break;
+              news = __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&place.news) != 0);
+            }
+            if (!news) break;
+          }
+          if (++at == 2) { at = 0; row_phase ^= 1; }
+        }
+      }
+    }
   } else {
-    // ------------------------------------------------------------------- the readers
-    // (a wait that gives up leaves the block's barriers as they are: every warp goes on, without the tiles, to the end)
-    bool ok = true;
-    int parity = 0;
+    // ------------------------------------------------------------------ the rows' ends
+    int at = 0;
+    uint32_t row_phase = 0;
+    int* done_words = reinterpret_cast<int*>(static_cast<char*>(p.a.workspace) + kWsLogprobsDone);
+    Part* parts = reinterpret_cast<Part*>(static_cast<char*>(p.a.workspace) + kWsScratch);
     for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
       const int64_t begin = share_begin(share), end = share_begin(share + 1);
-      for (int64_t u = begin; u < end;) {
-        const int row = int(u / upr), u0 = int(u - int64_t(row) * upr), u1 = int(std::min<int64_t>(upr, u0 + (end - u)));
-        const int mis = misaligned(row);
-        const int first = mis ? kPer : 0, last = (mis + vocab) / kPer * kPer;
-        const char* row_p = row_at(row);
-        const int target = p.a.targets[row];
-        const bool has_target = target >= 0 && target < vocab;
-        const float x_t = has_target ? L::one(row_p, target) : INFINITY;
-        Sums my = {-INFINITY, 0.f, 0.f, 0};
-        float best = -INFINITY;                          // largest x this thread has seen
-        auto push = [&](float x, int v) {
-          const int at = atomicAdd(&sm.n_list, 1);
-          if (at < LP_LIST) sm.list[at] = make_key(x, v);
-        };
-        auto add = [&](float x) {                        // x in reach of my.m
-          const float d = max_nan(fmaf(x, p.k, my.m == -INFINITY ? 0.f : -my.m), -200.f);
-          const float e = fast_exp2(d);
-          my.s += e;
-          my.t = fmaf(e, d, my.t);
-          my.above += x > x_t ? 1 : 0;
-        };
-        auto raise = [&](float mx) {                     // the thread's maximum becomes mx
-          const float m = mx * p.k;
-          if (my.s != 0.f) {
-            const float dist = my.m - m, f = exp2f(dist);
-            my.t = f * fmaf(my.s, dist, my.t);
-            my.s *= f;
-          }
-          my.m = m;
-        };
-        // the elements outside whole pieces: in front of the first one (with unit 0), behind the last one
-        {
-          const int n_front = u0 == 0 ? min(first - (mis ? mis : 0), vocab) : 0;                     // virtual mis .. first - 1
-          const int tail = max(last, min(first, mis + vocab)), n_back = mis + vocab - tail;            // virtual tail .. mis + vocab - 1
-          int v = -1;
-          if (tid < n_front) v = tid;
-          else if (tid >= 32 && tid - 32 < n_back && (tail + tid - 32) / LP_UNIT >= u0 && (tail + tid - 32) / LP_UNIT < u1) v = tail - mis + tid - 32;
-          if (v >= 0) {
-            const float x = L::one(row_p, v);
-            best = x;
-            raise(x);
-            add(x);
-            if (n_top > 0 && x > -INFINITY) push(x, v);
-          }
-        }
-        bool fresh = true;                               // no tile of the segment read yet
-        float bound = -INFINITY;
-        for (int v0 = u0 * LP_UNIT; v0 < u1 * LP_UNIT; v0 += LP_TILE) {
-          const int lo = max(v0, first), hi = min(min(v0 + LP_TILE, u1 * LP_UNIT), last);
-          ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status));
-          const int pieces = ok ? max(hi - lo, 0) / kPer : 0;
-          float x[LP_MINE];
-#pragma unroll
-          for (int i = 0; i < LP_MINE / kPer; ++i) {
-            const int at = i * LP_READERS + tid;
-            uint4 w = make_uint4(L::kEmpty, L::kEmpty, L::kEmpty, L::kEmpty);
-            if (at < pieces) w = *reinterpret_cast<const uint4*>(sm.ring[slot] + at * 16);
-            L::get(w, x + i * kPer);
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.empty[slot]);
-          if (++slot == S::kSlots) { slot = 0; phase ^= 1; }
-          float mx = x[0];
-#pragma unroll
-          for (int i = 1; i < LP_MINE; ++i) mx = max_nan(mx, x[i]);
-          const bool higher = !(mx <= best);
-          if (higher) {
-            best = max_nan(mx, best);
-            raise(best);
-          }
-#pragma unroll
-          for (int i = 0; i < LP_MINE; ++i) add(x[i]);
-          if (n_top > 0) {
-            if (higher) atomicMax(&sm.lane_max[parity][lane], ordered(best));
-            if (fresh) named_barrier_sync(1, LP_READERS);
-            bound = unordered(max(nth_largest(reinterpret_cast<volatile uint32_t*>(sm.lane_max[parity])[lane], n_top), ordered(-INFINITY)));
-            if (mx >= bound) {
-#pragma unroll
-              for (int i = 0; i < LP_MINE; ++i)
-                if (x[i] >= bound && x[i] > -INFINITY) push(x[i], lo - mis + ((i / kPer) * LP_READERS + tid) * kPer + i % kPer);
-            }
-          }
-          fresh = false;
-        }
-        my = warp_join(my);
-        if (lane == 0) sm.warp_sums[warp] = my;
-        named_barrier_sync(1, LP_READERS);
-        if (tid < 32) {
-          sm.lane_max[parity ^ 1][lane] = 0;
-          Sums v = lane < LP_WARPS ? sm.warp_sums[lane] : Sums{-INFINITY, 0.f, 0.f, 0};
-          v = warp_join(v);
-          if (lane == 0) sm.row = v;
-        }
-        // the alternatives of the segment: list -> top, sorted; 0 where there are fewer
-        const int n_list = sm.n_list;
-        auto sort_list = [&](int n) {
-          for (int i = tid; i < n; i += LP_READERS) {
-            const unsigned long long key = sm.list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += sm.list[j] > key ? 1 : 0;
-            if (rank < n_top) sm.top[rank] = key;
-          }
-        };
+      for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+        const Segment g = segment_at(row, u0, end);
+        RowPlace& place = sm.place[at];
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status));
+        Sums total = {-INFINITY, 0.f, 0.f, 0};
+        if (lane < LP_WARPS) total = place.sums[lane];
+        total = warp_join(total, p.k);
+        const int target = place.target;
+        const float x_t = place.x_t;
+        // the alternatives of the segment in falling order, 0 where there are fewer
+        Key top = 0;
         if (n_top > 0) {
-          if (tid < n_top) sm.top[tid] = 0;
-          named_barrier_sync(1, LP_READERS);
-          const int v_lo = max(u0 * LP_UNIT - mis, 0), v_hi = min(u1 * LP_UNIT - mis, vocab);
+          const int n_list = ok ? place.n_list : 0;
+          const int v_lo = max(g.u0 * LP_UNIT - g.mis, 0), v_hi = min(g.u1 * LP_UNIT - g.mis, vocab);
           if (n_list <= LP_LIST) {
-            sort_list(n_list);
-            if (n_list < n_top && warp == 0) {           // fewer than n_top entries above -infinity: the first that are -infinity
+            if (n_list > 64) {
+              // candidates of the first, low bounds: those that reach the last one go to the front of the list
+              Key k = 0;
+#pragma unroll
+              for (int q = 0; q < LP_WARPS; ++q) k = larger(k, place.best[q][lane]);
+              const Key bound = nth_largest(k, n_top);
+              int kept = 0;
+              for (int i = 0; i < n_list; i += 32) {
+                const Key c = i + lane < n_list ? place.list[i + lane] : 0;
+                const unsigned keep = __ballot_sync(0xffffffffu, c != 0 && c >= bound);
+                if (keep >> lane & 1u) place.list[kept + __popc(keep & ((1u << lane) - 1u))] = c;
+                kept += __popc(keep);
+              }
+              __syncwarp();
+              for (int i = 0; i < kept; i += 32) take(top, i + lane < kept ? place.list[i + lane] : 0, n_top - 1);
+            } else {
+              for (int i = 0; i < n_list; i += 32) take(top, i + lane < n_list ? place.list[i + lane] : 0, n_top - 1);
+            }
+            if (n_list < n_top && ok) {                  // fewer than n_top entries above -infinity: the first that are -infinity
               int have = n_list;
               for (int v = v_lo; v < v_hi && have < n_top; v += 32) {
-                const bool empty = v + lane < v_hi && L::one(row_p, v + lane) == -INFINITY;
-                const unsigned mask = __ballot_sync(0xffffffffu, empty);
-                const int at = have + __popc(mask & ((1u << lane) - 1u));
-                if (empty && at < n_top) sm.top[at] = make_key(-INFINITY, v + lane);
-                have += __popc(mask);
+                const bool empty = v + lane < v_hi && L::one(g.row_p, v + lane) == -INFINITY;
+                take(top, empty ? make_key(-INFINITY, v + lane) : 0, n_top - 1);
+                have += __popc(__ballot_sync(0xffffffffu, empty));
               }
             }
           } else {
-            // more candidates than the list holds: the largest key below the last one, n_top times over
-            unsigned long long below = ~0ull;
-            for (int i = 0; i < n_top; ++i) {
-              unsigned long long k = 0;
-              for (int v = v_lo + tid; v < v_hi; v += LP_READERS) {
-                const unsigned long long c = make_key(L::one(row_p, v), v);
-                if (c < below && c > k) k = c;
-              }
-#pragma unroll
-              for (int o = 16; o > 0; o >>= 1) {
-                const unsigned long long c = __shfl_xor_sync(0xffffffffu, k, o);
-                k = c > k ? c : k;
-              }
-              if (lane == 0) sm.list[warp] = k;
-              named_barrier_sync(1, LP_READERS);
-              for (int w = 0; w < LP_WARPS; ++w) k = sm.list[w] > k ? sm.list[w] : k;
-              if (tid == 0) sm.top[i] = k;
-              below = k;
-              named_barrier_sync(1, LP_READERS);
-            }
+            for (int v = v_lo; v < v_hi; v += 32) take(top, v + lane < v_hi ? make_key(L::one(g.row_p, v + lane), v + lane) : 0, n_top - 1);
           }
         }
-        named_barrier_sync(1, LP_READERS);
-        if (tid == 0) sm.n_list = 0;
-        bool whole = u1 - u0 == upr;
+        // the place goes back to the readers
+#pragma unroll
+        for (int q = 0; q < LP_WARPS; ++q) place.best[q][lane] = 0;
+        if (lane == 0) place.n_list = 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.row_empty[at]);
+        if (++at == 2) { at = 0; row_phase ^= 1; }
+
+        bool whole = g.u1 - g.u0 == upr;
         if (!whole) {
           // a divided row: this share's part, and the join where it is the last one to come
-          const int64_t r0 = int64_t(row) * upr, r1 = r0 + upr;
-          const int slot_of = 2 * share + (u0 == 0 ? 1 : 0);           // the beginning of a row is the share's end
-          // shares that hold the row's first and last unit
-          const int f = share_of(r0), l = share_of(r1 - 1);
-          Part& part = parts[slot_of];
-          if (tid == 0) part.sums = sm.row;
-          if (tid < n_top) part.keys[tid] = sm.top[tid];
+          const int64_t r0 = int64_t(g.row) * upr, r1 = r0 + upr;
+          const int f = share_of(r0), l = share_of(r1 - 1);            // shares that hold the row's first and last unit
+          Part& part = parts[2 * share + (g.u0 == 0 ? 1 : 0)];         // (the beginning of a row is the share's end)
+          if (lane == 0) part.sums = total;
+          if (lane < n_top) part.keys[lane] = top;
           __threadfence();
-          named_barrier_sync(1, LP_READERS);
-          if (tid == 0) {
-            const int n = atomicAdd(done_words + f, 1);
-            sm.flag = n == l - f;
-            if (n == l - f) done_words[f] = 0;
-          }
-          named_barrier_sync(1, LP_READERS);
-          whole = sm.flag != 0;
+          __syncwarp();
+          int n = 0;
+          if (lane == 0) n = atomicAdd(done_words + f, 1);
+          whole = __shfl_sync(0xffffffffu, n, 0) == l - f;
           if (whole) {
+            if (lane == 0) done_words[f] = 0;            // ready for the next call
             __threadfence();
             const int n_parts = l - f + 1;
             auto part_at = [&](int i) -> const Part& { return parts[2 * (f + i) + (i == 0 ? 1 : 0)]; };
-            if (warp == 0) {
-              Sums v = {-INFINITY, 0.f, 0.f, 0};
-              for (int i = lane; i < n_parts; i += 32) {
-                const float4 w = __ldcg(reinterpret_cast<const float4*>(&part_at(i).sums));
-                v = join(v, Sums{w.x, w.y, w.z, __float_as_int(w.w)});
-              }
-              v = warp_join(v);
-              if (lane == 0) sm.row = v;
+            total = Sums{-INFINITY, 0.f, 0.f, 0};
+            for (int i = lane; i < n_parts; i += 32) {
+              const float4 w = __ldcg(reinterpret_cast<const float4*>(&part_at(i).sums));
+              Sums v = {w.x, w.y, w.z, __float_as_int(w.w)};
+              const float to = max_nan(v.m, total.m);
+              raise(v, to, p.k);
+              raise(total, to, p.k);
+              total.s += v.s;
+              total.t += v.t;
+              total.above += v.above;
             }
+            total = warp_join(total, p.k);
             if (n_top > 0) {
-              // a part's last key is reached n_top times: what is below the largest of them is no alternative
-              unsigned long long least = 0;
-              for (int i = lane; i < n_parts; i += 32) {
-                const unsigned long long c = __ldcg(&part_at(i).keys[n_top - 1]);
-                least = c > least ? c : least;
-              }
+              // four parts' keys on their way at a time; each part's are in falling order
+              top = 0;
+              for (int i0 = 0; i0 < n_parts; i0 += 4) {
+                Key k[4];
 #pragma unroll
-              for (int o = 16; o > 0; o >>= 1) {
-                const unsigned long long c = __shfl_xor_sync(0xffffffffu, least, o);
-                least = c > least ? c : least;
+                for (int i = 0; i < 4; ++i) k[i] = i0 + i < n_parts && lane < n_top ? __ldcg(&part_at(i0 + i).keys[lane]) : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (i0 + i < n_parts) top = merge_sorted(top, k[i]);
               }
-              for (int i = tid; i < n_parts * n_top; i += LP_READERS) {
-                const unsigned long long c = __ldcg(&part_at(i / n_top).keys[i % n_top]);
-                if (c >= least && c != 0) sm.list[atomicAdd(&sm.n_list, 1)] = c;
-              }
-              if (tid < n_top) sm.top[tid] = 0;
-              named_barrier_sync(1, LP_READERS);
-              sort_list(sm.n_list);
             }
-            named_barrier_sync(1, LP_READERS);
-            if (tid == 0) sm.n_list = 0;
           }
         }
         if (whole) {
-          const Sums v = sm.row;
-          const float log2_s = log2f(v.s);
-          auto logprob = [&](float x) {
-            if (v.m == -INFINITY) return -INFINITY;
-            return kLn2 * (fmaf(x, p.k, -v.m) - log2_s);
-          };
-          if (tid == 0) {
-            p.a.logprob[row] = has_target ? logprob(x_t) : 0.f;
-            if (p.a.entropy) p.a.entropy[row] = v.m == -INFINITY ? 0.f : kLn2 * (log2_s - v.t / v.s);
-            if (p.a.rank) p.a.rank[row] = has_target ? v.above : -1;
+          const bool has_target = target >= 0 && target < vocab;
+          const float log2_s = log2f(total.s);
+          auto logprob = [&](float x) { return total.m == -INFINITY ? -INFINITY : kLn2 * (p.k * (x - total.m) - log2_s); };
+          if (lane == 0) {
+            p.a.logprob[g.row] = has_target ? logprob(x_t) : 0.f;
+            if (p.a.entropy) p.a.entropy[g.row] = total.m == -INFINITY ? 0.f : kLn2 * (log2_s - total.t / total.s);
+            if (p.a.rank) p.a.rank[g.row] = has_target ? total.above : -1;
             if (target >= vocab) atomicExch(p.a.status, kErrInvalidArg);
           }
-          if (tid < n_top) {
-            const unsigned long long key = sm.top[tid];
-            const int id = key == 0 ? -1 : int(0xffffffffu - unsigned(key));
-            p.a.top_ids[int64_t(row) * n_top + tid] = id;
-            p.a.top_logprobs[int64_t(row) * n_top + tid] = key == 0 ? __int_as_float(0x7fc00000) : logprob(unordered(uint32_t(key >> 32)));
+          if (lane < n_top) {
+            const int id = top == 0 ? -1 : int(0xffffffffu - unsigned(top));
+            p.a.top_ids[int64_t(g.row) * n_top + lane] = id;
+            p.a.top_logprobs[int64_t(g.row) * n_top + lane] = top == 0 ? __int_as_float(0x7fc00000) : logprob(unordered(uint32_t(top >> 32)));
           }
         }
-        named_barrier_sync(1, LP_READERS);               // the row's words are free for the next one
-        parity ^= 1;
-        u += u1 - u0;
       }
     }
   }
@@ -460,21 +702,18 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
   if (*abort_flag) drain_after_abort();
 }
 
-template <int TYPE>
-constexpr int lp_smem() {
-  return int(sizeof(LpSmem<TYPE>)) > kMinSmemBytes ? int(sizeof(LpSmem<TYPE>)) : kMinSmemBytes;
-}
-static_assert(lp_smem<HS_TYPE_F32>() <= 227 * 1024 && lp_smem<HS_TYPE_BF16>() <= 227 * 1024, "fits one SM");
+constexpr int kLpSmem = int(sizeof(LpSmem)) > kMinSmemBytes ? int(sizeof(LpSmem)) : kMinSmemBytes;
+static_assert(kLpSmem <= 227 * 1024, "fits one SM");
 static_assert(2 * kMaxShares * sizeof(Part) <= kWsScratchBytes, "two parts per share");
 static_assert(kWsLogprobsDone + kMaxShares * 4 <= kWsChunkQueue, "one word per share");
 
 }  // namespace
 
 cudaError_t token_logprobs_set_attributes() {
-  cudaError_t e = set_kernel_smem(token_logprobs_kernel<HS_TYPE_F32>, lp_smem<HS_TYPE_F32>());
+  cudaError_t e = set_kernel_smem(token_logprobs_kernel<HS_TYPE_F32>, kLpSmem);
   if (e != cudaSuccess) return e;
-  if ((e = set_kernel_smem(token_logprobs_kernel<HS_TYPE_BF16>, lp_smem<HS_TYPE_BF16>())) != cudaSuccess) return e;
-  return set_kernel_smem(token_logprobs_kernel<HS_TYPE_F16>, lp_smem<HS_TYPE_F16>());
+  if ((e = set_kernel_smem(token_logprobs_kernel<HS_TYPE_BF16>, kLpSmem)) != cudaSuccess) return e;
+  return set_kernel_smem(token_logprobs_kernel<HS_TYPE_F16>, kLpSmem);
 }
 
 cudaError_t launch_token_logprobs(const hs_token_logprobs_t& a, int sm_count, int sm_budget, cudaStream_t stream) {
@@ -486,9 +725,9 @@ cudaError_t launch_token_logprobs(const hs_token_logprobs_t& a, int sm_count, in
   p.shares = int(std::max<int64_t>(1, std::min<int64_t>(share_count(sm_count), units / LP_MIN_UNITS)));
   p.k = float(double(a.scale) * 1.4426950408889634074);
   const int grid = std::min(p.shares, sm_budget);
-  if (a.type == HS_TYPE_F32) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F32>, grid, LP_THREADS, lp_smem<HS_TYPE_F32>(), stream, true, p);
-  if (a.type == HS_TYPE_BF16) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_BF16>, grid, LP_THREADS, lp_smem<HS_TYPE_BF16>(), stream, true, p);
-  return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F16>, grid, LP_THREADS, lp_smem<HS_TYPE_F16>(), stream, true, p);
+  if (a.type == HS_TYPE_F32) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F32>, grid, LP_THREADS, kLpSmem, stream, true, p);
+  if (a.type == HS_TYPE_BF16) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_BF16>, grid, LP_THREADS, kLpSmem, stream, true, p);
+  return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F16>, grid, LP_THREADS, kLpSmem, stream, true, p);
 }
 
 }  // namespace hs
