@@ -151,6 +151,8 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t* a, int32_t sm_budg
   // (rows of the pool are counted in 32 bits, and so are the keys of a block table row)
   const int64_t rows = int64_t(a->n_layers) * 2 * a->num_pages * a->n_kv_heads * kPage;
   if (!tables_shape_ok(a->n_seqs, a->max_pages_per_seq) || rows >= (int64_t(1) << 31)) return HS_ERR_UNSUPPORTED_SHAPE;
+  // (so are the pages of all sequences and groups of heads one after the other, and the tiles of a chunk's tokens)
+  if (int64_t(a->n_seqs) * a->max_pages_per_seq * a->n_q_heads >= (int64_t(1) << 31) || int64_t(a->n_tokens) * a->n_q_heads >= (int64_t(1) << 31)) return HS_ERR_UNSUPPORTED_SHAPE;
   const Device* d = nullptr;
   const hs_status_t st = enter(sm_budget, &d);
   if (st != HS_OK) return st;

@@ -25,6 +25,7 @@ namespace {
 constexpr int PD_WARPS = 8, PD_THREADS = PD_WARPS * 32;
 constexpr int PD_RING_BYTES = 192 * 1024;
 constexpr int PD_MIN_PAGES = 16;                 // of a share: two per warp
+constexpr int PD_WORDS = 96;                      // 32-bit words of shared memory in front of the sequences' page counts
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct DecodeParams {
@@ -225,39 +226,12 @@ struct GroupState {
   }
 };
 
-// Adds parts first, first + 1, .. in order, two columns a thread; every thread of the block.  emit(head, column, o0, o1, max, sum).
-template <int DH, int ROWS, typename At, typename Emit>
-__device__ __forceinline__ void join_parts(int n, int heads, At at, Emit emit) {
-  for (int i = threadIdx.x; i < heads * (DH / 2); i += PD_THREADS) {
-    const int h = i / (DH / 2), c = 2 * (i - h * (DH / 2));
-    float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int j0 = 0; j0 < n; j0 += 8) {                  // eight on their way at a time
-      float2 ml[8], ov[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const PartOf<DH, ROWS>* part = at(min(j0 + u, n - 1));
-        ml[u] = __ldcg(&part->ml[h]);
-        ov[u] = __ldcg(reinterpret_cast<const float2*>(&part->o[h][c]));
-      }
-      float mn = m;
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (j0 + u < n) mn = fmaxf(mn, ml[u].x);
-      const float f0 = fast_exp2(m - finite_or_zero(mn));
-      m = mn;
-      l *= f0; o0 *= f0; o1 *= f0;
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (j0 + u < n) {
-          const float f = fast_exp2(ml[u].x - finite_or_zero(m));
-          l = fmaf(f, ml[u].y, l);
-          o0 = fmaf(f, ov[u].x, o0);
-          o1 = fmaf(f, ov[u].y, o1);
-        }
-    }
-    emit(h, c, o0, o1, m, l);
-  }
-}
+// What a warp's piece of the line leaves to be joined: the part of a group that began in front of the piece (place 0), and of one that
+// goes on behind it (place 1).
+struct Cut {
+  int g0, g1;                                            // the group's place in the line; g1 = 0: nothing
+  int row, head0, heads;
+};
 
 template <int DH, int NT, bool F16, bool MOD>
 __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __grid_constant__ DecodeParams p) {
@@ -269,10 +243,10 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   uint64_t* full_all = reinterpret_cast<uint64_t*>(smem + PD_RING_BYTES);
   int* words = reinterpret_cast<int*>(full_all + PD_WARPS * SLOTS);
   volatile int* abort_flag = words;
-  int* flag = words + 1;
-  int* warp_sum = words + 2;                             // [8]
-  int* cut = words + 16;                                 // [9][3]: runs of partial results of the share
-  int* page_begin = words + 64;                          // [n_seqs + 1]
+  int* last = words + 1;                                 // [2]: this block joins the shares of the group cut at the share's beginning / end
+  int* warp_sum = words + 4;                             // [8]
+  Cut(*cuts)[2] = reinterpret_cast<Cut(*)[2]>(words + 16);              // [8][2]
+  int* page_begin = words + PD_WORDS;                    // [n_seqs + 1]
   const hs_paged_attention_t& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n = a.n_seqs, heads_all = a.n_q_heads / a.n_kv_heads, units = a.n_kv_heads * p.chunks;
@@ -322,10 +296,11 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     if (tid == 0) page_begin[n] = total;
     __syncthreads();
   }
-  const int64_t line = int64_t(page_begin[n]) * units;
-  const int shares = int(min(int64_t(p.shares), max(int64_t(1), line / PD_MIN_PAGES)));
-  auto share_begin = [&](int b) { return line * b / shares; };
-  auto share_of = [&](int64_t x) { return int(((x + 1) * shares - 1) / line); };
+  // (the host has seen to it that places in the line are 32-bit numbers.)  Shares: the first `more` ones have one page more.
+  const int line = page_begin[n] * units;
+  const int shares = min(p.shares, max(1, line / PD_MIN_PAGES)), base = line / shares, more = line - base * shares;
+  auto share_begin = [&](int b) { return base * b + min(b, more); };
+  auto share_of = [&](int x) { return x < more * (base + 1) ? x / (base + 1) : more + (x - more * (base + 1)) / max(base, 1); };
 
   Part* warp_parts = reinterpret_cast<Part*>(static_cast<char*>(a.workspace) + kWsScratch);          // [share][warp][2]
   Part* share_parts = warp_parts + size_t(kMaxShares) * PD_WARPS * 2;                                // [share][2]
@@ -343,8 +318,8 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     int group_seq, group_unit;
     int key0;
   };
-  auto find_seq = [&](int64_t x) {                       // the sequence of a place in the line
-    const int y = int(x / units);
+  auto find_seq = [&](int x) {                           // the sequence of a place in the line
+    const int y = x / units;
     int lo = 0, hi = n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -353,11 +328,11 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     }
     return lo;
   };
-  auto look_up = [&](int64_t x, int64_t end) {
+  auto look_up = [&](int x, int end) {
     Item it = {-1, 0, 0, 0};
     if (x < end) {
       const int s = find_seq(x), pages = page_begin[s + 1] - page_begin[s];
-      const int r = int(x - int64_t(page_begin[s]) * units);
+      const int r = x - page_begin[s] * units;
       const int unit = r / pages, i = r - unit * pages;
       const SeqView v = view_seq(a, s);
       const int logical = page_runs(v, v.kv - 1, v.kv - 1, a.window).page(i);
@@ -377,10 +352,14 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   };
 
   for (int share = blockIdx.x; share < shares; share += gridDim.x) {
-    const int64_t b0 = share_begin(share), b1 = share_begin(share + 1);
-    const int64_t w0 = b0 + (b1 - b0) * warp / PD_WARPS, w1 = b0 + (b1 - b0) * (warp + 1) / PD_WARPS;
+    const int b0 = share_begin(share), b1 = share_begin(share + 1);
+    const int piece = (b1 - b0) / PD_WARPS, longer = (b1 - b0) % PD_WARPS;       // (the first `longer` warps have one page more)
+    auto piece_begin = [&](int w) { return b0 + piece * w + min(w, longer); };
+    const int w0 = piece_begin(warp), w1 = piece_begin(warp + 1);
     Item now = look_up(w0 + lane, w1), next = look_up(w0 + 32 + lane, w1);
-    const int n_pages = int(w1 - w0);
+    const int n_pages = w1 - w0;
+    if (lane < 2) cuts[warp][lane].g1 = 0;
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < SLOTS - 1; ++i) {
       const int c = __shfl_sync(0xffffffffu, now.coord, i);
@@ -390,13 +369,15 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     int seq = -1, unit = -1, heads = 0, from = 0, pos = 0, prefix = 0;
     const uint16_t* q = nullptr;
     int64_t row = 0;
-    int64_t g0 = 0, g1 = 0;                              // the group's place in the line
+    int g0 = 0, g1 = 0;                                  // the group's place in the line
     auto finish = [&]() {                                // the group that the warp has come to the end of, or of its part of
       if (g0 >= w0 && g1 <= w1) {
         const int head0 = (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT;
         st.store(static_cast<uint16_t*>(a.o) + row * a.o_stride + head0 * DH, a.lse ? a.lse + row * a.n_q_heads + head0 : nullptr, heads, lane);
       } else {
-        st.put(warp_parts + (share * PD_WARPS + warp) * 2 + (g0 >= w0 ? 1 : 0), heads, lane);
+        const int slot = g0 >= w0 ? 1 : 0;
+        st.put(warp_parts + (share * PD_WARPS + warp) * 2 + slot, heads, lane);
+        if (lane == 0) cuts[warp][slot] = Cut{g0, g1, int(row), (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT, heads};
       }
     };
     for (int i = 0; i < n_pages; ++i) {
@@ -422,7 +403,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
         prefix = v.prefix;
         row = v.row;
         const int pages = page_begin[s + 1] - page_begin[s];
-        g0 = int64_t(page_begin[s]) * units + int64_t(unit) * pages;
+        g0 = page_begin[s] * units + unit * pages;
         g1 = g0 + pages;
         const int in_head = (unit % p.chunks) * 8 * NT, head0 = (unit / p.chunks) * heads_all + in_head;
         heads = min(heads_all - in_head, 8 * NT);
@@ -447,68 +428,102 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     __threadfence_block();
     __syncthreads();
     // --------------------------------------------------------------- the joins
-    // Runs of parts in this share: part (warp, end), then (warp + 1, 0), .. of one group.  Every thread walks the eight warps' cuts.
-    int w = 0;
-    while (w < PD_WARPS) {
-      const int64_t c0 = b0 + (b1 - b0) * w / PD_WARPS, c1 = b0 + (b1 - b0) * (w + 1) / PD_WARPS;
-      if (c0 == c1) { ++w; continue; }
-      // the group at the end of warp w's piece (a part of it that begins here), or, for the first warp, the one cut in front of it
-      auto group_at = [&](int64_t x, int64_t& lo, int64_t& hi, int& s, int& g) {
-        s = find_seq(x);
-        const int pages = page_begin[s + 1] - page_begin[s];
-        const int64_t base = int64_t(page_begin[s]) * units;
-        g = int((x - base) / pages);
-        lo = base + int64_t(g) * pages;
-        hi = lo + pages;
-      };
-      auto join_run = [&](int first_warp, int first_end, int64_t lo, int64_t hi, int s, int g) {
-        int last_warp = first_warp;
-        while (last_warp + 1 < PD_WARPS && b0 + (b1 - b0) * (last_warp + 1) / PD_WARPS < hi) ++last_warp;
-        // (pieces of no page between them deliver nothing)
-        int count = 0, at_warp[PD_WARPS];
-        for (int x = first_warp; x <= last_warp; ++x)
-          if (b0 + (b1 - b0) * x / PD_WARPS < b0 + (b1 - b0) * (x + 1) / PD_WARPS) at_warp[count++] = x;
-        auto at = [&](int i) { return warp_parts + (share * PD_WARPS + at_warp[i]) * 2 + (i == 0 ? first_end : 0); };
-        const int in_head = (g % p.chunks) * 8 * NT, head0 = (g / p.chunks) * heads_all + in_head, hn = min(heads_all - in_head, 8 * NT);
-        const int64_t r = view_seq(a, s).row;
-        auto emit = [&](int h, int c, float o0, float o1, float m, float l) {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o) + r * a.o_stride + (head0 + h) * DH + c) = pack_16<F16>(o0 * inv, o1 * inv);
-          if (c == 0 && a.lse) a.lse[r * a.n_q_heads + head0 + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
-        };
-        if (lo >= b0 && hi <= b1) {
-          join_parts<DH, 8 * NT>(count, hn, at, emit);
-          return;
-        }
-        Part* mine = share_parts + share * 2 + (lo >= b0 ? 1 : 0);
-        join_parts<DH, 8 * NT>(count, hn, at, [&](int h, int c, float o0, float o1, float m, float l) {
-          __stcg(reinterpret_cast<float2*>(&mine->o[h][c]), make_float2(o0, o1));
-          if (c == 0) __stcg(&mine->ml[h], make_float2(m, l));
-        });
-        const int f = share_of(lo), e = share_of(hi - 1);
+    // A run of parts begins with a warp whose group goes on behind its piece (place 1), or, at the share's beginning, with the group that was
+    // cut there (place 0); the next warps' parts of it are in their places 0.  First the parts of this share are joined, then, where this block is the
+    // last one of a group's to come, the shares' -- by the same instructions: this code runs once a launch, and what it took was the time to fetch it.
+    constexpr int kItems = 8 * NT * (DH / 4);            // of a run: (head, four columns)
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+      if (pass == 1) {
+        // the groups that other shares have parts of: the one cut at the share's beginning, the one cut at its end
+        int tail = -1;
+#pragma unroll 1
+        for (int w = 0; w < PD_WARPS; ++w)
+          if (cuts[w][1].g1 > b1) tail = w;
+        if (cuts[0][0].g1 == 0 && tail < 0) break;
         __threadfence();
         __syncthreads();
-        if (tid == 0) {
-          const int before = atomicAdd(done_words + f, 1);
-          *flag = before == e - f;
-          if (before == e - f) done_words[f] = 0;        // ready for the next call
+        if (tid < 2) {
+          int is_last = 0;
+          if (tid == 0 ? cuts[0][0].g1 > 0 : tail >= 0) {
+            const Cut& cut = cuts[tid == 0 ? 0 : tail][tid];
+            const int f = share_of(cut.g0), e = share_of(cut.g1 - 1);
+            is_last = atomicAdd(done_words + f, 1) == e - f;
+            if (is_last) done_words[f] = 0;              // ready for the next call
+          }
+          last[tid] = is_last;
         }
         __syncthreads();
-        if (*flag) {
-          __threadfence();
-          join_parts<DH, 8 * NT>(e - f + 1, hn, [&](int i) { return share_parts + (f + i) * 2 + (i == 0 ? 1 : 0); }, emit);
-        }
-        __syncthreads();
-      };
-      int64_t lo, hi;
-      int s, g;
-      if (c0 == b0) {
-        group_at(c0, lo, hi, s, g);
-        if (lo < c0) join_run(w, 0, lo, hi, s, g);
+        if (last[0] + last[1] == 0) break;
+        __threadfence();
       }
-      group_at(c1 - 1, lo, hi, s, g);
-      if (lo >= c0 && hi > c1) join_run(w, 1, lo, hi, s, g);
-      ++w;
+#pragma unroll 1
+      for (int k = 0; k < 2 * PD_WARPS; ++k) {
+        const int w = k >> 1, slot = k & 1;
+        const Cut cut = cuts[w][slot];
+        if (cut.g1 == 0 || (slot == 0 && w > 0)) continue;
+        const bool within = cut.g0 >= b0 && cut.g1 <= b1;
+        const Part *first, *others;
+        int n_parts = 1;
+        if (pass == 0) {
+          while (w + n_parts < PD_WARPS && cuts[w + n_parts][0].g1 > 0 && cuts[w + n_parts][0].g0 == cut.g0) ++n_parts;
+          first = warp_parts + (share * PD_WARPS + w) * 2 + slot;
+          others = warp_parts + (share * PD_WARPS + w + 1) * 2;
+        } else {
+          if (within || !last[slot]) continue;
+          const int f = share_of(cut.g0);
+          n_parts = share_of(cut.g1 - 1) - f + 1;
+          first = share_parts + f * 2 + 1;
+          others = share_parts + (f + 1) * 2;
+        }
+#pragma unroll 1
+        for (int i = tid; i < kItems; i += PD_THREADS) {
+          const int h = i / (DH / 4), c = i % (DH / 4) * 4;
+          if (h >= cut.heads) break;
+          float m = -INFINITY, l = 0.f;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+          for (int j0 = 0; j0 < n_parts; j0 += 8) {      // eight parts on their way at a time
+            float2 ml[8];
+            float4 ov[8];
+            float mn = m;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int j = min(j0 + u, n_parts - 1);
+              const Part* part = j == 0 ? first : others + (j - 1) * 2;
+              ml[u] = __ldcg(&part->ml[h]);
+              ov[u] = __ldcg(reinterpret_cast<const float4*>(&part->o[h][c]));
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              if (j0 + u >= n_parts) ml[u] = make_float2(-INFINITY, 0.f);
+              mn = fmaxf(mn, ml[u].x);
+            }
+            const float zero = finite_or_zero(mn), f0 = fast_exp2(m - zero);
+            m = mn;
+            l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const float f = fast_exp2(ml[u].x - zero);         // (0 for a part that is not there; its outputs are another part's)
+              l = fmaf(f, ml[u].y, l);
+              o.x = fmaf(f, ov[u].x, o.x);
+              o.y = fmaf(f, ov[u].y, o.y);
+              o.z = fmaf(f, ov[u].z, o.z);
+              o.w = fmaf(f, ov[u].w, o.w);
+            }
+          }
+          if (within || pass == 1) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + int64_t(cut.row) * a.o_stride + (cut.head0 + h) * DH + c) =
+                make_uint2(pack_16<F16>(o.x * inv, o.y * inv), pack_16<F16>(o.z * inv, o.w * inv));
+            if (c == 0 && a.lse) a.lse[int64_t(cut.row) * a.n_q_heads + cut.head0 + h] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+          } else {
+            Part* mine = share_parts + share * 2 + slot;
+            __stcg(reinterpret_cast<float4*>(&mine->o[h][c]), o);
+            if (c == 0) __stcg(&mine->ml[h], make_float2(m, l));
+          }
+        }
+      }
     }
     fence_proxy_async();
     __syncthreads();
@@ -518,7 +533,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
 
 template <int DH>
 constexpr int pd_smem() {
-  return 1024 + PD_RING_BYTES + PD_WARPS * PageGeom<DH>::SLOTS * 8 + 64 * 4 + (HS_DEVICE_MAX_SEQS + 1) * 4;
+  return 1024 + PD_RING_BYTES + PD_WARPS * PageGeom<DH>::SLOTS * 8 + PD_WORDS * 4 + (HS_DEVICE_MAX_SEQS + 1) * 4;
 }
 static_assert(pd_smem<64>() <= 227 * 1024 && pd_smem<128>() <= 227 * 1024, "fits one SM");
 static_assert(size_t(kMaxShares) * (PD_WARPS + 1) * 2 * sizeof(PartOf<128, 16>) <= kWsScratchBytes, "parts of warps and shares");
