@@ -25,7 +25,7 @@ namespace {
 constexpr int PD_WARPS = 8, PD_THREADS = PD_WARPS * 32;
 constexpr int PD_RING_BYTES = 192 * 1024;
 constexpr int PD_MIN_PAGES = 16;                 // of a share: two per warp
-constexpr int PD_WORDS = 96;                      // 32-bit words of shared memory in front of the sequences' page counts
+constexpr int PD_WORDS = 160;                     // 32-bit words of shared memory in front of the sequences' page counts
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct DecodeParams {
@@ -44,6 +44,16 @@ struct PageGeom {
 };
 __device__ __forceinline__ int page_off(int key, int chunk) {       // of a 16-byte chunk of a key's row
   return (chunk >> 3) * 2048 + key * 128 + (((chunk & 7) ^ (key & 7)) << 4);
+}
+// The K and the V block of a page and head: read once in a step, so they are the first to leave the L2 again (the kernel's own code and the
+// partial results stay).
+__device__ __forceinline__ void load_page(void* dst, const CUtensorMap* m, uint64_t* bar, int row, int layer) {
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %3, %5}], [%2], %6;"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(0), "r"(row), "r"(layer * 2), "l"(policy)
+      : "memory");
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t t;
@@ -65,9 +75,20 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY
 // One partial result: ROWS heads of DH outputs relative to the maximum, then (maximum in log2 units, sum) per head.
 template <int DH, int ROWS>
 struct PartOf {
-  float o[ROWS][DH];
+  float o[ROWS][DH + 4];                                 // (four floats more: the warps write and read these without bank conflicts where they are in shared memory)
   float2 ml[ROWS];
 };
+// Reads of partial results, in shared memory or in global memory where another SM has written them.
+__device__ __forceinline__ float4 load_part(const float* p) {
+  float4 v;
+  asm volatile("ld.relaxed.gpu.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 load_part(const float2* p) {
+  float2 v;
+  asm volatile("ld.relaxed.gpu.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
+  return v;
+}
 
 // A group's running softmax in a warp.  This lane holds heads 8 t + 2 (lane % 4) and the next one, of the scores keys lane / 4 and lane / 4 + 8, of the
 // outputs coordinates lane / 4 and lane / 4 + 8 of every sixteen.
@@ -230,6 +251,7 @@ struct GroupState {
 // goes on behind it (place 1).
 struct Cut {
   int g0, g1;                                            // the group's place in the line; g1 = 0: nothing
+  void* part;
   int row, head0, heads;
 };
 
@@ -243,7 +265,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   uint64_t* full_all = reinterpret_cast<uint64_t*>(smem + PD_RING_BYTES);
   int* words = reinterpret_cast<int*>(full_all + PD_WARPS * SLOTS);
   volatile int* abort_flag = words;
-  int* last = words + 1;                                 // [2]: this block joins the shares of the group cut at the share's beginning / end
+  int* last = words + 1;                                 // of the runs, those whose shares this block joins
   int* warp_sum = words + 4;                             // [8]
   Cut(*cuts)[2] = reinterpret_cast<Cut(*)[2]>(words + 16);              // [8][2]
   int* page_begin = words + PD_WORDS;                    // [n_seqs + 1]
@@ -302,8 +324,8 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   auto share_begin = [&](int b) { return base * b + min(b, more); };
   auto share_of = [&](int x) { return x < more * (base + 1) ? x / (base + 1) : more + (x - more * (base + 1)) / max(base, 1); };
 
-  Part* warp_parts = reinterpret_cast<Part*>(static_cast<char*>(a.workspace) + kWsScratch);          // [share][warp][2]
-  Part* share_parts = warp_parts + size_t(kMaxShares) * PD_WARPS * 2;                                // [share][2]
+  Part* warp_parts = reinterpret_cast<Part*>(static_cast<char*>(a.workspace) + kWsScratch);          // [share][warp]
+  Part* share_parts = warp_parts + size_t(kMaxShares) * PD_WARPS;                                    // [share][2]
   int* done_words = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsAttnDone);
 
   uint8_t* ring = smem + warp * SLOTS * G::SLOT;
@@ -347,7 +369,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   };
   auto request = [&](int coord) {                        // lane 0
     mbar_expect_tx(&full[fill], G::SLOT);
-    tma_load_4d(ring + fill * G::SLOT, &p.tm, &full[fill], 0, max(coord, 0), 0, a.layer * 2);
+    load_page(ring + fill * G::SLOT, &p.tm, &full[fill], max(coord, 0), a.layer);
     if (++fill == SLOTS) fill = 0;
   };
 
@@ -370,14 +392,16 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     const uint16_t* q = nullptr;
     int64_t row = 0;
     int g0 = 0, g1 = 0;                                  // the group's place in the line
-    auto finish = [&]() {                                // the group that the warp has come to the end of, or of its part of
+    auto finish = [&](bool at_end) {                     // the group that the warp has come to the end of, or of its part of
       if (g0 >= w0 && g1 <= w1) {
         const int head0 = (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT;
         st.store(static_cast<uint16_t*>(a.o) + row * a.o_stride + head0 * DH, a.lse ? a.lse + row * a.n_q_heads + head0 : nullptr, heads, lane);
       } else {
         const int slot = g0 >= w0 ? 1 : 0;
-        st.put(warp_parts + (share * PD_WARPS + warp) * 2 + slot, heads, lane);
-        if (lane == 0) cuts[warp][slot] = Cut{g0, g1, int(row), (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT, heads};
+        // (at the end of its piece the warp's ring is idle and takes the part; before that it goes to the workspace)
+        Part* part = at_end ? reinterpret_cast<Part*>(ring) : warp_parts + share * PD_WARPS + warp;
+        st.put(part, heads, lane);
+        if (lane == 0) cuts[warp][slot] = Cut{g0, g1, part, int(row), (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT, heads};
       }
     };
     for (int i = 0; i < n_pages; ++i) {
@@ -394,7 +418,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
       const int s = __shfl_sync(0xffffffffu, now.group_seq, j), g = __shfl_sync(0xffffffffu, now.group_unit, j);
       const int key0 = __shfl_sync(0xffffffffu, now.key0, j), coord = __shfl_sync(0xffffffffu, now.coord, j);
       if (s != seq || g != unit) {
-        if (seq >= 0) finish();
+        if (seq >= 0) finish(false);
         seq = s;
         unit = g;
         const SeqView v = view_seq(a, s);
@@ -424,62 +448,55 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
       if (ok) st.page(k_base, k_base + G::BYTES, seen, pos - key0, p.score, lane);
       __syncwarp();                                      // every lane is done with the slot before lane 0 asks for its next page
     }
-    if (seq >= 0) finish();
+    if (seq >= 0) finish(true);
     __threadfence_block();
     __syncthreads();
     // --------------------------------------------------------------- the joins
     // A run of parts begins with a warp whose group goes on behind its piece (place 1), or, at the share's beginning, with the group that was
     // cut there (place 0); the next warps' parts of it are in their places 0.  First the parts of this share are joined, then, where this block is the
     // last one of a group's to come, the shares' -- by the same instructions: this code runs once a launch, and what it took was the time to fetch it.
-    constexpr int kItems = 8 * NT * (DH / 4);            // of a run: (head, four columns)
+    const int my_g0 = lane < 2 * PD_WARPS ? cuts[lane >> 1][lane & 1].g0 : 0, my_g1 = lane < 2 * PD_WARPS ? cuts[lane >> 1][lane & 1].g1 : 0;
+    const bool begins = my_g1 > 0 && (lane == 0 || (lane & 1));          // (of each warp's lanes: a place that a run begins with)
+    unsigned todo = __ballot_sync(0xffffffffu, begins);
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
       if (pass == 1) {
         // the groups that other shares have parts of: the one cut at the share's beginning, the one cut at its end
-        int tail = -1;
-#pragma unroll 1
-        for (int w = 0; w < PD_WARPS; ++w)
-          if (cuts[w][1].g1 > b1) tail = w;
-        if (cuts[0][0].g1 == 0 && tail < 0) break;
+        todo = __ballot_sync(0xffffffffu, begins && (my_g0 < b0 || my_g1 > b1));
+        if (todo == 0) break;
         __threadfence();
         __syncthreads();
-        if (tid < 2) {
-          int is_last = 0;
-          if (tid == 0 ? cuts[0][0].g1 > 0 : tail >= 0) {
-            const Cut& cut = cuts[tid == 0 ? 0 : tail][tid];
-            const int f = share_of(cut.g0), e = share_of(cut.g1 - 1);
-            is_last = atomicAdd(done_words + f, 1) == e - f;
-            if (is_last) done_words[f] = 0;              // ready for the next call
-          }
-          last[tid] = is_last;
+        bool is_last = false;
+        if (warp == 0 && todo >> lane & 1u) {
+          const int f = share_of(my_g0), e = share_of(my_g1 - 1);
+          is_last = atomicAdd(done_words + f, 1) == e - f;
+          if (is_last) done_words[f] = 0;                // ready for the next call
+        }
+        if (warp == 0) {
+          const unsigned mine = __ballot_sync(0xffffffffu, is_last);
+          if (lane == 0) *last = int(mine);
         }
         __syncthreads();
-        if (last[0] + last[1] == 0) break;
+        todo = unsigned(*last);
+        if (todo == 0) break;
         __threadfence();
       }
 #pragma unroll 1
-      for (int k = 0; k < 2 * PD_WARPS; ++k) {
-        const int w = k >> 1, slot = k & 1;
-        const Cut cut = cuts[w][slot];
-        if (cut.g1 == 0 || (slot == 0 && w > 0)) continue;
-        const bool within = cut.g0 >= b0 && cut.g1 <= b1;
-        const Part *first, *others;
-        int n_parts = 1;
+      for (; todo; todo &= todo - 1) {
+        const int k = __ffs(todo) - 1, w = k >> 1, slot = k & 1;
+        const int g0 = __shfl_sync(0xffffffffu, my_g0, k), g1 = __shfl_sync(0xffffffffu, my_g1, k);
+        const Cut& cut = cuts[w][slot];
+        const bool within = g0 >= b0 && g1 <= b1;
+        int n_parts = 1, f = 0;
         if (pass == 0) {
-          while (w + n_parts < PD_WARPS && cuts[w + n_parts][0].g1 > 0 && cuts[w + n_parts][0].g0 == cut.g0) ++n_parts;
-          first = warp_parts + (share * PD_WARPS + w) * 2 + slot;
-          others = warp_parts + (share * PD_WARPS + w + 1) * 2;
+          n_parts += __popc(__ballot_sync(0xffffffffu, !(lane & 1) && lane > k && my_g1 > 0 && my_g0 == g0));
         } else {
-          if (within || !last[slot]) continue;
-          const int f = share_of(cut.g0);
-          n_parts = share_of(cut.g1 - 1) - f + 1;
-          first = share_parts + f * 2 + 1;
-          others = share_parts + (f + 1) * 2;
+          f = share_of(g0);
+          n_parts = share_of(g1 - 1) - f + 1;
         }
 #pragma unroll 1
-        for (int i = tid; i < kItems; i += PD_THREADS) {
+        for (int i = tid; i < cut.heads * (DH / 4); i += PD_THREADS) {
           const int h = i / (DH / 4), c = i % (DH / 4) * 4;
-          if (h >= cut.heads) break;
           float m = -INFINITY, l = 0.f;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
@@ -490,9 +507,9 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
               const int j = min(j0 + u, n_parts - 1);
-              const Part* part = j == 0 ? first : others + (j - 1) * 2;
-              ml[u] = __ldcg(&part->ml[h]);
-              ov[u] = __ldcg(reinterpret_cast<const float4*>(&part->o[h][c]));
+              const Part* part = pass == 1 ? share_parts + (f + j) * 2 + (j == 0 ? 1 : 0) : static_cast<const Part*>(cuts[w + j][j == 0 ? slot : 0].part);
+              ml[u] = load_part(&part->ml[h]);
+              ov[u] = load_part(&part->o[h][c]);
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
@@ -536,7 +553,7 @@ constexpr int pd_smem() {
   return 1024 + PD_RING_BYTES + PD_WARPS * PageGeom<DH>::SLOTS * 8 + PD_WORDS * 4 + (HS_DEVICE_MAX_SEQS + 1) * 4;
 }
 static_assert(pd_smem<64>() <= 227 * 1024 && pd_smem<128>() <= 227 * 1024, "fits one SM");
-static_assert(size_t(kMaxShares) * (PD_WARPS + 1) * 2 * sizeof(PartOf<128, 16>) <= kWsScratchBytes, "parts of warps and shares");
+static_assert(size_t(kMaxShares) * (PD_WARPS + 2) * sizeof(PartOf<128, 16>) <= kWsScratchBytes, "parts of warps and shares");
 static_assert(kWsAttnDone + kMaxShares * 4 <= kWsLogprobsDone, "one word per share");
 
 using DecodeKernel = void (*)(DecodeParams);
