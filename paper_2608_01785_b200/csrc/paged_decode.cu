@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     const int piece = (b1 - b0) / PD_WARPS, longer = (b1 - b0) % PD_WARPS;       // (the first `longer` warps have one page more)
     auto piece_begin = [&](int w) { return b0 + piece * w + min(w, longer); };
     const int w0 = piece_begin(warp), w1 = piece_begin(warp + 1);
-    Item now = look_up(w0 + lane, w1), next = look_up(w0 + 32 + lane, w1);
+    Item now = look_up(w0 + lane, w1);
     const int n_pages = w1 - w0;
     if (lane < 2) cuts[warp][lane].g1 = 0;
     __syncwarp();
@@ -387,6 +387,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
       const int c = __shfl_sync(0xffffffffu, now.coord, i);
       if (lane == 0 && i < n_pages) request(c);
     }
+    Item next = look_up(w0 + 32 + lane, w1);
     GroupState<DH, NT, F16, MOD> st;
     int seq = -1, unit = -1, heads = 0, from = 0, pos = 0, prefix = 0;
     const uint16_t* q = nullptr;

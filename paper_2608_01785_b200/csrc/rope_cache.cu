@@ -5,6 +5,8 @@
 // that are copied.  A warp takes as many whole heads at a time as it has lanes for (four of 128 coordinates), so that its loads
 // and stores are runs of 128 bytes and more, and a lane has the same eight pairs in every head: consecutive heads of a token find their 64 bytes of the
 // table in L1.  The (token, heads) steps are dealt to the warps in contiguous runs of equal length, whatever the number of tokens.
+// Threads of a block x units a lane has on their way, us for 8000 rows of 36 heads of 128 / 1111 rows of 24 of 64 / 64 rows of 36: 1024 x 1 32.5 / 4.0 / 4.2,
+// 768 x 2 33.4 / 3.7 / 3.6, 512 x 4 35.0 / 3.5 / 3.1, 1024 x 4, whose registers spill, 47.8 / 6.4 / 5.2.
 #include <algorithm>
 
 #include "device_ops.h"
@@ -13,7 +15,7 @@
 namespace hs {
 namespace {
 
-constexpr int RC_THREADS = 1024, RT_THREADS = 512;
+constexpr int RC_THREADS = 768, RT_THREADS = 512;
 
 // Sixteen-byte pieces of eight elements of the source type -> eight floats.
 template <int TYPE>
@@ -23,8 +25,8 @@ struct Piece<HS_TYPE_F32> {
   float4 a, b;
   __device__ __forceinline__ void load(const void* p, int64_t at) {
     const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-    a = __ldcs(f);
-    b = __ldcs(f + 1);
+    a = f[0];
+    b = f[1];
   }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
@@ -34,7 +36,7 @@ struct Piece<HS_TYPE_F32> {
 template <int TYPE>
 struct Piece16 {
   uint4 v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at)); }
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at); }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -73,7 +75,7 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 
 template <int SRC, bool F16, bool INTERLEAVED>
 __global__ void __launch_bounds__(RC_THREADS, 1) rope_cache_kernel(const hs_rope_cache_t a) {
-  constexpr int kAhead = SRC == HS_TYPE_F32 ? 2 : 4;          // units a lane has on their way: 64 bytes each from fp32, 32 else
+  constexpr int kAhead = SRC == HS_TYPE_F32 ? 1 : 2;          // units a lane has on their way: 64 bytes each from fp32, 32 else
   extern __shared__ uint8_t unused_smem[];
   griddep_wait();
   const int lane = threadIdx.x & 31;
