@@ -434,14 +434,21 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
             if (!(seen2 & (1u << e))) sreg2[e] = to;
           }
         };
-        auto largest = [&](float sign) {              // of sign * score; four chains
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto largest = [&]() {                        // four chains
+          float mx[4];
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            mx[(e >> 1) & 1] = max_nan(mx[(e >> 1) & 1], max_nan(sign * __uint_as_float(sreg[e]), sign * __uint_as_float(sreg[e + 1])));
-            mx[2 + ((e >> 1) & 1)] = max_nan(mx[2 + ((e >> 1) & 1)], max_nan(sign * __uint_as_float(sreg2[e]), sign * __uint_as_float(sreg2[e + 1])));
-          }
-          return max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3]));
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e]));
+#pragma unroll
+          for (int e = 4; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e])));
+          return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        };
+        auto smallest = [&]() {
+          float mn[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mn[e] = fminf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e]));
+#pragma unroll
+          for (int e = 4; e < 32; ++e) mn[e & 3] = fminf(mn[e & 3], fminf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e])));
+          return fminf(fminf(mn[0], mn[1]), fminf(mn[2], mn[3]));
         };
         // Of a capped block that the whole warp sees, the polynomial of the largest score is the largest polynomial, and the reference is part of its
         // last multiply-add: nothing is written back in between.  A mask or a bias has to be applied in between.
@@ -449,14 +456,18 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         int direct = 0;                               // 3, 5: such a block, by the polynomial's degree; 0: the registers hold finished scores
         if (MOD) {
           int degree = 0;
+          bool all_seen = false;
           float top = 0.f;
           if (sc.out != 0.f) {
             if (masked) mask(0u);                     // (what is not seen must not decide which polynomial the others take)
-            top = largest(1.f);
-            const float low = largest(-1.f), u = row_valid ? fmaxf(top * top, low * low) : 0.f;         // (rows of padding hold anything)
-            if (__all_sync(0xffffffffu, u <= sc.limit5)) degree = __all_sync(0xffffffffu, u <= sc.limit3) ? 3 : 5;
+            top = largest();
+            const float low = smallest(), u = row_valid ? fmaxf(top * top, low * low) : 0.f;         // (rows of padding hold anything)
+            // one vote: the worst row's polynomial (6: degree three, 4: five, 0: none), 1 more where nothing is masked
+            const unsigned vote = __reduce_and_sync(0xffffffffu, (u <= sc.limit3 ? 6u : u <= sc.limit5 ? 4u : 0u) | (masked ? 0u : 1u));
+            degree = vote >= 6 ? 3 : vote >= 4 ? 5 : 0;
+            all_seen = vote & 1u;
           }
-          if (degree != 0 && a.slopes == nullptr && __all_sync(0xffffffffu, !masked)) {
+          if (degree != 0 && a.slopes == nullptr && all_seen) {
             direct = degree;
             float unused;
             if (degree == 3) split(odd_poly(f2(top, top), sc.c3, f2(0.f, 0.f)), mx, unused);
@@ -498,11 +509,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
               }
             }
             if (masked) mask(0xff800000u);          // -infinity
-            mx = largest(1.f);
+            mx = largest();
           }
         } else {
           if (masked) mask(0xff800000u);          // -infinity
-          mx = largest(1.f);
+          mx = largest();
         }
         // the reference maximum moves only when the block's maximum is far above it
         const float unit = MOD ? 1.f : sc.in;
