@@ -143,7 +143,7 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t* a, int32_t sm_budg
   if (a->n_layers < 1 || a->layer < 0 || a->layer >= a->n_layers || a->num_pages < 1 || a->max_pages_per_seq < 1) return HS_ERR_INVALID_ARG;
   if (a->type != HS_TYPE_BF16 && a->type != HS_TYPE_F16) return HS_ERR_INVALID_ARG;
   if (!a->tok_begin && (a->max_q_len != 1 || a->n_tokens < a->n_seqs)) return HS_ERR_INVALID_ARG;
-  if (!(a->cap >= 0.f) || !(a->scale > -1e30f && a->scale < 1e30f) || a->window < 0) return HS_ERR_INVALID_ARG;
+  if (!(a->cap >= 0.f && a->cap < 1e30f) || !(a->scale > -1e30f && a->scale < 1e30f) || a->window < 0) return HS_ERR_INVALID_ARG;
   if ((a->head_dim != 64 && a->head_dim != 128) || a->n_q_heads % a->n_kv_heads != 0 || a->n_q_heads > 1024) return HS_ERR_UNSUPPORTED_SHAPE;
   const int64_t q_row = int64_t(a->n_q_heads) * a->head_dim;
   if (a->q_stride < q_row || a->o_stride < q_row || a->q_stride % 8 || a->o_stride % 8) return HS_ERR_INVALID_ARG;

@@ -1,4 +1,4 @@
-"""CPU-only checks of the device-resident operators: the header, the library and the Python structs agree, wrong arguments are refused on the host
+"""CPU-only checks of the device-resident operators: the header, the library and the packed structs agree, wrong arguments are refused on the host
 before any GPU is asked for, and the plain definitions of the GPU tests agree with the framework's host-side page allocator."""
 import ctypes as C
 import os
@@ -17,8 +17,10 @@ from paper_2608_01785_b200 import device_ops as ops
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "horizonserve_device.h")
-STRUCTS = {"hs_step_tables_t": ops._STEP_TABLES, "hs_release_pages_t": ops._RELEASE_PAGES, "hs_rope_table_t": ops._ROPE_TABLE,
-           "hs_rope_cache_t": ops._ROPE_CACHE, "hs_paged_attention_t": ops._PAGED_ATTENTION, "hs_token_logprobs_t": ops._TOKEN_LOGPROBS}
+# The description structs as packed words ("i" int32, "q" int64, "P" pointer, "f", "d"), in the order of ops.EXPORTS.
+STRUCTS = {name: struct.Struct(fmt) for name, fmt in {
+    "hs_step_tables_t": "@4i13P", "hs_release_pages_t": "@3i7P", "hs_rope_table_t": "@4i5dP", "hs_rope_cache_t": "@8i3P3q3P4iPq2P",
+    "hs_paged_attention_t": "@11iPq6P2fiPq3P", "hs_token_logprobs_t": "@4iPqPf7P"}.items()}
 
 
 def text():
@@ -49,7 +51,7 @@ def test_every_declared_operator_is_exported_and_bound():
 
 
 @pytest.mark.parametrize("compiler", ["gcc", "g++"])
-def test_python_structs_are_the_headers(tmp_path, compiler):
+def test_packed_structs_are_the_headers(tmp_path, compiler):
     lines = []
     for name, packed in STRUCTS.items():
         lines.append(f'printf("%zu\\n", sizeof({name}));')
@@ -96,7 +98,7 @@ REFUSED = {
                         (dict(cache_type=0), INVALID), (dict(src_type=3), INVALID), (dict(layer=2), INVALID), (dict(layer=-1), INVALID), (dict(q=P + 8), INVALID),
                         (dict(q_out=P + 8), INVALID), (dict(kv_pool=P + 128), INVALID), (dict(max_position=0), INVALID)],
     "hs_paged_attention_t": [(dict(head_dim=96), SHAPE), (dict(n_kv_heads=3), SHAPE), (dict(n_q_heads=2048, q_stride=1 << 18, o_stride=1 << 18), SHAPE),
-                             (dict(cap=-1.0), INVALID), (dict(cap=NAN), INVALID), (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(window=-1), INVALID),
+                             (dict(cap=-1.0), INVALID), (dict(cap=NAN), INVALID), (dict(cap=INF), INVALID), (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(window=-1), INVALID),
                              (dict(max_q_len=0), INVALID), (dict(tok_begin=0, max_q_len=2), INVALID), (dict(tok_begin=0, n_tokens=3), INVALID),
                              (dict(q_stride=252), INVALID), (dict(o_stride=260), INVALID), (dict(q=P + 8), INVALID), (dict(kv_pool=P + 64), INVALID),
                              (dict(type=0), INVALID), (dict(layer=2), INVALID), (dict(workspace=P + 64), INVALID), (dict(n_seqs=4097, n_tokens=4097), SHAPE),
@@ -110,7 +112,8 @@ REFUSED = {
 
 @pytest.mark.parametrize("name", list(REFUSED))
 def test_wrong_arguments_are_refused_before_a_device_is_needed(name):
-    fn = ops._functions()[ops.EXPORTS[list(STRUCTS).index(name)]]
+    fn = C.CDLL(B.LIB_PATH)[ops.EXPORTS[list(STRUCTS).index(name)]]
+    fn.argtypes, fn.restype = [C.c_char_p, C.c_int32, C.c_void_p], C.c_int
     assert fn(None, 8, None) == INVALID
     for change, want in REFUSED[name]:
         values = {f: P for f in fields(name)} | GOOD[name] | change
