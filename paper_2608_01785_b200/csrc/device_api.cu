@@ -175,6 +175,7 @@ hs_status_t hs_op_token_logprobs(const hs_token_logprobs_t* a, int32_t sm_budget
   if (a->type < HS_TYPE_F32 || a->type > HS_TYPE_F16 || !aligned(a->logits, a->type == HS_TYPE_F32 ? 4 : 2)) return HS_ERR_INVALID_ARG;
   if (a->n_top < 0 || (a->n_top > 0 && (!a->top_ids || !a->top_logprobs)) || !(a->scale > 0.f && a->scale < 1e30f)) return HS_ERR_INVALID_ARG;
   if (a->n_top > HS_MAX_ALTERNATIVES || a->n_top > a->vocab || a->vocab >= (1 << 30)) return HS_ERR_UNSUPPORTED_SHAPE;
+  if (int64_t(a->n_rows) * (a->vocab / 1024 + 2) >= (int64_t(1) << 31)) return HS_ERR_UNSUPPORTED_SHAPE;        // (the kernel counts in units of 1024)
   const Device* d = nullptr;
   const hs_status_t st = enter(sm_budget, &d);
   if (st != HS_OK) return st;

@@ -30,7 +30,9 @@ constexpr int LP_UNIT = 1024;                                                   
 constexpr int LP_PIECES = 8, LP_SLOTS = 3;                                                 // 16-byte pieces of a tile per thread; tiles of the ring
 constexpr int LP_TILE_BYTES = LP_READERS * LP_PIECES * 16;
 constexpr int LP_LIST = 1472;                                                              // candidates of a row
-constexpr int LP_MIN_UNITS = 2;                                                            // of a share
+constexpr int LP_MIN_UNITS = 16;                                                           // of a part of a row
+constexpr int LP_ROW_COST = 36, LP_JOIN_COST = 54;                                         // units that take as long as a row's beginning and end, as a join
+constexpr int LP_JOIN_LOADS = 4;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 10.f;                                                             // log2 units that a logit may lie above its thread's reference
 
@@ -160,7 +162,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 using Key = unsigned long long;
 __device__ __forceinline__ Key larger(Key a, Key b) { return a > b ? a : b; }
 __device__ __forceinline__ Key smaller(Key a, Key b) { return a > b ? b : a; }
-// Lanes 0 .. 31 in falling order: a bitonic sequence (stages 16 .. 1), or any keys.
+// Lanes 0 .. 31 in falling order, from a sequence that rises and falls.
 __device__ __forceinline__ Key merge_lanes(Key v) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -170,44 +172,45 @@ __device__ __forceinline__ Key merge_lanes(Key v) {
   }
   return v;
 }
-__device__ __forceinline__ Key sort_lanes(Key v) {
-  const int lane = threadIdx.x & 31;
+// How many of the lanes' keys, which are all different, are larger.  (All 32 compared through the warp's scratch: 250 cycles; fifteen exchanges of a sorting
+// network took 700.)
+__device__ __noinline__ int rank_of(Key k, Key* scratch) {
+  scratch[threadIdx.x & 31] = k;
+  __syncwarp();
+  int n = 0;
 #pragma unroll
-  for (int size = 2; size < 32; size <<= 1) {
-#pragma unroll
-    for (int o = size >> 1; o > 0; o >>= 1) {
-      const Key w = __shfl_xor_sync(0xffffffffu, v, o);
-      v = ((lane & o) == 0) == ((lane & size) == 0) ? larger(v, w) : smaller(v, w);
-    }
+  for (int i = 0; i < 16; ++i) {
+    const ulonglong2 o = reinterpret_cast<const ulonglong2*>(scratch)[i];
+    n += (o.x > k ? 1 : 0) + (o.y > k ? 1 : 0);
   }
-  return merge_lanes(v);
+  __syncwarp();
+  return n;
 }
-// The n-th largest (n = 1 .. 32) of the lanes' keys, in every lane.  The values alone are sorted; where more of them are equal to the n-th than
-// are needed, the whole keys.
-__device__ __forceinline__ Key nth_largest(Key k, int n) {
-  const int lane = threadIdx.x & 31;
-  const uint32_t mine = uint32_t(k >> 32);
-  uint32_t v = mine;
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-    for (int o = size >> 1; o > 0; o >>= 1) {
-      const uint32_t w = __shfl_xor_sync(0xffffffffu, v, o);
-      v = ((lane & o) == 0) == (size == 32 || (lane & size) == 0) ? max(v, w) : min(v, w);
-    }
-  }
-  const uint32_t at = __shfl_sync(0xffffffffu, v, n - 1);
-  const int above = __popc(__ballot_sync(0xffffffffu, mine > at)), equal = __popc(__ballot_sync(0xffffffffu, mine == at));
-  if (above + equal > n) return __shfl_sync(0xffffffffu, sort_lanes(k), n - 1);
-  const uint32_t low = __reduce_min_sync(0xffffffffu, mine == at ? uint32_t(k) : 0xffffffffu);
-  return (Key(at) << 32) | low;
+// Empty keys made different from one another, and back.
+__device__ __forceinline__ Key distinct(Key k) { return k == 0 ? threadIdx.x & 31 : k; }
+__device__ __forceinline__ Key empty_again(Key k) { return k < 32 ? 0 : k; }
+// Lanes 0 .. 31 in falling order.
+__device__ __forceinline__ Key sort_lanes(Key k, Key* scratch) {
+  k = distinct(k);
+  const int rank = rank_of(k, scratch);
+  scratch[rank] = k;
+  __syncwarp();
+  k = scratch[threadIdx.x & 31];
+  __syncwarp();
+  return empty_again(k);
+}
+// The n-th largest (n = 1 .. 32) of the lanes' keys, in every lane.
+__device__ __forceinline__ Key nth_largest(Key k, int n, Key* scratch) {
+  k = distinct(k);
+  const int rank = rank_of(k, scratch);
+  return empty_again(__shfl_sync(0xffffffffu, k, __ffs(__ballot_sync(0xffffffffu, rank == n - 1)) - 1));
 }
 // The 32 largest of two sets in falling order.
 __device__ __forceinline__ Key merge_sorted(Key a, Key b) { return merge_lanes(larger(a, __shfl_sync(0xffffffffu, b, 31 - (threadIdx.x & 31)))); }
 // The same with 32 keys in any order, of which a later one than `last` in `a` does not count.
-__device__ __forceinline__ void take(Key& a, Key key, int last) {
-  const Key least = __shfl_sync(0xffffffffu, a, last);
-  if (__any_sync(0xffffffffu, key > least)) a = merge_sorted(a, sort_lanes(key));
+__device__ __noinline__ Key taken(Key a, Key key, Key* scratch) { return merge_sorted(a, sort_lanes(key, scratch)); }
+__device__ __forceinline__ void take(Key& a, Key key, int last, Key* scratch) {
+  if (__any_sync(0xffffffffu, key > __shfl_sync(0xffffffffu, a, last))) a = taken(a, key, scratch);
 }
 
 // What is known of a run of elements: reference M (about the maximum; -infinity: no element above it), s = sum 2^d, t = sum 2^d d with d = k (x - M), elements above the target.
@@ -244,6 +247,8 @@ struct Part {                                            // of a divided row, in
 struct LogprobsParams {
   hs_token_logprobs_t a;
   int shares, units_per_row;
+  int parts;                                             // of a row, one a share; 1: whole rows, any number a share; 0: units, cut anywhere
+  int base, more;                                        // rows or units of a share; shares with one more, the first ones
   float k;                                               // scale * log2(e)
 };
 
@@ -261,6 +266,8 @@ struct LpSmem {
   RowPlace place[2];
   uint64_t full[LP_SLOTS], empty[LP_SLOTS], row_full[2], row_empty[2], best_full[2], bound_full[2];
   int abort_flag;
+  Key joined[64];                                        // of the parts of a row
+  alignas(16) Key scratch[2][32];                        // of the warps that keep the bound and end the rows
 };
 
 template <int TYPE>
@@ -292,22 +299,27 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
   }
   if (tid < LP_READERS) sm.place[0].best[warp][lane] = sm.place[1].best[warp][lane] = 0;
   __syncthreads();
-  griddep_wait();
 
-  const int64_t units = int64_t(p.a.n_rows) * upr;
   // A share is a run of segments: units u0 .. u1 - 1 of a row.  Elements are counted from the 16-byte boundary at or below the row's
   // beginning ("virtual" indices); whole pieces of the row are first .. last - 1.
-  auto share_begin = [&](int b) { return units * b / p.shares; };
-  auto share_of = [&](int64_t u) { return int(((u + 1) * p.shares - 1) / units); };
+  auto share_begin = [&](int b) {
+    if (p.parts > 1) return b / p.parts * upr + b % p.parts * upr / p.parts;
+    return (b * p.base + min(b, p.more)) * (p.parts == 1 ? upr : 1);
+  };
+  auto share_of = [&](int u) {                           // (of shares that divide rows)
+    if (p.parts > 1) return u / upr * p.parts + (u % upr == 0 ? 0 : p.parts - 1);        // (asked of a row's first and last unit)
+    const int u_more = p.more * (p.base + 1);
+    return u < u_more ? u / (p.base + 1) : p.more + (u - u_more) / p.base;
+  };
   struct Segment {
     int row, u0, u1, mis, first, last;
     const char* row_p;
   };
-  auto segment_at = [&](int row, int u0, int64_t end) {               // the one that begins with unit u0 of a row, in a share that ends at `end`
+  auto segment_at = [&](int row, int u0, int end) {               // the one that begins with unit u0 of a row, in a share that ends at `end`
     Segment g;
     g.row = row;
     g.u0 = u0;
-    g.u1 = int(std::min<int64_t>(upr, end - int64_t(row) * upr));
+    g.u1 = min(upr, end - row * upr);
     g.mis = int((reinterpret_cast<uintptr_t>(p.a.logits) / L::kSize + uint64_t(g.row) * uint64_t(p.a.row_stride)) % kPer);
     g.first = g.mis ? kPer : 0;
     g.last = (g.mis + vocab) / kPer * kPer;
@@ -315,6 +327,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     return g;
   };
 
+  griddep_wait();
   // (a wait that gives up lets every role go on to its end, past the waits that follow, without what it waited for)
   bool ok = true;
   if (warp < LP_WARPS) {
@@ -323,17 +336,33 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     uint32_t phase = 0, row_phase = 0;
     auto target_of = [&](int row) { return row < p.a.n_rows ? p.a.targets[row] : -1; };
     auto target_logit = [&](const char* row_p, int target) { return target >= 0 && target < vocab ? L::one(row_p, target) : INFINITY; };
+    // the thread's element outside whole pieces, if it has one: in front of the first one (with unit 0), behind the last one
+    auto edge_of = [&](const Segment& g) {
+      const int n_front = g.mis && g.u0 == 0 ? min(g.first - g.mis, vocab) : 0;                     // virtual mis .. first - 1
+      const int tail = max(g.last, min(g.first, g.mis + vocab)), n_back = g.mis + vocab - tail;      // virtual tail .. mis + vocab - 1
+      if (tid < n_front) return tid;
+      return tid >= 32 && tid - 32 < n_back && (tail + tid - 32) / LP_UNIT >= g.u0 && (tail + tid - 32) / LP_UNIT < g.u1 ? tail - g.mis + tid - 32 : -1;
+    };
     for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
-      const int64_t begin = share_begin(share), end = share_begin(share + 1);
-      if (begin >= end) continue;
-      int row = int(begin / upr), u0 = int(begin % upr), target = target_of(row);
-      float x_t = target_logit(segment_at(row, u0, end).row_p, target);
-      for (; int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+      const int begin = share_begin(share), end = share_begin(share + 1);
+      int row = begin / upr, u0 = begin % upr, target = target_of(row);
+      const Segment g0 = segment_at(row, u0, end);
+      int edge = edge_of(g0);
+      float edge_x = edge >= 0 ? L::one(g0.row_p, edge) : 0.f, x_t = target_logit(g0.row_p, target);
+      for (; row * upr + u0 < end; ++row, u0 = 0) {
         const Segment g = segment_at(row, u0, end);
-        const bool more = int64_t(row + 1) * upr < end;  // the share goes on with the next row
+        const bool more = (row + 1) * upr < end;  // the share goes on with the next row
         const int next_target = more ? target_of(row + 1) : -1;
-        float next_x_t = INFINITY;                       // (asked for behind the first tile: a round trip to memory)
-        auto ask_target = [&]() { if (more) next_x_t = target_logit(g.row_p + p.a.row_stride * L::kSize, next_target); };
+        // its target's logit and its elements outside whole pieces are asked for behind this row's first tile: round trips to memory
+        float next_x_t = INFINITY, next_edge_x = 0.f;
+        int next_edge = -1;
+        auto ask_next = [&]() {
+          if (!more) return;
+          const Segment h = segment_at(row + 1, 0, end);
+          next_x_t = target_logit(h.row_p, next_target);
+          next_edge = edge_of(h);
+          if (next_edge >= 0) next_edge_x = L::one(h.row_p, next_edge);
+        };
         const bool count = p.a.rank != nullptr && target >= 0 && target < vocab;
         RowPlace& place = sm.place[at];
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_empty[at], row_phase ^ 1, abort_flag, p.a.status));
@@ -344,20 +373,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           const int i = atomicAdd(&place.n_list, 1);
           if (i < LP_LIST) place.list[i] = make_key(x, v);
         };
-        // the elements outside whole pieces: in front of the first one (with unit 0), behind the last one
-        {
-          const int n_front = g.mis && g.u0 == 0 ? min(g.first - g.mis, vocab) : 0;                     // virtual mis .. first - 1
-          const int tail = max(g.last, min(g.first, g.mis + vocab)), n_back = g.mis + vocab - tail;      // virtual tail .. mis + vocab - 1
-          int v = -1;
-          if (tid < n_front) v = tid;
-          else if (tid >= 32 && tid - 32 < n_back && (tail + tid - 32) / LP_UNIT >= g.u0 && (tail + tid - 32) / LP_UNIT < g.u1) v = tail - g.mis + tid - 32;
-          if (v >= 0) {
-            const float x = L::one(g.row_p, v);
-            m = x;
-            if (x != -INFINITY) s[0] = x - x + 1.f;                    // (NaN of NaN and of infinity)
-            above = x > x_t ? 1 : 0;
-            if (n_top > 0 && x > -INFINITY) push(x, v);
-          }
+        if (edge >= 0) {
+          m = edge_x;
+          if (edge_x != -INFINITY) s[0] = edge_x - edge_x + 1.f;       // (NaN of NaN and of infinity)
+          above = edge_x > x_t ? 1 : 0;
+          if (n_top > 0 && edge_x > -INFINITY) push(edge_x, edge);
         }
         for (int v0 = g.u0 * LP_UNIT; v0 < g.u1 * LP_UNIT; v0 += kTile) {
           const bool first = v0 == g.u0 * LP_UNIT;
@@ -431,7 +451,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             if (n_top > 0) look_for_candidates();
             give_back();
           }
-          if (first) ask_target();
+          if (first) ask_next();
           const bool higher = !(mx <= m) && !((mx - m) * p.k <= kSlack);          // (true of the first element above -infinity, and of NaN)
           if (higher) {
             const float to = max_nan(mx, m), d = max_nan(p.k * (m - to), -200.f), f = exp2f(d);      // (nothing so far: d = -infinity, s = t = 0)
@@ -500,6 +520,8 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         if (lane == 0) mbar_arrive(&sm.row_full[at]);
         if (++at == 2) { at = 0; row_phase ^= 1; }
         x_t = next_x_t;
+        edge = next_edge;
+        edge_x = next_edge_x;
         target = next_target;
       }
     }
@@ -509,8 +531,8 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
       int slot = 0;
       uint32_t phase = 0;
       for (int share = blockIdx.x; share < p.shares && ok; share += gridDim.x) {
-        const int64_t begin = share_begin(share), end = share_begin(share + 1);
-        for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end && ok; ++row, u0 = 0) {
+        const int begin = share_begin(share), end = share_begin(share + 1);
+        for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end && ok; ++row, u0 = 0) {
           const Segment g = segment_at(row, u0, end);
           for (int v = g.u0 * LP_UNIT; v < g.u1 * LP_UNIT; v += kTile) {
             const int lo = max(v, g.first), hi = min(min(v + kTile, g.u1 * LP_UNIT), g.last);
@@ -533,16 +555,17 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     // The first one of a segment from the first tile's largest keys; then again whenever a reader has found a candidate, until the next segment's
     // largest keys are there.  (This warp alone writes the word, and a bound that comes late finds nobody who reads it.)
     if (n_top > 0) {
+      Key* scratch = sm.scratch[0];
       int at = 0;
       uint32_t row_phase = 0;
       for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
-        const int64_t begin = share_begin(share), end = share_begin(share + 1);
-        for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+        const int begin = share_begin(share), end = share_begin(share + 1);
+        for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end; ++row, u0 = 0) {
           if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.best_full[at], row_phase, abort_flag, p.a.status));
           RowPlace& place = sm.place[at];
           const int next = at ^ 1;
           const uint32_t next_phase = at ? row_phase ^ 1 : row_phase;
-          const bool more = int64_t(row + 1) * upr < end || share + int(gridDim.x) < p.shares;
+          const bool more = (row + 1) * upr < end || share + int(gridDim.x) < p.shares;
           Key known = 0;
           for (bool first = true;; first = false) {
             if (lane == 0) place.news = 0;
@@ -550,7 +573,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             Key k = 0;
 #pragma unroll
             for (int q = 0; q < LP_WARPS; ++q) k = larger(k, reinterpret_cast<volatile Key*>(place.best[q])[lane]);
-            const Key bound = nth_largest(k, n_top);
+            const Key bound = nth_largest(k, n_top, scratch);
             if (first || bound > known) {
               known = bound;
               if (lane == 0) *reinterpret_cast<volatile Key*>(&place.bound) = bound;
@@ -576,13 +599,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     }
   } else {
     // ------------------------------------------------------------------ the rows' ends
+    Key* scratch = sm.scratch[1];
     int at = 0;
     uint32_t row_phase = 0;
     int* done_words = reinterpret_cast<int*>(static_cast<char*>(p.a.workspace) + kWsLogprobsDone);
     Part* parts = reinterpret_cast<Part*>(static_cast<char*>(p.a.workspace) + kWsScratch);
     for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
-      const int64_t begin = share_begin(share), end = share_begin(share + 1);
-      for (int row = int(begin / upr), u0 = int(begin % upr); int64_t(row) * upr + u0 < end; ++row, u0 = 0) {
+      const int begin = share_begin(share), end = share_begin(share + 1);
+      for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end; ++row, u0 = 0) {
         const Segment g = segment_at(row, u0, end);
         RowPlace& place = sm.place[at];
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status));
@@ -602,7 +626,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
               Key k = 0;
 #pragma unroll
               for (int q = 0; q < LP_WARPS; ++q) k = larger(k, place.best[q][lane]);
-              const Key bound = nth_largest(k, n_top);
+              const Key bound = nth_largest(k, n_top, scratch);
               int kept = 0;
               for (int i = 0; i < n_list; i += 32) {
                 const Key c = i + lane < n_list ? place.list[i + lane] : 0;
@@ -611,20 +635,20 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
                 kept += __popc(keep);
               }
               __syncwarp();
-              for (int i = 0; i < kept; i += 32) take(top, i + lane < kept ? place.list[i + lane] : 0, n_top - 1);
+              for (int i = 0; i < kept; i += 32) take(top, i + lane < kept ? place.list[i + lane] : 0, n_top - 1, scratch);
             } else {
-              for (int i = 0; i < n_list; i += 32) take(top, i + lane < n_list ? place.list[i + lane] : 0, n_top - 1);
+              for (int i = 0; i < n_list; i += 32) take(top, i + lane < n_list ? place.list[i + lane] : 0, n_top - 1, scratch);
             }
             if (n_list < n_top && ok) {                  // fewer than n_top entries above -infinity: the first that are -infinity
               int have = n_list;
               for (int v = v_lo; v < v_hi && have < n_top; v += 32) {
                 const bool empty = v + lane < v_hi && L::one(g.row_p, v + lane) == -INFINITY;
-                take(top, empty ? make_key(-INFINITY, v + lane) : 0, n_top - 1);
+                take(top, empty ? make_key(-INFINITY, v + lane) : 0, n_top - 1, scratch);
                 have += __popc(__ballot_sync(0xffffffffu, empty));
               }
             }
           } else {
-            for (int v = v_lo; v < v_hi; v += 32) take(top, v + lane < v_hi ? make_key(L::one(g.row_p, v + lane), v + lane) : 0, n_top - 1);
+            for (int v = v_lo; v < v_hi; v += 32) take(top, v + lane < v_hi ? make_key(L::one(g.row_p, v + lane), v + lane) : 0, n_top - 1, scratch);
           }
         }
         // the place goes back to the readers
@@ -638,7 +662,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         bool whole = g.u1 - g.u0 == upr;
         if (!whole) {
           // a divided row: this share's part, and the join where it is the last one to come
-          const int64_t r0 = int64_t(g.row) * upr, r1 = r0 + upr;
+          const int r0 = g.row * upr, r1 = r0 + upr;
           const int f = share_of(r0), l = share_of(r1 - 1);            // shares that hold the row's first and last unit
           Part& part = parts[2 * share + (g.u0 == 0 ? 1 : 0)];         // (the beginning of a row is the share's end)
           if (lane == 0) part.sums = total;
@@ -653,9 +677,29 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             __threadfence();
             const int n_parts = l - f + 1;
             auto part_at = [&](int i) -> const Part& { return parts[2 * (f + i) + (i == 0 ? 1 : 0)]; };
+            // As with the candidates: a key of each part such that no alternative lies below the n-th largest of them (n parts hold at least n_top keys up
+            // to theirs), then what reaches it of all parts' keys, 32 at a time.  What is known from the start is asked for at once.
+            const int known = min(n_parts, 32), depth = (n_top + known - 1) / known, n_keys = n_parts * n_top;
+            Key c[LP_JOIN_LOADS], k = 0;
+            int at_part = n_top > 0 ? lane / n_top : 0, at_key = n_top > 0 ? lane % n_top : 0;
+            const int part_step = n_top > 0 ? 32 / n_top : 0, key_step = n_top > 0 ? 32 % n_top : 0;
+            auto ask_keys = [&]() {
+#pragma unroll
+              for (int j = 0; j < LP_JOIN_LOADS; ++j) {
+                c[j] = at_part < n_parts ? __ldcg(&part_at(at_part).keys[at_key]) : 0;
+                at_part += part_step;
+                at_key += key_step;
+                if (at_key >= n_top) {
+                  at_key -= n_top;
+                  ++at_part;
+                }
+              }
+            };
+            if (n_top > 0) ask_keys();
             total = Sums{-INFINITY, 0.f, 0.f, 0};
             for (int i = lane; i < n_parts; i += 32) {
               const float4 w = __ldcg(reinterpret_cast<const float4*>(&part_at(i).sums));
+              if (n_top > 0) k = larger(k, __ldcg(&part_at(i).keys[depth - 1]));
               Sums v = {w.x, w.y, w.z, __float_as_int(w.w)};
               const float to = max_nan(v.m, total.m);
               raise(v, to, p.k);
@@ -666,16 +710,28 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             }
             total = warp_join(total, p.k);
             if (n_top > 0) {
-              // four parts' keys on their way at a time; each part's are in falling order
+              const Key bound = nth_largest(k, (n_top + depth - 1) / depth, scratch);
+              int held = 0;                              // keys that wait in sm.joined
               top = 0;
-              for (int i0 = 0; i0 < n_parts; i0 += 4) {
-                Key k[4];
+              for (int i0 = 0;;) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) k[i] = i0 + i < n_parts && lane < n_top ? __ldcg(&part_at(i0 + i).keys[lane]) : 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (i0 + i < n_parts) top = merge_sorted(top, k[i]);
+                for (int j = 0; j < LP_JOIN_LOADS; ++j) {
+                  const unsigned keep = __ballot_sync(0xffffffffu, c[j] != 0 && c[j] >= bound);
+                  if (keep == 0) continue;
+                  if (keep >> lane & 1u) sm.joined[held + __popc(keep & ((1u << lane) - 1u))] = c[j];
+                  held += __popc(keep);
+                  __syncwarp();
+                  if (held >= 32) {
+                    held -= 32;
+                    take(top, sm.joined[held + lane], n_top - 1, scratch);
+                  }
+                  __syncwarp();
+                }
+                i0 += 32 * LP_JOIN_LOADS;
+                if (i0 >= n_keys) break;
+                ask_keys();
               }
+              if (held > 0) take(top, lane < held ? sm.joined[lane] : 0, n_top - 1, scratch);
             }
           }
         }
@@ -721,8 +777,18 @@ cudaError_t launch_token_logprobs(const hs_token_logprobs_t& a, int sm_count, in
   p.a = a;
   const int per = a.type == HS_TYPE_F32 ? 4 : 8;
   p.units_per_row = (a.vocab + per - 1 + LP_UNIT - 1) / LP_UNIT;
-  const int64_t units = int64_t(a.n_rows) * p.units_per_row;
-  p.shares = int(std::max<int64_t>(1, std::min<int64_t>(share_count(sm_count), units / LP_MIN_UNITS)));
+  const int units = a.n_rows * p.units_per_row;           // (below 2^31: checked)
+  // By what the longest share takes, in units of 1024 elements: whole rows, equal parts of each row, or equal shares that are cut anywhere.
+  const int most = share_count(sm_count), upr = p.units_per_row;
+  const int parts = std::min(most / std::min(a.n_rows, most), upr / LP_MIN_UNITS);
+  const int64_t whole = int64_t((a.n_rows + most - 1) / most) * (upr + LP_ROW_COST);
+  const int64_t divided = parts > 1 ? (upr + parts - 1) / parts + LP_ROW_COST + LP_JOIN_COST : whole;
+  const int64_t anywhere = units / most + (a.n_rows / most + 2) * LP_ROW_COST + LP_JOIN_COST;
+  p.parts = whole <= std::min(divided, anywhere) ? 1 : divided <= anywhere ? parts : 0;
+  const int pieces = p.parts > 0 ? a.n_rows * p.parts : units;
+  p.shares = std::min(most, pieces);
+  p.base = pieces / p.shares;
+  p.more = pieces % p.shares;
   p.k = float(double(a.scale) * 1.4426950408889634074);
   const int grid = std::min(p.shares, sm_budget);
   if (a.type == HS_TYPE_F32) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F32>, grid, LP_THREADS, kLpSmem, stream, true, p);
