@@ -37,7 +37,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 10.f;                                                             // log2 units that a logit may lie above its thread's reference
 
 // 16-byte pieces of logits as 32-bit words.  kFloor: what stands for -infinity where its weight is to be 0 and its distance finite; right
-// for rows whose maximum is above kLow.
+// for rows whose maximum lies between kLow and -kLow.
 template <int TYPE>
 struct Logit;
 template <>
@@ -327,7 +327,6 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     return g;
   };
 
-  griddep_wait();
   // (a wait that gives up lets every role go on to its end, past the waits that follow, without what it waited for)
   bool ok = true;
   if (warp < LP_WARPS) {
@@ -343,11 +342,12 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
       if (tid < n_front) return tid;
       return tid >= 32 && tid - 32 < n_back && (tail + tid - 32) / LP_UNIT >= g.u0 && (tail + tid - 32) / LP_UNIT < g.u1 ? tail - g.mis + tid - 32 : -1;
     };
-    for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
-      const int begin = share_begin(share), end = share_begin(share + 1);
-      int row = begin / upr, u0 = begin % upr, target = target_of(row);
-      const Segment g0 = segment_at(row, u0, end);
-      int edge = edge_of(g0);
+    int begin = share_begin(blockIdx.x), end = share_begin(blockIdx.x + 1);
+    Segment g0 = segment_at(begin / upr, begin % upr, end);
+    int edge = edge_of(g0);
+    griddep_wait();                                      // (the divisions do not wait for the kernel in front)
+    for (int share = blockIdx.x; share < p.shares;) {
+      int row = g0.row, u0 = g0.u0, target = target_of(row);
       float edge_x = edge >= 0 ? L::one(g0.row_p, edge) : 0.f, x_t = target_logit(g0.row_p, target);
       for (; row * upr + u0 < end; ++row, u0 = 0) {
         const Segment g = segment_at(row, u0, end);
@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             // loop, it held its warp up for 3300 cycles, longer than two tiles take.)
             for (unsigned who = __ballot_sync(0xffffffffu, reaches(mx, lo - g.mis)); who; who &= who - 1) {
               const int of = __ffs(who) - 1;
+              const float top = __shfl_sync(0xffffffffu, mx, of);
 #pragma unroll 1
               for (int e0 = 0; e0 < LP_PIECES * kPer; e0 += 32) {
                 const int e = e0 + lane, i = (e / kPer * LP_READERS + warp * 32 + of) * kPer + e % kPer, v = lo - g.mis + i;
@@ -421,17 +422,17 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
                 const bool hit = x > -INFINITY && reaches(x, v);
                 const unsigned hits = __ballot_sync(0xffffffffu, hit);
                 if (hits == 0) continue;
-                const uint32_t top = __reduce_max_sync(0xffffffffu, hit ? ordered(x) : 0u);
-                const int at_v = int(__reduce_min_sync(0xffffffffu, hit && ordered(x) == top ? unsigned(v) : 0xffffffffu));
+                const Key key = make_key(x, v);
+                const unsigned at_top = __ballot_sync(0xffffffffu, x == top);
+                const Key largest = __shfl_sync(0xffffffffu, key, __ffs(at_top | 0x80000000u) - 1);
                 int i_list = 0;
                 if (lane == 0) {
                   i_list = atomicAdd(&place.n_list, __popc(hits));
-                  const Key k = make_key(unordered(top), at_v);
-                  if (k > place.best[warp][of]) place.best[warp][of] = k;
+                  if (at_top != 0 && largest > place.best[warp][of]) place.best[warp][of] = largest;
                   place.news = 1;
                 }
                 i_list = __shfl_sync(0xffffffffu, i_list, 0) + __popc(hits & ((1u << lane) - 1u));
-                if (hit && i_list < LP_LIST) place.list[i_list] = make_key(x, v);
+                if (hit && i_list < LP_LIST) place.list[i_list] = key;
               }
             }
           };
@@ -464,7 +465,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             if (to == INFINITY) s[0] = to - to;          // (a row with infinity has no sum)
           }
           const float from = m == -INFINITY ? 0.f : m, c = -from * p.k;
-          const bool apart = !full || !(from > L::kLow) || p.k > 100.f;         // one piece after the other: a ragged chunk, or logits near the type's lowest (or NaN)
+          // one piece after the other: a tile that holds little (a round of pieces takes 390 cycles so, eight take 1200 otherwise), or logits near the
+          // type's limits (or NaN)
+          const bool apart = pieces <= 3 * LP_READERS || !(fabsf(from) < -L::kLow) || p.k > 100.f;
           if (!apart) {
 #pragma unroll
             for (int i = 0; i < LP_PIECES; ++i) {
@@ -524,9 +527,17 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         edge_x = next_edge_x;
         target = next_target;
       }
+      share += gridDim.x;
+      if (share < p.shares) {
+        begin = share_begin(share);
+        end = share_begin(share + 1);
+        g0 = segment_at(begin / upr, begin % upr, end);
+        edge = edge_of(g0);
+      }
     }
   } else if (warp == LP_WARPS + 2) {
     // ------------------------------------------------------------ the tiles' requests
+    griddep_wait();
     if (lane == 0) {
       int slot = 0;
       uint32_t phase = 0;
@@ -554,6 +565,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     // --------------------------------------------------------------- the bounds of rows
     // The first one of a segment from the first tile's largest keys; then again whenever a reader has found a candidate, until the next segment's
     // largest keys are there.  (This warp alone writes the word, and a bound that comes late finds nobody who reads it.)
+    griddep_wait();
     if (n_top > 0) {
       Key* scratch = sm.scratch[0];
       int at = 0;
@@ -599,6 +611,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
     }
   } else {
     // ------------------------------------------------------------------ the rows' ends
+    griddep_wait();
     Key* scratch = sm.scratch[1];
     int at = 0;
     uint32_t row_phase = 0;
