@@ -25,6 +25,11 @@ namespace {
 constexpr int PD_WARPS = 8, PD_THREADS = PD_WARPS * 32;
 constexpr int PD_RING_BYTES = 192 * 1024;
 constexpr int PD_MIN_PAGES = 16;                 // of a share: two per warp
+// How the line is cut, by what the longest share has to do in pages: a join of shares takes as long as PD_JOIN_COST pages and one for each part; cuts inside
+// groups, which give a block two groups and two joins, as PD_CUT_COST.  us by groups / anywhere: 2 sequences of 81 keys, 16 heads on 4 of 128, 6.7 /
+// 13.4; 16 of 128 .. 1024, 16 on 4 of 64, 12.0 / 14.3; 3 of 20001 .. 32768, 16 on 2 of 128, 24.3 / 29.0; 64 of 512 .. 4096, 28 on 4 of 128, 68.0 / 63.1;
+// 47 of 2713, 28 on 4 of 64, 47.6 / 38.6.
+constexpr int PD_MIN_PART = 8, PD_JOIN_COST = 20, PD_CUT_COST = 66;
 constexpr int PD_WORDS = 160;                     // 32-bit words of shared memory in front of the sequences' page counts
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -33,6 +38,7 @@ struct DecodeParams {
   hs_paged_attention_t a;
   ScoreScale score;
   int shares, chunks;                            // chunks: groups per KV head
+  int groups, parts;                             // most whole groups that a share can have; parts of a group that there are shares for
 };
 
 template <int DH>
@@ -252,7 +258,7 @@ struct GroupState {
 struct Cut {
   int g0, g1;                                            // the group's place in the line; g1 = 0: nothing
   void* part;
-  int row, head0, heads;
+  int row, head0, heads, group;                          // group: its number, sequence by sequence
 };
 
 template <int DH, int NT, bool F16, bool MOD>
@@ -266,8 +272,8 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   int* words = reinterpret_cast<int*>(full_all + PD_WARPS * SLOTS);
   volatile int* abort_flag = words;
   int* last = words + 1;                                 // of the runs, those whose shares this block joins
-  int* warp_sum = words + 4;                             // [8]
-  Cut(*cuts)[2] = reinterpret_cast<Cut(*)[2]>(words + 16);              // [8][2]
+  int *warp_sum = words + 2, *warp_max = words + 10;     // [8] each
+  Cut(*cuts)[2] = reinterpret_cast<Cut(*)[2]>(words + 20);              // [8][2]
   int* page_begin = words + PD_WORDS;                    // [n_seqs + 1]
   const hs_paged_attention_t& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -282,9 +288,10 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   griddep_wait();
 
   // ---------------------------------------------------------------- the plan
+  int most_pages = 0;                                    // of a group
   {
     const int per = (n + PD_THREADS - 1) / PD_THREADS, s0 = tid * per;
-    int mine = 0;
+    int mine = 0, longest = 0;
     for (int i = 0; i < per; ++i) {
       const int s = s0 + i;
       if (s >= n) break;
@@ -300,6 +307,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
       }
       page_begin[s] = mine;
       mine += pages;
+      longest = max(longest, pages);
     }
     int inc = mine;
 #pragma unroll
@@ -307,22 +315,46 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
       const int x = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += x;
     }
-    if (lane == 31) warp_sum[warp] = inc;
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (lane == 31) {
+      warp_sum[warp] = inc;
+      warp_max[warp] = longest;
+    }
     __syncthreads();
     int before = inc - mine, total = 0;
     for (int w = 0; w < PD_WARPS; ++w) {
       if (w < warp) before += warp_sum[w];
       total += warp_sum[w];
+      most_pages = max(most_pages, warp_max[w]);
     }
     for (int i = 0; i < per && s0 + i < n; ++i) page_begin[s0 + i] += before;
     if (tid == 0) page_begin[n] = total;
     __syncthreads();
   }
-  // (the host has seen to it that places in the line are 32-bit numbers.)  Shares: the first `more` ones have one page more.
-  const int line = page_begin[n] * units;
-  const int shares = min(p.shares, max(1, line / PD_MIN_PAGES)), base = line / shares, more = line - base * shares;
-  auto share_begin = [&](int b) { return base * b + min(b, more); };
+  // (the host has seen to it that places in the line are 32-bit numbers.)  Shares are whole groups, p.groups or one fewer each; or parts of `part` pages
+  // of a group, as many shares for each as the longest has parts; or equal pieces of the line, the first `more` ones with one page more.
+  const int line = page_begin[n] * units, equal = max(line / p.shares, PD_MIN_PAGES);
+  const int parts = min(p.parts, max(int(sqrtf(float(most_pages))), 1)), part = max((most_pages + parts - 1) / parts, PD_MIN_PART);
+  const int whole_cost = p.groups * most_pages, part_cost = p.parts > 1 ? part + PD_JOIN_COST + parts : whole_cost;
+  const bool by_groups = min(whole_cost, part_cost) <= equal + PD_JOIN_COST + PD_CUT_COST + most_pages / equal;
+  const int per_group = !by_groups ? 0 : whole_cost <= part_cost ? 1 : (most_pages + part - 1) / part;        // shares; 1: whole groups
+  const int cuttable = per_group == 0 ? line : n * units * per_group;
+  const int shares = per_group == 0 ? min(p.shares, max(1, line / PD_MIN_PAGES)) : min(p.shares, cuttable), base = cuttable / shares, more = cuttable - base * shares;
+  auto group_begin = [&](int g) {
+    const int s = min(g / units, n), pages = s < n ? page_begin[s + 1] - page_begin[s] : 0;
+    return page_begin[s] * units + (g - s * units) * pages;
+  };
+  auto share_begin = [&](int b) {
+    if (per_group > 1) {
+      const int g = b / per_group, s = min(g / units, n), pages = s < n ? page_begin[s + 1] - page_begin[s] : 0;
+      return page_begin[s] * units + (g - s * units) * pages + min((b - g * per_group) * part, pages);
+    }
+    const int x = base * b + min(b, more);
+    return per_group == 1 ? group_begin(x) : x;
+  };
   auto share_of = [&](int x) { return x < more * (base + 1) ? x / (base + 1) : more + (x - more * (base + 1)) / max(base, 1); };
+  auto first_share = [&](int g0, int group) { return per_group > 1 ? group * per_group : share_of(g0); };          // of a divided group
+  auto last_share = [&](int g0, int g1, int group) { return per_group > 1 ? group * per_group + (g1 - g0 - 1) / part : share_of(g1 - 1); };
 
   Part* warp_parts = reinterpret_cast<Part*>(static_cast<char*>(a.workspace) + kWsScratch);          // [share][warp]
   Part* share_parts = warp_parts + size_t(kMaxShares) * PD_WARPS;                                    // [share][2]
@@ -402,7 +434,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
         // (at the end of its piece the warp's ring is idle and takes the part; before that it goes to the workspace)
         Part* part = at_end ? reinterpret_cast<Part*>(ring) : warp_parts + share * PD_WARPS + warp;
         st.put(part, heads, lane);
-        if (lane == 0) cuts[warp][slot] = Cut{g0, g1, part, int(row), (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT, heads};
+        if (lane == 0) cuts[warp][slot] = Cut{g0, g1, part, int(row), (unit / p.chunks) * heads_all + (unit % p.chunks) * 8 * NT, heads, seq * units + unit};
       }
     };
     for (int i = 0; i < n_pages; ++i) {
@@ -457,6 +489,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
     // cut there (place 0); the next warps' parts of it are in their places 0.  First the parts of this share are joined, then, where this block is the
     // last one of a group's to come, the shares' -- by the same instructions: this code runs once a launch, and what it took was the time to fetch it.
     const int my_g0 = lane < 2 * PD_WARPS ? cuts[lane >> 1][lane & 1].g0 : 0, my_g1 = lane < 2 * PD_WARPS ? cuts[lane >> 1][lane & 1].g1 : 0;
+    const int my_group = lane < 2 * PD_WARPS ? cuts[lane >> 1][lane & 1].group : 0;
     const bool begins = my_g1 > 0 && (lane == 0 || (lane & 1));          // (of each warp's lanes: a place that a run begins with)
     unsigned todo = __ballot_sync(0xffffffffu, begins);
 #pragma unroll 1
@@ -469,7 +502,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
         __syncthreads();
         bool is_last = false;
         if (warp == 0 && todo >> lane & 1u) {
-          const int f = share_of(my_g0), e = share_of(my_g1 - 1);
+          const int f = first_share(my_g0, my_group), e = last_share(my_g0, my_g1, my_group);
           is_last = atomicAdd(done_words + f, 1) == e - f;
           if (is_last) done_words[f] = 0;                // ready for the next call
         }
@@ -492,8 +525,8 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
         if (pass == 0) {
           n_parts += __popc(__ballot_sync(0xffffffffu, !(lane & 1) && lane > k && my_g1 > 0 && my_g0 == g0));
         } else {
-          f = share_of(g0);
-          n_parts = share_of(g1 - 1) - f + 1;
+          f = first_share(g0, cut.group);
+          n_parts = last_share(g0, g1, cut.group) - f + 1;
         }
 #pragma unroll 1
         for (int i = tid; i < cut.heads * (DH / 4); i += PD_THREADS) {
@@ -588,6 +621,9 @@ cudaError_t launch_paged_decode(const hs_paged_attention_t& a, const CUtensorMap
   const int heads = a.n_q_heads / a.n_kv_heads;
   const bool two = heads > 8;
   p.chunks = (heads + (two ? 16 : 8) - 1) / (two ? 16 : 8);
+  const int n_groups = a.n_seqs * a.n_kv_heads * p.chunks;
+  p.groups = (n_groups + p.shares - 1) / p.shares;
+  p.parts = std::max(p.shares / n_groups, 1);
   const int grid = std::min(p.shares, sm_budget);
   return launch_step_kernel(pick(a.head_dim, two, a.type == HS_TYPE_F16, a.cap > 0.f || a.slopes != nullptr), grid, PD_THREADS,
                             a.head_dim == 128 ? pd_smem<128>() : pd_smem<64>(), stream, true, p);
