@@ -166,7 +166,7 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t* a, int32_t sm_budg
   if (!encode_rows(&tm_kv, a->kv_pool, rows, a->head_dim, a->head_dim, kPage) ||
       !encode_rows(&tm_q, a->q, a->n_tokens, q_row, a->q_stride, paged_chunk_tile_tokens(a->n_q_heads, a->n_kv_heads)))
     return report_cuda_error("tensor map", cudaErrorInvalidValue);
-  return launched("paged chunk attention", launch_paged_chunk(*a, tm_kv, tm_q, sm_budget, stream));
+  return launched("paged chunk attention", launch_paged_chunk(*a, tm_kv, tm_q, d->sm_count, sm_budget, stream));
 }
 
 hs_status_t hs_op_token_logprobs(const hs_token_logprobs_t* a, int32_t sm_budget, void* cuda_stream) {

@@ -13,6 +13,7 @@ constexpr size_t kWsTables = 0;              // one word: blocks that are done
 constexpr size_t kWsAttnDone = 1024;         // one word per share: parts delivered of the group that begins in it
 constexpr size_t kWsLogprobsDone = 4096;     // the same for logit rows
 constexpr size_t kWsChunkQueue = 8192;       // work queue of the chunk attention, and blocks that have left it
+constexpr size_t kWsChunkDone = 16 << 10;    // its divided items: warps' rows of parts delivered, tile by tile
 constexpr size_t kWsScratch = 64 << 10;
 constexpr size_t kWsScratchBytes = HS_DEVICE_WORKSPACE_BYTES - kWsScratch;
 // Shares that the work of a split operator is cut into: one per SM of the device, never more than this.
@@ -33,7 +34,7 @@ cudaError_t launch_rope_cache(const hs_rope_cache_t& a, int sm_budget, cudaStrea
 cudaError_t paged_decode_set_attributes();
 cudaError_t launch_paged_decode(const hs_paged_attention_t& a, const CUtensorMap& tm_kv_page, int sm_count, int sm_budget, cudaStream_t stream);
 cudaError_t paged_chunk_set_attributes();
-cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_budget, cudaStream_t stream);
+cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_count, int sm_budget, cudaStream_t stream);
 int paged_chunk_tile_tokens(int n_q_heads, int n_kv_heads);      // token rows of tm_q's box
 
 cudaError_t token_logprobs_set_attributes();

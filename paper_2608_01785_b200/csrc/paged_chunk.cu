@@ -12,6 +12,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_scores.cuh"
 
@@ -20,6 +21,9 @@ namespace {
 
 constexpr int PC_THREADS = 448, PC_KEYS = 64, PC_STAGES = 4;
 constexpr int PC_TMEM = 512;
+constexpr int PC_MIN_BLOCKS = 4, PC_DIVIDED = 12;       // key blocks of a part of an item; of an item that is divided
+constexpr int PC_JOIN_ROWS = 2;
+constexpr float PC_JOIN_FACTOR = 3.f;
 constexpr int PC_HEADS = 16;               // query heads of an item at most: eight tokens of each fill a tile
 constexpr float kRefSlack = 8.f;           // log2 units by which a row's running maximum may exceed its reference
 constexpr float kLn2 = 0.6931471805599453f;
@@ -29,7 +33,7 @@ struct Geom {
   static constexpr int HALVES = DH / 64;
   static constexpr int Q_BYTES = HALVES * 16384;        // one tile: [half][128 rows][128 B]
   static constexpr int KV_BYTES = HALVES * 8192;        // K (or V) of one block: [half][4 pages][16 keys][128 B]
-  static constexpr int SMEM = 1024 + 2 * Q_BYTES + 2 * PC_STAGES * KV_BYTES + 1024 + (HS_DEVICE_MAX_SEQS + 1) * 4;
+  static constexpr int SMEM = 1024 + 2 * Q_BYTES + 2 * PC_STAGES * KV_BYTES + 1024 + (HS_DEVICE_MAX_SEQS + 1) * 4 + kMaxShares * 4;
   // tensor-memory columns: S(tile, buffer) at tile * 128 + buffer * 64, P over its first 32 columns; O(tile) at 256 + tile * DH
   static constexpr int S0 = 0, O0 = 256;
 };
@@ -40,18 +44,36 @@ struct ChunkParams {
   hs_paged_attention_t a;
   ScoreScale score;
   int chunks, tile_tokens;                 // groups of heads per KV head; tokens per tile
+  int shares;                              // items or parts of items that the device works on at a time
 };
 
-// Geometry of one item, the same in every role.
+// How the items' keys are divided: into parts of `blocks` key blocks, `parts` for the longest.
+struct Division {
+  int parts, blocks;
+};
+// A tile's part of an item in the workspace: outputs relative to the row's reference, then (reference in log2 units, sum) per row.
+template <int DH>
+struct TilePart {
+  float o[128][DH];
+  float2 ml[128];
+};
+
+// Geometry of one item, or of one part of it, the same in every role.
 struct ItemView {
-  int valid;                         // 0: no more items
+  int valid;                         // 0: no more items; -1: a part without key blocks
   int seq, head0, hk, heads;         // first query head, KV head, query heads
   int row0, pos0;                    // first token row and its position
-  int n_tok_t[2];                    // tokens of tile A / B (0 = tile absent)
+  int n_tok_a, n_tok_b;              // tokens of tile A / B (0 = tile absent)
   int kv, prefix, from, end;         // keys of the sequence; seen by some row: j < prefix, or from <= j < end
   int n_prefix, first;               // key blocks 0 .. n_prefix - 1, then first, first + 1, ..
-  int nblk_t[2], nblk;               // key blocks per tile and of the item
-  __device__ __forceinline__ int key0(int j) const { return (j < n_prefix ? j : first + j - n_prefix) * PC_KEYS; }
+  int item, part, parts_a, parts_b;  // the item's number, which of its parts, and how many each tile has (1: not divided)
+  int block0;                        // the part's first key block
+  int nblk_a, nblk_b, nblk;          // key blocks per tile and of the part
+  template <bool DIVIDED>
+  __device__ __forceinline__ int key0(int j) const {
+    if (DIVIDED) j += block0;
+    return (j < n_prefix ? j : first + j - n_prefix) * PC_KEYS;
+  }
   // Whether some row sees key j, a key of the page that begins at k0, every key of the block that begins at k0.
   __device__ __forceinline__ bool sees(int j) const { return j < prefix || (j >= from && j < end); }
   __device__ __forceinline__ bool sees_page(int k0) const { return k0 < prefix || (k0 + 15 >= from && k0 < end); }
@@ -66,8 +88,8 @@ struct Barriers {
   uint64_t ring_full[2], ring_empty[2];
   ItemView ring_view[2];
   uint32_t tmem_base;
-  int abort_flag;
-  int warp_sum[PC_THREADS / 32];
+  int abort_flag, n_joins;
+  int warp_sum[PC_THREADS / 32], warp_most[PC_THREADS / 32];
 };
 static_assert(sizeof(Barriers) <= 1024, "barrier block");
 
@@ -99,11 +121,17 @@ __host__ __device__ constexpr uint32_t idesc_16(int M, int N) {
 // The n lowest bits (all for n >= 32, none for n <= 0).
 __device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-__device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* item_begin, int idx) {
+template <bool DIVIDED>
+__device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* item_begin, Division div, int idx) {
   ItemView v{};
   const hs_paged_attention_t& a = p.a;
   const int n = a.n_seqs, units = a.n_kv_heads * p.chunks, heads_all = a.n_q_heads / a.n_kv_heads, Mt = p.tile_tokens;
-  const int pair = idx / units, unit = idx - pair * units;
+  v.item = idx;
+  if (DIVIDED) {
+    v.item = idx / div.parts;
+    v.part = idx - v.item * div.parts;
+  }
+  const int pair = v.item / units, unit = v.item - pair * units;
   if (pair >= item_begin[n]) return v;
   int lo = 0, hi = n;
   while (hi - lo > 1) {
@@ -123,8 +151,8 @@ __device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* i
   v.row0 = sv.row + tok;
   v.pos0 = sv.kv - sv.rows + tok;
   const int n_tok = min(sv.rows - tok, 2 * Mt);
-  v.n_tok_t[0] = min(n_tok, Mt);
-  v.n_tok_t[1] = n_tok - v.n_tok_t[0];
+  v.n_tok_a = min(n_tok, Mt);
+  v.n_tok_b = n_tok - v.n_tok_a;
   v.kv = sv.kv;
   v.prefix = sv.prefix;
   v.from = a.window > 0 && v.pos0 >= a.window ? v.pos0 - a.window + 1 : 0;
@@ -132,13 +160,95 @@ __device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* i
   v.n_prefix = (v.prefix + PC_KEYS - 1) / PC_KEYS;
   v.first = max(v.from / PC_KEYS, v.n_prefix);
   // (at least one block, so that rows that see no key take the same way)
-  v.nblk_t[0] = max(v.n_prefix + max((max(v.pos0 + v.n_tok_t[0], 0) + PC_KEYS - 1) / PC_KEYS - v.first, 0), 1);
-  v.nblk_t[1] = v.n_tok_t[1] > 0 ? max(v.n_prefix + max((v.end + PC_KEYS - 1) / PC_KEYS - v.first, 0), 1) : 0;
-  v.nblk = max(v.nblk_t[0], v.nblk_t[1]);
+  v.nblk_a = max(v.n_prefix + max((max(v.pos0 + v.n_tok_a, 0) + PC_KEYS - 1) / PC_KEYS - v.first, 0), 1);
+  v.nblk_b = v.n_tok_b > 0 ? max(v.n_prefix + max((v.end + PC_KEYS - 1) / PC_KEYS - v.first, 0), 1) : 0;
+  v.parts_a = v.parts_b = 1;
+  if (DIVIDED && div.parts > 1) {
+    v.block0 = v.part * div.blocks;
+    v.parts_a = (v.nblk_a + div.blocks - 1) / div.blocks;
+    v.parts_b = (v.nblk_b + div.blocks - 1) / div.blocks;
+    v.nblk_a = min(max(v.nblk_a - v.block0, 0), div.blocks);
+    v.nblk_b = min(max(v.nblk_b - v.block0, 0), div.blocks);
+  }
+  v.nblk = max(v.nblk_a, v.nblk_b);
+  if (DIVIDED && v.nblk == 0) v.valid = -1;
   return v;
 }
 
-template <int DH, bool F16, bool MOD>
+// Joins the parts of a tile's rows, in order, by all warps of the block: the lanes lie along a row, PC_JOIN_ROWS rows of a warp and eight parts of each are on
+// their way at a time.
+template <int DH, bool F16>
+__device__ __forceinline__ void join_tile(const ChunkParams& p, const ItemView& v, Division div, int t) {
+  using Vec = std::conditional_t<DH == 128, float4, float2>;
+  const hs_paged_attention_t& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Mt = p.tile_tokens;
+  const int n_tok = t ? v.n_tok_b : v.n_tok_a, n_parts = t ? v.parts_b : v.parts_a, n_rows = v.heads * n_tok;
+  const TilePart<DH>* tile_parts = reinterpret_cast<const TilePart<DH>*>(static_cast<const char*>(a.workspace) + kWsScratch) + v.item * div.parts * 2 + t;
+#pragma unroll 1
+  for (int q0 = warp * PC_JOIN_ROWS; q0 < n_rows; q0 += PC_THREADS / 32 * PC_JOIN_ROWS) {
+    int r[PC_JOIN_ROWS];
+    float top[PC_JOIN_ROWS], l[PC_JOIN_ROWS], o[PC_JOIN_ROWS][4];
+#pragma unroll
+    for (int i = 0; i < PC_JOIN_ROWS; ++i) {
+      const int q = min(q0 + i, n_rows - 1);
+      r[i] = q / n_tok * Mt + q % n_tok;
+      top[i] = -INFINITY;
+      l[i] = o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    }
+#pragma unroll 1
+    for (int k0 = 0; k0 < n_parts; k0 += 8) {
+      Vec x[PC_JOIN_ROWS][8];
+      float2 ml[PC_JOIN_ROWS];                           // of part k0 + lane % 8
+#pragma unroll
+      for (int i = 0; i < PC_JOIN_ROWS; ++i) {
+        ml[i] = k0 + (lane & 7) < n_parts ? __ldcg(&tile_parts[2 * (k0 + (lane & 7))].ml[r[i]]) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[i][u] = __ldcg(reinterpret_cast<const Vec*>(tile_parts[2 * min(k0 + u, n_parts - 1)].o[r[i]]) + lane);
+      }
+#pragma unroll
+      for (int i = 0; i < PC_JOIN_ROWS; ++i) {
+        float next = fmaxf(ml[i].x, __shfl_xor_sync(0xffffffffu, ml[i].x, 1));
+        next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, 2));
+        next = fmaxf(fmaxf(next, __shfl_xor_sync(0xffffffffu, next, 4)), top[i]);
+        const float zero = next == -INFINITY ? 0.f : next, f0 = fast_exp2(top[i] - zero), f = fast_exp2(ml[i].x - zero);      // (0 for a part that is not there)
+        top[i] = next;
+        float sum = f * ml[i].y;
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+        l[i] = fmaf(l[i], f0, sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] *= f0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float w = __shfl_sync(0xffffffffu, f, u);
+          o[i][0] = fmaf(w, x[i][u].x, o[i][0]);
+          o[i][1] = fmaf(w, x[i][u].y, o[i][1]);
+          if constexpr (DH == 128) {
+            o[i][2] = fmaf(w, x[i][u].z, o[i][2]);
+            o[i][3] = fmaf(w, x[i][u].w, o[i][3]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PC_JOIN_ROWS; ++i) {
+      if (q0 + i >= n_rows) break;
+      const int64_t row = v.row0 + t * Mt + r[i] % Mt;
+      const int head = v.head0 + r[i] / Mt;
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH);
+      if constexpr (DH == 128) {
+        reinterpret_cast<uint2*>(dst)[lane] = make_uint2(pack_16<F16>(o[i][0] * inv, o[i][1] * inv), pack_16<F16>(o[i][2] * inv, o[i][3] * inv));
+      } else {
+        dst[lane] = pack_16<F16>(o[i][0] * inv, o[i][1] * inv);
+      }
+      if (lane == 0 && a.lse) a.lse[row * a.n_q_heads + head] = l[i] == 0.f ? -INFINITY : kLn2 * (top[i] + log2f(l[i]));
+    }
+  }
+}
+
+template <int DH, bool F16, bool MOD, bool DIVIDED>
 __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid_constant__ ChunkParams p) {
   using G_ = Geom<DH>;
   extern __shared__ uint8_t smem_raw[];
@@ -148,6 +258,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   uint8_t* v_smem = k_smem + PC_STAGES * G_::KV_BYTES;
   Barriers* bar = reinterpret_cast<Barriers*>(v_smem + PC_STAGES * G_::KV_BYTES);
   int* item_begin = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(bar) + 1024);
+  int* joins = item_begin + HS_DEVICE_MAX_SEQS + 1;         // [tiles of divided items]: those that this block joins
   volatile int* abort_flag = &bar->abort_flag;
   const hs_paged_attention_t& a = p.a;
 
@@ -175,6 +286,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       mbar_init(&bar->ring_empty[i], 13);     // eight softmax warps, two MMA warps, three further producers
     }
     bar->abort_flag = 0;
+    bar->n_joins = 0;
     fence_barrier_init();
     tma_prefetch_desc(&p.tm_kv);
     tma_prefetch_desc(&p.tm_q);
@@ -188,15 +300,18 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   tc_fence_after_sync();
   const uint32_t tmem = bar->tmem_base;
   griddep_wait();
+  Division div = {1, 0};
   {
-    // the plan: pairs of tiles of all sequences, summed
+    // the plan: pairs of tiles of all sequences, summed, and the most key blocks that one can have
     const int n = a.n_seqs, per = (n + PC_THREADS - 1) / PC_THREADS, s0 = int(threadIdx.x) * per;
-    int mine = 0;
+    int mine = 0, most = 1;
     for (int i = 0; i < per && s0 + i < n; ++i) {
       const SeqView v = view_seq(a, s0 + i);
       if (v.error && blockIdx.x == 0) atomicExch(a.status, v.error);
       item_begin[s0 + i] = mine;
       mine += (v.rows + 2 * Mt - 1) / (2 * Mt);
+      const int all = (v.kv + PC_KEYS - 1) / PC_KEYS;
+      if (DIVIDED && v.rows > 0) most = max(most, a.window > 0 ? min(all, (v.prefix + PC_KEYS - 1) / PC_KEYS + (min(a.window, v.kv) + min(v.rows, 2 * Mt)) / PC_KEYS + 2) : all);
     }
     int inc = mine;
 #pragma unroll
@@ -204,15 +319,28 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       const int x = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += x;
     }
-    if (lane == 31) bar->warp_sum[warp] = inc;
+    if (DIVIDED) most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) {
+      bar->warp_sum[warp] = inc;
+      if (DIVIDED) bar->warp_most[warp] = most;
+    }
     __syncthreads();
     int before = inc - mine, total = 0;
     for (int w = 0; w < PC_THREADS / 32; ++w) {
       if (w < warp) before += bar->warp_sum[w];
       total += bar->warp_sum[w];
+      if (DIVIDED) most = max(most, bar->warp_most[w]);
     }
     for (int i = 0; i < per && s0 + i < n; ++i) item_begin[s0 + i] += before;
     if (threadIdx.x == 0) item_begin[n] = total;
+    // Where the items are at most half of what the device works on, long ones are divided.  (A part more costs the join about as much as a block: most is
+    // gained at the square root.)
+    const int items = total * a.n_kv_heads * p.chunks;
+    if (DIVIDED && items > 0 && 2 * items <= p.shares && most >= PC_DIVIDED) {
+      const int parts = min(p.shares / items, int(sqrtf(PC_JOIN_FACTOR * float(most))));
+      div.blocks = max((most + parts - 1) / parts, PC_MIN_BLOCKS);
+      div.parts = (most + div.blocks - 1) / div.blocks;
+    }
     __syncthreads();
   }
 
@@ -229,7 +357,14 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
     const int kv = pi >> 1, w0 = (pi & 1) * 2;          // K or V; first of its two pages in a block
     int q_next = int(blockIdx.x);                       // lane 0 of the lead: the next item's number
     ItemView v_next{};
-    if (pi == 0 && lane == 0) v_next = make_view(p, item_begin, q_next);
+    auto next_view = [&]() {
+      v_next = make_view<DIVIDED>(p, item_begin, div, q_next);
+      while (DIVIDED && v_next.valid < 0) {                          // (the queue ends)
+        q_next = int(gridDim.x) + atomicAdd(queue, 1);
+        v_next = make_view<DIVIDED>(p, item_begin, div, q_next);
+      }
+    };
+    if (pi == 0 && lane == 0) next_view();
     for (;;) {
       bool ok = true;
       ItemView v;
@@ -259,7 +394,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       auto page_id = [&](int j0) {
         const int j = j0 + (lane >> 2);
         if (j >= v.nblk) return -1;
-        const int k0 = v.key0(j) + (lane & 3) * 16;
+        const int k0 = v.template key0<DIVIDED>(j) + (lane & 3) * 16;
         if (!v.sees_page(k0)) return -1;
         const int id = table[k0 >> 4];
         if (id >= 0 && id < a.num_pages) return id;
@@ -271,7 +406,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         if (lane == 0) ok = mbar_wait(&bar->q_empty, (n_items_seen & 1) ^ 1, abort_flag, a.status);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (ok) {
-          const int n_tiles = v.n_tok_t[1] > 0 ? 2 : 1;
+          const int n_tiles = v.n_tok_b > 0 ? 2 : 1;
           const int n_copies = n_tiles * v.heads * G_::HALVES;
           if (pi == 0 && lane == 0) mbar_expect_tx(&bar->q_full, n_copies * Mt * 128);
           for (int cidx = pi + 4 * lane; cidx < n_copies; cidx += 128) {      // (tile, head, half), half fastest
@@ -285,7 +420,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       for (int kb = 0; kb < v.nblk && ok; ++kb) {
         if (pi == 0 && lane == 0) {
           if (kb == max(0, v.nblk - 4)) q_next = int(gridDim.x) + atomicAdd(queue, 1);
-          if (kb == v.nblk - 2 && v.nblk > 2) v_next = make_view(p, item_begin, q_next);
+          if (kb == v.nblk - 2 && v.nblk > 2) next_view();
         }
         if ((kb & 7) == 0) {
           pg_cur = pg_next;
@@ -313,7 +448,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         ok = __shfl_sync(0xffffffffu, ok, 0);
       }
       if (!ok) break;
-      if (pi == 0 && lane == 0 && v.nblk <= 2) v_next = make_view(p, item_begin, q_next);   // (a short item: not before its own requests are out)
+      if (pi == 0 && lane == 0 && v.nblk <= 2) next_view();   // (a short item: not before its own requests are out)
       blk_base += v.nblk;
     }
   } else if (warp == 9 || warp == 10) {
@@ -333,7 +468,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       auto pv_block = [&](const ItemView& v, int j) -> bool {
         const uint32_t gb = blk_base + j, vst = gb % PC_STAGES;
         if (!mbar_wait(&bar->v_full[vst], (gb / PC_STAGES) & 1, abort_flag, a.status)) return false;
-        if (j >= v.nblk_t[t]) {                                     // nothing of this tile in the block
+        if (j >= (t ? v.nblk_b : v.nblk_a)) {                                     // nothing of this tile in the block
           mbar_arrive(&bar->v_empty[vst]);
           return true;
         }
@@ -356,7 +491,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         mbar_arrive(&bar->ring_empty[rs]);
         if (++rs == 2) { rs = 0; rph ^= 1; }
         if (!v.valid) break;
-        const int nblk = v.nblk_t[t];
+        const int nblk = (t ? v.nblk_b : v.nblk_a);
         if (!mbar_wait(&bar->q_full, n_items_seen & 1, abort_flag, a.status)) break;
         ++n_items_seen;
         if (nblk == 0) mbar_arrive(&bar->q_empty);
@@ -400,7 +535,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       if (lane == 0) mbar_arrive(&bar->ring_empty[rs]);
       if (++rs == 2) { rs = 0; rph ^= 1; }
       if (!v.valid) break;
-      const int nblk = v.nblk_t[t], n_tok = v.n_tok_t[t];
+      const int nblk = (t ? v.nblk_b : v.nblk_a), n_tok = (t ? v.n_tok_b : v.n_tok_a);
       if (nblk == 0) { blk_base += v.nblk; continue; }            // the item has no tile for this warp group
       const int hg = r / Mt, tok = r - hg * Mt;
       const bool row_valid = hg < v.heads && tok < n_tok;
@@ -416,7 +551,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         ok = mbar_wait(&bar->s_full[t][buf], bph, abort_flag, a.status);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         tc_fence_after_sync();
-        const int key0 = v.key0(j);
+        const int key0 = v.template key0<DIVIDED>(j);
         tmem_ld32(tmem + lane_base + s_col + buf * PC_KEYS, sreg);
         tmem_ld32(tmem + lane_base + s_col + buf * PC_KEYS + 32, sreg2);
         tmem_ld_wait();
@@ -592,21 +727,48 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       ok = mbar_wait(&bar->o_full[t][(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag, a.status);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after_sync();
-      const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
       const int64_t row = v.row0 + t * Mt + tok;
       uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
-      if (row_valid && a.lse)
-        a.lse[row * a.n_q_heads + v.head0 + hg] = l_run == 0.f ? -INFINITY : kLn2 * (m_ref * (MOD ? 1.f : sc.in) + log2f(l_run));
+      const float m_log2 = m_ref * (MOD ? 1.f : sc.in);
+      if (!DIVIDED || (t ? v.parts_b : v.parts_a) == 1) {
+        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+        if (row_valid && a.lse) a.lse[row * a.n_q_heads + v.head0 + hg] = l_run == 0.f ? -INFINITY : kLn2 * (m_log2 + log2f(l_run));
 #pragma unroll
-      for (int c = 0; c < DH / 32; ++c) {
-        tmem_ld32(tmem + lane_base + o_col + c * 32, sreg);
-        tmem_ld_wait();
-        if (row_valid) {
-          uint32_t w[16];
+        for (int c = 0; c < DH / 32; ++c) {
+          tmem_ld32(tmem + lane_base + o_col + c * 32, sreg);
+          tmem_ld_wait();
+          if (row_valid) {
+            uint32_t w[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) w[e] = pack_16<F16>(__uint_as_float(sreg[2 * e]) * inv, __uint_as_float(sreg[2 * e + 1]) * inv);
+            for (int e = 0; e < 16; ++e) w[e] = pack_16<F16>(__uint_as_float(sreg[2 * e]) * inv, __uint_as_float(sreg[2 * e + 1]) * inv);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4*>(dst + c * 32 + u * 8) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4*>(dst + c * 32 + u * 8) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+          }
+        }
+      } else {
+        // A part: its rows go to the workspace.  The block that delivers a tile's last rows joins them before it leaves.
+        TilePart<DH>* tile_parts = reinterpret_cast<TilePart<DH>*>(static_cast<char*>(a.workspace) + kWsScratch) + v.item * div.parts * 2 + t;
+        TilePart<DH>& mine = tile_parts[2 * v.part];
+#pragma unroll
+        for (int c = 0; c < DH / 32; ++c) {
+          tmem_ld32(tmem + lane_base + o_col + c * 32, sreg);
+          tmem_ld_wait();
+          if (row_valid) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              __stcg(reinterpret_cast<float4*>(&mine.o[r][c * 32 + u * 4]), make_float4(__uint_as_float(sreg[4 * u]), __uint_as_float(sreg[4 * u + 1]), __uint_as_float(sreg[4 * u + 2]),
+                                                         __uint_as_float(sreg[4 * u + 3])));
+          }
+        }
+        if (row_valid) __stcg(&mine.ml[r], make_float2(m_ref == -INFINITY ? -INFINITY : m_log2, l_run));
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) {
+          int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsChunkDone) + v.item * 2 + t;
+          if (atomicAdd(done, 1) == 4 * (t ? v.parts_b : v.parts_a) - 1) {           // (one for each warp)
+            *done = 0;                                   // ready for the next call
+            joins[atomicAdd(&bar->n_joins, 1)] = v.item * 2 + t;
+          }
         }
       }
       tc_fence_before_sync();
@@ -619,6 +781,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   if (*abort_flag) drain_after_abort();
   tc_fence_before_sync();
   __syncthreads();
+  if (DIVIDED && bar->n_joins > 0) {
+    __threadfence();
+#pragma unroll 1
+    for (int i = 0; i < bar->n_joins; ++i) join_tile<DH, F16>(p, make_view<DIVIDED>(p, item_begin, div, (joins[i] >> 1) * div.parts), div, joins[i] & 1);
+  }
   if (warp == 9) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, PC_TMEM);
@@ -637,16 +804,19 @@ template <int DH>
 constexpr int pc_smem() {
   return Geom<DH>::SMEM > kMinSmemBytes ? Geom<DH>::SMEM : kMinSmemBytes;
 }
-static_assert(kWsChunkQueue + 8 <= kWsScratch, "two words");
+static_assert(kWsChunkQueue + 8 <= kWsChunkDone, "two words");
+static_assert(kWsChunkDone + kMaxShares * 4 <= kWsScratch, "a word for both tiles of every divided item");
+static_assert(size_t(kMaxShares) * 2 * sizeof(TilePart<128>) <= kWsScratchBytes, "two tiles of every part");
 
 using ChunkKernel = void (*)(ChunkParams);
-ChunkKernel pick(int dh, bool f16, bool mod) {
-  if (dh == 128) {
-    if (f16) return mod ? paged_chunk_kernel<128, true, true> : paged_chunk_kernel<128, true, false>;
-    return mod ? paged_chunk_kernel<128, false, true> : paged_chunk_kernel<128, false, false>;
-  }
-  if (f16) return mod ? paged_chunk_kernel<64, true, true> : paged_chunk_kernel<64, true, false>;
-  return mod ? paged_chunk_kernel<64, false, true> : paged_chunk_kernel<64, false, false>;
+template <int DH, bool DIVIDED>
+ChunkKernel pick(bool f16, bool mod) {
+  if (f16) return mod ? paged_chunk_kernel<DH, true, true, DIVIDED> : paged_chunk_kernel<DH, true, false, DIVIDED>;
+  return mod ? paged_chunk_kernel<DH, false, true, DIVIDED> : paged_chunk_kernel<DH, false, false, DIVIDED>;
+}
+ChunkKernel pick(int dh, bool f16, bool mod, bool divided) {
+  if (dh == 128) return divided ? pick<128, true>(f16, mod) : pick<128, false>(f16, mod);
+  return divided ? pick<64, true>(f16, mod) : pick<64, false>(f16, mod);
 }
 
 }  // namespace
@@ -657,16 +827,17 @@ int paged_chunk_tile_tokens(int n_q_heads, int n_kv_heads) {
 }
 
 cudaError_t paged_chunk_set_attributes() {
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 16; ++i) {
     const int dh = i & 1 ? 128 : 64;
-    const cudaError_t e = set_kernel_smem(pick(dh, i & 2, i & 4), dh == 128 ? pc_smem<128>() : pc_smem<64>());
+    const cudaError_t e = set_kernel_smem(pick(dh, i & 2, i & 4, i & 8), dh == 128 ? pc_smem<128>() : pc_smem<64>());
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
-cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_budget, cudaStream_t stream) {
+cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_count, int sm_budget, cudaStream_t stream) {
   ChunkParams p{};
+  p.shares = share_count(sm_count);
   p.tm_kv = tm_kv;
   p.tm_q = tm_q;
   p.a = a;
@@ -674,7 +845,12 @@ cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap&
   const int heads = a.n_q_heads / a.n_kv_heads;
   p.chunks = (heads + PC_HEADS - 1) / PC_HEADS;
   p.tile_tokens = paged_chunk_tile_tokens(a.n_q_heads, a.n_kv_heads);
-  return launch_step_kernel(pick(a.head_dim, a.type == HS_TYPE_F16, a.cap > 0.f || a.slopes != nullptr), sm_budget, PC_THREADS,
+  // The kernel that can divide items is taken where every call of this shape has few of them.  (What it carries for that costs it 1 to 6 % on
+  // items that are not divided: two chunks of 614 tokens, 28 heads on 4, 29.1 / 31.0 us.)
+  const int64_t tokens = 2 * p.tile_tokens;
+  const int64_t pairs = std::min(int64_t(a.n_seqs) * ((a.max_q_len + tokens - 1) / tokens), a.n_tokens / tokens + a.n_seqs);
+  const bool divided = 2 * pairs * a.n_kv_heads * p.chunks <= p.shares && int64_t(a.max_pages_per_seq) * HS_PAGE_SIZE > (PC_DIVIDED - 1) * PC_KEYS;
+  return launch_step_kernel(pick(a.head_dim, a.type == HS_TYPE_F16, a.cap > 0.f || a.slopes != nullptr, divided), sm_budget, PC_THREADS,
                             a.head_dim == 128 ? pc_smem<128>() : pc_smem<64>(), stream, true, p);
 }
 

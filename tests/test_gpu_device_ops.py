@@ -583,3 +583,50 @@ def test_refusals(ws, status):
         ops.step_tables(ctx, ctx[:2], free, count, bt3, ctx, *out, count, ws, status)
     torch.cuda.synchronize()
     assert int(status) == 0
+
+
+# ------------------------------------------------------------------------------------------------- how work is divided over the device
+@pytest.mark.parametrize("cap,window,prefix,bias", [(0.0, 0, 0, False), (30.0, 900, 0, True), (0.0, 1000, 1200, False)])
+@pytest.mark.parametrize("hq,hkv,dim", [(7, 1, 128), (16, 2, 64), (12, 1, 128), (34, 2, 64)])
+@pytest.mark.parametrize("q,kv", [([4], [2000]), ([1, 30], [3000, 50]), ([20, 0], [5003, 800]), ([3, 70, 40], [1500, 70, 900]), ([2, 2], [0, 1400])])
+def test_chunks_of_few_rows_divide_long_sequences(cap, window, prefix, bias, hq, hkv, dim, q, kv, ws, status):
+    check_attention(attention_case(sum(kv), kv, q, hq, hkv, dim, torch.bfloat16, cap, window, prefix, bias), ws, status)
+
+
+@pytest.mark.parametrize("cap,window,prefix,bias", [(0.0, 0, 0, False), (30.0, 700, 0, True), (0.0, 500, 650, False)])
+@pytest.mark.parametrize("hq,hkv,dim,kv", [
+    (16, 16, 64, [40, 7, 0, 33, 64, 1, 90, 16, 17, 31]),     # whole groups, several a share
+    (8, 1, 64, [9000, 100, 0, 700]),                          # parts of groups, most groups with fewer than the longest
+    (12, 2, 128, [2000, 1999, 3]),                            # and with two tiles of heads
+    (2, 2, 64, [2400] * 79 + [5]),                            # more groups than shares, too long to stay whole: cut anywhere
+])
+def test_decode_by_groups_parts_and_pieces(cap, window, prefix, bias, hq, hkv, dim, kv, ws, status):
+    check_attention(attention_case(len(kv), kv, [1] * len(kv), hq, hkv, dim, torch.bfloat16, cap, window, prefix, bias), ws, status)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype,n_top", [(149, 152064, torch.bfloat16, 20), (3, 152064, torch.float32, 32), (20, 60001, torch.float16, 1), (300, 20000, torch.float32, 5),
+                                                    (64, 152064, torch.float32, 20), (1, 300001, torch.bfloat16, 32)])
+def test_token_logprobs_of_whole_and_divided_rows(rows, vocab, dtype, n_top, ws, status):
+    g = torch.Generator().manual_seed(rows + vocab)
+    x = (3 * torch.randn(rows, vocab, generator=g)).to(dtype).to(DEV)
+    check_logprobs(x, torch.randint(0, vocab, (rows,), generator=g).tolist(), n_top, 0.9, ws, status, budgets=(11,))
+
+
+@pytest.mark.parametrize("dtype,large", [(torch.float32, 3e38), (torch.bfloat16, 3e38), (torch.float16, 65504.0)])
+@pytest.mark.parametrize("vocab", [100, 3000, 70000])
+def test_token_logprobs_of_logits_near_the_types_limits(dtype, large, vocab, ws, status):
+    """Rows with a few logits at the largest values of the type, of either sign: only those at the top have a probability."""
+    x = torch.randn(3, vocab, generator=torch.Generator().manual_seed(5))
+    x[0, 17] = x[0, vocab - 3] = large
+    x[1] = -large
+    x[1, 40] = x[1, 41] = x[1, vocab // 2] = x[1, vocab - 1] = -large / 2
+    x[2, ::2] = -large
+    x[2, 50] = large
+    x = x.to(dtype).to(DEV)
+    got = run_logprobs(x, [17, 41, 50], 4, 1.0, ws, status)
+    want = torch.tensor([-math.log(2), -math.log(4), 0.0])
+    # the values at the top are equal, and the others' weights are 0: sums of 2, 4 and 1
+    assert float((got["logprob"].cpu() - want).abs().max()) <= 1e-6 and float((got["entropy"].cpu() + want).abs().max()) <= 1e-6
+    assert got["rank"].tolist() == [0, 0, 0]
+    assert got["top_ids"][0, :2].tolist() == [17, vocab - 3] and got["top_ids"][1].tolist() == [40, 41, vocab // 2, vocab - 1] and int(got["top_ids"][2, 0]) == 50
+    assert int(status) == 0
