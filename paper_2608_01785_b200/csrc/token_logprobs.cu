@@ -34,6 +34,7 @@ constexpr int LP_MIN_UNITS = 16;                                                
 constexpr int LP_ROW_COST = 36, LP_JOIN_COST = 54;                                         // units that take as long as a row's beginning and end, as a join
 constexpr int LP_JOIN_LOADS = 4;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFar = 1e6f;                                                               // log2 units from zero: fp32 there still has steps of 2^-4
 constexpr float kSlack = 10.f;                                                             // log2 units that a logit may lie above its thread's reference
 
 // 16-byte pieces of logits as 32-bit words.  kFloor: what stands for -infinity where its weight is to be 0 and its distance finite; right
@@ -367,6 +368,12 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         RowPlace& place = sm.place[at];
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_empty[at], row_phase ^ 1, abort_flag, p.a.status));
         float m = -INFINITY;                             // the thread's reference: its maximum, or up to kSlack below it
+        // The distances are k x - (k m rounded to fp32): by this they are too large, all alike, until the row's end takes it out again.  (Of a
+        // reference far from zero they are k (x - m).)
+        auto slip = [&](float m) {
+          const float km = __fmul_rn(m, p.k);
+          return fabsf(km) < kFar ? fmaf(m, p.k, -km) : 0.f;
+        };
         float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};      // its sums, even and odd elements
         int above = 0;
         auto push = [&](float x, int v) {
@@ -375,7 +382,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         };
         if (edge >= 0) {
           m = edge_x;
-          if (edge_x != -INFINITY) s[0] = edge_x - edge_x + 1.f;       // (NaN of NaN and of infinity)
+          if (edge_x != -INFINITY) {
+            const float d = slip(m);
+            s[0] = edge_x - edge_x + exp2f(d);           // (NaN of NaN and of infinity)
+            t[0] = s[0] * d;
+          }
           above = edge_x > x_t ? 1 : 0;
           if (n_top > 0 && edge_x > -INFINITY) push(edge_x, edge);
         }
@@ -455,7 +466,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           if (first) ask_next();
           const bool higher = !(mx <= m) && !((mx - m) * p.k <= kSlack);          // (true of the first element above -infinity, and of NaN)
           if (higher) {
-            const float to = max_nan(mx, m), d = max_nan(p.k * (m - to), -200.f), f = exp2f(d);      // (nothing so far: d = -infinity, s = t = 0)
+            const float to = max_nan(mx, m), d = max_nan(p.k * (m - to) - slip(m) + slip(to), -200.f), f = exp2f(d);      // (nothing so far: s = t = 0)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               t[i] = f * fmaf(s[i], d, t[i]);
@@ -464,10 +475,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             m = to;
             if (to == INFINITY) s[0] = to - to;          // (a row with infinity has no sum)
           }
-          const float from = m == -INFINITY ? 0.f : m, c = -from * p.k;
+          const float from = m == -INFINITY ? 0.f : m, c = -__fmul_rn(from, p.k);
+          const bool far = !(fabsf(c) < kFar);
           // one piece after the other: a tile that holds little (a round of pieces takes 390 cycles so, eight take 1200 otherwise), or logits near the
-          // type's limits (or NaN)
-          const bool apart = pieces <= 3 * LP_READERS || !(fabsf(from) < -L::kLow) || p.k > 100.f;
+          // type's limits (or NaN), or a scale by which kFloor would not stand for -infinity or leave fp32
+          const bool apart = pieces <= 3 * LP_READERS || far || !(from > L::kLow) || p.k > 100.f || p.k < 0.03f;
           if (!apart) {
 #pragma unroll
             for (int i = 0; i < LP_PIECES; ++i) {
@@ -495,7 +507,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
               L::get(q, x);
 #pragma unroll
               for (int e = 0; e < kPer; ++e) {
-                const float d = max_nan((x[e] - from) * p.k, -126.f), weight = fast_exp2(d);
+                const float d = max_nan(far ? (x[e] - from) * p.k : fmaf(x[e], p.k, c), -126.f), weight = fast_exp2(d);
                 s[0] += weight;
                 t[0] = fmaf(weight, d, t[0]);
               }
@@ -511,7 +523,8 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           }
           if (++slot == LP_SLOTS) { slot = 0; phase ^= 1; }
         }
-        const Sums mine = warp_join(Sums{m, s[0] + s[1], t[0] + t[1], above}, p.k);
+        const float e = slip(m), back = exp2f(-e), sum = s[0] + s[1];
+        const Sums mine = warp_join(Sums{m, back * sum, back * fmaf(sum, -e, t[0] + t[1]), above}, p.k);
         if (lane == 0) {
           place.sums[warp] = mine;
           if (warp == 0) {

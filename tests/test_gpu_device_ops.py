@@ -630,3 +630,13 @@ def test_token_logprobs_of_logits_near_the_types_limits(dtype, large, vocab, ws,
     assert got["rank"].tolist() == [0, 0, 0]
     assert got["top_ids"][0, :2].tolist() == [17, vocab - 3] and got["top_ids"][1].tolist() == [40, 41, vocab // 2, vocab - 1] and int(got["top_ids"][2, 0]) == 50
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("scale", [1e-4, 0.05, 60.0, 1e4])
+def test_token_logprobs_of_unusual_scales(dtype, scale, ws, status):
+    g = torch.Generator().manual_seed(8)
+    x = 3 * torch.randn(4, 40000, generator=g)
+    x[:, ::3] = -math.inf
+    x = x.to(dtype).to(DEV)
+    check_logprobs(x, [1, 3, 20000, 39998], 7, scale, ws, status)
