@@ -12,7 +12,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "paged_scores.cuh"
 
@@ -22,7 +21,6 @@ namespace {
 constexpr int PC_THREADS = 448, PC_KEYS = 64, PC_STAGES = 4;
 constexpr int PC_TMEM = 512;
 constexpr int PC_MIN_BLOCKS = 4, PC_DIVIDED = 12;       // key blocks of a part of an item; of an item that is divided
-constexpr int PC_JOIN_ROWS = 2;
 constexpr float PC_JOIN_FACTOR = 3.f;
 constexpr int PC_HEADS = 16;               // query heads of an item at most: eight tokens of each fill a tile
 constexpr float kRefSlack = 8.f;           // log2 units by which a row's running maximum may exceed its reference
@@ -51,10 +49,11 @@ struct ChunkParams {
 struct Division {
   int parts, blocks;
 };
-// A tile's part of an item in the workspace: outputs relative to the row's reference, then (reference in log2 units, sum) per row.
+// A tile's part of an item in the workspace: outputs relative to the row's reference, four coordinates of all rows after one another (threads have a row
+// each, and write and read side by side), then (reference in log2 units, sum) per row.
 template <int DH>
 struct TilePart {
-  float o[128][DH];
+  float4 o[DH / 4][128];
   float2 ml[128];
 };
 
@@ -175,77 +174,69 @@ __device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* i
   return v;
 }
 
-// Joins the parts of a tile's rows, in order, by all warps of the block: the lanes lie along a row, PC_JOIN_ROWS rows of a warp and eight parts of each are on
-// their way at a time.
+// Joins the parts of a tile's rows, in order: a thread has a row and a third of its coordinates; two times four coordinates of eight parts are on their way at
+// a time.
 template <int DH, bool F16>
 __device__ __forceinline__ void join_tile(const ChunkParams& p, const ItemView& v, Division div, int t) {
-  using Vec = std::conditional_t<DH == 128, float4, float2>;
+  constexpr int OF = DH / 4, MINE = ((OF + 2) / 3 + 1) & ~1;    // (12, 12 and 8 of 32; 6, 6 and 4 of 16)
+  static_assert(3 * MINE >= OF && PC_THREADS >= 3 * 128, "three groups of threads");
   const hs_paged_attention_t& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Mt = p.tile_tokens;
-  const int n_tok = t ? v.n_tok_b : v.n_tok_a, n_parts = t ? v.parts_b : v.parts_a, n_rows = v.heads * n_tok;
+  const int r = threadIdx.x & 127, c0 = int(threadIdx.x >> 7) * MINE, Mt = p.tile_tokens, hg = r / Mt, tok = r - hg * Mt;
+  if (c0 >= OF || hg >= v.heads || tok >= (t ? v.n_tok_b : v.n_tok_a)) return;
+  const int n_parts = t ? v.parts_b : v.parts_a;
   const TilePart<DH>* tile_parts = reinterpret_cast<const TilePart<DH>*>(static_cast<const char*>(a.workspace) + kWsScratch) + v.item * div.parts * 2 + t;
-#pragma unroll 1
-  for (int q0 = warp * PC_JOIN_ROWS; q0 < n_rows; q0 += PC_THREADS / 32 * PC_JOIN_ROWS) {
-    int r[PC_JOIN_ROWS];
-    float top[PC_JOIN_ROWS], l[PC_JOIN_ROWS], o[PC_JOIN_ROWS][4];
+  float top = -INFINITY, l = 0.f;
+  float4 o[MINE];
 #pragma unroll
-    for (int i = 0; i < PC_JOIN_ROWS; ++i) {
-      const int q = min(q0 + i, n_rows - 1);
-      r[i] = q / n_tok * Mt + q % n_tok;
-      top[i] = -INFINITY;
-      l[i] = o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  for (int i = 0; i < MINE; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int k0 = 0; k0 < n_parts; k0 += 8) {
+    float2 ml[8];
+    float next = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) ml[u] = k0 + u < n_parts ? __ldcg(&tile_parts[2 * (k0 + u)].ml[r]) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) next = fmaxf(next, ml[u].x);
+    const float zero = next == -INFINITY ? 0.f : next, f0 = fast_exp2(top - zero);
+    top = next;
+    l *= f0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      ml[u].x = fast_exp2(ml[u].x - zero);               // (0 for a part that is not there)
+      l = fmaf(ml[u].x, ml[u].y, l);
     }
-#pragma unroll 1
-    for (int k0 = 0; k0 < n_parts; k0 += 8) {
-      Vec x[PC_JOIN_ROWS][8];
-      float2 ml[PC_JOIN_ROWS];                           // of part k0 + lane % 8
 #pragma unroll
-      for (int i = 0; i < PC_JOIN_ROWS; ++i) {
-        ml[i] = k0 + (lane & 7) < n_parts ? __ldcg(&tile_parts[2 * (k0 + (lane & 7))].ml[r[i]]) : make_float2(-INFINITY, 0.f);
+    for (int i = 0; i < MINE; i += 2) {
+      if (c0 + i >= OF) break;
+      float4 x[2][8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[i][u] = __ldcg(reinterpret_cast<const Vec*>(tile_parts[2 * min(k0 + u, n_parts - 1)].o[r[i]]) + lane);
-      }
+      for (int u = 0; u < 8; ++u)
 #pragma unroll
-      for (int i = 0; i < PC_JOIN_ROWS; ++i) {
-        float next = fmaxf(ml[i].x, __shfl_xor_sync(0xffffffffu, ml[i].x, 1));
-        next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, 2));
-        next = fmaxf(fmaxf(next, __shfl_xor_sync(0xffffffffu, next, 4)), top[i]);
-        const float zero = next == -INFINITY ? 0.f : next, f0 = fast_exp2(top[i] - zero), f = fast_exp2(ml[i].x - zero);      // (0 for a part that is not there)
-        top[i] = next;
-        float sum = f * ml[i].y;
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-        l[i] = fmaf(l[i], f0, sum);
+        for (int e = 0; e < 2; ++e) x[e][u] = k0 + u < n_parts ? __ldcg(&tile_parts[2 * (k0 + u)].o[c0 + i + e][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] *= f0;
+      for (int e = 0; e < 2; ++e) {
+        float4& to = o[i + e];
+        to.x *= f0; to.y *= f0; to.z *= f0; to.w *= f0;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const float w = __shfl_sync(0xffffffffu, f, u);
-          o[i][0] = fmaf(w, x[i][u].x, o[i][0]);
-          o[i][1] = fmaf(w, x[i][u].y, o[i][1]);
-          if constexpr (DH == 128) {
-            o[i][2] = fmaf(w, x[i][u].z, o[i][2]);
-            o[i][3] = fmaf(w, x[i][u].w, o[i][3]);
-          }
+          to.x = fmaf(ml[u].x, x[e][u].x, to.x);
+          to.y = fmaf(ml[u].x, x[e][u].y, to.y);
+          to.z = fmaf(ml[u].x, x[e][u].z, to.z);
+          to.w = fmaf(ml[u].x, x[e][u].w, to.w);
         }
       }
     }
-#pragma unroll
-    for (int i = 0; i < PC_JOIN_ROWS; ++i) {
-      if (q0 + i >= n_rows) break;
-      const int64_t row = v.row0 + t * Mt + r[i] % Mt;
-      const int head = v.head0 + r[i] / Mt;
-      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-      uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH);
-      if constexpr (DH == 128) {
-        reinterpret_cast<uint2*>(dst)[lane] = make_uint2(pack_16<F16>(o[i][0] * inv, o[i][1] * inv), pack_16<F16>(o[i][2] * inv, o[i][3] * inv));
-      } else {
-        dst[lane] = pack_16<F16>(o[i][0] * inv, o[i][1] * inv);
-      }
-      if (lane == 0 && a.lse) a.lse[row * a.n_q_heads + head] = l[i] == 0.f ? -INFINITY : kLn2 * (top[i] + log2f(l[i]));
-    }
   }
+  const int64_t row = v.row0 + t * Mt + tok;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
+#pragma unroll
+  for (int i = 0; i < MINE; i += 2) {
+    if (c0 + i >= OF) break;
+    *reinterpret_cast<uint4*>(dst + (c0 + i) * 4) = make_uint4(pack_16<F16>(o[i].x * inv, o[i].y * inv), pack_16<F16>(o[i].z * inv, o[i].w * inv),
+                                                             pack_16<F16>(o[i + 1].x * inv, o[i + 1].y * inv), pack_16<F16>(o[i + 1].z * inv, o[i + 1].w * inv));
+  }
+  if (c0 == 0 && a.lse) a.lse[row * a.n_q_heads + v.head0 + hg] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
 }
 
 template <int DH, bool F16, bool MOD, bool DIVIDED>
@@ -756,7 +747,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           if (row_valid) {
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-              __stcg(reinterpret_cast<float4*>(&mine.o[r][c * 32 + u * 4]), make_float4(__uint_as_float(sreg[4 * u]), __uint_as_float(sreg[4 * u + 1]), __uint_as_float(sreg[4 * u + 2]),
+              __stcg(&mine.o[c * 8 + u][r], make_float4(__uint_as_float(sreg[4 * u]), __uint_as_float(sreg[4 * u + 1]), __uint_as_float(sreg[4 * u + 2]),
                                                          __uint_as_float(sreg[4 * u + 3])));
           }
         }
