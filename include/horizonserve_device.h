@@ -156,13 +156,15 @@ hs_status_t hs_op_rope_cache(const hs_rope_cache_t *a, int32_t sm_budget, void *
  *     o = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)   (natural logarithm).
  * A row that sees no key gives o = 0 and lse = -infinity.  Scores, maxima, sums and o are held in fp32; the softmax weights are
  * rounded to the cache's type for the product with v.
- * max_q_len: no sequence has more rows in this call (a captured loop's bound).  1 selects the form for single tokens, which
- * splits the work evenly over the device along the cache.  The work is planned on the device from the lengths.
+ * max_q_len: no sequence has more rows in this call (a captured loop's bound).  1 selects the form for single tokens.  The work is planned on
+ * the device from the lengths; where there is little of it, it is divided along the cache, and joined in an order that does not depend on the budget.
  * Only pages that hold a key some row sees are looked up, so block table entries that a window has left behind may be anything.
  * Status INVALID_ARG: tok_begin that falls, leaves 0 .. n_tokens or gives a sequence more than max_q_len rows; none of the sequence's rows
  * are computed.  Status BAD_BLOCK_TABLE: a page id outside the pool, or a kv_len that is negative or beyond the block table row;
  * nothing outside the pool is read, and the sequence's rows are not defined.
- * head_dim 64 or 128.  q and o rows 16-byte aligned, strides multiples of 8; kv_pool 256-byte aligned.  n_seqs <= HS_DEVICE_MAX_SEQS.
+ * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale and cap finite, cap and window >= 0.  q and o rows 16-byte aligned,
+ * strides multiples of 8; kv_pool 256-byte aligned.  n_seqs <= HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27; below 2^31: that times
+ * n_q_heads, n_tokens * n_q_heads, and the pool's rows (n_layers * 2 * num_pages * n_kv_heads * 16).
  */
 typedef struct {
   int32_t n_seqs, n_tokens;               /* n_tokens: rows of q, o and lse (at least tok_begin[n_seqs]) */
@@ -195,7 +197,7 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t *a, int32_t sm_budg
  * A negative target: logprob 0, rank -1.  A target >= vocab: the same, and status INVALID_ARG.  Entries of -infinity (masked
  * tokens) count as probability 0; a row of nothing else has L = -infinity, and its logprobs are -infinity and its entropy 0.
  * A row that holds NaN or +infinity has NaN for L, logprob and entropy; which alternatives it names is not defined (ids -1 .. vocab - 1).
- * Logits of any row stride and alignment of their type; sums in fp32.
+ * Logits of any row stride and alignment of their type; sums in fp32.  n_rows * (vocab / 1024 + 2) below 2^31.
  */
 typedef struct {
   int32_t n_rows, vocab;       /* n_rows >= 1, 1 <= vocab < 2^30 */

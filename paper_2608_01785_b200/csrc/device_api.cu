@@ -73,7 +73,7 @@ bool encode_rows(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool tables_shape_ok(int n_seqs, int max_pages) { return n_seqs <= HS_DEVICE_MAX_SEQS && int64_t(n_seqs) * max_pages < (int64_t(1) << 27); }
+bool tables_shape_ok(int n_seqs, int max_pages) { return n_seqs <= HS_DEVICE_MAX_SEQS && int64_t(n_seqs) * max_pages <= (int64_t(1) << 27); }
 bool workspace_ok(const void* w) { return w && aligned(w, 256); }
 
 }  // namespace
