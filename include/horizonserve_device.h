@@ -18,7 +18,8 @@
  * results do not depend on sm_budget.  Besides
  *   - The description structs are read before the call returns; integers in them are element counts, strides count elements.
  *   - `status`: a device int, zero on entry, that receives an hs_status_t when a value that only the device knows is wrong
- *     (each call says which); the outputs are then as the call says.  It is left alone when nothing is wrong.
+ *     (each call says which); the outputs are then as the call says.  It is left alone when nothing is wrong.  HS_ERR_TIMEOUT: a bounded wait inside
+ *     a kernel ran out; the outputs are not defined, and the workspace is to be zeroed before its next use.
  *   - `workspace`: HS_DEVICE_WORKSPACE_BYTES of device memory, 256-byte aligned, zeroed once before its first use.  Every call
  *     leaves its control words at zero.  Two calls whose kernels can overlap on the GPU need two workspaces.
  *   - Errors that the host can see are returned and nothing is launched: INVALID_ARG (NULL, misaligned or inconsistent),

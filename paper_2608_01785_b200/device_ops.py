@@ -18,7 +18,6 @@ WORKSPACE_BYTES = 32 << 20
 MAX_SEQS = 4096
 MAX_ALTERNATIVES = 32
 PAGE = 16
-TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = range(4)
 EXPORTS = ("hs_op_step_tables", "hs_op_release_pages", "hs_op_rope_table", "hs_op_rope_cache", "hs_op_paged_attention", "hs_op_token_logprobs")
 
