@@ -1,13 +1,12 @@
 // Rotary positions on q and k together with the scatter of k and v into the paged cache, and the table of cos / sin they use.
 //
-// Every element is read once and written once; what bounds the kernel is memory, by its latency more than its rate: 8000 rows of 36 heads of 128 in
-// bf16, 152 MB, take 34 us, 4.4 TB/s.  A unit is sixteen coordinates of one head of one
-// token, two 16-byte pieces of the result: eight pairs that rotate -- (i, i + rot / 2) or (2 i, 2 i + 1) -- or sixteen coordinates
-// that are copied.  A warp takes as many whole heads at a time as it has lanes for (four of 128 coordinates), so that its loads
-// and stores are runs of 128 bytes and more, and a lane has the same eight pairs in every head: consecutive heads of a token find their 64 bytes of the
-// table in L1.  The (token, heads) steps are dealt to the warps in contiguous runs of equal length, whatever the number of tokens.
-// Threads of a block x units a lane has on their way, us for 8000 rows of 36 heads of 128 / 1111 rows of 24 of 64 / 64 rows of 36: 1024 x 1 32.5 / 4.0 / 4.2,
-// 768 x 2 33.4 / 3.7 / 3.6, 512 x 4 35.0 / 3.5 / 3.1, 1024 x 4, whose registers spill, 47.8 / 6.4 / 5.2.
+// Every element is read once and written once; what bounds the kernel is memory, by its latency more than its rate: 8000 rows of 36 heads of 128 in bf16, 152 MB,
+// take 31.7 us, 4.8 TB/s.  A unit is sixteen coordinates of one head of one token, two 16-byte pieces of the result: eight pairs that rotate -- (i, i + rot / 2) or
+// (2 i, 2 i + 1) -- or sixteen coordinates that are copied.  A warp takes as many whole heads at a time as it has lanes for (four of 128 coordinates), so that its
+// loads and stores are runs of 128 bytes and more, and a lane has the same eight pairs in every head: it keeps their 64 bytes of the table until the token changes (read for
+// every head, from L1, 34.4 us).  The (token, heads) steps are dealt to the warps in contiguous runs of equal length, whatever the number of tokens.
+// Threads of a block x units a lane has on their way, us for 8000 rows of 36 heads of 128 / 1111 rows of 24 of 64 / 64 rows of 36 from fp32: 1024 x 1 34.4 / 4.2 / 5.2,
+// 768 x 2 31.7 / 3.5 / 3.9, 640 x 2 31.7 / 3.8 / 3.5, 512 x 2 32.5 / 3.5 / 3.2, 512 x 3 31.6 / 3.7 / 3.2; 640 x 2 is the best of them by a little over nine such sizes.
 #include <algorithm>
 
 #include "device_ops.h"
@@ -16,7 +15,7 @@
 namespace hs {
 namespace {
 
-constexpr int RC_THREADS = 768, RT_THREADS = 512;
+constexpr int RC_THREADS = 640, RT_THREADS = 512;
 
 // Sixteen-byte pieces of eight elements of the source type -> eight floats.
 template <int TYPE>
@@ -93,38 +92,61 @@ __global__ void __launch_bounds__(RC_THREADS, 1) rope_cache_kernel(const hs_rope
   uint16_t* pool = static_cast<uint16_t*>(a.kv_pool) + int64_t(a.layer) * 2 * a.num_pages * a.n_kv_heads * 16 * a.head_dim;
   const int64_t half_pool = int64_t(a.num_pages) * a.n_kv_heads * 16 * a.head_dim;       // K pages, then V pages
 
+  // The lane's eight pairs of the table are the token's, whatever the head: they are fetched when the token changes, with the first rows' loads, as its position is
+  // known by then.
+  int pos = -1, slot = -1, next_pos = -1, next_slot = -1;
+  if (w < end) {
+    next_pos = a.tok_pos[tok];
+    next_slot = a.tok_slot[tok];
+  }
+  bool fresh = true, placed = false;
+  float4 cs[4];
   while (w < end) {
     Piece<SRC> x[kAhead], y[kAhead];
-    int tk[kAhead], hd[kAhead], pos[kAhead], slot[kAhead];
+    int hd[kAhead];
+    if (fresh) {
+      pos = next_pos;
+      slot = next_slot;
+      placed = pos >= 0 && pos < a.max_position;
+      if (tok + 1 < a.n_tokens) {
+        next_pos = a.tok_pos[tok + 1];
+        next_slot = a.tok_slot[tok + 1];
+      }
+      if (turns && placed) {
+        const float4* from = reinterpret_cast<const float4*>(a.table + (int64_t(pos) * (a.rotary_dim >> 1) + u * 8) * 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cs[i] = __ldg(from + i);
+      }
+    }
+    const int64_t t = tok;
+    fresh = false;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int head = step * heads + hg;
-      hd[j] = w < end && hg < heads && head < n_heads ? head : -1;
-      tk[j] = tok;
-      if (w < end) {
-        pos[j] = a.tok_pos[tok];
-        slot[j] = a.tok_slot[tok];
-      }
+      hd[j] = !fresh && w < end && hg < heads && head < n_heads ? head : -1;
       if (hd[j] >= 0) {
         const void* src;
         int64_t at;
         if (head < a.n_q_heads) {
           src = a.q;
-          at = tok * a.q_stride + head * a.head_dim;
+          at = t * a.q_stride + head * a.head_dim;
         } else if (head < a.n_q_heads + a.n_kv_heads) {
           src = a.k;
-          at = tok * a.k_stride + (head - a.n_q_heads) * a.head_dim;
+          at = t * a.k_stride + (head - a.n_q_heads) * a.head_dim;
         } else {
           src = a.v;
-          at = tok * a.v_stride + (head - a.n_q_heads - a.n_kv_heads) * a.head_dim;
+          at = t * a.v_stride + (head - a.n_q_heads - a.n_kv_heads) * a.head_dim;
         }
         x[j].load(src, at + lo);
         y[j].load(src, at + hi);
       }
-      ++w;
-      if (++step == steps) {
-        step = 0;
-        ++tok;
+      if (!fresh) {
+        ++w;
+        if (++step == steps) {                           // the next token's rows are another round's
+          step = 0;
+          ++tok;
+          fresh = true;
+        }
       }
     }
 #pragma unroll
@@ -132,37 +154,34 @@ __global__ void __launch_bounds__(RC_THREADS, 1) rope_cache_kernel(const hs_rope
       if (hd[j] < 0) continue;
       const int head = hd[j];
       const bool is_q = head < a.n_q_heads, is_v = head >= a.n_q_heads + a.n_kv_heads;
-      const bool placed = pos[j] >= 0 && pos[j] < a.max_position;
       float p[8], q[8];
       x[j].get(p);
       y[j].get(q);
       if (turns && !is_v && placed) {
-        const float4* cs = reinterpret_cast<const float4*>(a.table + (int64_t(pos[j]) * (a.rotary_dim >> 1) + u * 8) * 2);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 t = __ldg(cs + i);                 // two pairs' (cos, sin)
+        for (int i = 0; i < 4; ++i) {                     // two pairs' (cos, sin)
           if (INTERLEAVED) {
             float (&z)[8] = i < 2 ? p : q;
-            rotate_pair(z[4 * (i & 1)], z[4 * (i & 1) + 1], t.x, t.y);
-            rotate_pair(z[4 * (i & 1) + 2], z[4 * (i & 1) + 3], t.z, t.w);
+            rotate_pair(z[4 * (i & 1)], z[4 * (i & 1) + 1], cs[i].x, cs[i].y);
+            rotate_pair(z[4 * (i & 1) + 2], z[4 * (i & 1) + 3], cs[i].z, cs[i].w);
           } else {
-            rotate_pair(p[2 * i], q[2 * i], t.x, t.y);
-            rotate_pair(p[2 * i + 1], q[2 * i + 1], t.z, t.w);
+            rotate_pair(p[2 * i], q[2 * i], cs[i].x, cs[i].y);
+            rotate_pair(p[2 * i + 1], q[2 * i + 1], cs[i].z, cs[i].w);
           }
         }
       }
       uint16_t* dst;
       if (is_q) {
-        dst = static_cast<uint16_t*>(a.q_out) + tk[j] * a.q_out_stride + head * a.head_dim;
+        dst = static_cast<uint16_t*>(a.q_out) + t * a.q_out_stride + head * a.head_dim;
         if (!placed) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) p[i] = q[i] = 0.f;
         }
       } else {
-        const int page = slot[j] >> 4;
-        if (slot[j] < 0 || !placed || page >= a.num_pages) continue;
+        const int page = slot >> 4;
+        if (slot < 0 || !placed || page >= a.num_pages) continue;
         const int hk = head - a.n_q_heads - (is_v ? a.n_kv_heads : 0);
-        dst = pool + (is_v ? half_pool : 0) + ((int64_t(page) * a.n_kv_heads + hk) * 16 + (slot[j] & 15)) * a.head_dim;
+        dst = pool + (is_v ? half_pool : 0) + ((int64_t(page) * a.n_kv_heads + hk) * 16 + (slot & 15)) * a.head_dim;
       }
       *reinterpret_cast<uint4*>(dst + lo) = pack8<F16>(p);
       *reinterpret_cast<uint4*>(dst + hi) = pack8<F16>(q);
