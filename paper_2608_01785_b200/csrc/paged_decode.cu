@@ -32,7 +32,7 @@ constexpr int PD_RING_BYTES = 192 * 1024;
 constexpr int PD_MIN_PAGES = 16;                 // of a share: two per warp
 // How the line is cut, by what the longest share has to do in pages: a join of shares takes as long as PD_JOIN_COST pages and one for each part; cuts inside
 // groups, which give a block two groups and two joins, as PD_CUT_COST.  us by groups / anywhere: 2 sequences of 81 keys, 16 heads on 4 of 128, 6.7 /
-// 13.4; 16 of 128 .. 1024, 16 on 4 of 64, 12.0 / 14.3; 3 of 20001 .. 32768, 16 on 2 of 128, 24.3 / 29.0; 64 of 512 .. 4096, 28 on 4 of 128, 68.0 / 63.1;
+// 13.4; 16 of 128 .. 1024, 16 on 4 of 64, 12.0 / 14.3; 3 of 20001 .. 32768, 16 on 2 of 128, 23.8 / 29.0; 64 of 512 .. 4096, 28 on 4 of 128, 68.0 / 63.1;
 // 47 of 2713, 28 on 4 of 64, 47.6 / 38.6.
 constexpr int PD_MIN_PART = 8, PD_JOIN_COST = 20, PD_CUT_COST = 66;
 constexpr int PD_WORDS = 160;                     // 32-bit words of shared memory in front of the sequences' page counts

@@ -20,7 +20,7 @@
 // tile, for the first bound.
 //
 // 2047 rows of 152064 bf16 logits, five alternatives: 161 us, 3.9 TB/s, six tenths of what a copy reaches.  What bounds it is instruction issue: sums and entropy alone take
-// 128 us, the alternatives 25, the rank 10.  64 rows of fp32, twenty alternatives: 22.4 us, a row's beginning and end and the join being
+// 128 us, the alternatives 25, the rank 10.  64 rows of fp32, twenty alternatives: 21.7 us, a row's beginning and end and the join being
 // two thirds of it.  Not kept: rings of 4 KB per warp (193 us where this took 173), 8 .. 28 reader warps (180 .. 231), half of the exponentials as polynomials (213),
 // a thread's own loop over its candidates (324).
 #include <algorithm>
