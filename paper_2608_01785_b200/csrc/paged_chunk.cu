@@ -180,21 +180,17 @@ __device__ __forceinline__ ItemView make_view(const ChunkParams& p, const int* i
   return v;
 }
 
-// Joins the parts of a tile's rows, in order: a thread has a row and a third of its coordinates; two times four coordinates of eight parts are on their way at
-// a time.
+// Joins the parts of a tile's rows, in order: a thread has a row and some of its coordinates, the fewer the fewer rows there are; eight of them in eight parts
+// are on their way at a time.
 template <int DH, bool F16>
 __device__ __forceinline__ void join_tile(const ChunkParams& p, const ItemView& v, Division div, int t) {
-  constexpr int OF = DH / 4, MINE = ((OF + 2) / 3 + 1) & ~1;    // (12, 12 and 8 of 32; 6, 6 and 4 of 16)
-  static_assert(3 * MINE >= OF && PC_THREADS >= 3 * 128, "three groups of threads");
   const hs_paged_attention_t& a = p.a;
-  const int r = threadIdx.x & 127, c0 = int(threadIdx.x >> 7) * MINE, Mt = p.tile_tokens, hg = r / Mt, tok = r - hg * Mt;
-  if (c0 >= OF || hg >= v.heads || tok >= (t ? v.n_tok_b : v.n_tok_a)) return;
-  const int n_parts = t ? v.parts_b : v.parts_a;
+  const int n_tok = t ? v.n_tok_b : v.n_tok_a, n_parts = t ? v.parts_b : v.parts_a, n_rows = v.heads * n_tok;
+  const int side = (n_rows + 31) & ~31, groups = PC_THREADS / side, group = int(threadIdx.x) / side, q = int(threadIdx.x) - group * side;
+  if (q >= n_rows || group >= groups) return;
+  const int hg = q / n_tok, tok = q - hg * n_tok, r = hg * p.tile_tokens + tok;
   const TilePart<DH>* tile_parts = reinterpret_cast<const TilePart<DH>*>(static_cast<const char*>(a.workspace) + kWsScratch) + v.item * div.parts * 2 + t;
   float top = -INFINITY, l = 0.f;
-  float4 o[MINE];
-#pragma unroll
-  for (int i = 0; i < MINE; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
   for (int k0 = 0; k0 < n_parts; k0 += 8) {
     float2 ml[8];
@@ -203,46 +199,46 @@ __device__ __forceinline__ void join_tile(const ChunkParams& p, const ItemView& 
     for (int u = 0; u < 8; ++u) ml[u] = k0 + u < n_parts ? __ldcg(&tile_parts[2 * (k0 + u)].ml[r]) : make_float2(-INFINITY, 0.f);
 #pragma unroll
     for (int u = 0; u < 8; ++u) next = fmaxf(next, ml[u].x);
-    const float zero = next == -INFINITY ? 0.f : next, f0 = fast_exp2(top - zero);
+    const float zero = next == -INFINITY ? 0.f : next;
+    l *= fast_exp2(top - zero);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) l = fmaf(fast_exp2(ml[u].x - zero), ml[u].y, l);
     top = next;
-    l *= f0;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      ml[u].x = fast_exp2(ml[u].x - zero);               // (0 for a part that is not there)
-      l = fmaf(ml[u].x, ml[u].y, l);
-    }
-#pragma unroll
-    for (int i = 0; i < MINE; i += 2) {
-      if (c0 + i >= OF) break;
+  }
+  const int64_t row = v.row0 + t * p.tile_tokens + tok;
+  const float zero = top == -INFINITY ? 0.f : top, inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
+#pragma unroll 1
+  for (int c = 2 * group; c < DH / 4; c += 2 * groups) {
+    float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+    for (int k0 = 0; k0 < n_parts; k0 += 8) {
+      float m[8];
       float4 x[2][8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < 8; ++u) {
+        const bool there = k0 + u < n_parts;
+        const TilePart<DH>& from = tile_parts[2 * (k0 + u)];
+        m[u] = there ? __ldcg(&from.ml[r].x) : -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e][u] = k0 + u < n_parts ? __ldcg(&tile_parts[2 * (k0 + u)].o[c0 + i + e][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int e = 0; e < 2; ++e) x[e][u] = there ? __ldcg(&from.o[c + e][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float4& to = o[i + e];
-        to.x *= f0; to.y *= f0; to.z *= f0; to.w *= f0;
+      for (int u = 0; u < 8; ++u) {
+        const float f = fast_exp2(m[u] - zero);          // (0 for a part that is not there)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          to.x = fmaf(ml[u].x, x[e][u].x, to.x);
-          to.y = fmaf(ml[u].x, x[e][u].y, to.y);
-          to.z = fmaf(ml[u].x, x[e][u].z, to.z);
-          to.w = fmaf(ml[u].x, x[e][u].w, to.w);
+        for (int e = 0; e < 2; ++e) {
+          o[e].x = fmaf(f, x[e][u].x, o[e].x);
+          o[e].y = fmaf(f, x[e][u].y, o[e].y);
+          o[e].z = fmaf(f, x[e][u].z, o[e].z);
+          o[e].w = fmaf(f, x[e][u].w, o[e].w);
         }
       }
     }
+    *reinterpret_cast<uint4*>(dst + c * 4) = make_uint4(pack_16<F16>(o[0].x * inv, o[0].y * inv), pack_16<F16>(o[0].z * inv, o[0].w * inv),
+                                                       pack_16<F16>(o[1].x * inv, o[1].y * inv), pack_16<F16>(o[1].z * inv, o[1].w * inv));
   }
-  const int64_t row = v.row0 + t * Mt + tok;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
-#pragma unroll
-  for (int i = 0; i < MINE; i += 2) {
-    if (c0 + i >= OF) break;
-    *reinterpret_cast<uint4*>(dst + (c0 + i) * 4) = make_uint4(pack_16<F16>(o[i].x * inv, o[i].y * inv), pack_16<F16>(o[i].z * inv, o[i].w * inv),
-                                                             pack_16<F16>(o[i + 1].x * inv, o[i + 1].y * inv), pack_16<F16>(o[i + 1].z * inv, o[i + 1].w * inv));
-  }
-  if (c0 == 0 && a.lse) a.lse[row * a.n_q_heads + v.head0 + hg] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
+  if (group == 0 && a.lse) a.lse[row * a.n_q_heads + v.head0 + hg] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
 }
 
 template <int DH, bool F16, bool MOD, bool DIVIDED>
