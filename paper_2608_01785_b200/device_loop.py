@@ -124,7 +124,8 @@ class DeviceLoop:
         self.top_ids.index_copy_(0, owner, b["top_ids"])
 
     def prefill(self, prompts: Sequence[Sequence[int]]) -> None:
-        """Runs all prompts as one chunk (at most max_prompt_tokens tokens) and samples each request's first token."""
+        """Runs all prompts as one chunk (at most max_prompt_tokens tokens) and samples each request's first token.  Prompts that do not fit the pool or the block
+        tables leave a status and the requests as they were."""
         b, lens = self._prompt_buffers, [len(p) for p in prompts]
         assert len(lens) == self.n and min(lens) >= 1 and sum(lens) <= b["tokens"].numel()
         ops.step_tables(self.ctx_len, torch.tensor(lens, dtype=torch.int32, device=self.device), self.free_list, self.free_count, self.tables, b["kv_len"], b["begin"],
@@ -133,8 +134,11 @@ class DeviceLoop:
         b["tokens"].zero_()
         b["tokens"][:len(flat)] = torch.tensor(flat, dtype=torch.int32, device=self.device)
         self._layers(b, max(max(lens), 2))
-        b["rows"].copy_(b["begin"][1:] - 1)
-        self._sample(b, torch.arange(self.n, device=self.device))
+        # (a request without rows -- every one of them, where the tables were refused -- has no last row: row 0 stands for it, and what that gives goes to the
+        # spare entry)
+        first, last = b["begin"][:-1], b["begin"][1:]
+        b["rows"].copy_((last - 1).clamp(min=0))
+        self._sample(b, torch.where(last > first, torch.arange(self.n, device=self.device), self.n))
         self.ctx_len.copy_(b["kv_len"])
 
     def _decode(self) -> None:

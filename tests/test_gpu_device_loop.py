@@ -139,3 +139,20 @@ def test_example_runs(capsys):
     from paper_2608_01785_b200 import device_loop
     device_loop.main(["--requests", "3", "--tokens", "8"])
     assert "pages free again" in capsys.readouterr().out
+
+
+@pytest.mark.parametrize("pages,positions,status", [(12, 160, "OUT_OF_PAGES"), (40, 80, "INVALID_ARG")])
+def test_prompts_that_do_not_fit_leave_the_requests_as_they_were(pages, positions, status):
+    from paper_2608_01785_b200 import binding as B
+    dims, w, prompts = make()                              # 13 pages, the longest 90 tokens
+    loop = DeviceLoop(dims, w, 5, pages, positions, sum(map(len, prompts)))
+    loop.last_token[:5] = torch.arange(5, dtype=torch.int32, device="cuda")
+    names = ("ctx_len", "tables", "free_count", "free_list", "pool")
+    before = {k: getattr(loop, k).clone() for k in names}
+    loop.prefill(prompts)
+    torch.cuda.synchronize()
+    assert int(loop.status) == getattr(B, "HS_ERR_" + status)
+    for k in names:
+        assert torch.equal(getattr(loop, k), before[k]), k
+    assert loop.last_token[:5].tolist() == [0, 1, 2, 3, 4] and loop.logprob[:5].tolist() == [0] * 5 and bool((loop.top_ids[:5] == 0).all())
+    loop.close()
