@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       const int hi = min(max(pos, v.prefix - 1), v.kv - 1), lo = a.window > 0 ? pos - a.window + 1 : 0;
       const float slope = MOD && a.slopes && row_valid ? a.slopes[v.head0 + hg] * 1.4426950408889634f : 0.f;
 
-      float m_ref = -INFINITY, l_run = 0.f;       // (MOD: in log2 units; else of the raw scores)
+      float m_ref = -INFINITY, l_run = 0.f;       // (MOD: in log2 units; else of the raw scores, whose scale is positive)
       uint32_t sreg[32], sreg2[32];
       for (int j = 0; j < nblk; ++j, ++g) {
         const uint32_t buf = g & 1, bph = (g >> 1) & 1;
@@ -843,7 +843,10 @@ cudaError_t launch_paged_chunk(const hs_paged_attention_t& a, const CUtensorMap&
   const int64_t tokens = 2 * p.tile_tokens;
   const int64_t pairs = std::min(int64_t(a.n_seqs) * ((a.max_q_len + tokens - 1) / tokens), a.n_tokens / tokens + a.n_seqs);
   const bool divided = 2 * pairs * a.n_kv_heads * p.chunks <= p.shares && int64_t(a.max_pages_per_seq) * HS_PAGE_SIZE > (PC_DIVIDED - 1) * PC_KEYS;
-  return launch_step_kernel(pick(a.head_dim, a.type == HS_TYPE_F16, a.cap > 0.f || a.slopes != nullptr, divided), sm_budget, PC_THREADS,
+  // Without a cap and slopes the kernel masks and compares raw scores and multiplies by the scale in the exponent: right for a positive scale only.  The other
+  // instantiation scales first.
+  const bool modified = a.cap > 0.f || a.slopes != nullptr || !(a.scale > 0.f);
+  return launch_step_kernel(pick(a.head_dim, a.type == HS_TYPE_F16, modified, divided), sm_budget, PC_THREADS,
                             a.head_dim == 128 ? pc_smem<128>() : pc_smem<64>(), stream, true, p);
 }
 
