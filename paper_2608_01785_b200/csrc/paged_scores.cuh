@@ -1,5 +1,7 @@
 // What the two forms of the paged attention share: a row's view of the keys, and what becomes of a score.
 #pragma once
+#include <cmath>
+
 #include "device_ops.h"
 #include "ptx.cuh"
 
@@ -25,15 +27,22 @@ inline ScoreScale score_scale(float scale, float cap) {
   r.in = cap > 0.f ? float(double(scale) / cap) : float(scale * l2e);
   r.out = cap > 0.f ? float(cap * l2e) : 0.f;
   r.limit3 = r.limit5 = -1.f;
+  // A polynomial is used where all its coefficients are normal numbers of fp32, so that none is lost: its highest one, out in^7 (or in^11) times p3[3] (p5[5]), is
+  // the first to go under where the cap is large for the scale (degree five: scale 1 / 128 with a cap of 100).
   const double in = double(scale) / cap, out = double(cap) * l2e;
-  if (cap > 0.f && cap < 1e6f && in > 1e-3 / 64 && in < 1e2) {       // (the powers stay far inside fp32)
-    r.limit3 = float(0.35 * 0.35 / (in * in));
-    r.limit5 = float(0.7 * 0.7 / (in * in));
+  if (cap > 0.f && cap < 1e6f && in > 0.0 && in < 1e2) {
+    bool normal3 = true, normal5 = true;
     double f = out * in;
     for (int i = 0; i < 6; ++i, f *= in * in) {
-      if (i < 4) r.c3[i] = float(f * p3[i]);
+      if (i < 4) {
+        r.c3[i] = float(f * p3[i]);
+        normal3 = normal3 && std::isnormal(r.c3[i]);
+      }
       r.c5[i] = float(f * p5[i]);
+      normal5 = normal5 && std::isnormal(r.c5[i]);
     }
+    if (normal3) r.limit3 = float(0.35 * 0.35 / (in * in));
+    if (normal5) r.limit5 = float(0.7 * 0.7 / (in * in));
   }
   return r;
 }

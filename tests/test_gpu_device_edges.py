@@ -1,8 +1,11 @@
 """Arguments at their ends, on a B200: scales and caps of every size, lengths up to the limit, page tables and logits that hold what they should not."""
+import math
+
 import pytest
 import torch
 
-from tests.test_gpu_device_ops import attention_case, check_attention, status, ws  # noqa: F401
+from tests import device_ref as ref
+from tests.test_gpu_device_ops import attention_case, check_attention, run_attention, status, ws  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +20,34 @@ def test_attention_of_scales_that_are_not_positive(scale, q, kv, cap, window, pr
     c = attention_case(11, kv, q, 8, 2, 64, dtype, cap, window, prefix, bias)
     c["scale"] = scale
     check_attention(c, ws, status)
+
+
+@pytest.mark.parametrize("scale,cap", [(128 ** -0.5, 50.0), (1 / 128, 100.0), (1 / 64, 300.0), (128 ** -0.5, 1000.0), (128 ** -0.5, 2000.0), (0.01, 40000.0)])
+@pytest.mark.parametrize("q", [[1] * 6, [40, 1, 2, 33, 64, 7]])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_of_caps_of_every_size(scale, cap, q, bias, dtype, ws, status):
+    """Scores up to a given share y of the cap, of either sign, one sequence for each y: the sum of a row is that of its largest score."""
+    ys, dim, kv = [0.2, 0.345, 0.5, 0.6, 0.69, 0.95], 128, [200, 130, 77, 300, 64, 140]
+    c = attention_case(12, kv, q, 4, 2, dim, dtype, cap, 0, 0, bias, poison=False)
+    c["scale"] = scale
+    u = torch.tensor([1.0, -1.0, -1.0, 1.0] * (dim // 4))
+    row = 0
+    for s, y in enumerate(ys):
+        want = y * cap / (scale * dim)                     # of the products of a coordinate of q and of k
+        a = torch.tensor(2.0 ** round(math.log2(want) / 2))
+        c["q"][row:row + q[s]] = (a * u).to(dtype)
+        row += q[s]
+        for j in range(kv[s]):
+            share = (1.0, -0.8, 0.0, 0.5, -1.0, 0.7, 0.1)[j % 7]
+            c["pool"][1, 0, int(c["tables"][s, j // 16]), :, j % 16] = (want / a * share * u).to(dtype)
+    o, lse = run_attention(c, ws, status)
+    want_o, want_lse = ref.attention(c["q"].double(), c["pool"][1].double(), c["tables"], kv, q, None, None if c["slopes"] is None else c["slopes"].double(), scale, cap, 0)
+    # q . k is exact in fp32 (128 equal products of 16 bits and a sign).  The capped score is within 4e-9 cap of the polynomial, which is added up in at
+    # most seven roundings of about its value (or 3e-7 cap by the exponential), and the bias, the maximum's distance and the change to natural
+    # logarithms round four times more: 11 of 2^-24 of at most 0.75 cap + 2^-8 of the bias's slope, below 1e-6 cap.  Weights and outputs as in check_attention.
+    tol = 1e-6 * cap + 3e-5
+    vmax, r = float(c["pool"][1, 1].abs().max()), 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11
+    assert float((lse.cpu().double() - want_lse).abs().max()) <= tol
+    assert float((o.cpu().double() - want_o).abs().max()) <= (2 * r + 2 * tol) * vmax
+    assert int(status) == 0
