@@ -1,5 +1,6 @@
 // What the two forms of the paged attention share: a row's view of the keys, and what becomes of a score.
 #pragma once
+#include <cfloat>
 #include <cmath>
 
 #include "device_ops.h"
@@ -24,7 +25,8 @@ inline ScoreScale score_scale(float scale, float cap) {
   const double p3[4] = {0.9999998477158822, -0.3333165701286625, 0.13283323562153154, -0.048376919236770864};
   const double p5[6] = {0.9999999197418465, -0.3333286097994273, 0.13325353247878916, -0.05338380790998526, 0.019735207866603637, -0.00487424220323607};
   ScoreScale r{};
-  r.in = cap > 0.f ? float(double(scale) / cap) : float(scale * l2e);
+  // (beyond fp32's range the largest number of it: every score but 0 is at the cap then, and 0 stays 0)
+  r.in = cap > 0.f ? float(std::fmax(std::fmin(double(scale) / cap, FLT_MAX), -FLT_MAX)) : float(scale * l2e);
   r.out = cap > 0.f ? float(cap * l2e) : 0.f;
   r.limit3 = r.limit5 = -1.f;
   // A polynomial is used where all its coefficients are normal numbers of fp32, so that none is lost: its highest one, out in^7 (or in^11) times p3[3] (p5[5]), is

@@ -51,3 +51,14 @@ def test_attention_of_caps_of_every_size(scale, cap, q, bias, dtype, ws, status)
     assert float((lse.cpu().double() - want_lse).abs().max()) <= tol
     assert float((o.cpu().double() - want_o).abs().max()) <= (2 * r + 2 * tol) * vmax
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("scale,cap", [(0.125, 1e-40), (1e20, 1e-25), (-1e20, 1e-25)])
+@pytest.mark.parametrize("q", [[1, 1], [9, 70]])
+def test_attention_of_caps_far_below_the_scale(scale, cap, q, ws, status):
+    """scale / cap is beyond fp32; every score is the cap or, where q . k is 0, 0."""
+    c = attention_case(13, [40, 130], q, 4, 2, 64, torch.bfloat16, cap, 0, 0, False)
+    c["scale"] = scale
+    c["q"][0] = 0
+    c["q"][-1, 1] = 0
+    check_attention(c, ws, status)
