@@ -722,7 +722,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       tc_fence_after_sync();
       const int64_t row = v.row0 + t * Mt + tok;
       uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + (v.head0 + hg) * DH;
-      const float m_log2 = m_ref * (MOD ? 1.f : sc.in);
+      // (a rounding of its own, so that both instantiations give a row the same bits: left to itself the compiler fuses it into lse's sum in one of them)
+      const float m_log2 = MOD ? m_ref : __fmul_rn(m_ref, sc.in);
       if (!DIVIDED || (t ? v.parts_b : v.parts_a) == 1) {
         const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
         if (row_valid && a.lse) a.lse[row * a.n_q_heads + v.head0 + hg] = l_run == 0.f ? -INFINITY : kLn2 * (m_log2 + log2f(l_run));

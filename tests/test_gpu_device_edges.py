@@ -1,6 +1,7 @@
 """Arguments at their ends, on a B200: scales and caps of every size, lengths up to the limit, page tables and logits that hold what they should not."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -62,3 +63,14 @@ def test_attention_of_caps_far_below_the_scale(scale, cap, q, ws, status):
     c["q"][0] = 0
     c["q"][-1, 1] = 0
     check_attention(c, ws, status)
+
+
+@pytest.mark.parametrize("q", [[40], [200], [3, 70]])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (30.0, False), (0.0, True)])
+def test_chunks_do_not_depend_on_the_width_of_the_block_table(q, cap, bias, ws, status):
+    """The same call with columns behind every sequence's pages, by which the launch takes the kernel that can divide items: the same bits."""
+    c = attention_case(15, [448, 300][:len(q)], q, 8, 2, 64, torch.bfloat16, cap, 0, 0, bias)
+    o, lse = run_attention(c, ws, status)
+    c["tables"] = np.concatenate([c["tables"], np.full((len(q), 60), -1, dtype=np.int32)], 1)
+    wide_o, wide_lse = run_attention(c, ws, status)
+    assert torch.equal(o, wide_o) and torch.equal(lse, wide_lse) and int(status) == 0
