@@ -60,7 +60,7 @@ extern "C" {
  *                      free_count outside 0 .. num_pages
  * A page id outside 0 .. num_pages - 1, popped or owned, gives its tokens the slot -1 and the status BAD_BLOCK_TABLE.
  * kv_len may be ctx_len, and free_count_out may be free_count (a loop that advances in place); otherwise no arrays overlap.
- * n_seqs 1 .. HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27.
+ * n_seqs 1 .. HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27; a request has at most 2^31 - 64 tokens (here and in the calls below), however long its row.
  */
 typedef struct {
   int32_t n_seqs, max_pages_per_seq, num_pages, max_tokens;
@@ -161,7 +161,7 @@ hs_status_t hs_op_rope_cache(const hs_rope_cache_t *a, int32_t sm_budget, void *
  * the device from the lengths; where there is little of it, it is divided along the cache, and joined in an order that does not depend on the budget.
  * Only pages that hold a key some row sees are looked up, so block table entries that a window has left behind may be anything.
  * Status INVALID_ARG: tok_begin that falls, leaves 0 .. n_tokens or gives a sequence more than max_q_len rows; none of the sequence's rows
- * are computed.  Status BAD_BLOCK_TABLE: a page id outside the pool, or a kv_len that is negative or beyond the block table row;
+ * are computed.  Status BAD_BLOCK_TABLE: a page id outside the pool, or a kv_len that is negative or beyond the block table row (or 2^31 - 64);
  * nothing outside the pool is read, and the sequence's rows are not defined.
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale and cap finite, cap and window >= 0.  q and o rows 16-byte aligned,
  * strides multiples of 8; kv_pool 256-byte aligned.  n_seqs <= HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27; below 2^31: that times

@@ -19,6 +19,10 @@ constexpr size_t kWsScratchBytes = HS_DEVICE_WORKSPACE_BYTES - kWsScratch;
 // Shares that the work of a split operator is cut into: one per SM of the device, never more than this.
 constexpr int kMaxShares = 160;
 
+// Tokens of a sequence whose block table row has that many pages.  Lengths, and lengths rounded up to whole pages or blocks of 64 keys, are 32-bit numbers, so
+// the last 64 tokens of a row of 2^27 pages are not to be had.
+__host__ __device__ inline int row_tokens(int max_pages) { return max_pages < (1 << 27) - 4 ? max_pages * HS_PAGE_SIZE : ((1 << 27) - 4) * HS_PAGE_SIZE; }
+
 inline int share_count(int sm_count) { return sm_count < kMaxShares ? sm_count : kMaxShares; }
 
 constexpr int kErrOutOfPages = HS_ERR_OUT_OF_PAGES, kErrBadBlockTable = HS_ERR_BAD_BLOCK_TABLE;

@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(PD_THREADS, 1) paged_decode_kernel(const __gri
   };
   auto look_up = [&](int x, int end) {
     Item it = {-1, 0, 0, 0};
-    if (x < end) {
+    if (unsigned(x) < unsigned(end)) {                   // (x may be up to 64 places behind a line that ends just below 2^31)
       const int s = find_seq(x), pages = page_begin[s + 1] - page_begin[s];
       const int r = x - page_begin[s] * units;
       const int unit = r / pages, i = r - unit * pages;

@@ -134,7 +134,7 @@ __device__ __forceinline__ SeqView view_seq(const hs_paged_attention_t& a, int s
   SeqView v;
   v.error = 0;
   v.kv = a.kv_len[s];
-  const int most = a.max_pages_per_seq * HS_PAGE_SIZE;
+  const int most = row_tokens(a.max_pages_per_seq);
   if (v.kv < 0 || v.kv > most) {
     v.error = kErrBadBlockTable;
     v.kv = v.kv < 0 ? 0 : most;

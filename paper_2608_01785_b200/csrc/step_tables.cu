@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(TB_THREADS, 1) step_tables_kernel(const hs_ste
   const int free_count = *a.free_count;
   int ctx[TB_PER_THREAD], q[TB_PER_THREAD], wrong = 0;
   unsigned long long mine = 0;
-  const int most = a.max_pages_per_seq * 16;
+  const int most = row_tokens(a.max_pages_per_seq);
 #pragma unroll
   for (int i = 0; i < TB_PER_THREAD; ++i) {
     const int s = tid * TB_PER_THREAD + i;
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(TB_THREADS, 1) step_tables_kernel(const hs_ste
   }
   wrong = __syncthreads_or(wrong);                       // (the sums are in shared memory for everybody, too)
   int error = 0;
-  if (wrong || n_tokens > a.max_tokens || free_count < 0 || free_count > a.num_pages) error = kErrInvalidArg;
+  if (wrong || unsigned(n_tokens) > unsigned(a.max_tokens) || free_count < 0 || free_count > a.num_pages) error = kErrInvalidArg;
   else if (n_new > free_count) error = kErrOutOfPages;
   if (error) n_tokens = n_new = 0;
 
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(TB_THREADS, 1) release_pages_kernel(const hs_r
     const int s = tid * TB_PER_THREAD + i;
     done[i] = s < n && a.done[s] != 0;
     const int ctx = done[i] ? a.ctx_len[s] : 0;
-    if (ctx < 0 || ctx > a.max_pages_per_seq * 16) wrong = 1;
+    if (ctx < 0 || ctx > row_tokens(a.max_pages_per_seq)) wrong = 1;
     pages[i] = wrong ? 0 : (ctx + 15) >> 4;
     mine += unsigned(pages[i]);
   }

@@ -5,8 +5,10 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2608_01785_b200 import binding as B
+from paper_2608_01785_b200 import device_ops as ops
 from tests import device_ref as ref
-from tests.test_gpu_device_ops import attention_case, check_attention, run_attention, status, ws  # noqa: F401
+from tests.test_gpu_device_ops import DEV, attention_case, check_attention, control_words_are_zero, i32, run_attention, status, ws  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +76,53 @@ def test_chunks_do_not_depend_on_the_width_of_the_block_table(q, cap, bias, ws, 
     c["tables"] = np.concatenate([c["tables"], np.full((len(q), 60), -1, dtype=np.int32)], 1)
     wide_o, wide_lse = run_attention(c, ws, status)
     assert torch.equal(o, wide_o) and torch.equal(lse, wide_lse) and int(status) == 0
+
+
+LONGEST = 2 ** 31 - 64                                      # of a sequence
+
+
+def test_the_longest_block_table_row(ws, status):
+    """One request whose row has all the pages that a call can have: short and longest lengths, and one beyond."""
+    width = 1 << 27
+    tables = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    free, count = i32([7, 6, 5]), i32([3])
+    outs = [torch.empty(m, dtype=torch.int32, device=DEV) for m in (2, 40, 40, 40)]
+    kv = i32([0])
+    ops.step_tables(i32([0]), i32([20]), free, count, tables, kv, *outs, count, ws, status)
+    assert int(status) == B.HS_ERR_BAD_BLOCK_TABLE            # (pages 5 and 6 of a pool of three)
+    status.zero_()
+    count.fill_(3)
+    free = i32([2, 1, 0])
+    ctx = i32([0])
+    ops.step_tables(ctx, i32([20]), free, count, tables, ctx, *outs, count, ws, status)
+    assert int(status) == 0 and int(ctx) == 20 and int(count) == 1 and tables[0, :3].tolist() == [0, 1, -1]
+    assert outs[3][:20].tolist() == list(range(20)) and outs[3][20:].tolist() == [-1] * 20
+    ops.release_pages(i32([1]), ctx, tables, free, count, ws, status)
+    assert int(status) == 0 and int(ctx) == 0 and free.tolist() == [2, 1, 0] and tables[0, :3].tolist() == [-1] * 3
+    tables[0, -5:] = 2
+    ctx.fill_(LONGEST - 3)
+    for q, why in ((3, 0), (4, B.HS_ERR_INVALID_ARG), (2 ** 31 - 1, B.HS_ERR_INVALID_ARG)):
+        status.zero_()
+        kv.fill_(-9)
+        outs[2].fill_(-9)
+        ops.step_tables(ctx, i32([q]), free, count, tables, kv, *outs, count, ws, status)
+        assert int(status) == why and int(kv) == LONGEST - (0 if why == 0 else 3)
+        assert outs[2][:4].tolist() == ([LONGEST - 3, LONGEST - 2, LONGEST - 1, -1] if why == 0 else [-1] * 4)
+    assert control_words_are_zero(ws)
+
+
+@pytest.mark.parametrize("q,cap", [([1], 0.0), ([40], 0.0), ([40], 30.0), ([200], 0.0)])
+def test_attention_at_the_longest_length(q, cap, ws, status):
+    """Under a window, so that a sequence of 2^31 - 64 keys looks at the pages of one of 448."""
+    near, width = 448, 1 << 27
+    c = attention_case(14, [near], q, 8, 2, 64, torch.bfloat16, cap, 100, 0, False)
+    o, lse = run_attention(c, ws, status)
+    tables = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    tables[0, (LONGEST - near) // 16:LONGEST // 16] = i32(c["tables"][0, :near // 16])
+    args = [c["q"].to(DEV), c["pool"].to(DEV), 1, tables]
+    begin = i32([0, q[0]])
+    got, got_lse = torch.empty_like(args[0]), torch.empty_like(lse)
+    ops.paged_attention(*args, i32([LONGEST]), got, ws, status, lse=got_lse, tok_begin=begin, max_q_len=q[0], scale=c["scale"], cap=cap, window=100)
+    assert int(status) == 0 and torch.equal(got, o) and torch.equal(got_lse, lse)
+    ops.paged_attention(*args, i32([LONGEST + 1]), got, ws, status, tok_begin=begin, max_q_len=q[0], scale=c["scale"], cap=cap, window=100)
+    assert int(status) == B.HS_ERR_BAD_BLOCK_TABLE and control_words_are_zero(ws)
