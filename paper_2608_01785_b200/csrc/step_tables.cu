@@ -113,12 +113,14 @@ __global__ void __launch_bounds__(TB_THREADS, 1) step_tables_kernel(const hs_ste
 
   const int stride = gridDim.x * TB_THREADS, first = blockIdx.x * TB_THREADS + tid;
   int bad_page = 0;
-  for (int t = first; t < a.max_tokens; t += stride) {
+  // (a capacity just below 2^31 is one that the last step of t passes)
+  for (unsigned u = first; u < unsigned(a.max_tokens); u += stride) {
+    const int t = int(u);
     int seq = -1, pos = -1, slot = -1;
     if (t < n_tokens) {
       seq = find(tok_begin, n, t);
       const int c = a.ctx_len[seq], owned = (c + 15) >> 4;
-      pos = c + t - tok_begin[seq];
+      pos = c + (t - tok_begin[seq]);
       const int i = (pos >> 4) - owned;                  // of the pages this step allocates, or negative
       const int page = i >= 0 ? a.free_list[free_count - 1 - page_begin[seq] - i] : a.block_tables[size_t(seq) * a.max_pages_per_seq + (pos >> 4)];
       if (page >= 0 && page < a.num_pages) slot = page * 16 + (pos & 15);

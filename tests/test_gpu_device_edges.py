@@ -126,3 +126,18 @@ def test_attention_at_the_longest_length(q, cap, ws, status):
     assert int(status) == 0 and torch.equal(got, o) and torch.equal(got_lse, lse)
     ops.paged_attention(*args, i32([LONGEST + 1]), got, ws, status, tok_begin=begin, max_q_len=q[0], scale=c["scale"], cap=cap, window=100)
     assert int(status) == B.HS_ERR_BAD_BLOCK_TABLE and control_words_are_zero(ws)
+
+
+def test_a_step_with_room_for_almost_all_tokens_that_a_number_counts(ws, status):
+    """Per-token arrays of 2^31 - 100 entries (8.6 GB each), which no whole number of the grid's threads fits below 2^31."""
+    cap = 2 ** 31 - 100
+    tok = [torch.zeros(cap, dtype=torch.int32, device=DEV) for _ in range(3)]
+    count, kv = i32([3]), i32([0, 0])
+    ops.step_tables(i32([0, 0]), i32([20, 1]), i32([0, 1, 2]), count, torch.full((2, 4), -1, dtype=torch.int32, device=DEV), kv, i32([0] * 3), *tok, count, ws, status)
+    assert int(status) == 0 and kv.tolist() == [20, 1] and int(count) == 0
+    # (pages 2 and 1 for the first request, 0 for the second)
+    assert [t[19:23].tolist() for t in tok] == [[0, 1, -1, -1], [19, 0, -1, -1], [19, 0, -1, -1]]
+    for t in tok:
+        for i in range(21, cap, 1 << 28):
+            assert bool((t[i:i + (1 << 28)] == -1).all())
+    assert control_words_are_zero(ws)
