@@ -58,7 +58,8 @@ extern "C" {
  *     OUT_OF_PAGES     the stack holds fewer pages than the step needs
  *     INVALID_ARG      a negative length, a request that outgrows its block table row, more than max_tokens tokens, or
  *                      free_count outside 0 .. num_pages
- * A page id outside 0 .. num_pages - 1, popped or owned, gives its tokens the slot -1 and the status BAD_BLOCK_TABLE.
+ * A page id outside 0 .. num_pages - 1, popped or owned, gives its tokens the slot -1 and the status BAD_BLOCK_TABLE; the step is done otherwise, a popped one is
+ * in the block table, and hs_op_release_pages does not take it back.
  * kv_len may be ctx_len, and free_count_out may be free_count (a loop that advances in place); otherwise no arrays overlap.
  * n_seqs 1 .. HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27; a request has at most 2^31 - 64 tokens (here and in the calls below), however long its row.
  */
@@ -80,7 +81,9 @@ hs_status_t hs_op_step_tables(const hs_step_tables_t *a, int32_t sm_budget, void
 /*
  * Gives the pages of finished requests back: request s with done[s] != 0 pushes its ceil(ctx_len[s] / 16) pages onto the stack,
  * the last page first, requests in order (the order of hs_kv_free); their block table entries become -1 and ctx_len[s] becomes 0.
- * Status INVALID_ARG, and nothing changes: a negative length or one beyond the block table row, or more pages than the stack has room for.
+ * The lengths, the block tables and the stack stay as they were (entries of free_list behind the stack's top apart), with the status
+ *     INVALID_ARG      a negative length or one beyond the block table row, or more pages than the stack has room for
+ *     BAD_BLOCK_TABLE  one of the pages is outside 0 .. num_pages - 1
  */
 typedef struct {
   int32_t n_seqs, max_pages_per_seq, num_pages;

@@ -9,7 +9,7 @@
 namespace hs {
 
 // The caller's workspace.  Control words are zero between calls; scratch holds nothing across calls.
-constexpr size_t kWsTables = 0;              // one word: blocks that are done
+constexpr size_t kWsTables = 0;              // two words: blocks that are done; whether one of them found a page outside the pool
 constexpr size_t kWsAttnDone = 1024;         // one word per share: parts delivered of the group that begins in it
 constexpr size_t kWsLogprobsDone = 4096;     // the same for logit rows
 constexpr size_t kWsChunkQueue = 8192;       // work queue of the chunk attention, and blocks that have left it

@@ -60,6 +60,7 @@ __device__ __forceinline__ bool last_block(int* done) {
     __threadfence();
     last = atomicAdd(done, 1) == int(gridDim.x) - 1;
     if (last) *done = 0;                                 // ready for the next call
+    __threadfence();
   }
   __syncthreads();
   return last != 0;
@@ -183,17 +184,36 @@ __global__ void __launch_bounds__(TB_THREADS, 1) release_pages_kernel(const hs_r
   if (tid == 0) page_begin[n] = n_back;
   wrong = __syncthreads_or(wrong);
   const bool ok = !wrong && free_count >= 0 && n_back <= a.num_pages - free_count;
+  // What lies behind the stack's top belongs to nobody: the pages go there first, and are on the stack when the last block moves its top.  If one of them is
+  // outside the pool it does not, and puts the block tables' entries back from there instead.
+  int* words = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsTables);
+  auto entry_of = [&](int i) {                            // of the i-th page that goes back: a request's last page first
+    const int s = find(page_begin, n, i);
+    return a.block_tables + size_t(s) * a.max_pages_per_seq + (page_begin[s + 1] - 1 - i);
+  };
+  bool bad_page = false;
   if (ok) {
     for (int i = blockIdx.x * TB_THREADS + tid; i < n_back; i += gridDim.x * TB_THREADS) {
-      const int s = find(page_begin, n, i);
-      int32_t* entry = a.block_tables + size_t(s) * a.max_pages_per_seq + (page_begin[s + 1] - 1 - i);      // the last page first
-      a.free_list[free_count + i] = *entry;
+      int32_t* entry = entry_of(i);
+      const int page = *entry;
+      bad_page |= page < 0 || page >= a.num_pages;
+      a.free_list[free_count + i] = page;
       *entry = -1;
     }
   }
-  if (!last_block(reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsTables))) return;
+  if (bad_page) atomicExch(words + 1, 1);
+  if (!last_block(words)) return;
   if (!ok) {
     if (tid == 0) atomicExch(a.status, kErrInvalidArg);
+    return;
+  }
+  if (__ldcg(words + 1) != 0) {
+    for (int i = tid; i < n_back; i += TB_THREADS) *entry_of(i) = __ldcg(a.free_list + free_count + i);
+    __syncthreads();
+    if (tid == 0) {
+      words[1] = 0;                                      // ready for the next call
+      atomicExch(a.status, kErrBadBlockTable);
+    }
     return;
   }
 #pragma unroll

@@ -141,3 +141,34 @@ def test_a_step_with_room_for_almost_all_tokens_that_a_number_counts(ws, status)
         for i in range(21, cap, 1 << 28):
             assert bool((t[i:i + (1 << 28)] == -1).all())
     assert control_words_are_zero(ws)
+
+
+@pytest.mark.parametrize("n", [3, 1500])
+@pytest.mark.parametrize("wrong", [-1, "beyond"])
+def test_release_of_a_row_that_holds_no_page(n, wrong, ws, status):
+    """A page id outside the pool is not put on the stack: nothing is given back, and the status says why."""
+    rng = np.random.default_rng(n)
+    ctx = rng.integers(1, 100, n)
+    num_pages = sum(ref.pages(c) for c in ctx) + 3
+    tables, free = ref.random_tables(rng, ctx, 7, num_pages)
+    done = rng.integers(0, 2, n)
+    done[1] = 1
+    pad = free.tolist() + [-5] * (num_pages - len(free))
+    keep = int(tables[1, ref.pages(ctx[1]) - 1])
+    tables[1, ref.pages(ctx[1]) - 1] = num_pages if wrong == "beyond" else wrong
+    for budget in (None, 1, 5):
+        status.zero_()
+        t = [i32(done), i32(ctx), i32(tables), i32(pad), i32([len(free)])]
+        ops.release_pages(*t, ws, status, sm_budget=budget)
+        assert int(status) == B.HS_ERR_BAD_BLOCK_TABLE
+        assert t[1].tolist() == ctx.tolist() and np.array_equal(t[2].cpu().numpy(), tables) and int(t[4]) == len(free) and t[3][:len(free)].tolist() == free.tolist()
+        assert control_words_are_zero(ws)
+        # and mended, the same call is done
+        status.zero_()
+        t[2][1, ref.pages(ctx[1]) - 1] = keep
+        whole = tables.copy()
+        whole[1, ref.pages(ctx[1]) - 1] = keep
+        want = ref.release_pages(done, ctx, whole, pad, len(free))
+        ops.release_pages(*t, ws, status, sm_budget=budget)
+        assert int(status) == 0 and t[1].tolist() == [int(x) for x in want[0]] and np.array_equal(t[2].cpu().numpy(), want[1])
+        assert int(t[4]) == want[3] and t[3][:want[3]].tolist() == [int(x) for x in want[2][:want[3]]] and control_words_are_zero(ws)
