@@ -200,7 +200,8 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t *a, int32_t sm_budg
  *     top_ids[i], top_logprobs[i] = the i-th largest x_v's index, ties to the lowest index, and its l_v - L
  * A negative target: logprob 0, rank -1.  A target >= vocab: the same, and status INVALID_ARG.  Entries of -infinity (masked
  * tokens) count as probability 0; a row of nothing else has L = -infinity, and its logprobs are -infinity and its entropy 0.
- * A row that holds NaN or +infinity has NaN for L, logprob and entropy; which alternatives it names is not defined (ids -1 .. vocab - 1).
+ * A row that holds NaN or +infinity has NaN for L, logprob and entropy; which alternatives it names is not defined (ids -1 .. vocab - 1); its rank is as above, and
+ * NaN is above nothing and has nothing above it.
  * Logits of any row stride and alignment of their type; sums in fp32.  n_rows * (vocab / 1024 + 2) below 2^31.
  */
 typedef struct {

@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
               }
             }
           }
-          if (count && mx > x_t) above += L::above(w, x_t);
+          if (count && !(mx <= x_t)) above += L::above(w, x_t);          // (a maximum that is not a number says nothing about the others)
           if (!early) {
             if (n_top > 0) {
               if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status));

@@ -8,7 +8,7 @@ import torch
 from paper_2608_01785_b200 import binding as B
 from paper_2608_01785_b200 import device_ops as ops
 from tests import device_ref as ref
-from tests.test_gpu_device_ops import DEV, attention_case, check_attention, control_words_are_zero, i32, run_attention, status, ws  # noqa: F401
+from tests.test_gpu_device_ops import DEV, NAN, attention_case, check_attention, control_words_are_zero, i32, run_attention, run_logprobs, status, ws  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -172,3 +172,19 @@ def test_release_of_a_row_that_holds_no_page(n, wrong, ws, status):
         ops.release_pages(*t, ws, status, sm_budget=budget)
         assert int(status) == 0 and t[1].tolist() == [int(x) for x in want[0]] and np.array_equal(t[2].cpu().numpy(), want[1])
         assert int(t[4]) == want[3] and t[3][:want[3]].tolist() == [int(x) for x in want[2][:want[3]]] and control_words_are_zero(ws)
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 9), (2, 5001), (4, 5001), (3, 152064), (150, 40000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_rank_in_rows_that_are_not_numbers(rows, vocab, dtype, ws, status):
+    """The logits above the target are counted whatever else the row holds; none is above a target that is not a number."""
+    g = torch.Generator().manual_seed(vocab)
+    x = (3 * torch.randn(rows, vocab, generator=g)).to(dtype)
+    targets = torch.randint(0, vocab, (rows,), generator=g).tolist()
+    for r in range(rows - 1):
+        x[r, torch.randint(0, vocab, (vocab // 500 + 1,), generator=g)] = NAN
+        x[r, torch.randint(0, vocab, (2,), generator=g)] = math.inf
+    targets[0] = int(x[0].isnan().nonzero()[0])
+    got = run_logprobs(x.to(DEV), targets, 5, 1.0, ws, status)
+    assert got["rank"].tolist() == [int((x[r] > x[r, t]).sum()) for r, t in enumerate(targets)]
+    assert bool(got["logprob"][:rows - 1].isnan().all()) and bool(got["logprob"][rows - 1:].isfinite().all()) and int(status) == 0
