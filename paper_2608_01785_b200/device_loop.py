@@ -19,6 +19,8 @@ import torch
 from . import binding as B
 from . import device_ops as ops
 
+HEAD_ROWS = 128                       # rows that one hs_head_step samples from
+
 
 @dataclass(frozen=True)
 class LoopDims:
@@ -52,6 +54,8 @@ class DeviceLoop:
     step sampled, request by request."""
 
     def __init__(self, dims: LoopDims, weights, n_requests: int, num_pages: int, max_positions: int, max_prompt_tokens: int, n_top: int = 5, sm_budget=None):
+        if not 1 <= n_requests <= ops.MAX_SEQS:
+            raise ValueError(f"n_requests: 1 .. {ops.MAX_SEQS} are possible")
         self.dims, self.w, self.n, self.budget = dims, weights, n_requests, sm_budget
         d = self.device = weights["embed"].device
         i32 = lambda *s, fill=0: torch.full(s, fill, dtype=torch.int32, device=d)  # noqa: E731
@@ -66,7 +70,7 @@ class DeviceLoop:
         # (one entry more, for the rows that pad a step)
         self.last_token, self.logprob = i32(n_requests + 1), torch.zeros(n_requests + 1, device=d)
         self.top_ids = i32(n_requests + 1, n_top)
-        cfg = B.make_head_config(dims.d_model, dims.vocab, dims.rms_eps, min(max(n_requests, 1), 128), d.index or 0)
+        cfg = B.make_head_config(dims.d_model, dims.vocab, dims.rms_eps, min(n_requests, HEAD_ROWS), d.index or 0)
         self._head_ws = torch.zeros(B.hs_head_workspace_bytes(cfg) + 256, dtype=torch.uint8, device=d)
         at = (self._head_ws.data_ptr() + 255) // 256 * 256
         self.head = B.hs_head_create(cfg, weights["g_final"].data_ptr(), weights["w_vocab"].data_ptr(), at)
@@ -116,7 +120,9 @@ class DeviceLoop:
 
     def _sample(self, b, owner) -> None:
         """Greedy tokens of the rows b["rows"] of the residual stream, their log probabilities and alternatives, to the requests `owner`."""
-        B.hs_head_step(self.head, b["x"].data_ptr(), b["rows"].data_ptr(), self.n, b["logits"].data_ptr(), b["sampled"].data_ptr(), self._budget(), self._stream())
+        for i in range(0, self.n, HEAD_ROWS):
+            B.hs_head_step(self.head, b["x"].data_ptr(), b["rows"][i:].data_ptr(), min(HEAD_ROWS, self.n - i), b["logits"][i:].data_ptr(), b["sampled"][i:].data_ptr(),
+                           self._budget(), self._stream())
         ops.token_logprobs(b["logits"], b["sampled"], b["logprob"], self.workspace, self.status, top_ids=b["top_ids"], top_logprobs=b["top_logprobs"],
                            sm_budget=self.budget)
         self.last_token.index_copy_(0, owner, b["sampled"])

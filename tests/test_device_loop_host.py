@@ -73,3 +73,23 @@ def test_a_prefill_samples_from_the_last_rows(head, monkeypatch):
     assert [r for rows, _ in head.rows for r in rows] == [9, 29, 30]
     assert loop.last_token[:3].tolist() == [7, 7, 7] and loop.ctx_len.tolist() == [10, 20, 1]
     loop.close()
+
+
+@pytest.mark.parametrize("n", [128, 129, 300])
+def test_any_number_of_requests_is_sampled_in_slices_of_the_heads_rows(head, monkeypatch, n):
+    tables(monkeypatch, list(range(n + 1)), 0)
+    loop = DeviceLoop(DIMS, make_weights(DIMS, device="cpu"), n, n, 16, n)
+    loop.prefill([[5]] * n)
+    assert [r for rows, _ in head.rows for r in rows] == list(range(n)) and loop.last_token[:n].tolist() == [7] * n
+    y, logits, tokens = (loop._prompt_buffers[k].data_ptr() for k in ("x", "logits", "sampled"))
+    at = 0
+    for rows, pointers in head.rows:
+        assert pointers == (y, logits + 4 * DIMS.vocab * at, tokens + 4 * at)
+        at += len(rows)
+    loop.close()
+
+
+@pytest.mark.parametrize("n", [0, -1, 4097])
+def test_a_number_of_requests_that_no_call_takes_is_refused_at_once(head, n):
+    with pytest.raises(ValueError, match="n_requests"):
+        DeviceLoop(DIMS, make_weights(DIMS, device="cpu"), n, 8, 16, 8)

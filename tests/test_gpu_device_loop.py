@@ -156,3 +156,27 @@ def test_prompts_that_do_not_fit_leave_the_requests_as_they_were(pages, position
         assert torch.equal(getattr(loop, k), before[k]), k
     assert loop.last_token[:5].tolist() == [0, 1, 2, 3, 4] and loop.logprob[:5].tolist() == [0] * 5 and bool((loop.top_ids[:5] == 0).all())
     loop.close()
+
+
+def test_more_requests_than_the_head_samples_at_once():
+    """300 requests, three slices of the head's rows: some of each against the plain model, with the tolerances of test_loop_matches_the_plain_model."""
+    dims = LoopDims(n_layers=1)
+    w = make_weights(dims, 3)
+    g = torch.Generator().manual_seed(4)
+    prompts = [torch.randint(0, dims.vocab, (int(torch.randint(1, 30, (1,), generator=g)),), generator=g).tolist() for _ in range(300)]
+    loop = DeviceLoop(dims, w, 300, 900, 64, sum(map(len, prompts)))
+    loop.prefill(prompts)
+    some = (0, 1, 127, 128, 129, 255, 256, 299)
+    seqs = {s: list(prompts[s]) for s in some}
+    for _ in range(3):
+        torch.cuda.synchronize()
+        assert int(loop.status) == 0
+        for s in some:
+            logits, token = reference(dims, w, seqs[s])[-1], int(loop.last_token[s])
+            spread = float(logits.std())
+            assert abs(float(loop.logprob[s]) - float(torch.log_softmax(logits, -1)[token])) <= 0.1 * spread
+            assert float(logits[token]) >= float(logits.max()) - 0.15 * spread and int(loop.top_ids[s, 0]) == token
+            seqs[s].append(token)
+        loop.step()
+    assert loop.ctx_len.tolist() == [len(p) + 3 for p in prompts]
+    loop.close()
