@@ -38,6 +38,9 @@ constexpr int LP_LIST = 1472;                                                   
 constexpr int LP_MIN_UNITS = 16;                                                           // of a part of a row
 constexpr int LP_ROW_COST = 36, LP_JOIN_COST = 54;                                         // units that take as long as a row's beginning and end, as a join
 constexpr int LP_JOIN_LOADS = 4;
+// A row whose list overflows is looked through by one warp (12 ns an element of a masked bf16 row, 22 of a rising fp32 one) while the others wait for its place: a wait
+// gives up after that much more.
+constexpr unsigned long long LP_WAIT_NS = 100;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFar = 1e6f;                                                               // log2 units from zero: fp32 there still has steps of 2^-4
 constexpr float kSlack = 10.f;                                                             // log2 units that a logit may lie above its thread's reference
@@ -256,6 +259,7 @@ struct LogprobsParams {
   int parts;                                             // of a row, one a share; 1: whole rows, any number a share; 0: units, cut anywhere
   int base, more;                                        // rows or units of a share; shares with one more, the first ones
   float k;                                               // scale * log2(e)
+  unsigned long long wait_ns;                            // after which a wait gives up
 };
 
 // What the readers leave of a row for the warp that ends it.
@@ -371,7 +375,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         };
         const bool count = p.a.rank != nullptr && target >= 0 && target < vocab;
         RowPlace& place = sm.place[at];
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_empty[at], row_phase ^ 1, abort_flag, p.a.status));
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_empty[at], row_phase ^ 1, abort_flag, p.a.status, p.wait_ns));
         float m = -INFINITY;                             // the thread's reference: its maximum, or up to kSlack below it
         // The distances are k x - (k m rounded to fp32): by this they are too large, all alike, until the row's end takes it out again.  (Of a
         // reference far from zero they are k (x - m).)
@@ -398,7 +402,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         for (int v0 = g.u0 * LP_UNIT; v0 < g.u1 * LP_UNIT; v0 += kTile) {
           const bool first = v0 == g.u0 * LP_UNIT;
           const int lo = max(v0, g.first), hi = min(min(v0 + kTile, g.u1 * LP_UNIT), g.last);
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status));
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status, p.wait_ns));
           const int pieces = ok ? max(hi - lo, 0) / kPer : 0;
           const uint8_t* tile = sm.ring[slot];
           uint32_t w[LP_PIECES * 4];
@@ -521,7 +525,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           if (count && !(mx <= x_t)) above += L::above(w, x_t);          // (a maximum that is not a number says nothing about the others)
           if (!early) {
             if (n_top > 0) {
-              if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status));
+              if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status, p.wait_ns));
               look_for_candidates();
             }
             give_back();
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           const Segment g = segment_at(row, u0, end);
           for (int v = g.u0 * LP_UNIT; v < g.u1 * LP_UNIT; v += kTile) {
             const int lo = max(v, g.first), hi = min(min(v + kTile, g.u1 * LP_UNIT), g.last);
-            ok = mbar_wait(&sm.empty[slot], phase ^ 1, abort_flag, p.a.status);
+            ok = mbar_wait(&sm.empty[slot], phase ^ 1, abort_flag, p.a.status, p.wait_ns);
             if (!ok) break;
             if (hi > lo) {
               mbar_expect_tx(&sm.full[slot], (hi - lo) * L::kSize);
@@ -591,7 +595,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
       for (int share = blockIdx.x; share < p.shares; share += gridDim.x) {
         const int begin = share_begin(share), end = share_begin(share + 1);
         for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end; ++row, u0 = 0) {
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.best_full[at], row_phase, abort_flag, p.a.status));
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.best_full[at], row_phase, abort_flag, p.a.status, p.wait_ns));
           RowPlace& place = sm.place[at];
           const int next = at ^ 1;
           const uint32_t next_phase = at ? row_phase ^ 1 : row_phase;
@@ -613,7 +617,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
             bool news = false;
             const unsigned long long t0 = globaltimer_ns();
             while (ok && !news && !*abort_flag) {
-              if (globaltimer_ns() - t0 > kWaitLimitNs) {
+              if (globaltimer_ns() - t0 > p.wait_ns) {
                 *abort_flag = 1;
                 atomicExch(p.a.status, kErrTimeout);
               }
@@ -640,7 +644,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
       for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end; ++row, u0 = 0) {
         const Segment g = segment_at(row, u0, end);
         RowPlace& place = sm.place[at];
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status));
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status, p.wait_ns));
         Sums total = {-INFINITY, 0.f, 0.f, 0};
         if (lane < LP_WARPS) total = place.sums[lane];
         total = warp_join(total, p.k);
@@ -823,6 +827,7 @@ cudaError_t launch_token_logprobs(const hs_token_logprobs_t& a, int sm_count, in
   p.base = pieces / p.shares;
   p.more = pieces % p.shares;
   p.k = float(double(a.scale) * 1.4426950408889634074);
+  p.wait_ns = kWaitLimitNs + LP_WAIT_NS * static_cast<unsigned long long>(a.vocab);
   const int grid = std::min(p.shares, sm_budget);
   if (a.type == HS_TYPE_F32) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_F32>, grid, LP_THREADS, kLpSmem, stream, true, p);
   if (a.type == HS_TYPE_BF16) return launch_step_kernel(token_logprobs_kernel<HS_TYPE_BF16>, grid, LP_THREADS, kLpSmem, stream, true, p);

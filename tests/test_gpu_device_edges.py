@@ -188,3 +188,23 @@ def test_rank_in_rows_that_are_not_numbers(rows, vocab, dtype, ws, status):
     got = run_logprobs(x.to(DEV), targets, 5, 1.0, ws, status)
     assert got["rank"].tolist() == [int((x[r] > x[r, t]).sum()) for r, t in enumerate(targets)]
     assert bool(got["logprob"][:rows - 1].isnan().all()) and bool(got["logprob"][rows - 1:].isfinite().all()) and int(status) == 0
+
+
+def test_token_logprobs_of_long_rows_that_one_warp_looks_through(ws, status):
+    """Rows whose first tile is masked, and so long that the warp that finds their alternatives takes longer than the 2 s of an ordinary wait; blocks of three rows each,
+    whose readers wait for it meanwhile."""
+    rows, vocab, last = 148, 220_000_000, 4096
+    x = torch.full((rows, vocab), -math.inf, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    x[:, vocab - last:] = (3 * torch.randn(rows, last, generator=g, device=DEV)).bfloat16()
+    got = run_logprobs(x, [vocab - 1 - r for r in range(rows)], 3, 1.0, ws, status, budget=50)
+    assert int(status) == 0
+    part = x[:, vocab - last:].cpu().double()
+    lp = torch.log_softmax(part, 1)
+    for r in range(rows):
+        order = torch.sort(-part[r], stable=True).indices[:3]
+        assert got["top_ids"][r].tolist() == (order + vocab - last).tolist() and int(got["rank"][r]) == int((part[r] > part[r, last - 1 - r]).sum())
+        # (as in check_logprobs: logits below 20)
+        assert abs(float(got["logprob"][r]) - float(lp[r, last - 1 - r])) <= 2e-5
+    del x
+    torch.cuda.empty_cache()
