@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(RC_THREADS, 1) rope_cache_kernel(const hs_rope
     }
   }
   // (a row that cannot be placed is reported by one thread of the grid per row)
-  for (int64_t t = blockIdx.x * RC_THREADS + threadIdx.x; t < a.n_tokens; t += gridDim.x * RC_THREADS) {
+  for (unsigned t = blockIdx.x * RC_THREADS + threadIdx.x; t < unsigned(a.n_tokens); t += gridDim.x * RC_THREADS) {
     const int p = a.tok_pos[t], s = a.tok_slot[t];
     if (s >= 0 && (p < 0 || p >= a.max_position || (s >> 4) >= a.num_pages)) atomicExch(a.status, kErrInvalidArg);
   }

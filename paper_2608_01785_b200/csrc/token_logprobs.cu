@@ -38,8 +38,8 @@ constexpr int LP_LIST = 1472;                                                   
 constexpr int LP_MIN_UNITS = 16;                                                           // of a part of a row
 constexpr int LP_ROW_COST = 36, LP_JOIN_COST = 54;                                         // units that take as long as a row's beginning and end, as a join
 constexpr int LP_JOIN_LOADS = 4;
-// A row whose list overflows is looked through by one warp (12 ns an element of a masked bf16 row, 22 of a rising fp32 one) while the others wait for its place: a wait
-// gives up after that much more.
+// A row whose list overflows is looked through by one warp (12 ns an element of a masked bf16 row, 22 of a rising fp32 one) while the others wait for its place: such
+// a wait gives up after that much more.
 constexpr unsigned long long LP_WAIT_NS = 100;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFar = 1e6f;                                                               // log2 units from zero: fp32 there still has steps of 2^-4
@@ -259,7 +259,7 @@ struct LogprobsParams {
   int parts;                                             // of a row, one a share; 1: whole rows, any number a share; 0: units, cut anywhere
   int base, more;                                        // rows or units of a share; shares with one more, the first ones
   float k;                                               // scale * log2(e)
-  unsigned long long wait_ns;                            // after which a wait gives up
+  unsigned long long wait_ns;                            // after which a wait gives up that may be for the end of a row
 };
 
 // What the readers leave of a row for the warp that ends it.
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
         for (int v0 = g.u0 * LP_UNIT; v0 < g.u1 * LP_UNIT; v0 += kTile) {
           const bool first = v0 == g.u0 * LP_UNIT;
           const int lo = max(v0, g.first), hi = min(min(v0 + kTile, g.u1 * LP_UNIT), g.last);
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status, p.wait_ns));
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[slot], phase, abort_flag, p.a.status));
           const int pieces = ok ? max(hi - lo, 0) / kPer : 0;
           const uint8_t* tile = sm.ring[slot];
           uint32_t w[LP_PIECES * 4];
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
           if (count && !(mx <= x_t)) above += L::above(w, x_t);          // (a maximum that is not a number says nothing about the others)
           if (!early) {
             if (n_top > 0) {
-              if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status, p.wait_ns));
+              if (first && ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.bound_full[at], row_phase, abort_flag, p.a.status));
               look_for_candidates();
             }
             give_back();
@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) token_logprobs_kernel(const __g
       for (int row = begin / upr, u0 = begin % upr; row * upr + u0 < end; ++row, u0 = 0) {
         const Segment g = segment_at(row, u0, end);
         RowPlace& place = sm.place[at];
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status, p.wait_ns));
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.row_full[at], row_phase, abort_flag, p.a.status));
         Sums total = {-INFINITY, 0.f, 0.f, 0};
         if (lane < LP_WARPS) total = place.sums[lane];
         total = warp_join(total, p.k);
