@@ -159,14 +159,17 @@ hs_status_t hs_op_rope_cache(const hs_rope_cache_t *a, int32_t sm_budget, void *
  *     x_j = scale * q . k_j,   x_j = cap * tanh(x_j / cap) if cap > 0,   x_j -= slopes[h] * |p - j| if slopes are given,
  *     o = sum_j softmax(x)_j v_j,   lse = log sum_j exp(x_j)   (natural logarithm).
  * A row that sees no key gives o = 0 and lse = -infinity.  Scores, maxima, sums and o are held in fp32; the softmax weights are
- * rounded to the cache's type for the product with v.
- * max_q_len: no sequence has more rows in this call (a captured loop's bound).  1 selects the form for single tokens.  The work is planned on
+ * rounded to the cache's type for the product with v (relative to a maximum, before they are divided by their sum).
+ * What the cache holds at keys that no row of the call sees may be anything.  A key that some rows of a chunk see and others do not has a finite v: an infinity or
+ * NaN there may reach its neighbours.
+ * max_q_len: no sequence has more rows in this call (a captured loop's bound).  1 selects the form for single tokens; any other takes tiles of 128 rows of heads and
+ * tokens, for sequences with one row too, so a step of prompt chunks and many single tokens is better given as two calls, one for each.  The work is planned on
  * the device from the lengths; where there is little of it, it is divided along the cache, and joined in an order that does not depend on the budget.
  * Only pages that hold a key some row sees are looked up, so block table entries that a window has left behind may be anything.
  * Status INVALID_ARG: tok_begin that falls, leaves 0 .. n_tokens or gives a sequence more than max_q_len rows; none of the sequence's rows
  * are computed.  Status BAD_BLOCK_TABLE: a page id outside the pool, or a kv_len that is negative or beyond the block table row (or 2^31 - 64);
  * nothing outside the pool is read, and the sequence's rows are not defined.
- * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale and cap finite, cap and window >= 0.  q and o rows 16-byte aligned,
+ * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale (of either sign, or 0) and cap below 1e30, cap and window >= 0.  q and o rows 16-byte aligned,
  * strides multiples of 8; kv_pool 256-byte aligned.  n_seqs <= HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^27; below 2^31: that times
  * n_q_heads, n_tokens * n_q_heads, and the pool's rows (n_layers * 2 * num_pages * n_kv_heads * 16).
  */
@@ -203,6 +206,8 @@ hs_status_t hs_op_paged_attention(const hs_paged_attention_t *a, int32_t sm_budg
  * A row that holds NaN or +infinity has NaN for L, logprob and entropy; which alternatives it names is not defined (ids -1 .. vocab - 1); its rank is as above, and
  * NaN is above nothing and has nothing above it.
  * Logits of any row stride and alignment of their type; sums in fp32.  n_rows * (vocab / 1024 + 2) below 2^31.
+ * With alternatives, rows whose first 64 KB are -infinity (a vocabulary masked down to its upper end), rows that rise from end to end and rows of
+ * nothing but NaN are slow: one warp looks for theirs, 12 to 22 ns an element.  A call of such rows takes 20 to 170 times as long.
  */
 typedef struct {
   int32_t n_rows, vocab;       /* n_rows >= 1, 1 <= vocab < 2^30 */

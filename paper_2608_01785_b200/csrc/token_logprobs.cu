@@ -8,7 +8,9 @@
 // of them over the sixteen warps, lane by lane, are 32 keys of distinct elements, and the n_top-th largest of those is a bound that no
 // alternative lies below.  What reaches the bound is written to a list: about 32 ln(32 / (32 - n_top)) elements of the row reach the final
 // one (31 at n_top = 20), and its logarithm of them come while it rises.  The list becomes the alternatives by running top 32 of a warp,
-// 32 keys at a time, sorted and merged in the lanes.  A list that overflows is made again from the row itself.
+// 32 keys at a time, sorted and merged in the lanes.  A list that overflows is made again from the row itself, by that warp alone: where the first tile of a segment holds
+// nothing above -infinity there is no bound behind it, and rows that rise outrun theirs.  us for ordinary rows / all but the last 4096 masked / rising:
+// 64 of 152064 fp32, twenty alternatives, 30 / 606 / 1640 (with the events around it); 2047 of 152064 bf16, five, 175 / 25050 / 30200.
 //
 // Work.  A share, what a block does at a time, is whole rows, one of a row's equal parts, or, in units of 1024 elements, an equal piece of all rows put after one
 // another -- the end of a row, whole rows and the beginning of one --, whichever takes its longest share the least time (at the launch).  The block that delivers
@@ -19,8 +21,8 @@
 // memory, where rows take turns with two places, and goes on with the next row.  The readers wait for one another once in a row, behind its first
 // tile, for the first bound.
 //
-// 2047 rows of 152064 bf16 logits, five alternatives: 161 us, 3.9 TB/s, six tenths of what a copy reaches.  What bounds it is instruction issue: sums and entropy alone take
-// 128 us, the alternatives 25, the rank 10.  64 rows of fp32, twenty alternatives: 21.7 us, a row's beginning and end and the join being
+// 2047 rows of 152064 bf16 logits, five alternatives: 162 us, 3.8 TB/s, six tenths of what a copy reaches.  What bounds it is instruction issue: sums and entropy alone take
+// 128 us, the alternatives 25, the rank 10.  64 rows of fp32, twenty alternatives: 21.8 us, a row's beginning and end and the join being
 // two thirds of it.  Not kept: rings of 4 KB per warp (193 us where this took 173), 8 .. 28 reader warps (180 .. 231), half of the exponentials as polynomials (213),
 // a thread's own loop over its candidates (324).
 #include <algorithm>
