@@ -12,13 +12,14 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libhorizonserve.so")
 BINDING = os.path.join(_HERE, "_device_binding.so")
 SOURCES = ["api.cu", "gemm.cu", "gemm_skinny.cu", "small_step.cu", "metadata.cu", "attention.cu", "attention_prefill.cu", "norm.cu", "noalloc.cu", "diag.cu", "head.cu", "step_tables.cu", "rope_cache.cu", "paged_decode.cu",
-           "paged_chunk.cu", "token_logprobs.cu", "device_api.cu", "plan.cc", "control.cc"]
-HEADERS = ["hs_internal.h", "kernels.h", "ptx.cuh", "attention_decode.cuh", "weight_stream.cuh", "device_ops.h", "paged_scores.cuh",
+           "paged_chunk.cu", "token_logprobs.cu", "beam_select.cu", "shared_pages.cu", "shared_attention.cu", "device_api.cu", "plan.cc", "control.cc"]
+HEADERS = ["hs_internal.h", "kernels.h", "ptx.cuh", "attention_decode.cuh", "weight_stream.cuh", "device_ops.h", "paged_scores.cuh", "paged_tiles.cuh", "block_scan.cuh",
            os.path.join("..", "..", "include", "horizonserve.h"),
            os.path.join("..", "..", "include", "horizonserve_ops.h"),
            os.path.join("..", "..", "include", "horizonserve_control.h"),
            os.path.join("..", "..", "include", "horizonserve_head.h"),
-           os.path.join("..", "..", "include", "horizonserve_device.h")]
+           os.path.join("..", "..", "include", "horizonserve_device.h"),
+           os.path.join("..", "..", "include", "horizonserve_beams.h")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
 
@@ -35,7 +36,7 @@ def _stale() -> bool:
 
 
 def _binding_stale() -> bool:
-    return _older(BINDING, [os.path.join(CSRC, "device_binding.cpp"), os.path.join(CSRC, HEADERS[-1]), os.path.join(CSRC, "..", "..", "include", "horizonserve.h")])
+    return _older(BINDING, [os.path.join(CSRC, "device_binding.cpp"), *(os.path.join(CSRC, "..", "..", "include", f"horizonserve{n}.h") for n in ("", "_device", "_beams"))])
 
 
 def _start_binding():

@@ -1,0 +1,619 @@
+// The best continuations of every request over its beams and the vocabulary, in one pass over the logits.
+//
+//   row b of a request     L_b = log sum_v exp(scale x_v),   its n_out largest x_v
+//   request                the n_out largest  weight_b (S_b + scale x_v - L_b)  of all its beams' largest
+//
+// Work.  An item is a row or one of its equal parts.  Four teams of eight warps share a block, each with an item of its own from a queue, so that one team's
+// beginning and end hide behind the others' streams.  A thread reads four 16-byte pieces of a tile while it works on the last tile's, and keeps
+//   M, s        a whole number M near the maximum in log2 units, and s = sum 2^(k x - M), k = scale log2(e): references are changed and joined by exact
+//               powers of two.  k is the sum of two fp32 numbers, and a tile's sum is added with its rounding error kept, so that log s is good to about 1e-7.
+//               (A part whose largest logit is 2^20 of those units from zero, as in a row masked with its type's lowest number from end to end, is
+//               summed a second time with that logit as its reference.)
+//   best, tile  its largest logit, and the first tile that has it.
+// At an item's end the n_out-th largest of 64 groups of four threads' (best, tile) bounds its n_out largest logits from below: only threads whose
+// own pair reaches it can hold one, a few of 256, and the team looks through their pieces once more (the L2 has them), lists what reaches the bound and
+// ranks the list.  The main loop carries no list and no test per element for it.
+// The team that delivers a request's last item makes the choice: L_b from the parts, candidates' scores in 64 bits, the same bound, list and ranks.
+#include <algorithm>
+
+#include "paged_scores.cuh"
+
+namespace hs {
+namespace {
+
+constexpr int BS_TEAMS = 4, BS_TEAM = 256, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
+constexpr int BS_PIECES = 4, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
+constexpr int BS_LIST = 512;                                             // candidates that a team ranks at a time
+constexpr int BS_MAX_PARTS = 64;                                         // of a row
+constexpr float BS_FAR = 1048576.f;                                      // log2 units from zero beyond which references are logits
+constexpr float BS_SLACK = 16.f;                                         // log2 units that a logit may lie above its thread's reference
+
+using Key = unsigned long long;
+
+struct SelectPart {                                      // of a row, in the workspace
+  double s;                                              // sum of 2^(k (x - ref) - m)
+  float m, ref;
+  int bad, unused;                                       // bad: the part holds NaN or +infinity
+  Key keys[HS_MAX_BEAMS];                                // falling; 0: none
+};
+struct SelectParams {
+  hs_beam_select_t a;
+  int parts, items;                                      // of a row; of all rows
+  double k;                                              // scale log2(e)
+  float k_hi, k_lo;                                      // k rounded towards zero, and what that leaves out (above zero)
+};
+struct alignas(16) SelectTeam {
+  Key best[BS_WARPS][32];
+  Key group[64];
+  Key list[BS_LIST], flat[BS_LIST];
+  float score[BS_LIST];
+  double sum[BS_WARPS], lse[HS_MAX_BEAMS];
+  float m[BS_WARPS], top[BS_WARPS], base[HS_MAX_BEAMS], weight[HS_MAX_BEAMS], ref[HS_MAX_BEAMS];
+  int state[HS_MAX_BEAMS];                               // of a beam: 0: no continuation, 1: in use, 2: done
+  Key bound;
+  int flagged[BS_WARPS][32];
+  int n_list, bad, next, last;
+};
+
+// Whole numbers in the order of the floats.  (-0 counts as 0; no NaN comes here.)
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u ^ (u & 0x80000000u ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float float_of(uint32_t u) { return __uint_as_float(u ^ (u & 0x80000000u ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ Key order_of(double x) {
+  const Key u = Key(__double_as_longlong(x + 0.0));
+  return u ^ (u >> 63 ? ~0ull : 1ull << 63);
+}
+// The larger logit is the larger key, and of equal ones the lower token.
+__device__ __forceinline__ Key token_key(float x, int v) { return (Key(order_of(x)) << 32) | (0xffffffffu - unsigned(v)); }
+__device__ __forceinline__ int token_of(Key k) { return int(0xffffffffu - unsigned(k)); }
+__device__ __forceinline__ float logit_of(Key k) { return float_of(uint32_t(k >> 32)); }
+
+// The kPer logits of a 16-byte piece.
+template <int TYPE>
+struct Piece {
+  static constexpr int kPer = TYPE == HS_TYPE_F32 ? 4 : 8, kSize = 16 / kPer;
+  static __device__ __forceinline__ void get(const uint4& w, float (&x)[kPer]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (TYPE == HS_TYPE_F32) {
+        x[i] = __uint_as_float(u[i]);
+      } else if constexpr (TYPE == HS_TYPE_BF16) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+      }
+    }
+  }
+  static __device__ __forceinline__ float largest(const uint4& w) {          // or NaN
+    if constexpr (TYPE == HS_TYPE_F32) {
+      return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+    } else if constexpr (TYPE == HS_TYPE_BF16) {
+      const __nv_bfloat162* v = reinterpret_cast<const __nv_bfloat162*>(&w);
+      const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
+      return max_nan(__low2float(m), __high2float(m));
+    } else {
+      const __half2* v = reinterpret_cast<const __half2*>(&w);
+      const __half2 m = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
+      return max_nan(__low2float(m), __high2float(m));
+    }
+  }
+};
+
+// A row as 16-byte pieces, counted from the boundary at or below its beginning: the row is elements mis .. end - 1 of them.
+template <int TYPE>
+struct Row {
+  using P = Piece<TYPE>;
+  const char* base;
+  int mis, end;
+  __device__ __forceinline__ Row(const hs_beam_select_t& a, int row) {
+    const char* p = static_cast<const char*>(a.logits) + int64_t(row) * a.row_stride * P::kSize;
+    mis = int((reinterpret_cast<uintptr_t>(p) & 15u) / P::kSize);
+    base = p - mis * P::kSize;
+    end = mis + a.vocab;
+  }
+  __device__ __forceinline__ int tiles() const { return (end + BS_TILE_PIECES * P::kPer - 1) / (BS_TILE_PIECES * P::kPer); }
+  __device__ __forceinline__ uint4 whole(int piece) const {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(base + int64_t(piece) * 16));
+    return v;
+  }
+  // Any piece: what lies outside the row is -infinity.
+  __device__ __forceinline__ uint4 any(int piece) const {
+    const int e0 = piece * P::kPer;
+    if (e0 >= mis && e0 + P::kPer <= end) return whole(piece);
+    constexpr uint32_t none = TYPE == HS_TYPE_F32 ? 0xff800000u : TYPE == HS_TYPE_BF16 ? 0xff80u : 0xfc00u;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = P::kSize == 4 ? none : none | none << 16;
+#pragma unroll
+    for (int i = 0; i < P::kPer; ++i) {
+      if (e0 + i < mis || e0 + i >= end) continue;
+      if constexpr (P::kSize == 4) {
+        w[i] = reinterpret_cast<const uint32_t*>(base)[e0 + i];
+      } else {
+        const uint32_t h = reinterpret_cast<const uint16_t*>(base)[e0 + i];
+        w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | h << 16 : (w[i / 2] & 0xffff0000u) | h;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// The n-th largest of 64 groups' keys (each the largest of four threads'), by the team's first warp; 0 where fewer groups have one.
+__device__ __forceinline__ void find_bound(SelectTeam& t, int n, int lane) {
+  Key g[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    g[h] = t.best[4 * h][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) g[h] = max(g[h], t.best[4 * h + w][lane]);
+    t.group[32 * h + lane] = g[h];
+  }
+  if (lane == 0) t.bound = 0;
+  __syncwarp();
+  int above[2] = {0, 0};
+#pragma unroll 8
+  for (int j = 0; j < 64; j += 2) {
+    const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&t.group[j]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      above[h] += o.x > g[h] || (o.x == g[h] && j < 32 * h + lane) ? 1 : 0;
+      above[h] += o.y > g[h] || (o.y == g[h] && j + 1 < 32 * h + lane) ? 1 : 0;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (above[h] == n - 1) t.bound = g[h];
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid_constant__ SelectParams p) {
+  using P = Piece<TYPE>;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  const hs_beam_select_t& a = p.a;
+  const int team = int(threadIdx.x) / BS_TEAM, tid = int(threadIdx.x) % BS_TEAM, warp = tid >> 5, lane = tid & 31;
+  SelectTeam& t = reinterpret_cast<SelectTeam*>(smem_raw)[team];
+  auto team_sync = [&]() { named_barrier_sync(1 + team, BS_TEAM); };
+  const int n_out = a.n_out;
+  int* queue = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSelectQueue);
+  int* done_words = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSelectDone);
+  SelectPart* parts = reinterpret_cast<SelectPart*>(static_cast<char*>(a.workspace) + kWsScratch);
+  griddep_wait();
+
+  int item = int(blockIdx.x) * BS_TEAMS + team;
+  while (item < p.items) {
+    const int row = item / p.parts, part_i = item - row * p.parts;
+    const bool ended = a.done != nullptr && a.done[row] != 0;
+    if (tid == 0) {
+      t.next = int(gridDim.x) * BS_TEAMS + atomicAdd(queue, 1);
+      t.n_list = 0;
+      t.bad = 0;
+    }
+    SelectPart& part = parts[item];
+    if (!ended) {
+      const Row<TYPE> r(a, row);
+      const int tiles = r.tiles(), tile0 = int(int64_t(tiles) * part_i / p.parts), tile1 = int(int64_t(tiles) * (part_i + 1) / p.parts);
+      // ------------------------------------------------------------------ the stream
+      float m = -INFINITY, s = 0.f, lost = 0.f, best = -INFINITY;
+      int best_tile = 0, bad = 0;
+      auto inside = [&](int tile) {                      // every piece of the tile lies in the row
+        return tile * BS_TILE_PIECES * P::kPer >= r.mis && (tile + 1) * BS_TILE_PIECES * P::kPer <= r.end;
+      };
+      auto load = [&](int tile, uint4 (&w)[BS_PIECES]) {
+        if (inside(tile)) {
+#pragma unroll
+          for (int i = 0; i < BS_PIECES; ++i) w[i] = r.whole(tile * BS_TILE_PIECES + i * BS_TEAM + tid);
+        } else {
+#pragma unroll
+          for (int i = 0; i < BS_PIECES; ++i) w[i] = r.any(tile * BS_TILE_PIECES + i * BS_TEAM + tid);
+        }
+      };
+      uint4 next[BS_PIECES];
+      if (tile0 < tile1) load(tile0, next);
+#pragma unroll 1
+      for (int tile = tile0; tile < tile1; ++tile) {
+        uint4 w[BS_PIECES];
+#pragma unroll
+        for (int i = 0; i < BS_PIECES; ++i) w[i] = next[i];
+        if (tile + 1 < tile1) load(tile + 1, next);
+        float top = P::largest(w[0]);
+#pragma unroll
+        for (int i = 1; i < BS_PIECES; ++i) top = max_nan(top, P::largest(w[i]));
+        if (!(top < INFINITY)) bad = 1;
+        if (top > best) {
+          best = top;
+          best_tile = tile;
+          const float up = top * p.k_hi;
+          if (!(up <= m + BS_SLACK)) {                   // (m is -infinity at first)
+            const float to = ceilf(fminf(fmaxf(up, -BS_FAR), BS_FAR));
+            if (m > -INFINITY) {
+              const float f = exp2f(m - to);             // (whole numbers: exact)
+              s *= f;
+              lost *= f;
+            }
+            m = to;
+          }
+        }
+        const float ref = m > -INFINITY ? -m : 0.f;
+        const F2 hi2 = f2(p.k_hi, p.k_hi), lo2 = f2(p.k_lo, p.k_lo), ref2 = f2(ref, ref);
+        F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+        for (int i = 0; i < BS_PIECES; ++i) {
+          float x[P::kPer];
+          P::get(w[i], x);
+#pragma unroll
+          for (int e = 0; e < P::kPer; e += 2) {
+            const F2 x2 = f2(x[e], x[e + 1]);
+            float d0, d1;
+            split(fma2(x2, lo2, fma2(x2, hi2, ref2)), d0, d1);
+            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], f2(fast_exp2(d0), fast_exp2(d1)));
+          }
+        }
+        float s0, s1;
+        split(add2(sum[0], sum[1]), s0, s1);
+        const float y = (s0 + s1) - lost, z = s + y;     // (what the addition rounds away is taken from the next one)
+        lost = (z - s) - y;
+        s = z;
+      }
+      // ------------------------------------------------------------------ the item's sum, and the bound of its largest
+      {
+        const float wm = float_of(__reduce_max_sync(0xffffffffu, order_of(m)));
+        float v = m > -INFINITY ? s * exp2f(m - wm) : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        const float top = float_of(__reduce_max_sync(0xffffffffu, order_of(best)));
+        if (lane == 0) {
+          t.m[warp] = wm;
+          t.sum[warp] = double(v);
+          t.top[warp] = top;
+        }
+      }
+      const Key mine = best > -INFINITY ? (Key(order_of(best)) << 32) | (0xffffffffu - unsigned(best_tile)) : 0ull;
+      t.best[warp][lane] = mine;
+      team_sync();
+      if (bad) t.bad = 1;
+      if (warp == 0) find_bound(t, n_out, lane);
+      float top = t.top[0], ref = 0.f;
+#pragma unroll
+      for (int w = 1; w < BS_WARPS; ++w) top = fmaxf(top, t.top[w]);
+      team_sync();
+      if (top > -INFINITY && top < INFINITY && !(fabsf(top * p.k_hi) < BS_FAR)) {
+        ref = top;
+        float v = 0.f;
+#pragma unroll 1
+        for (int tile = tile0; tile < tile1; ++tile) {
+          load(tile, next);
+#pragma unroll
+          for (int i = 0; i < BS_PIECES; ++i) {
+            float x[P::kPer];
+            P::get(next[i], x);
+#pragma unroll
+            for (int e = 0; e < P::kPer; ++e) v += exp2f((x[e] - ref) * p.k_hi);
+          }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) {
+          t.m[warp] = 0.f;
+          t.sum[warp] = double(v);
+        }
+      }
+      // ------------------------------------------------------------------ what reaches it
+      Key least = t.bound;                               // first a (logit, tile), then a key
+      bool by_tile = true;
+      for (;;) {
+        const float least_x = logit_of(least);
+        const int least_tile = by_tile && least ? int(0xffffffffu - unsigned(least)) : 0;
+        const bool look = mine != 0 && (by_tile ? mine >= least : best >= least_x);
+        const unsigned who = __ballot_sync(0xffffffffu, look);
+        if (look) t.flagged[warp][__popc(who & ((1u << lane) - 1u))] = tid;
+        __syncwarp();
+        const int per = (tile1 - tile0) * BS_PIECES, total = __popc(who) * per;
+        for (int at = 0; at < total; at += 128) {
+          uint4 w[4];
+          int piece[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int i = at + 32 * u + lane, f = i / per, q = i - f * per;
+            piece[u] = i < total ? (tile0 + q / BS_PIECES) * BS_TILE_PIECES + (q % BS_PIECES) * BS_TEAM + t.flagged[warp][f] : -1;
+            if (piece[u] >= 0) w[u] = r.any(piece[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (piece[u] < 0) continue;
+            if (least != 0 && !(P::largest(w[u]) >= least_x)) continue;
+            float x[P::kPer];
+            P::get(w[u], x);
+            const int tile = piece[u] / BS_TILE_PIECES;
+#pragma unroll
+            for (int e = 0; e < P::kPer; ++e) {
+              const Key key = token_key(x[e], piece[u] * P::kPer + e - r.mis);
+              const bool in = x[e] > -INFINITY && (least == 0 || (by_tile ? x[e] > least_x || (x[e] == least_x && tile <= least_tile) : key >= least));
+              if (in) {
+                const int n = atomicAdd(&t.n_list, 1);
+                if (n < BS_LIST) t.list[n] = key;
+              }
+            }
+          }
+        }
+        team_sync();
+        const int n = t.n_list;
+        if (n <= BS_LIST) break;
+        // The list has run over: the n_out-th largest of the keys that it holds is a bound that fewer reach.
+        for (int i = tid; i < BS_LIST; i += BS_TEAM) {
+          int above = 0;
+          for (int j = 0; j < BS_LIST; ++j) above += t.list[j] > t.list[i] ? 1 : 0;
+          if (above == n_out - 1) t.bound = t.list[i];
+        }
+        team_sync();
+        least = t.bound;
+        by_tile = false;
+        if (tid == 0) t.n_list = 0;
+        team_sync();
+      }
+      const int n = t.n_list;
+      for (int i = tid; i < n; i += BS_TEAM) {
+        const Key k = t.list[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += t.list[j] > k ? 1 : 0;
+        if (above < n_out) part.keys[above] = k;
+      }
+      if (tid >= n && tid < n_out) part.keys[tid] = 0;
+      if (tid == 0) {
+        float top = t.m[0];
+        for (int w = 1; w < BS_WARPS; ++w) top = fmaxf(top, t.m[w]);
+        double sum = 0.0;
+        for (int w = 0; w < BS_WARPS; ++w)
+          if (t.m[w] > -INFINITY) sum += t.sum[w] * double(exp2f(t.m[w] - top));
+        part.m = top;
+        part.ref = ref;
+        part.s = sum;
+        part.bad = t.bad;
+      }
+    }
+    __threadfence();
+    team_sync();
+    const int request = row / a.n_beams;
+    if (tid == 0) {
+      const int all = a.n_beams * p.parts;
+      t.last = atomicAdd(done_words + request, 1) == all - 1;
+      if (t.last) done_words[request] = 0;               // ready for the next call
+      t.n_list = 0;
+    }
+    team_sync();
+    if (t.last) {
+      // -------------------------------------------------------------------- the request's choice
+      __threadfence();
+      const int row0 = request * a.n_beams;
+      for (int b = warp; b < a.n_beams; b += BS_WARPS) {
+        const bool over = a.done != nullptr && a.done[row0 + b] != 0;
+        // (parts of a row may have different references: how far they are apart is worked out in 64 bits)
+        double far = -INFINITY, s = 0.0;
+        float m = -INFINITY, ref = 0.f;
+        int bad = 0;
+        if (!over) {
+          for (int i = lane; i < p.parts; i += 32) {
+            const SelectPart& q = parts[size_t(row0 + b) * p.parts + i];
+            const float qm = __ldcg(&q.m), qr = __ldcg(&q.ref);
+            bad |= __ldcg(&q.bad);
+            if (qm > -INFINITY && p.k * double(qr) + double(qm) > far) {
+              far = p.k * double(qr) + double(qm);
+              m = qm;
+              ref = qr;
+            }
+          }
+        }
+        bad = __any_sync(0xffffffffu, bad);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const double of = __shfl_xor_sync(0xffffffffu, far, o);
+          const float om = __shfl_xor_sync(0xffffffffu, m, o), other = __shfl_xor_sync(0xffffffffu, ref, o);
+          if (of > far || (of == far && (om > m || (om == m && other > ref)))) {
+            far = of;
+            m = om;
+            ref = other;
+          }
+        }
+        if (!over) {
+          for (int i = lane; i < p.parts; i += 32) {
+            const SelectPart& q = parts[size_t(row0 + b) * p.parts + i];
+            const float qm = __ldcg(&q.m);
+            if (qm > -INFINITY) s += __ldcg(&q.s) * exp2(p.k * (double(__ldcg(&q.ref)) - double(ref)) + (double(qm) - double(m)));
+          }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) {
+          const double lse = (double(m) + log2(s)) * 0.69314718055994530942;         // and scale ref
+          t.lse[b] = lse;
+          t.ref[b] = ref;
+          t.base[b] = a.scores[row0 + b];
+          t.weight[b] = a.weight ? a.weight[row0 + b] : 1.f;
+          t.state[b] = over ? 2 : bad || m == -INFINITY ? 0 : 1;
+          if (a.lse) a.lse[row0 + b] = over ? 0.f : bad ? NAN : m == -INFINITY ? -INFINITY : float(double(a.scale) * double(ref) + lse);
+        }
+      }
+      team_sync();
+      // Candidate c: beam, part and place in the part's keys.
+      const int per_beam = p.parts * n_out, n_cand = a.n_beams * per_beam;
+      auto candidate = [&](int c, Key& rank, Key& flat, float& score) {
+        const int b = c / per_beam, i = c - b * per_beam;
+        rank = 0;
+        double s;
+        if (t.state[b] == 2) {
+          if (i > 0) return;
+          s = double(t.base[b]);
+          flat = (Key(b) << 32) | unsigned(a.end_token);
+        } else {
+          const Key k = t.state[b] == 1 ? __ldcg(&parts[size_t(row0 + b) * p.parts + i / n_out].keys[i % n_out]) : 0;
+          if (k == 0) return;
+          s = double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]);
+          flat = (Key(b) << 32) | unsigned(token_of(k));
+        }
+        const double ranked = double(t.weight[b]) * s;
+        if (!(ranked > -INFINITY)) return;
+        rank = order_of(ranked);
+        score = float(s);
+      };
+      Key top = 0;
+      for (int c = tid; c < n_cand; c += BS_TEAM) {
+        Key rank, flat;
+        float score;
+        candidate(c, rank, flat, score);
+        top = max(top, rank);
+      }
+      t.best[warp][lane] = top;
+      team_sync();
+      if (warp == 0) find_bound(t, n_out, lane);
+      team_sync();
+      const Key least = t.bound;
+      for (int c = tid; c < n_cand; c += BS_TEAM) {
+        Key rank, flat;
+        float score;
+        candidate(c, rank, flat, score);
+        if (rank == 0 || rank < least) continue;
+        const int n = atomicAdd(&t.n_list, 1);
+        if (n < BS_LIST) {
+          t.list[n] = rank;
+          t.flat[n] = flat;
+          t.score[n] = score;
+        }
+      }
+      team_sync();
+      int n = t.n_list;
+      if (n > BS_LIST) {
+        // More ties than the list holds: one continuation after the other, each the best behind the last.
+        Key last_rank = ~0ull, last_flat = 0;
+        int found = 0;
+        for (; found < n_out; ++found) {
+          Key rank_b = 0, flat_b = ~0ull;
+          float score_b = 0.f;
+          for (int c = tid; c < n_cand; c += BS_TEAM) {
+            Key rank, flat;
+            float score;
+            candidate(c, rank, flat, score);
+            if (rank == 0 || !(rank < last_rank || (rank == last_rank && flat > last_flat))) continue;
+            if (rank > rank_b || (rank == rank_b && flat < flat_b)) {
+              rank_b = rank;
+              flat_b = flat;
+              score_b = score;
+            }
+          }
+          t.list[tid] = rank_b;                          // (the list's upper half collects what is found)
+          t.flat[tid] = flat_b;
+          t.score[tid] = score_b;
+          team_sync();
+          if (warp == 0) {
+            int w = lane;
+            for (int i = lane + 32; i < BS_TEAM; i += 32)
+              if (t.list[i] > t.list[w] || (t.list[i] == t.list[w] && t.flat[i] < t.flat[w])) w = i;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+              const int v = __shfl_xor_sync(0xffffffffu, w, o);
+              if (t.list[v] > t.list[w] || (t.list[v] == t.list[w] && (t.flat[v] < t.flat[w] || (t.flat[v] == t.flat[w] && v < w)))) w = v;
+            }
+            if (lane == 0) {
+              t.list[BS_TEAM + found] = t.list[w];
+              t.flat[BS_TEAM + found] = t.flat[w];
+              t.score[BS_TEAM + found] = t.score[w];
+            }
+          }
+          team_sync();
+          last_rank = t.list[BS_TEAM + found];
+          last_flat = t.flat[BS_TEAM + found];
+          if (last_rank == 0) break;
+        }
+        if (tid < found) {
+          t.list[tid] = t.list[BS_TEAM + tid];
+          t.flat[tid] = t.flat[BS_TEAM + tid];
+          t.score[tid] = t.score[BS_TEAM + tid];
+        }
+        n = found;
+        team_sync();
+      }
+      auto put = [&](int place, float score, int parent, int token, int over) {
+        const int64_t at = int64_t(request) * n_out + place;
+        a.out_score[at] = score;
+        a.out_parent[at] = parent;
+        a.out_token[at] = token;
+        if (a.out_done) a.out_done[at] = over;
+      };
+      for (int i = tid; i < n; i += BS_TEAM) {
+        const Key k = t.list[i], f = t.flat[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += t.list[j] > k || (t.list[j] == k && t.flat[j] < f) ? 1 : 0;
+        if (above >= n_out) continue;
+        const int b = int(f >> 32), token = int(unsigned(f));
+        put(above, t.score[i], row0 + b, token, t.state[b] == 2 || token == a.end_token ? 1 : 0);
+      }
+      if (tid >= n && tid < n_out) put(tid, -INFINITY, -1, -1, 0);
+    }
+    item = t.next;
+    team_sync();                                         // (everybody has read what the next item writes over)
+  }
+  __syncthreads();
+  // the last block to leave puts the queue back to zero
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (atomicAdd(queue + 1, 1) == int(gridDim.x) - 1) {
+      queue[0] = 0;
+      queue[1] = 0;
+    }
+  }
+}
+
+constexpr int kSelectSmem = BS_TEAMS * int(sizeof(SelectTeam)) > kMinSmemBytes ? BS_TEAMS * int(sizeof(SelectTeam)) : kMinSmemBytes;
+static_assert(sizeof(SelectTeam) % 16 == 0 && kSelectSmem <= 227 * 1024, "fits one SM");
+static_assert(BS_LIST >= BS_TEAM + HS_MAX_BEAMS, "the list's upper half holds the continuations");
+constexpr int64_t kMaxRows = 65536;
+static_assert(kMaxRows * sizeof(SelectPart) <= kWsScratchBytes, "a part per row");
+static_assert(kWsSelectQueue + 8 <= kWsSelectDone && kWsSelectDone + HS_DEVICE_MAX_SEQS * 4 <= kWsSharedQueue, "one word per request");
+
+using SelectKernel = void (*)(SelectParams);
+SelectKernel pick(int type) {
+  return type == HS_TYPE_F32 ? beam_select_kernel<HS_TYPE_F32> : type == HS_TYPE_BF16 ? beam_select_kernel<HS_TYPE_BF16> : beam_select_kernel<HS_TYPE_F16>;
+}
+
+}  // namespace
+
+cudaError_t beam_select_set_attributes() {
+  for (int type = HS_TYPE_F32; type <= HS_TYPE_F16; ++type) {
+    const cudaError_t e = set_kernel_smem(pick(type), kSelectSmem);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_beam_select(const hs_beam_select_t& a, int sm_count, int sm_budget, cudaStream_t stream) {
+  SelectParams p{};
+  p.a = a;
+  const double k = p.k = double(a.scale) * 1.4426950408889634074;
+  p.k_hi = float(k);
+  if (double(p.k_hi) > k) p.k_hi = std::nextafterf(p.k_hi, 0.f);
+  // (above zero, so that -infinity stays -infinity under both)
+  p.k_lo = std::max(float(k - double(p.k_hi)), 1e-37f);
+  // Rows are cut into equal parts so that the teams' rounds are even and short; a round costs its tiles and about two more for the item's end.
+  const int64_t rows = int64_t(a.n_requests) * a.n_beams;
+  const int per = a.type == HS_TYPE_F32 ? 4 : 8, tiles = (a.vocab + per - 1 + BS_TILE_PIECES * per - 1) / (BS_TILE_PIECES * per);
+  const int64_t teams = int64_t(share_count(sm_count)) * BS_TEAMS;
+  int64_t least = -1;
+  p.parts = 1;
+  for (int parts = 1; parts <= std::min(tiles, BS_MAX_PARTS) && rows * parts <= std::max(rows, 4 * teams); ++parts) {
+    const int64_t cost = (rows * parts + teams - 1) / teams * ((tiles + parts - 1) / parts + 2);
+    if (least < 0 || cost < least) {
+      least = cost;
+      p.parts = parts;
+    }
+  }
+  p.items = int(rows * p.parts);
+  const int grid = int(std::min<int64_t>(sm_budget, (p.items + BS_TEAMS - 1) / BS_TEAMS));
+  return launch_step_kernel(pick(a.type), grid, BS_THREADS, kSelectSmem, stream, true, p);
+}
+
+}  // namespace hs

@@ -1,4 +1,4 @@
-// The device-resident operators (include/horizonserve_device.h) on torch tensors: what device_ops.py calls.
+// The device-resident operators (include/horizonserve_device.h, include/horizonserve_beams.h) on torch tensors: what device_ops.py calls.
 //
 // A captured loop pays for these checks once, a loop of single calls every time, and there they are most of a small operator's time: in Python they took
 // 5 us of a call whose kernel takes 4.  So the checks, the description struct and the call are made here; device_ops.py keeps the signatures and
@@ -14,7 +14,7 @@
 #include <limits>
 #include <type_traits>
 
-#include "../../include/horizonserve_device.h"
+#include "../../include/horizonserve_beams.h"
 
 namespace {
 
@@ -121,6 +121,11 @@ struct Entries {
   decltype(&hs_op_rope_cache) rope_cache;
   decltype(&hs_op_paged_attention) paged_attention;
   decltype(&hs_op_token_logprobs) token_logprobs;
+  decltype(&hs_op_beam_select) beam_select;
+  decltype(&hs_op_fork_pages) fork_pages;
+  decltype(&hs_op_copy_pages) copy_pages;
+  decltype(&hs_op_compact_pages) compact_pages;
+  decltype(&hs_op_shared_attention) shared_attention;
 } entries;
 
 // One call on the current stream of device d, as the status.
@@ -288,22 +293,175 @@ long token_logprobs(PyObject* const* o) {
   return call(entries.token_logprobs, a, d, o[10]);
 }
 
-// bind(addresses of the six C entry points in the order of Entries)
+// [requests, beams or continuations] of T: its address, and the second size.
+template <typename T>
+T* per_request(PyObject* o, int64_t n, int d, const char* what, int64_t& size) {
+  const at::Tensor& t = tensor(o, what);
+  if (t.dim() != 2 || t.size(0) != n) refuse("%s: one row per request is wanted", what);
+  size = t.size(1);
+  return vec<T>(o, -1, d, what);
+}
+
+long beam_select(PyObject* const* o) {
+  const at::Tensor &x = tensor(o[0], "logits"), &scores = tensor(o[1], "scores");
+  const int d = device_of(x), type = type_of(x);
+  if (type < 0 || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) != 1)) refuse("logits: [rows, vocab] in fp32, bf16 or fp16 with contiguous rows is wanted");
+  if (scores.dim() != 2 || scores.size(0) * scores.size(1) != x.size(0)) refuse("scores: [requests, beams] for the rows of logits is wanted");
+  const int64_t n = scores.size(0), beams = scores.size(1), v = x.size(1);
+  hs_beam_select_t a{};
+  a.n_requests = int32(n, "requests");
+  a.n_beams = int32(beams, "beams");
+  a.vocab = int32(v, "vocab");
+  a.type = type;
+  a.logits = x.data_ptr();
+  a.row_stride = x.size(0) > 1 ? x.stride(0) : v;
+  a.scores = vec<float>(o[1], -1, d, "scores");
+  int64_t k = 0;
+  a.out_score = per_request<float>(o[2], n, d, "out_score", k);
+  a.n_out = int32(k, "continuations");
+  a.out_parent = vec<int32_t>(o[3], n * k, d, "out_parent");
+  a.out_token = vec<int32_t>(o[4], n * k, d, "out_token");
+  a.workspace = scratch(o[5], d);
+  a.status = vec<int32_t>(o[6], 1, d, "status");
+  a.done = vec<int32_t>(o[7], n * beams, d, "done");
+  a.weight = vec<float>(o[8], n * beams, d, "weight");
+  a.out_done = vec<int32_t>(o[9], n * k, d, "out_done");
+  a.lse = vec<float>(o[10], n * beams, d, "lse");
+  a.end_token = int32(o[11], "end_token");
+  a.scale = float(number(o[12]));
+  return call(entries.beam_select, a, d, o[13]);
+}
+
+long fork_pages(PyObject* const* o) {
+  const at::Tensor& parent = tensor(o[0], "parent");
+  const int d = device_of(parent);
+  const int64_t n = parent.numel();
+  hs_fork_pages_t a{};
+  a.n_rows = int32(n, "rows");
+  a.parent = vec<int32_t>(o[0], n, d, "parent");
+  a.ctx_len = vec<int32_t>(o[1], n, d, "ctx_len");
+  a.block_tables = table_rows(o[2], n, d, a.max_pages_per_seq);
+  const int64_t pages = tensor(o[4], "free_list").numel();
+  a.num_pages = int32(pages, "pages");
+  a.shares = vec<int32_t>(o[3], pages, d, "shares");
+  a.free_list = vec<int32_t>(o[4], pages, d, "free_list");
+  a.free_count = vec<int32_t>(o[5], 1, d, "free_count");
+  a.copy_src = vec<int32_t>(o[6], n, d, "copy_src");
+  a.copy_dst = vec<int32_t>(o[7], n, d, "copy_dst");
+  a.copy_len = vec<int32_t>(o[8], n, d, "copy_len");
+  a.workspace = scratch(o[9], d);
+  a.status = vec<int32_t>(o[10], 1, d, "status");
+  return call(entries.fork_pages, a, d, o[11]);
+}
+
+long copy_pages(PyObject* const* o) {
+  const at::Tensor& t = tensor(o[0], "kv_pool");
+  if (t.dim() == 0 || t.size(0) < 1) refuse("kv_pool: a contiguous [layers, 2, pages, kv heads, 16, head_dim] tensor is wanted");
+  PyObject* zero = PyLong_FromLong(0);
+  if (!zero) throw Refused{};
+  Pool kv;
+  try {
+    kv = pool(o[0], zero);
+  } catch (...) {
+    Py_DECREF(zero);
+    throw;
+  }
+  Py_DECREF(zero);
+  const int d = kv.device;
+  const int64_t n = tensor(o[1], "src").numel();
+  hs_copy_pages_t a{};
+  a.n_copies = int32(n, "copies");
+  a.type = kv.type;
+  a.n_layers = kv.layers;
+  a.num_pages = kv.pages;
+  a.n_kv_heads = kv.heads;
+  a.head_dim = kv.dim;
+  a.kv_pool = kv.p;
+  a.src = vec<int32_t>(o[1], n, d, "src");
+  a.dst = vec<int32_t>(o[2], n, d, "dst");
+  a.status = vec<int32_t>(o[3], 1, d, "status");
+  a.length = vec<int32_t>(o[4], n, d, "length");
+  return call(entries.copy_pages, a, d, o[5]);
+}
+
+long compact_pages(PyObject* const* o) {
+  const at::Tensor& ctx = tensor(o[1], "ctx_len");
+  const int d = device_of(ctx);
+  const int64_t n = ctx.numel(), pages = tensor(o[4], "free_list").numel(), copies = tensor(o[6], "copy_src").numel();
+  hs_compact_pages_t a{};
+  a.n_keep = int32(o[0], "n_keep");
+  a.n_rows = int32(n, "rows");
+  a.ctx_len = vec<int32_t>(o[1], n, d, "ctx_len");
+  a.block_tables = table_rows(o[2], n, d, a.max_pages_per_seq);
+  a.num_pages = int32(pages, "pages");
+  a.shares = vec<int32_t>(o[3], pages, d, "shares");
+  a.free_list = vec<int32_t>(o[4], pages, d, "free_list");
+  a.free_count = vec<int32_t>(o[5], 1, d, "free_count");
+  a.max_copies = int32(copies, "copies");
+  a.copy_src = vec<int32_t>(o[6], copies, d, "copy_src");
+  a.copy_dst = vec<int32_t>(o[7], copies, d, "copy_dst");
+  a.workspace = scratch(o[8], d);
+  a.status = vec<int32_t>(o[9], 1, d, "status");
+  return call(entries.compact_pages, a, d, o[10]);
+}
+
+long shared_attention(PyObject* const* o) {
+  const Pool kv = pool(o[1], o[2]);
+  const at::Tensor &q = tensor(o[0], "q"), &out = tensor(o[7], "o");
+  const int d = kv.device;
+  if (type_of(q) != kv.type || type_of(out) != kv.type) refuse("q, o: the pool's type is wanted");
+  if (q.dim() != 3) refuse("q: [sequences, heads, head_dim] is wanted");
+  const int64_t n = q.size(0), hq = q.size(1), groups = tensor(o[6], "shared_len").numel();
+  hs_shared_attention_t a{};
+  a.n_seqs = int32(n, "sequences");
+  a.n_groups = int32(groups, "groups");
+  a.n_q_heads = int32(hq, "query heads");
+  a.n_kv_heads = kv.heads;
+  a.head_dim = kv.dim;
+  a.type = kv.type;
+  a.n_layers = kv.layers;
+  a.layer = kv.layer;
+  a.num_pages = kv.pages;
+  a.q = rows(q, n, hq, kv.dim, d, "q", a.q_stride);
+  a.kv_pool = kv.p;
+  a.block_tables = table_rows(o[3], n, d, a.max_pages_per_seq);
+  a.kv_len = vec<int32_t>(o[4], n, d, "kv_len");
+  a.group_begin = vec<int32_t>(o[5], groups + 1, d, "group_begin");
+  a.shared_len = vec<int32_t>(o[6], groups, d, "shared_len");
+  a.o = rows(out, n, hq, kv.dim, d, "o", a.o_stride);
+  a.workspace = scratch(o[8], d);
+  a.status = vec<int32_t>(o[9], 1, d, "status");
+  a.lse = vec<float>(o[10], n * hq, d, "lse");
+  a.slopes = vec<float>(o[11], hq, d, "slopes");
+  a.scale = o[12] == Py_None ? float(1.0 / std::sqrt(double(kv.dim))) : float(number(o[12]));
+  a.cap = float(number(o[13]));
+  return call(entries.shared_attention, a, d, o[14]);
+}
+
+// bind(addresses of the C entry points in the order of Entries)
+constexpr int kEntries = 11;
 long bind(PyObject* const* o) {
-  void* p[6];
-  for (int i = 0; i < 6; ++i) {
+  void* p[kEntries];
+  for (int i = 0; i < kEntries; ++i) {
     p[i] = PyLong_AsVoidPtr(o[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) refuse("an entry point is missing");
       throw Refused{};
     }
   }
-  entries.step_tables = reinterpret_cast<decltype(entries.step_tables)>(p[0]);
-  entries.release_pages = reinterpret_cast<decltype(entries.release_pages)>(p[1]);
-  entries.rope_table = reinterpret_cast<decltype(entries.rope_table)>(p[2]);
-  entries.rope_cache = reinterpret_cast<decltype(entries.rope_cache)>(p[3]);
-  entries.paged_attention = reinterpret_cast<decltype(entries.paged_attention)>(p[4]);
-  entries.token_logprobs = reinterpret_cast<decltype(entries.token_logprobs)>(p[5]);
+  int i = 0;
+  auto next = [&](auto& fn) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(p[i++]); };
+  next(entries.step_tables);
+  next(entries.release_pages);
+  next(entries.rope_table);
+  next(entries.rope_cache);
+  next(entries.paged_attention);
+  next(entries.token_logprobs);
+  next(entries.beam_select);
+  next(entries.fork_pages);
+  next(entries.copy_pages);
+  next(entries.compact_pages);
+  next(entries.shared_attention);
   return 0;
 }
 
@@ -328,13 +486,18 @@ PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<FN, ARGS>)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<bind, 6>("bind"),
+PyMethodDef methods[] = {method<bind, kEntries>("bind"),
                          method<step_tables, 14>("step_tables"),
                          method<release_pages, 8>("release_pages"),
                          method<rope_table, 9>("rope_table"),
                          method<rope_cache, 12>("rope_cache"),
                          method<paged_attention, 17>("paged_attention"),
                          method<token_logprobs, 11>("token_logprobs"),
+                         method<beam_select, 14>("beam_select"),
+                         method<fork_pages, 12>("fork_pages"),
+                         method<copy_pages, 6>("copy_pages"),
+                         method<compact_pages, 11>("compact_pages"),
+                         method<shared_attention, 15>("shared_attention"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_device_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,9 +1,9 @@
-// Launchers of the operators of horizonserve_device.h.  Each takes the caller's description, already checked, and the device's SM
+// Launchers of the operators of horizonserve_device.h and horizonserve_beams.h.  Each takes the caller's description, already checked, and the device's SM
 // count; it enqueues one persistent kernel of at most sm_budget blocks.
 #pragma once
 #include <cuda_runtime.h>
 
-#include "../../include/horizonserve_device.h"
+#include "../../include/horizonserve_beams.h"
 #include "kernels.h"
 
 namespace hs {
@@ -14,8 +14,12 @@ constexpr size_t kWsAttnDone = 1024;         // one word per share: parts delive
 constexpr size_t kWsLogprobsDone = 4096;     // the same for logit rows
 constexpr size_t kWsChunkQueue = 8192;       // work queue of the chunk attention, and blocks that have left it
 constexpr size_t kWsChunkDone = 16 << 10;    // its divided items: warps' rows of parts delivered, tile by tile
+constexpr size_t kWsSelectQueue = 24 << 10;  // work queue of the beam selection, and blocks that have left it
+constexpr size_t kWsSelectDone = 28 << 10;   // one word per request: parts of its rows that are done
+constexpr size_t kWsSharedQueue = 48 << 10;  // shared attention: one word per share, parts delivered of the item that begins in it
 constexpr size_t kWsScratch = 64 << 10;
-constexpr size_t kWsScratchBytes = HS_DEVICE_WORKSPACE_BYTES - kWsScratch;
+constexpr size_t kWsPageBits = HS_DEVICE_WORKSPACE_BYTES - (HS_BEAMS_MAX_PAGES / 8);   // a bit per page of the pool, zero between calls
+constexpr size_t kWsScratchBytes = kWsPageBits - kWsScratch;
 // Shares that the work of a split operator is cut into: one per SM of the device, never more than this.
 constexpr int kMaxShares = 160;
 
@@ -43,5 +47,19 @@ int paged_chunk_tile_tokens(int n_q_heads, int n_kv_heads);      // token rows o
 
 cudaError_t token_logprobs_set_attributes();
 cudaError_t launch_token_logprobs(const hs_token_logprobs_t& a, int sm_count, int sm_budget, cudaStream_t stream);
+
+cudaError_t beam_select_set_attributes();
+cudaError_t launch_beam_select(const hs_beam_select_t& a, int sm_count, int sm_budget, cudaStream_t stream);
+
+cudaError_t shared_pages_set_attributes();
+cudaError_t launch_fork_pages(const hs_fork_pages_t& a, int sm_budget, cudaStream_t stream);
+cudaError_t launch_copy_pages(const hs_copy_pages_t& a, int sm_budget, cudaStream_t stream);
+cudaError_t launch_compact_pages(const hs_compact_pages_t& a, int sm_budget, cudaStream_t stream);
+
+cudaError_t shared_attention_set_attributes();
+cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_count, int sm_budget,
+                                    cudaStream_t stream);
+int shared_attention_tile_heads(int n_q_heads, int n_kv_heads);  // of tm_q's box: query heads,
+int shared_attention_tile_seqs(int n_q_heads, int n_kv_heads);   // and sequences
 
 }  // namespace hs

@@ -1,0 +1,366 @@
+// Pages that several rows of block tables hold: rows that continue other rows, copies of pages, a pool that is made smaller.
+//
+// Fork.  Row i becomes what row parent[i] was.  With children_p the rows that name p, a full page of row p loses one holder and gains children_p:
+//     shares[page] += children_p - 1,   and a page whose count falls below zero has no holder left
+// (a count is the holders but the first; partial sums never fall below it while a holder goes on, so the addition that takes it below zero is the
+// only one of its page).  Everything else follows from parent and ctx_len alone, so every block works it out for itself: children, first successors, the copies'
+// places on the stack by one running sum.  The tables are changed in place: a block has eight columns of all rows in shared memory before it writes
+// them, so no block waits for another; the last one to end sweeps the bits of freed pages, in order, onto the stack.  Rows that share a page in a column
+// are neighbours as a rule (beams of a request): their counts are added up first, mostly to zero, which spares the atomics on a prompt's pages.
+//
+// Copy.  A warp takes one head of one page and layer, K or V, at a time: up to 16 rows that follow one another, eight 16-byte pieces a lane on their way.
+//
+// Compact.  Bits of the free pages; running sums of the bits number the free pages below the bound and the used ones above it; then tables, counts, stack and
+// copy list from those numbers.  Three small kernels, one after the other.
+#include <algorithm>
+
+#include "block_scan.cuh"
+#include "device_ops.h"
+#include "ptx.cuh"
+
+namespace hs {
+namespace {
+
+constexpr int SP_THREADS = 1024, SP_PER_THREAD = HS_DEVICE_MAX_SEQS / SP_THREADS;
+constexpr int SP_COLUMNS = 8, SP_RUN = 32;               // columns of a block's slice; rows whose counts are added up before they go to memory
+constexpr int SP_FORK_SMEM = HS_DEVICE_MAX_SEQS * (4 * 4 + SP_COLUMNS * 4);
+static_assert(SP_FORK_SMEM <= 227 * 1024, "fits one SM");
+static_assert(HS_BEAMS_MAX_PAGES % 32 == 0 && HS_COMPACT_MAX_PAGES <= HS_BEAMS_MAX_PAGES, "a bit per page");
+
+__device__ __forceinline__ unsigned* page_bits(void* workspace) { return reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kWsPageBits); }
+__device__ __forceinline__ int owned_pages(int ctx) { return (ctx + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE; }
+
+__global__ void __launch_bounds__(SP_THREADS, 1) fork_pages_kernel(const hs_fork_pages_t a) {
+  extern __shared__ int smem[];
+  __shared__ unsigned long long warp_sums[32];
+  __shared__ int most;
+  griddep_wait();
+  const int n = a.n_rows, tid = threadIdx.x;
+  int* ctx = smem;                                       // [n] each, as they were
+  int* children = smem + n;
+  int* first = smem + 2 * n;                             // successor
+  int* place = smem + 3 * n;                             // of the row's copy among the copies, -1: none
+  int* slice = smem + 4 * n;                             // [n][SP_COLUMNS]
+  if (tid == 0) most = 0;
+  for (int i = tid; i < n; i += SP_THREADS) {
+    children[i] = 0;
+    first[i] = n;
+  }
+  __syncthreads();
+  const int free_count = *a.free_count;
+  int wrong = 0;
+  for (int i = tid; i < n; i += SP_THREADS) {
+    const int c = a.ctx_len[i], p = a.parent[i];
+    if (c < 0 || c > row_tokens(a.max_pages_per_seq) || p < -1 || p >= n) wrong = 1;
+    ctx[i] = c;
+    if (p >= 0 && p < n) {
+      atomicAdd(&children[p], 1);
+      atomicMin(&first[p], i);
+    }
+    if (!wrong) atomicMax(&most, owned_pages(c));
+  }
+  wrong = __syncthreads_or(wrong);
+  unsigned long long mine = 0, n_copies = 0;
+  if (!wrong) {
+#pragma unroll
+    for (int u = 0; u < SP_PER_THREAD; ++u) {
+      const int i = tid * SP_PER_THREAD + u;
+      if (i >= n) continue;
+      const int p = a.parent[i];
+      place[i] = p >= 0 && ctx[p] % HS_PAGE_SIZE != 0 && first[p] != i ? 0 : -1;
+      mine += place[i] == 0 ? 1 : 0;
+    }
+  }
+  unsigned long long at = block_scan(mine, warp_sums, n_copies);
+  if (!wrong) {
+#pragma unroll
+    for (int u = 0; u < SP_PER_THREAD; ++u) {
+      const int i = tid * SP_PER_THREAD + u;
+      if (i < n && place[i] == 0) place[i] = int(at++);
+    }
+  }
+  __syncthreads();
+  const int error = wrong || free_count < 0 || free_count > a.num_pages ? kErrInvalidArg : int(n_copies) > free_count ? kErrOutOfPages : 0;
+  if (error) {
+    for (int i = int(blockIdx.x) * SP_THREADS + tid; i < n; i += int(gridDim.x) * SP_THREADS) {
+      a.copy_src[i] = a.copy_dst[i] = -1;
+      a.copy_len[i] = 0;
+    }
+    if (blockIdx.x == 0 && tid == 0) atomicExch(a.status, error);
+    return;
+  }
+  if (blockIdx.x == 0) {
+    for (int i = tid; i < n; i += SP_THREADS) {
+      if (place[i] >= 0) continue;
+      a.copy_src[i] = a.copy_dst[i] = -1;
+      a.copy_len[i] = 0;
+    }
+  }
+
+  unsigned* bits = page_bits(a.workspace);
+  int* words = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsTables);        // blocks that are done; whether a page was freed
+  bool bad_page = false, freed = false;
+  auto inside = [&](int page) { return page >= 0 && page < a.num_pages; };
+  for (int c0 = int(blockIdx.x) * SP_COLUMNS; c0 < most; c0 += int(gridDim.x) * SP_COLUMNS) {
+    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
+      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS;
+      slice[x] = c < owned_pages(ctx[i]) ? a.block_tables[int64_t(i) * a.max_pages_per_seq + c] : -1;
+    }
+    __syncthreads();
+    // holders that full pages gain and lose; a last page that is not full is lost by a row that nobody continues
+    auto change = [&](int i, int c) { return c < ctx[i] / HS_PAGE_SIZE ? children[i] - 1 : children[i] == 0 ? -1 : 0; };
+    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
+      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS;
+      if (c >= owned_pages(ctx[i])) continue;
+      const int page = slice[x];
+      if (!inside(page)) {
+        bad_page = true;
+        continue;
+      }
+      auto same = [&](int j) { return slice[j * SP_COLUMNS + x % SP_COLUMNS] == page; };
+      if (i % SP_RUN != 0 && same(i - 1)) continue;      // (entries that a row does not own are -1 here)
+      int by = change(i, c);
+      for (int j = i + 1; j < n && j % SP_RUN != 0 && same(j); ++j) by += change(j, c);
+      if (by == 0) continue;
+      const int was = atomicAdd(&a.shares[page], by);
+      if (was >= 0 && was + by < 0) {
+        atomicOr(&bits[page >> 5], 1u << (page & 31));
+        freed = true;
+      }
+    }
+    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
+      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS, p = a.parent[i];
+      int32_t* entry = a.block_tables + int64_t(i) * a.max_pages_per_seq + c;
+      if (p < 0 || c >= owned_pages(ctx[p])) {
+        if (c < owned_pages(ctx[i])) *entry = -1;
+        continue;
+      }
+      int page = slice[p * SP_COLUMNS + x % SP_COLUMNS];
+      if (place[i] >= 0 && c == ctx[p] / HS_PAGE_SIZE) {
+        const int from = page;
+        page = a.free_list[free_count - 1 - place[i]];
+        const bool ok = inside(from) && inside(page);
+        bad_page |= !ok;
+        a.copy_src[i] = ok ? from : -1;
+        a.copy_dst[i] = ok ? page : -1;
+        a.copy_len[i] = ok ? ctx[p] % HS_PAGE_SIZE : 0;
+      }
+      *entry = page;
+    }
+    __syncthreads();
+  }
+  if (bad_page) atomicExch(a.status, kErrBadBlockTable);
+  if (freed) atomicExch(words + 1, 1);
+  if (!last_block(words)) return;
+  for (int i = tid; i < n; i += SP_THREADS) {
+    const int p = a.parent[i];
+    a.ctx_len[i] = p >= 0 ? ctx[p] : 0;
+  }
+  int top = free_count - int(n_copies);
+  if (__ldcg(words + 1) != 0) {
+    // freed pages in rising order, a run of words a thread
+    const int n_words = (a.num_pages + 31) / 32, per = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per, n_words), w1 = min(w0 + per, n_words);
+    unsigned long long count = 0, total = 0;
+    for (int w = w0; w < w1; ++w) count += __popc(__ldcg(bits + w));
+    __syncthreads();                                     // (warp_sums)
+    int to = top + int(block_scan(count, warp_sums, total));
+    for (int w = w0; w < w1; ++w) {
+      unsigned left = __ldcg(bits + w);
+      if (left == 0) continue;
+      bits[w] = 0;                                       // ready for the next call
+      for (; left; left &= left - 1) {
+        const int page = w * 32 + __ffs(left) - 1;
+        a.shares[page] = 0;
+        if (to < a.num_pages) a.free_list[to] = page;
+        ++to;
+      }
+    }
+    top = min(top + int(total), a.num_pages);
+    if (tid == 0) words[1] = 0;
+  }
+  if (tid == 0) *a.free_count = top;
+}
+
+// ------------------------------------------------------------------------------------------------------------ copies
+constexpr int CP_THREADS = 1024, CP_UNROLL = 8;
+
+__global__ void __launch_bounds__(CP_THREADS, 1) copy_pages_kernel(const hs_copy_pages_t a) {
+  const int lane = threadIdx.x & 31;
+  const int pieces = a.head_dim / 8;                     // of a token
+  const int units = a.n_layers * 2 * a.n_kv_heads, n = a.n_copies * units;
+  const int stride = int(gridDim.x) * (CP_THREADS / 32);
+  uint4* pool = static_cast<uint4*>(a.kv_pool);
+  griddep_wait();
+  // A warp's heads follow one another in steps of the grid: neighbouring warps have neighbouring heads of a page.
+  for (unsigned x = blockIdx.x * (CP_THREADS / 32) + (threadIdx.x >> 5); x < unsigned(n); x += unsigned(stride)) {
+    const int rest = int(x) / a.n_kv_heads, head = int(x) - rest * a.n_kv_heads, i = rest / (2 * a.n_layers), layer = rest - i * 2 * a.n_layers;
+    const int src = a.src[i], dst = a.dst[i], tokens = a.length ? a.length[i] : HS_PAGE_SIZE;
+    if (src == -1 || dst == -1) continue;
+    if (src < 0 || src >= a.num_pages || dst < 0 || dst >= a.num_pages || tokens < 0 || tokens > HS_PAGE_SIZE) {
+      if (lane == 0) atomicExch(a.status, tokens < 0 || tokens > HS_PAGE_SIZE ? kErrInvalidArg : kErrBadBlockTable);
+      continue;
+    }
+    const int64_t block = int64_t(HS_PAGE_SIZE) * pieces;             // pieces of one head of a page
+    const uint4* from = pool + ((int64_t(layer) * a.num_pages + src) * a.n_kv_heads + head) * block;
+    uint4* to = pool + ((int64_t(layer) * a.num_pages + dst) * a.n_kv_heads + head) * block;
+    const int count = tokens * pieces;
+    for (int at = 0; at < count; at += 32 * CP_UNROLL) {
+      uint4 v[CP_UNROLL];
+#pragma unroll
+      for (int u = 0; u < CP_UNROLL; ++u)
+        if (at + 32 * u + lane < count) v[u] = __ldcs(from + at + 32 * u + lane);
+#pragma unroll
+      for (int u = 0; u < CP_UNROLL; ++u)
+        if (at + 32 * u + lane < count) __stcs(to + at + 32 * u + lane, v[u]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ compaction
+// What the kernels of one call leave one another in the workspace.
+struct Compaction {
+  int moves, low, free_pages, wrong;                     // used pages from n_keep up; free ones below; all free ones; whether something is wrong
+};
+__device__ __forceinline__ Compaction* plan_of(const hs_compact_pages_t& a) { return reinterpret_cast<Compaction*>(static_cast<char*>(a.workspace) + kWsScratch); }
+__device__ __forceinline__ int* targets_of(const hs_compact_pages_t& a) { return reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsScratch + 256); }      // [n_keep]
+__device__ __forceinline__ int* numbers_of(const hs_compact_pages_t& a) { return targets_of(a) + a.n_keep; }        // [num_pages - n_keep]: of a move, -1 for a free page
+__device__ __forceinline__ int* sources_of(const hs_compact_pages_t& a) { return targets_of(a) + a.num_pages; }     // [num_pages - n_keep]
+static_assert(256 + size_t(HS_COMPACT_MAX_PAGES) * 2 * sizeof(int) <= kWsScratchBytes, "three lists of pages");
+
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_mark_kernel(const hs_compact_pages_t a) {
+  griddep_wait();
+  const int count = *a.free_count, first = int(blockIdx.x) * SP_THREADS + threadIdx.x, stride = int(gridDim.x) * SP_THREADS;
+  Compaction* plan = plan_of(a);
+  unsigned* bits = page_bits(a.workspace);
+  const int n = count < 0 || count > a.num_pages ? 0 : count;
+  for (int i = first; i < n; i += stride) {
+    const int page = a.free_list[i];
+    if (page >= 0 && page < a.num_pages) atomicOr(&bits[page >> 5], 1u << (page & 31));
+  }
+  if (first == 0) plan->wrong = 0;
+}
+
+// Numbers the pages: a block its share of the words, behind the sums of all words in front of it.
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_number_kernel(const hs_compact_pages_t a) {
+  __shared__ unsigned long long warp_sums[32];
+  __shared__ unsigned long long all;
+  griddep_wait();
+  const int tid = threadIdx.x, n_words = (a.num_pages + 31) / 32, keep = a.n_keep;
+  const unsigned* bits = page_bits(a.workspace);
+  const int per_block = (n_words + int(gridDim.x) - 1) / int(gridDim.x), b0 = min(int(blockIdx.x) * per_block, n_words), b1 = min(b0 + per_block, n_words);
+  // free pages below the bound (upper half) and used ones from it up
+  auto below = [&](int w) { return keep <= w * 32 ? 0u : keep >= w * 32 + 32 ? ~0u : (1u << (keep - w * 32)) - 1u; };
+  auto exists = [&](int w) { return a.num_pages >= w * 32 + 32 ? ~0u : (1u << (a.num_pages - w * 32)) - 1u; };
+  auto counts = [&](unsigned free, int w) {
+    return (static_cast<unsigned long long>(__popc(free & below(w))) << 32) + __popc(~free & ~below(w) & exists(w));
+  };
+  unsigned long long before = 0;
+  for (int w = tid; w < b0; w += SP_THREADS) before += counts(__ldcg(bits + w), w);
+  block_scan(before, warp_sums, before);
+  if (tid == 0) all = before;
+  __syncthreads();
+  const int per = (b1 - b0 + SP_THREADS - 1) / SP_THREADS, w0 = min(b0 + tid * per, b1), w1 = min(w0 + per, b1);
+  unsigned long long mine = 0, total = 0;
+  int free_high = 0;
+  for (int w = w0; w < w1; ++w) mine += counts(__ldcg(bits + w), w);
+  unsigned long long at = all + block_scan(mine, warp_sums, total);
+  int low = int(at >> 32), number = int(unsigned(at));
+  int *targets = targets_of(a), *numbers = numbers_of(a), *sources = sources_of(a);
+  for (int w = w0; w < w1; ++w) {
+    const unsigned free = __ldcg(bits + w);
+    for (unsigned left = free & below(w); left; left &= left - 1) targets[low++] = w * 32 + __ffs(left) - 1;
+    for (unsigned left = ~below(w) & exists(w); left; left &= left - 1) {
+      const int bit = __ffs(left) - 1, page = w * 32 + bit;
+      const bool used = !(free >> bit & 1u);
+      free_high += used ? 0 : 1;
+      numbers[page - keep] = used ? number : -1;
+      if (used) sources[number++] = page;
+    }
+  }
+  Compaction* plan = plan_of(a);
+  if (int(blockIdx.x) == (n_words - 1) / per_block && tid == 0) {
+    const unsigned long long end = all + total;
+    plan->moves = int(unsigned(end));
+    plan->low = int(end >> 32);
+    plan->free_pages = int(end >> 32) + (a.num_pages - keep - int(unsigned(end)));
+  }
+  // lengths that no row can have
+  int wrong = 0;
+  for (int i = int(blockIdx.x) * SP_THREADS + tid; i < a.n_rows; i += int(gridDim.x) * SP_THREADS) wrong |= a.ctx_len[i] < 0 || a.ctx_len[i] > row_tokens(a.max_pages_per_seq);
+  if (wrong) atomicExch(&plan->wrong, 1);
+}
+
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_move_kernel(const hs_compact_pages_t a) {
+  griddep_wait();
+  const Compaction plan = *plan_of(a);
+  const int *targets = targets_of(a), *numbers = numbers_of(a), *sources = sources_of(a);
+  const int first = int(blockIdx.x) * SP_THREADS + threadIdx.x, stride = int(gridDim.x) * SP_THREADS, keep = a.n_keep;
+  unsigned* bits = page_bits(a.workspace);
+  for (int w = first; w < (a.num_pages + 31) / 32; w += stride) bits[w] = 0;           // ready for the next call
+  const int error = plan.wrong || plan.free_pages != *a.free_count || plan.moves > a.max_copies ? kErrInvalidArg : plan.moves > plan.low ? kErrOutOfPages : 0;
+  const int moves = error ? 0 : plan.moves;
+  for (int k = first; k < a.max_copies; k += stride) {
+    a.copy_src[k] = k < moves ? sources[k] : -1;
+    a.copy_dst[k] = k < moves ? targets[k] : -1;
+  }
+  if (error) {
+    if (first == 0) atomicExch(a.status, error);
+    return;
+  }
+  for (int k = first; k < moves; k += stride) {
+    a.shares[targets[k]] = a.shares[sources[k]];
+    a.shares[sources[k]] = 0;
+  }
+  // the highest free page at the bottom of the stack
+  const int low = plan.low - moves, high = a.num_pages - keep;
+  for (int k = first; k < low + high; k += stride) a.free_list[low + high - 1 - k] = k < low ? targets[moves + k] : keep + k - low;
+  // a warp a row's run of entries
+  const int lane = threadIdx.x & 31, width = (a.max_pages_per_seq + 31) / 32;
+  bool bad_page = false;
+  for (int64_t x = first >> 5; x < int64_t(a.n_rows) * width; x += stride >> 5) {
+    const int row = int(x / width), c = int(x - int64_t(row) * width) * 32 + lane;
+    if (c >= owned_pages(a.ctx_len[row])) continue;
+    int32_t* entry = a.block_tables + int64_t(row) * a.max_pages_per_seq + c;
+    const int page = *entry;
+    if (page < 0 || page >= a.num_pages) {
+      bad_page = true;
+    } else if (page >= keep) {
+      const int k = numbers[page - keep];
+      if (k >= 0) *entry = targets[k];
+      else bad_page = true;
+    }
+  }
+  if (bad_page) atomicExch(a.status, kErrBadBlockTable);
+}
+
+int grid_for(int64_t work, int64_t per_block, int sm_budget) { return int(std::max<int64_t>(1, std::min<int64_t>((work + per_block - 1) / per_block, sm_budget))); }
+
+}  // namespace
+
+cudaError_t shared_pages_set_attributes() {
+  cudaError_t e = set_kernel_smem(fork_pages_kernel, std::max(SP_FORK_SMEM, kMinSmemBytes));
+  if (e == cudaSuccess) e = set_kernel_smem(copy_pages_kernel, kMinSmemBytes);
+  if (e == cudaSuccess) e = set_kernel_smem(compact_mark_kernel, kMinSmemBytes);
+  if (e == cudaSuccess) e = set_kernel_smem(compact_number_kernel, kMinSmemBytes);
+  return e == cudaSuccess ? set_kernel_smem(compact_move_kernel, kMinSmemBytes) : e;
+}
+
+cudaError_t launch_fork_pages(const hs_fork_pages_t& a, int sm_budget, cudaStream_t stream) {
+  const int smem = std::max(a.n_rows * (4 * 4 + SP_COLUMNS * 4), kMinSmemBytes);
+  return launch_step_kernel(fork_pages_kernel, grid_for(a.max_pages_per_seq, SP_COLUMNS, sm_budget), SP_THREADS, smem, stream, true, a);
+}
+
+cudaError_t launch_copy_pages(const hs_copy_pages_t& a, int sm_budget, cudaStream_t stream) {
+  const int64_t heads = int64_t(a.n_copies) * a.n_layers * 2 * a.n_kv_heads;
+  return launch_step_kernel(copy_pages_kernel, grid_for(heads, 1, sm_budget), CP_THREADS, kMinSmemBytes, stream, true, a);
+}
+
+cudaError_t launch_compact_pages(const hs_compact_pages_t& a, int sm_budget, cudaStream_t stream) {
+  cudaError_t e = launch_step_kernel(compact_mark_kernel, grid_for(a.num_pages, SP_THREADS, sm_budget), SP_THREADS, kMinSmemBytes, stream, true, a);
+  if (e == cudaSuccess) e = launch_step_kernel(compact_number_kernel, grid_for(a.num_pages, 32 * 64, sm_budget), SP_THREADS, kMinSmemBytes, stream, true, a);
+  if (e != cudaSuccess) return e;
+  const int64_t entries = std::max<int64_t>(int64_t(a.n_rows) * ((a.max_pages_per_seq + 31) / 32 * 32), a.num_pages);
+  return launch_step_kernel(compact_move_kernel, grid_for(entries, SP_THREADS, sm_budget), SP_THREADS, kMinSmemBytes, stream, true, a);
+}
+
+}  // namespace hs

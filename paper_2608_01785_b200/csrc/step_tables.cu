@@ -12,6 +12,7 @@
 // in one pass over their entries: 4.2 us for seven, 4.8 for 64 requests' 16384, 6.9 for 256000.
 #include <algorithm>
 
+#include "block_scan.cuh"
 #include "device_ops.h"
 #include "ptx.cuh"
 
@@ -20,28 +21,6 @@ namespace {
 
 constexpr int TB_THREADS = 1024, TB_PER_THREAD = HS_DEVICE_MAX_SEQS / TB_THREADS;
 static_assert(2 * (HS_DEVICE_MAX_SEQS + 1) * 4 <= kMinSmemBytes, "both sums in shared memory");
-
-// Exclusive running sums over the block's threads of a pair of counts below 2^31, packed in 64 bits; `total` is the same in every thread.
-__device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long* warp_sums, unsigned long long& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  unsigned long long inc = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long x = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += x;
-  }
-  if (lane == 31) warp_sums[warp] = inc;
-  __syncthreads();
-  unsigned long long w = warp_sums[lane];               // (32 warps)
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long x = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += x;
-  }
-  total = __shfl_sync(0xffffffffu, w, 31);
-  const unsigned long long before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
-  return (warp > 0 ? before : 0ull) + inc - v;
-}
 
 // The last s in 0 .. n - 1 with begin[s] <= x; begin has n + 1 entries and begin[n] > x.
 __device__ __forceinline__ int find(const int* begin, int n, int x) {
@@ -52,19 +31,6 @@ __device__ __forceinline__ int find(const int* begin, int n, int x) {
     else hi = mid;
   }
   return lo;
-}
-
-__device__ __forceinline__ bool last_block(int* done) {
-  __shared__ int last;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    last = atomicAdd(done, 1) == int(gridDim.x) - 1;
-    if (last) *done = 0;                                 // ready for the next call
-    __threadfence();
-  }
-  __syncthreads();
-  return last != 0;
 }
 
 __global__ void __launch_bounds__(TB_THREADS, 1) step_tables_kernel(const hs_step_tables_t a, const int in_place) {
