@@ -29,6 +29,7 @@ extern "C" {
 
 #define HS_MAX_BEAMS 32           /* beams of a request, and continuations that a call gives it */
 #define HS_BEAMS_MAX_PAGES (1 << 24)   /* pages of a pool in hs_op_fork_pages */
+#define HS_SHARED_MAX_SEQS 2048        /* sequences of a call of hs_op_shared_attention */
 #define HS_COMPACT_MAX_PAGES (1 << 21) /* and in hs_op_compact_pages */
 
 /*
@@ -149,7 +150,7 @@ hs_status_t hs_op_compact_pages(const hs_compact_pages_t *a, int32_t sm_budget, 
  * Status INVALID_ARG: group_begin that falls or leaves 0 .. n_seqs, a negative shared_len; nothing is computed.  Status BAD_BLOCK_TABLE: a page id outside
  * the pool, or a kv_len that is negative or beyond the block table row (or 2^31 - 64); nothing outside the pool is read, and the rows of the group are not defined.
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale and cap as in hs_op_paged_attention.  q and o rows 16-byte aligned, strides multiples
- * of 8; kv_pool 256-byte aligned.  n_groups <= n_seqs <= HS_DEVICE_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^26; below 2^30: that times n_q_heads; below 2^31: the pool's
+ * of 8; kv_pool 256-byte aligned.  n_groups <= n_seqs <= HS_SHARED_MAX_SEQS, n_seqs * max_pages_per_seq at most 2^26; below 2^30: that times n_q_heads; below 2^31: the pool's
  * rows (n_layers * 2 * num_pages * n_kv_heads * 16).
  */
 typedef struct {

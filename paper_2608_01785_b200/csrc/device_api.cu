@@ -258,17 +258,15 @@ hs_status_t hs_op_shared_attention(const hs_shared_attention_t* a, int32_t sm_bu
   const int64_t rows = int64_t(a->n_layers) * 2 * a->num_pages * a->n_kv_heads * kPage;
   if (!tables_shape_ok(a->n_seqs, a->max_pages_per_seq) || rows >= (int64_t(1) << 31)) return HS_ERR_UNSUPPORTED_SHAPE;
   // (the blocks of all tiles one after the other are counted in 32 bits, and so are the keys of a tile)
-  if (int64_t(a->n_seqs) * a->max_pages_per_seq > (int64_t(1) << 26) || int64_t(a->n_seqs) * a->max_pages_per_seq * a->n_q_heads >= (int64_t(1) << 30))
+  if (a->n_seqs > HS_SHARED_MAX_SEQS || int64_t(a->n_seqs) * a->max_pages_per_seq > (int64_t(1) << 26) || int64_t(a->n_seqs) * a->max_pages_per_seq * a->n_q_heads >= (int64_t(1) << 30))
     return HS_ERR_UNSUPPORTED_SHAPE;
   const Device* d = nullptr;
   const hs_status_t st = enter(sm_budget, &d);
   if (st != HS_OK) return st;
-  CUtensorMap tm_kv, tm_q;
-  if (!encode_rows(&tm_kv, a->kv_pool, rows, a->head_dim, a->head_dim, kPage) ||
-      !encode_heads(&tm_q, a->q, a->n_seqs, a->n_q_heads, a->head_dim, a->q_stride, shared_attention_tile_seqs(a->n_q_heads, a->n_kv_heads),
-                    shared_attention_tile_heads(a->n_q_heads, a->n_kv_heads)))
-    return report_cuda_error("tensor map", cudaErrorInvalidValue);
-  return launched("shared attention", launch_shared_attention(*a, tm_kv, tm_q, d->sm_count, sm_budget, static_cast<cudaStream_t>(cuda_stream)));
+  CUtensorMap tm_q;
+  const SharedTile tile = shared_attention_tile(*a);
+  if (!encode_heads(&tm_q, a->q, a->n_seqs, a->n_q_heads, a->head_dim, a->q_stride, tile.seqs, tile.heads)) return report_cuda_error("tensor map", cudaErrorInvalidValue);
+  return launched("shared attention", launch_shared_attention(*a, tm_q, d->sm_count, sm_budget, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

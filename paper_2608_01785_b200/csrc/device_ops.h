@@ -57,9 +57,10 @@ cudaError_t launch_copy_pages(const hs_copy_pages_t& a, int sm_budget, cudaStrea
 cudaError_t launch_compact_pages(const hs_compact_pages_t& a, int sm_budget, cudaStream_t stream);
 
 cudaError_t shared_attention_set_attributes();
-cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_count, int sm_budget,
-                                    cudaStream_t stream);
-int shared_attention_tile_heads(int n_q_heads, int n_kv_heads);  // of tm_q's box: query heads,
-int shared_attention_tile_seqs(int n_q_heads, int n_kv_heads);   // and sequences
+cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtensorMap& tm_q, int sm_count, int sm_budget, cudaStream_t stream);
+struct SharedTile {
+  int heads, seqs, copies;                                       // of tm_q's box: query heads, sequences; how often a tile's rows stand in the matrix
+};
+SharedTile shared_attention_tile(const hs_shared_attention_t& a);
 
 }  // namespace hs

@@ -1,18 +1,22 @@
 // Attention of one new token per sequence over the paged cache, where the sequences of a group share their first keys, on the 5th-generation
 // tensor cores; planned on the device.
 //
-//   tile      sequences of one group that follow one another, all query heads of one KV head: up to 128 rows of a matrix, sequence after sequence.
+//   tile      sequences of one group that follow one another, all query heads of one KV head: up to 128 rows of a matrix, sequence after sequence.  Where groups
+//             are small (a rule on the call's shape) a tile is 64 rows, which stand in the matrix twice: each copy's softmax has half of a block's keys.
 //   keys      the tile's keys are one line of blocks of 64: the group's shared pages, read once for all rows, then the pages of each sequence's own keys, one sequence
 //             behind the other.  A row sees the shared keys and a run of the others; what it does not see is masked, and a warp whose 32 rows see nothing
-//             of a block gives it the weight 0 and goes on.  (The products with rows that see nothing cost nothing that counts: a block's two products take 256 cycles
-//             of the tensor cores, its 32 KB take 1400 to come.)
-//   streams   a block of threads works on one tile at a time with two running softmaxes over the same rows, for the even and the odd blocks: S = Q K^T into tensor memory,
-//             one thread per row, P back over S, O += P V.  They are added at the tile's end.
-//   shares    all tiles' lines, one after the other, are cut into equal shares, about one per SM of the device, wherever the cut falls.  A tile that is cut leaves its
+//             of a block gives it the weight 0 and goes on.  (The products with rows that see nothing cost little: a block's two products take a third of
+//             the time that its 32 KB take to come.)
+//   teams     two to a thread block, each with a running softmax of its own: a warp that fetches, one that issues S = Q K^T into tensor memory and O += P V, four with one
+//             thread per row.  K and V come by 16-byte asynchronous copies: a page's 4 KB are too small a box for the tensor copies, 16 of which a block took
+//             1400 cycles.  V rows that no row sees are filled with zeros by the copy.
+//   shares    all tiles' lines, one after the other, are cut into equal shares, about one per SM of the device, wherever the cut falls, and each share into halves for
+//             the teams.  Both teams come last to the tile in the middle, which is added up over them there.  A tile that is cut between shares leaves its
 //             parts in the workspace; the block that delivers the last one joins them, in order.  Where the cuts lie depends on the lengths and the device,
 //             never on the budget, and a block takes one share after the other.
 //
-// Every block plans for itself, from the lengths, in shared memory.
+// Every block plans for itself, from the lengths, in shared memory.  The softmax works through a block 32 keys at a time in rolled loops, as it is few warps' instructions
+// that have to be fetched: unrolled over 64 keys with all its variants the same work took twice as long.
 #include <math.h>
 
 #include <algorithm>
@@ -22,19 +26,19 @@
 namespace hs {
 namespace {
 
-constexpr int SA_THREADS = 448, SA_KEYS = 64, SA_STAGES = 4, SA_ROWS = 128;
-constexpr int SA_TMEM = 512;
+constexpr int SA_THREADS = 384, SA_KEYS = 64, SA_ROWS = 128, SA_MAX_SEQS = HS_SHARED_MAX_SEQS;
+constexpr int SA_TMEM = 512, SA_TEAM_TMEM = 256;         // columns: of a team, S (two buffers of 64, P over their first 32) and O
 constexpr int SA_ITEM_COST = 3;                          // blocks that take as long as a tile's beginning and end
 constexpr int SA_MIN_SHARE = 6, SA_MIN_PART = 2;         // blocks, with the tiles' costs; blocks of a part
 constexpr float kRefSlack = 8.f;                         // log2 units by which a row's running maximum may exceed its reference
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct SharedParams {
-  CUtensorMap tm_kv, tm_q;
+  CUtensorMap tm_q;
   hs_shared_attention_t a;
   ScoreScale score;
   int heads, chunks;                                     // query heads of a tile; groups of them per KV head
-  int tile_seqs;                                         // sequences of a tile
+  int tile_seqs, copies;                                 // sequences of a tile; how often its rows stand in the matrix: 1 or 2
   int shares;                                            // at most
 };
 
@@ -45,7 +49,7 @@ struct RowsPart {
   float2 ml[SA_ROWS];
 };
 
-// One item -- a tile, or the part of it that a share has -- the same in every role.
+// One item -- a tile, or the part of it that a team has -- the same in every role.
 struct Item {
   int valid;
   int seq0, n_seq;                                       // the tile's sequences
@@ -54,20 +58,22 @@ struct Item {
   int shared_pages, shared_blocks;
   int block0, n_blocks;                                  // of the tile's line
   int parts, slot;                                       // parts of the tile (1: not cut), and where this one goes
+  int middle;                                            // the other team has a part of this part
   int number, unused;                                    // of the tile and its head, in the line
   int begin[SA_ROWS + 1];                                // own pages in front of each sequence's
   int kv[SA_ROWS];                                       // keys of each sequence
 };
-struct Barriers {
-  uint64_t q_full, q_empty;
-  uint64_t k_full[SA_STAGES], k_empty[SA_STAGES], v_full[SA_STAGES], v_empty[SA_STAGES];
-  uint64_t s_full[2][2], p_full[2][2], o_full[2][2];
-  uint64_t ring_full[2], ring_empty[2];
-  uint64_t end_full, end_read;                           // an item's end: (reference, sum) of all rows are there; O has been read
-  alignas(16) int v_keys[SA_STAGES][4];                              // keys of each page of a V block that some row sees, the first ones
+struct alignas(16) Team {
+  uint64_t q_full, q_empty, k_full[2], v_full[2], s_full[2], p_full[2], o_full[2];
+  uint64_t ring_full[2], ring_empty[2], end;
+  float2 ml[SA_ROWS];                                    // (reference, sum) of rows, at an item's end
+  Item ring[2];
+};
+struct alignas(16) Block {
   uint32_t tmem_base;
   int abort_flag, n_joins;
   int warp_sum[SA_THREADS / 32];
+  int joins[kMaxShares];                                 // tiles that this block joins
 };
 
 template <int DH>
@@ -75,15 +81,27 @@ struct SharedGeom {
   static constexpr int HALVES = DH / 64;
   static constexpr int Q_BYTES = HALVES * 16384;         // [half][128 rows][128 B]
   static constexpr int KV_BYTES = HALVES * 8192;         // K (or V) of a block: [half][4 pages][16 keys][128 B]
-  static constexpr int O0 = 256;                         // tensor-memory columns: S(stream, buffer) at stream * 128 + buffer * 64, O(stream) from here on
-  static constexpr int BARRIERS = Q_BYTES + 2 * SA_STAGES * KV_BYTES, ITEMS = BARRIERS + 1024, ML = ITEMS + 2 * int(sizeof(Item)),
-                       JOINS = ML + 2 * SA_ROWS * 8, PLAN = JOINS + kMaxShares * 4;
+  static constexpr int TEAM_BYTES = Q_BYTES + 4 * KV_BYTES;        // Q, two K blocks, two V blocks
+  static constexpr int COPY_ROWS = 512 / (DH * 2), COPIES = HS_PAGE_SIZE / COPY_ROWS;        // keys that a warp copies at a time; times for a page
+  static constexpr int O0 = 128;                         // of a team's tensor-memory columns
+  static constexpr int TEAMS = 2 * TEAM_BYTES, BLOCK = TEAMS + 2 * int(sizeof(Team)), PLAN = BLOCK + int(sizeof(Block));
   // the plan: costs of tiles (running sums), shared pages of groups; first sequences and tiles of groups in 16 bits
-  static constexpr int SMEM = 1024 + PLAN + (HS_DEVICE_MAX_SEQS + 2) * (4 + 4 + 2 + 2);
+  static constexpr int SMEM = 1024 + PLAN + (SA_MAX_SEQS + 2) * (4 + 4 + 2 + 2);
 };
-static_assert(sizeof(Barriers) <= 1024 && sizeof(Item) % 8 == 0 && SharedGeom<128>::SMEM <= 227 * 1024, "fits one SM");
+static_assert(sizeof(Team) % 16 == 0 && sizeof(Block) % 16 == 0 && SharedGeom<128>::SMEM <= 227 * 1024, "fits one SM");
 static_assert(size_t(kMaxShares) * 2 * sizeof(RowsPart<128>) <= kWsScratchBytes, "two parts per share");
-static_assert(kWsSharedQueue + kMaxShares * 4 <= kWsScratch && HS_DEVICE_MAX_SEQS < 65536, "one word per share");
+static_assert(sizeof(RowsPart<128>) <= SharedGeom<128>::TEAM_BYTES && sizeof(RowsPart<64>) <= SharedGeom<64>::TEAM_BYTES, "a team's rows of the tile in the middle");
+static_assert(1024 + kMaxShares * SA_ROWS * 4 <= SharedGeom<64>::TEAMS, "weights of a join");
+static_assert(kWsSharedQueue + kMaxShares * 4 <= kWsScratch && SA_MAX_SEQS < 65536, "one word per share");
+
+// 32 lanes x 16 consecutive 32-bit columns, registers -> tensor memory.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 
 // Running sums over the whole block of values(0) .. values(n - 1), a run of them a thread: put(i, sum in front of i); returns the sum of all.
 template <typename V, typename U>
@@ -128,6 +146,7 @@ struct Plan {
   const int *cost, *shared;                              // [tiles + 1], [groups]
   const uint16_t *group, *tile;                          // [groups + 1]: first sequence, first tile
   int tiles, line, shares;
+  int base, more;                                        // of the line for a share; shares with one more, the first ones
 };
 
 template <int DH, bool F16, bool MOD>
@@ -135,44 +154,38 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   using G_ = SharedGeom<DH>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* q_smem = smem;
-  uint8_t* k_smem = q_smem + G_::Q_BYTES;
-  uint8_t* v_smem = k_smem + SA_STAGES * G_::KV_BYTES;
-  Barriers* bar = reinterpret_cast<Barriers*>(smem + G_::BARRIERS);
-  Item* ring = reinterpret_cast<Item*>(smem + G_::ITEMS);
-  float2(*ml)[SA_ROWS] = reinterpret_cast<float2(*)[SA_ROWS]>(smem + G_::ML);            // [stream][row]
-  int* joins = reinterpret_cast<int*>(smem + G_::JOINS);                                 // tiles that this block joins
+  Block* bar = reinterpret_cast<Block*>(smem + G_::BLOCK);
   volatile int* abort_flag = &bar->abort_flag;
   const hs_shared_attention_t& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = int(threadIdx.x);
+  // Warps 0 .. 3 and 4 .. 7 are the teams' softmax warps (of tensor memory lanes 32 (warp % 4) on), 8 and 10 fetch, 9 and 11 issue the products.
+  const int team = warp < 8 ? warp >> 2 : (warp - 8) >> 1;
+  Team& tm = reinterpret_cast<Team*>(smem + G_::TEAMS)[team];
+  uint8_t* q_smem = smem + team * G_::TEAM_BYTES;
+  uint8_t* k_smem = q_smem + G_::Q_BYTES;
+  uint8_t* v_smem = k_smem + 2 * G_::KV_BYTES;
   const int n_seqs = a.n_seqs, n_groups = a.n_groups, units = a.n_kv_heads * p.chunks;
   const int most_keys = row_tokens(a.max_pages_per_seq);
 
-  if (tid == 0) {
-    mbar_init(&bar->q_full, 1);
-    mbar_init(&bar->q_empty, 2);                         // one arrival per MMA thread
-    for (int i = 0; i < SA_STAGES; ++i) {
-      mbar_init(&bar->k_full[i], 2);
-      mbar_init(&bar->k_empty[i], 1);
-      mbar_init(&bar->v_full[i], 2);
-      mbar_init(&bar->v_empty[i], 1);
-    }
-    for (int t = 0; t < 2; ++t)
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&bar->s_full[t][i], 1);
-        mbar_init(&bar->p_full[t][i], 128);
-        mbar_init(&bar->o_full[t][i], 1);
-      }
+  if (tid < 2) {
+    Team& t = reinterpret_cast<Team*>(smem + G_::TEAMS)[tid];
+    mbar_init(&t.q_full, 1);
+    mbar_init(&t.q_empty, 4);                            // one arrival per softmax warp, here and below
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bar->ring_full[i], 1);
-      mbar_init(&bar->ring_empty[i], 13);                // eight softmax warps, two MMA warps, three further producers
+      mbar_init(&t.k_full[i], 32);                       // one per lane of the warp that fetches, behind its copies
+      mbar_init(&t.v_full[i], 32);
+      mbar_init(&t.s_full[i], 1);
+      mbar_init(&t.p_full[i], 4);
+      mbar_init(&t.o_full[i], 1);
+      mbar_init(&t.ring_full[i], 1);
+      mbar_init(&t.ring_empty[i], 5);                    // four softmax warps and the one that issues products
     }
-    mbar_init(&bar->end_full, 256);
-    mbar_init(&bar->end_read, 256);
+    mbar_init(&t.end, 4);
+    fence_barrier_init();
+  }
+  if (tid == 0) {
     bar->abort_flag = 0;
     bar->n_joins = 0;
-    fence_barrier_init();
-    tma_prefetch_desc(&p.tm_kv);
     tma_prefetch_desc(&p.tm_q);
   }
   if (warp == 9) {
@@ -190,9 +203,14 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   Plan plan;
   {
     int* cost = reinterpret_cast<int*>(smem + G_::PLAN);
-    int* shared = cost + HS_DEVICE_MAX_SEQS + 2;
-    uint16_t* group = reinterpret_cast<uint16_t*>(shared + HS_DEVICE_MAX_SEQS + 2);
-    uint16_t* tile = group + HS_DEVICE_MAX_SEQS + 2;
+    int* shared = cost + SA_MAX_SEQS + 2;
+    uint16_t* group = reinterpret_cast<uint16_t*>(shared + SA_MAX_SEQS + 2);
+    uint16_t* tile = group + SA_MAX_SEQS + 2;
+    // (a thread's first sequences: their lengths are asked for before the groups are known, and kept)
+    constexpr int MINE = 2;
+    int kv[MINE], of[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) kv[i] = tid + i * SA_THREADS < n_seqs ? a.kv_len[tid + i * SA_THREADS] : 0;
     int wrong = 0;
     for (int g = tid; g <= n_groups; g += SA_THREADS) {
       const int b = a.group_begin[g];
@@ -200,35 +218,57 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       group[g] = uint16_t(b);
       shared[g] = 0x7fffffff;                            // (the fewest keys of a sequence that has some)
     }
+    for (int t = tid; t < n_seqs; t += SA_THREADS) cost[t] = 0;
     wrong = __syncthreads_or(wrong);
     if (wrong) {
       if (tid == 0 && blockIdx.x == 0) atomicExch(a.status, kErrInvalidArg);
       if (warp == 9) tmem_dealloc(tmem, SA_TMEM);
       return;
     }
+    const int s_begin = group[0], s_end = group[n_groups];
+    // every sequence of a group: its keys and its group
+    auto each = [&](auto use) {
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const int s = tid + i * SA_THREADS;
+        if (s >= s_begin && s < s_end && kv[i] > 0) use(s, kv[i], of[i]);
+      }
+      for (int s = tid + MINE * SA_THREADS; s < s_end; s += SA_THREADS) {
+        const int keys = s >= s_begin ? keys_of(s) : 0;
+        if (keys > 0) use(s, keys, find_last(group, n_groups, s));
+      }
+    };
+    int bad = 0;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int s = tid + i * SA_THREADS;
+      if (s < s_begin || s >= s_end) continue;
+      bad |= kv[i] < 0 || kv[i] > most_keys;
+      kv[i] = min(max(kv[i], 0), most_keys);
+      of[i] = find_last(group, n_groups, s);
+    }
+    if (blockIdx.x == 0) {
+      for (int s = tid + MINE * SA_THREADS; s < s_end; s += SA_THREADS) bad |= s >= s_begin && (a.kv_len[s] < 0 || a.kv_len[s] > most_keys);
+      if (bad) atomicExch(a.status, kErrBadBlockTable);
+    }
+    each([&](int, int keys, int g) { atomicMin(&shared[g], keys); });
     plan.tiles = running_sums(n_groups, bar->warp_sum, [&](int g) { return (int(group[g + 1]) - int(group[g]) + p.tile_seqs - 1) / p.tile_seqs; },
-                              [&](int g, int sum) { tile[g] = uint16_t(sum); });
+                              [&](int g, int sum) {
+                                tile[g] = uint16_t(sum);
+                                shared[g] = shared[g] == 0x7fffffff ? 0 : min(shared[g], a.shared_len[g]) / HS_PAGE_SIZE;
+                              });
     if (tid == 0) tile[n_groups] = uint16_t(plan.tiles);
-    const int s_end = group[n_groups];
-    for (int s = int(group[0]) + tid; s < s_end; s += SA_THREADS) {
-      const int kv = a.kv_len[s];
-      if ((kv < 0 || kv > most_keys) && blockIdx.x == 0) atomicExch(a.status, kErrBadBlockTable);
-      const int keys = keys_of(s);
-      if (keys > 0) atomicMin(&shared[find_last(group, n_groups, s)], keys);
-    }
-    for (int t = tid; t < plan.tiles; t += SA_THREADS) cost[t] = 0;
-    __syncthreads();
-    for (int g = tid; g < n_groups; g += SA_THREADS) shared[g] = shared[g] == 0x7fffffff ? 0 : min(shared[g], a.shared_len[g]) / HS_PAGE_SIZE;
-    __syncthreads();
-    for (int s = int(group[0]) + tid; s < s_end; s += SA_THREADS) {
-      const int g = find_last(group, n_groups, s), keys = keys_of(s);
-      if (keys > 0) atomicAdd(&cost[tile[g] + (s - group[g]) / p.tile_seqs], (keys + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE - shared[g]);
-    }
+    each([&](int s, int keys, int g) {
+      atomicAdd(&cost[int(tile[g]) + (s - int(group[g])) / p.tile_seqs], (keys + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE - shared[g]);
+    });
     __syncthreads();
     // (at least one block, so that rows that see no key take the same way)
-    for (int t = tid; t < plan.tiles; t += SA_THREADS) cost[t] = max((shared[find_last(tile, n_groups, t)] + 3) / 4 + (cost[t] + 3) / 4, 1) + SA_ITEM_COST;
-    __syncthreads();
-    const int all = running_sums(plan.tiles, bar->warp_sum, [&](int t) { return cost[t]; }, [&](int t, int sum) { cost[t] = sum; });
+    const int all = running_sums(plan.tiles, bar->warp_sum,
+                                 [&](int t) {
+                                   const int common = shared[t < n_groups && tile[t] == t && tile[t + 1] > t ? t : find_last(tile, n_groups, t)];
+                                   return max((common + 3) / 4 + (cost[t] + 3) / 4, 1) + SA_ITEM_COST;
+                                 },
+                                 [&](int t, int sum) { cost[t] = sum; });
     if (tid == 0) cost[plan.tiles] = all;
     __syncthreads();
     plan.cost = cost;
@@ -237,118 +277,246 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     plan.tile = tile;
     plan.line = all * units;
     plan.shares = max(1, min(p.shares, plan.line / SA_MIN_SHARE));
+    plan.base = plan.line / plan.shares;
+    plan.more = plan.line - plan.base * plan.shares;
   }
   // An item's number is tile * units + unit; its place in the line is the sum of the costs in front of it.
-  auto cost_of = [&](int number) { return plan.cost[number / units + 1] - plan.cost[number / units]; };
+  auto blocks_of = [&](int number) { return plan.cost[number / units + 1] - plan.cost[number / units] - SA_ITEM_COST; };
   auto place_of = [&](int number) {
     const int t = number / units;
     return plan.cost[t] * units + (number - t * units) * (plan.cost[t + 1] - plan.cost[t]);
   };
-  auto share_begin = [&](int k) { return int(int64_t(plan.line) * k / plan.shares); };
-  auto number_at = [&](int x) {                          // of the item that has place x
-    if (x >= plan.line) return plan.tiles * units;
+  auto share_begin = [&](int k) { return plan.base * k + min(k, plan.more); };
+  auto number_at = [&](int x) {                          // of the item that has place x of the line
     const int t = find_last(plan.cost, plan.tiles, x / units);
     return t * units + (x - plan.cost[t] * units) / (plan.cost[t + 1] - plan.cost[t]);
   };
   // The block of an item in front of which the cut at place x falls; not so near an end that a part would be too short.
-  auto cut_block = [&](int number, int x) {
-    if (number >= plan.tiles * units) return 0;
-    const int blocks = cost_of(number) - SA_ITEM_COST, b = x - place_of(number) - SA_ITEM_COST;
+  auto cut_block = [&](int place, int blocks, int x) {
+    const int b = x - place - SA_ITEM_COST;
     return b < SA_MIN_PART ? 0 : b > blocks - SA_MIN_PART ? blocks : b;
   };
-  auto first_share = [&](int number) {                   // that has a place of the item
-    const int x = place_of(number);
-    int k = int(int64_t(x) * plan.shares / plan.line);
-    while (k + 1 < plan.shares && share_begin(k + 1) <= x) ++k;
-    while (share_begin(k) > x) --k;
-    return k;
+  auto first_share = [&](int x) {                        // the share that has place x
+    const int x_more = plan.more * (plan.base + 1);
+    return x < x_more ? x / (plan.base + 1) : plan.more + (x - x_more) / plan.base;
+  };
+  // Whether both teams have blocks of the item in their share.
+  auto middle_of = [&](int share, int number) {
+    const int x0 = share_begin(share), x1 = share_begin(share + 1), xm = x0 + (x1 - x0) / 2, place = place_of(number), blocks = blocks_of(number);
+    const int end = place + blocks + SA_ITEM_COST;
+    if (place >= xm || end <= xm) return 0;
+    const int from = place < x0 ? cut_block(place, blocks, x0) : 0, at = cut_block(place, blocks, xm), to = end > x1 ? cut_block(place, blocks, x1) : blocks;
+    return from < at && at < to ? 1 : 0;
+  };
+
+  // The shares' parts of an item: block ranges between the cuts that fall into it; how many there are (a warp asks).
+  auto count_parts = [&](int number, int place, int blocks) {
+    const int end = place + blocks + SA_ITEM_COST, f = first_share(place);
+    int parts = 0;
+    for (int k0 = f; k0 < plan.shares && share_begin(k0) < end; k0 += 32) {
+      const int k = k0 + lane;
+      bool has = false;
+      if (k < plan.shares && share_begin(k) < end) {
+        const int from = k == f ? 0 : cut_block(place, blocks, share_begin(k));
+        has = from < (share_begin(k + 1) < end ? cut_block(place, blocks, share_begin(k + 1)) : blocks);
+      }
+      parts += __popc(__ballot_sync(0xffffffffu, has));
+    }
+    return parts;
   };
 
   int rs = 0;
   uint32_t rph = 0;                                      // item ring slot / phase
   uint32_t items_seen = 0;
-  uint32_t blk_base = 0;                                 // blocks of all earlier items of this thread block (K / V ring position)
+  uint32_t g = 0;                                        // blocks of this team's earlier items
+  float m_ref = -INFINITY, l_run = 0.f;                  // softmax: of a row (MOD: in log2 units; else of the raw scores, whose scale is positive)
+  const int copies = p.copies, copy_rows = SA_ROWS / copies;
+  uint32_t sreg[32];                                     // softmax: 32 scores, or 32 columns of O
 
-  if (warp == 8 || warp >= 11) {
-    // ========================================================== TMA producers ==
-    // Producer 0 (warp 8) finds the items and loads pages 0, 1 of every K block; producer 1 pages 2, 3 of K; producers 2 and 3 the same of V.  Producer 0
-    // loads the Q tile.  Lane l holds the id of page l % 4 of the current eight blocks' l / 4.
-    const int pi = warp == 8 ? 0 : warp - 10;
-    const int kv = pi >> 1, w0 = (pi & 1) * 2;
-    int share = plan.tiles > 0 ? int(blockIdx.x) : plan.shares, number = -1, last = -1;           // the lead's: the share, its next item, its last one
-    for (;;) {
-      bool ok = true;
-      if (pi == 0) {
-        if (lane == 0) ok = mbar_wait(&bar->ring_empty[rs], rph ^ 1, abort_flag, a.status);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        Item& it = ring[rs];
-        // the next item that has blocks
-        int b0 = 0, b1 = 0;
-        for (;;) {
-          if (number < 0) {
-            if (share >= plan.shares) break;
-            number = number_at(share_begin(share));
-            last = number_at(share_begin(share + 1) - 1);
-          }
-          const int x0 = share_begin(share), x1 = share_begin(share + 1), place = place_of(number), cost = cost_of(number);
-          b0 = place < x0 ? cut_block(number, x0) : 0;
-          b1 = place + cost > x1 ? cut_block(number, x1) : cost - SA_ITEM_COST;
-          if (b0 < b1) break;
-          if (number == last) {
-            number = -1;
-            share += int(gridDim.x);
-          } else {
-            ++number;
+  // The rows' outputs of an item that has ended, 32 columns at a time: from tensor memory, scaled by f, the other copy's added to the first copy's.
+  // use(columns' place, values) is called by the threads of the first copy.  Returns false where a wait has given up.
+  const int r = tid & 127;                               // row of the matrix = lane of tensor memory
+  const uint32_t t_lane = tmem + team * SA_TEAM_TMEM + (uint32_t((warp & 3) * 32) << 16);
+  uint32_t end_phase = 0;
+  auto team_wait = [&]() {                               // the team's softmax warps
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&tm.end);
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(&tm.end, end_phase, abort_flag, a.status));
+    end_phase ^= 1;
+    return ok;
+  };
+  // (reference, sum) of the thread's row over its copies; f: what the thread's own outputs count
+  auto row_total = [&](float& f, bool& ok) {
+    const float m_log2 = m_ref == -INFINITY ? -INFINITY : MOD ? m_ref : __fmul_rn(m_ref, p.score.in);
+    f = 1.f;
+    ok = true;
+    if (copies == 1) return make_float2(m_log2, l_run);
+    tm.ml[r] = make_float2(m_log2, l_run);
+    ok = team_wait();
+    const float2 x = tm.ml[r & 63], y = tm.ml[(r & 63) + 64];
+    const float top = fmaxf(x.x, y.x), zero = top == -INFINITY ? 0.f : top;
+    f = fast_exp2(m_log2 - zero);
+    return make_float2(top, fmaf(x.y, fast_exp2(x.x - zero), y.y * fast_exp2(y.x - zero)));
+  };
+  auto each_columns = [&](float f, auto use) {
+    float4* other = reinterpret_cast<float4*>(q_smem);   // [columns / 4][64 rows]: the second copy's rows (Q is read no more)
+    bool ok = true;
+    if (copies == 2 && r >= 64) {
+#pragma unroll 1
+      for (int c = 0; c < DH; c += 32) {
+        tmem_ld32(t_lane + G_::O0 + c, sreg);
+        tmem_ld_wait();
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          other[(c / 4 + u) * 64 + r - 64] = make_float4(__uint_as_float(sreg[4 * u]) * f, __uint_as_float(sreg[4 * u + 1]) * f, __uint_as_float(sreg[4 * u + 2]) * f,
+                                                         __uint_as_float(sreg[4 * u + 3]) * f);
+      }
+    }
+    if (copies == 2) ok = team_wait();
+    if (copies == 1 || r < 64) {
+#pragma unroll 1
+      for (int c = 0; c < DH; c += 32) {
+        tmem_ld32(t_lane + G_::O0 + c, sreg);
+        tmem_ld_wait();
+        float x[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(sreg[e]) * f;
+        if (copies == 2) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float4 y = other[(c / 4 + u) * 64 + r];
+            x[4 * u] += y.x;
+            x[4 * u + 1] += y.y;
+            x[4 * u + 2] += y.z;
+            x[4 * u + 3] += y.w;
           }
         }
-        if (number < 0) {
-          if (lane == 0) it.valid = 0;
-        } else {
-          const int t = number / units, unit = number - t * units, g = find_last(plan.tile, n_groups, t);
-          const int s0 = int(plan.group[g]) + (t - int(plan.tile[g])) * p.tile_seqs, n = min(int(plan.group[g + 1]) - s0, p.tile_seqs);
-          const int shared_pages = plan.shared[g];
-          int table = int(plan.group[g]);
-          if (shared_pages > 0) {
-            for (int s = table + lane;; s += 32) {       // (one of the group's has keys)
-              const unsigned some = __ballot_sync(0xffffffffu, s < int(plan.group[g + 1]) && keys_of(s) > 0);
-              if (some) {
-                table = s - lane + __ffs(some) - 1;
-                break;
-              }
-              if (s - lane >= int(plan.group[g + 1])) break;
-            }
-          }
-          int sum = 0;
-          for (int i = 0; i < n; i += 32) {
-            const int keys = i + lane < n ? keys_of(s0 + i + lane) : 0;
-            const int pages = keys > 0 ? (keys + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE - shared_pages : 0;
-            int inc = pages;
+        use(c, x);
+      }
+    }
+    return ok;
+  };
+  // Finished rows, or a part of them in the workspace.
+  auto deliver = [&](const Item& it, float2 total, float f, auto more) {
+    const int row_in = copies == 2 ? r & 63 : r, i_seq = row_in / p.heads, h = row_in - i_seq * p.heads;
+    const bool mine = r < copy_rows && i_seq < it.n_seq && h < it.heads;
+    const int64_t row = it.seq0 + i_seq;
+    const int head = it.head0 + h;
+    const float inv = total.y == 0.f ? 0.f : 1.f / total.y;
+    uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH;
+    RowsPart<DH>& part = reinterpret_cast<RowsPart<DH>*>(static_cast<char*>(a.workspace) + kWsScratch)[it.slot];
+    const bool whole = it.parts == 1;
+    if (mine) {
+      if (!whole) __stcg(&part.ml[r], total);
+      else if (a.lse) a.lse[row * a.n_q_heads + head] = total.y == 0.f ? -INFINITY : kLn2 * (total.x + log2f(total.y));
+    }
+    return each_columns(f, [&](int c, float(&x)[32]) {
+      more(c, x);
+      if (!mine) return;
+      if (whole) {
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int x = __shfl_up_sync(0xffffffffu, inc, o);
-              if (lane >= o) inc += x;
-            }
-            if (i + lane < n) {
-              it.begin[i + lane] = sum + inc - pages;
-              it.kv[i + lane] = keys;
-            }
-            sum += __shfl_sync(0xffffffffu, inc, 31);
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<uint4*>(dst + c + u * 8) = make_uint4(pack_16<F16>(x[8 * u] * inv, x[8 * u + 1] * inv), pack_16<F16>(x[8 * u + 2] * inv, x[8 * u + 3] * inv),
+                                                                  pack_16<F16>(x[8 * u + 4] * inv, x[8 * u + 5] * inv), pack_16<F16>(x[8 * u + 6] * inv, x[8 * u + 7] * inv));
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) __stcg(&part.o[c / 4 + u][r], make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]));
+      }
+    });
+  };
+  // A part has arrived, by one of its four warps (n = 1) or all of it (n = 4).
+  auto arrived = [&](const Item& it, int n) {
+    int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + first_share(place_of(it.number));
+    if (atomicAdd(done, n) == 4 * it.parts - n) {
+      *done = 0;                                         // ready for the next call
+      bar->joins[atomicAdd(&bar->n_joins, 1)] = it.number;
+    }
+  };
+
+#pragma unroll 1
+  for (int share = plan.tiles > 0 ? int(blockIdx.x) : plan.shares; share < plan.shares; share += int(gridDim.x)) {
+    const int x0 = share_begin(share), x1 = share_begin(share + 1), xm = x0 + (x1 - x0) / 2;
+    if (warp == 8 || warp == 10) {
+      // ============================================================ fetching ==
+      // Items from this team's half of the share, the first team's in rising order, the second's in falling order, so that both come to the middle last.
+      // A copy of a warp is 512 bytes: COPY_ROWS keys of a page.  This lane's 16 bytes are chunk (lane % chunks of a key) of key lane / chunks of each; they go where
+      // the 128-byte swizzle has them: chunk c of key r of a 64-coordinate half at r * 128 + ((c ^ r % 8) * 16).
+      constexpr int CHUNKS = DH / 8;
+      const int chunk = lane % CHUNKS, key = lane / CHUNKS;
+      const int64_t page_bytes = int64_t(a.n_kv_heads) * (HS_PAGE_SIZE * DH * 2);
+      const uint32_t to = uint32_t((chunk >> 3) * 8192 + key * 128 + (((chunk & 7) ^ key) << 4));
+      const int xa = team == 0 ? x0 : xm, xb = team == 0 ? xm : x1;
+      const int first = xa < xb ? number_at(xa) : 0, last = xa < xb ? number_at(xb - 1) : -1;
+      bool ok = true;
+      int t_cached = -1;                                 // the tile whose sequences are in the ring's other slot
+      for (int i = 0; ok; ++i) {
+        // the next item that has blocks
+        int number = 0, t = 0, unit = 0, place = 0, blocks = 0, b0 = 0, b1 = 0;
+        bool some = false;
+        for (; i <= last - first && !some; ++i) {
+          number = team == 0 ? first + i : last - i;
+          t = number / units;
+          unit = number - t * units;
+          blocks = plan.cost[t + 1] - plan.cost[t] - SA_ITEM_COST;
+          place = plan.cost[t] * units + unit * (blocks + SA_ITEM_COST);
+          b0 = place < xa ? cut_block(place, blocks, xa) : 0;
+          b1 = place + blocks + SA_ITEM_COST > xb ? cut_block(place, blocks, xb) : blocks;
+          some = b0 < b1;
+        }
+        --i;
+        if (lane == 0) ok = mbar_wait(&tm.ring_empty[rs], rph ^ 1, abort_flag, a.status);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        Item& it = tm.ring[rs];
+        if (!some) {
+          if (lane == 0) {
+            it.valid = 0;
+            mbar_arrive(&tm.ring_full[rs]);
           }
-          // the shares that have parts of the item
-          const int place = place_of(number), end = place + cost_of(number), f = first_share(number);
-          int parts = 0;
-          for (int k0 = f; share_begin(k0) < end; k0 += 32) {
-            const int k = k0 + lane;
-            bool has = false;
-            if (k < plan.shares && share_begin(k) < end) {
-              const int from = k == f ? 0 : cut_block(number, share_begin(k));
-              const int to = share_begin(k + 1) < end ? cut_block(number, share_begin(k + 1)) : cost_of(number) - SA_ITEM_COST;
-              has = from < to;
+          if (++rs == 2) { rs = 0; rph ^= 1; }
+          break;
+        }
+        {
+          const int grp = find_last(plan.tile, n_groups, t);
+          const int g_begin = plan.group[grp], g_end = plan.group[grp + 1], s0 = g_begin + (t - int(plan.tile[grp])) * p.tile_seqs, n = min(g_end - s0, p.tile_seqs);
+          const int shared_pages = plan.shared[grp];
+          int table = g_begin, sum = 0;
+          if (t == t_cached) {                           // the other slot has the same tile of another head
+            const Item& prev = tm.ring[rs ^ 1];
+            for (int k = lane; k < n; k += 32) {
+              it.begin[k] = prev.begin[k];
+              it.kv[k] = prev.kv[k];
             }
-            parts += __popc(__ballot_sync(0xffffffffu, has));
-            if (k0 + 32 >= plan.shares) break;
+            table = prev.table;
+            sum = prev.begin[n];
+          } else {
+            if (shared_pages > 0) {
+              for (int s = g_begin; s < g_end; s += 32) {          // (one of the group's has keys)
+                const unsigned who = __ballot_sync(0xffffffffu, s + lane < g_end && keys_of(s + lane) > 0);
+                if (who) {
+                  table = s + __ffs(who) - 1;
+                  break;
+                }
+              }
+            }
+            for (int k = 0; k < n; k += 32) {
+              const int keys = k + lane < n ? keys_of(s0 + k + lane) : 0;
+              const int pages = keys > 0 ? (keys + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE - shared_pages : 0;
+              int inc = pages;
+#pragma unroll
+              for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += x;
+              }
+              if (k + lane < n) {
+                it.begin[k + lane] = sum + inc - pages;
+                it.kv[k + lane] = keys;
+              }
+              sum += __shfl_sync(0xffffffffu, inc, 31);
+            }
+            t_cached = t;
           }
+          const int parts = count_parts(number, place, blocks);
           if (lane == 0) {
             it.valid = 1;
             it.seq0 = s0;
@@ -363,423 +531,447 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
             it.block0 = b0;
             it.n_blocks = b1 - b0;
             it.parts = parts;
-            it.slot = 2 * share + (place < share_begin(share) ? 0 : 1);
+            it.slot = 2 * share + (place < x0 ? 0 : 1);
+            it.middle = middle_of(share, number);
             it.number = number;
             it.begin[n] = sum;
           }
-          if (number == last) {
-            number = -1;
-            share += int(gridDim.x);
-          } else {
-            ++number;
-          }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar->ring_full[rs]);
-      } else {
-        ok = mbar_wait(&bar->ring_full[rs], rph, abort_flag, a.status);
-        if (!__all_sync(0xffffffffu, ok)) break;
-      }
-      const Item& it = ring[rs];
-      // (a copy of what is needed: the slot is released at once, and the lead's own stays until the other roles have released it)
-      const int valid = it.valid;
-      if (!valid) break;
-      const int n_seq = it.n_seq, hk = it.hk, shared_pages = it.shared_pages, shared_blocks = it.shared_blocks, block0 = it.block0, n_blocks = it.n_blocks;
-      // Page l % 4 of block j0 + l / 4 of the item: its id, -1 where there is none, and how many of its keys are seen.
-      int pages_keys = 0;
-      auto page_id = [&](int j0) {
-        const int j = j0 + (lane >> 2);
-        pages_keys = 0;
-        if (j >= n_blocks) return -1;
-        int u = (block0 + j) * 4 + (lane & 3), id, keys = HS_PAGE_SIZE;
-        if (block0 + j < shared_blocks) {
-          if (u >= shared_pages) return -1;
-          id = a.block_tables[int64_t(it.table) * a.max_pages_per_seq + u];
-        } else {
+        if (lane == 0) mbar_arrive(&tm.ring_full[rs]);
+        const int n_seq = it.n_seq, n_blocks = it.n_blocks, block0 = it.block0, shared_pages = it.shared_pages, shared_blocks = it.shared_blocks;
+        const int own_pages = it.begin[n_seq];
+        // Lane l looks up page l % 4 of block j0 + l / 4: its id and how many of its keys are seen (0: there is no such page).
+        int keys = 0;
+        auto look_up = [&](int j0) {
+          const int j = j0 + (lane >> 2);
+          keys = 0;
+          if (j >= n_blocks) return 0;
+          int u = (block0 + j) * 4 + (lane & 3);
+          if (block0 + j < shared_blocks) {
+            if (u >= shared_pages) return 0;
+            keys = HS_PAGE_SIZE;
+            return a.block_tables[int64_t(it.table) * a.max_pages_per_seq + u];
+          }
           u -= shared_blocks * 4;
-          if (u >= it.begin[n_seq]) return -1;
-          const int i = find_last(it.begin, n_seq, u), page = shared_pages + u - it.begin[i];
-          id = a.block_tables[int64_t(it.seq0 + i) * a.max_pages_per_seq + page];
-          keys = min(it.kv[i] - page * HS_PAGE_SIZE, HS_PAGE_SIZE);
-        }
-        if (id >= 0 && id < a.num_pages) {
-          pages_keys = keys;
-          return id;
-        }
-        atomicExch(a.status, kErrBadBlockTable);
-        return -1;
-      };
-      int pg_next = page_id(0), keys_next = pages_keys, pg_cur = -1, keys_cur = 0;
-      if (pi == 0) {
-        if (lane == 0) {
-          ok = mbar_wait(&bar->q_empty, (items_seen & 1) ^ 1, abort_flag, a.status);
-          if (ok) {
-            mbar_expect_tx(&bar->q_full, G_::HALVES * p.heads * p.tile_seqs * 128);
-            for (int h = 0; h < G_::HALVES; ++h)
-              asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-                               smem_u32(q_smem + h * 16384)),
-                           "l"(reinterpret_cast<uint64_t>(&p.tm_q)), "r"(smem_u32(&bar->q_full)), "r"(h * 64), "r"(it.head0), "r"(it.seq0)
+          if (u >= own_pages) return 0;
+          const int k = find_last(it.begin, n_seq, u), page = shared_pages + u - it.begin[k];
+          keys = min(it.kv[k] - page * HS_PAGE_SIZE, HS_PAGE_SIZE);
+          return a.block_tables[int64_t(it.seq0 + k) * a.max_pages_per_seq + page];
+        };
+        // An id and its keys in one word (the pool has fewer than 2^26 pages); a page outside the pool has no keys.
+        auto checked = [&](int id, int n) {
+          if (n > 0 && (id < 0 || id >= a.num_pages)) {
+            atomicExch(a.status, kErrBadBlockTable);
+            n = 0;
+          }
+          return n > 0 ? (n << 26) | id : 0;
+        };
+        // K or V of block j, whose pages are in `pages`
+        const char* pool = static_cast<const char*>(a.kv_pool) + (int64_t(a.layer * 2) * a.num_pages * a.n_kv_heads + it.hk) * (HS_PAGE_SIZE * DH * 2) + lane * 16;
+        auto fetch = [&](int j, int kv, int pages) {
+          const uint32_t b = g + j, buf = b & 1;
+          // a slot is free when the products with what it held are done
+          if (b >= 2) {
+            ok = __all_sync(0xffffffffu, mbar_wait(kv ? &tm.o_full[buf] : &tm.s_full[buf], ((b - 2) >> 1) & 1, abort_flag, a.status));
+            if (!ok) return;
+          }
+          const uint32_t dst = smem_u32((kv ? v_smem : k_smem) + buf * G_::KV_BYTES) + to;
+          const char* src_kv = pool + kv * int64_t(a.num_pages) * page_bytes;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int word = __shfl_sync(0xffffffffu, pages, (j & 7) * 4 + w), n = word >> 26;
+            if (n == 0 && !kv) continue;                 // (scores of no key; V has to be finite everywhere)
+            const char* src = src_kv + int64_t(word & ((1 << 26) - 1)) * page_bytes;
+#pragma unroll
+            for (int c = 0; c < G_::COPIES; ++c)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((dst ^ (((c * G_::COPY_ROWS) & 7) << 4)) + w * 2048 + c * G_::COPY_ROWS * 128),
+                           "l"(src + c * 512), "r"(c * G_::COPY_ROWS + key < n ? 16 : 0)
                            : "memory");
           }
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-      }
-      ++items_seen;
-      for (int kb = 0; kb < n_blocks && ok; ++kb) {
-        if ((kb & 7) == 0) {
-          pg_cur = pg_next;
-          keys_cur = keys_next;
-          pg_next = page_id(kb + 8);
-          keys_next = pages_keys;
-        }
-        const uint32_t gb = blk_base + kb;
-        const uint32_t st = gb % SA_STAGES, ph = (gb / SA_STAGES) & 1;
-        uint64_t* full = kv ? &bar->v_full[st] : &bar->k_full[st];
-        uint8_t* dst = (kv ? v_smem : k_smem) + st * G_::KV_BYTES;
-        const int l0 = (kb & 7) * 4 + w0;
-        const int id0 = __shfl_sync(0xffffffffu, pg_cur, l0), id1 = __shfl_sync(0xffffffffu, pg_cur, l0 + 1);
-        const int keys0 = __shfl_sync(0xffffffffu, keys_cur, l0), keys1 = __shfl_sync(0xffffffffu, keys_cur, l0 + 1);
-        if (lane == 0) {
-          ok = mbar_wait(kv ? &bar->v_empty[st] : &bar->k_empty[st], ph ^ 1, abort_flag, a.status);
-          if (ok) {
-            if (kv) {
-              bar->v_keys[st][w0] = keys0;
-              bar->v_keys[st][w0 + 1] = keys1;
-            }
-            const int mine = (id0 >= 0) + (id1 >= 0);
-            if (mine > 0) mbar_expect_tx(full, mine * G_::HALVES * 2048);
-            else mbar_arrive(full);                      // nothing to fetch, but the block counts on two arrivals
-            for (int w = 0; w < 2; ++w) {
-              const int id = w ? id1 : id0;
-              if (id < 0) continue;
-              const int row = (((a.layer * 2 + kv) * a.num_pages + id) * a.n_kv_heads + hk) * 16;
-              for (int h = 0; h < G_::HALVES; ++h) tma_load_2d(dst + h * 8192 + (w0 + w) * 2048, &p.tm_kv, full, h * 64, row);
-            }
-          }
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-      }
-      __syncwarp();
-      if (pi != 0 && lane == 0) mbar_arrive(&bar->ring_empty[rs]);
-      if (++rs == 2) { rs = 0; rph ^= 1; }
-      if (!ok) break;
-      blk_base += n_blocks;
-    }
-  } else if (warp == 9 || warp == 10) {
-    // ============================================================ MMA issuers ==
-    // One issuing thread per stream (warp 9: even blocks of an item, warp 10: odd ones).
-    if (lane == 0) {
-      const int t = warp - 9;
-      constexpr uint32_t idesc_s = idesc_16<F16>(128, SA_KEYS);
-      constexpr uint32_t idesc_pv = idesc_16<F16>(128, DH) | (1u << 16);   // B (= V) is MN-major
-      const uint64_t q_desc = umma_desc_kmajor_sw128(smem_u32(q_smem));
-      const uint64_t k_desc0 = umma_desc_kmajor_sw128(smem_u32(k_smem));
-      const uint64_t v_desc0 = umma_desc_mnmajor_sw128(smem_u32(v_smem), 8192, 1024);
-      const uint32_t d_o = tmem + G_::O0 + t * DH, s_base = tmem + t * 128;
-      uint32_t g_s = 0, g_pv = 0;                        // blocks of this stream whose S / whose P V has been issued, over all items
-      bool ok = true;
-      auto pv_block = [&](int j) -> bool {               // block j of the item
-        const uint32_t gb = blk_base + j, vst = gb % SA_STAGES;
-        if (!mbar_wait(&bar->v_full[vst], (gb / SA_STAGES) & 1, abort_flag, a.status)) return false;
-        const uint32_t buf = g_pv & 1, bph = (g_pv >> 1) & 1;
-        if (!mbar_wait(&bar->p_full[t][buf], bph, abort_flag, a.status)) return false;
-        tc_fence_after_sync();
-        const uint64_t vdesc = v_desc0 + uint64_t(vst * (G_::KV_BYTES >> 4));
-        const uint32_t a_p = s_base + buf * SA_KEYS, acc0 = j < 2 ? 0u : 1u;     // the stream's first block overwrites O
-#pragma unroll
-        for (int pg = 0; pg < 4; ++pg)                   // 16 keys (one page) per MMA: 8 columns of P
-          umma_ts(d_o, a_p + 8 * pg, vdesc + uint64_t(pg * (2048 >> 4)), idesc_pv, pg != 0 ? 1u : acc0);
-        umma_commit(&bar->o_full[t][buf]);
-        umma_commit(&bar->v_empty[vst]);
-        ++g_pv;
-        return true;
-      };
-      for (;;) {
-        if (!mbar_wait(&bar->ring_full[rs], rph, abort_flag, a.status)) break;
-        const int valid = ring[rs].valid, n_blocks = ring[rs].n_blocks;
-        mbar_arrive(&bar->ring_empty[rs]);
-        if (++rs == 2) { rs = 0; rph ^= 1; }
-        if (!valid) break;
-        if (!mbar_wait(&bar->q_full, items_seen & 1, abort_flag, a.status)) break;
-        ++items_seen;
-        if (t >= n_blocks) mbar_arrive(&bar->q_empty);
-        for (int j = t; j < n_blocks && ok; j += 2) {
-          const uint32_t gb = blk_base + j, kst = gb % SA_STAGES;
-          if (!mbar_wait(&bar->k_full[kst], (gb / SA_STAGES) & 1, abort_flag, a.status)) { ok = false; break; }
-          tc_fence_after_sync();
-          const uint32_t buf = g_s & 1;
-          const uint64_t kdesc = k_desc0 + uint64_t(kst * (G_::KV_BYTES >> 4));
-#pragma unroll
-          for (int ks = 0; ks < DH / 16; ++ks)
-            umma_bf16(s_base + buf * SA_KEYS, q_desc + uint64_t((ks >> 2) * (16384 >> 4) + 2 * (ks & 3)),
-                      kdesc + uint64_t((ks >> 2) * (8192 >> 4) + 2 * (ks & 3)), idesc_s, ks != 0);
-          umma_commit(&bar->s_full[t][buf]);
-          umma_commit(&bar->k_empty[kst]);               // the K slot, once these scores are computed
-          if (j + 2 >= n_blocks) umma_commit(&bar->q_empty);       // and the Q tile after the stream's last scores
-          ++g_s;
-          if (j >= 2) ok = pv_block(j - 2);              // overlaps the softmax of block j
-        }
-        if (ok && t < n_blocks) ok = pv_block((n_blocks - 1 - t) / 2 * 2 + t);
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(kv ? &tm.v_full[buf] : &tm.k_full[buf])) : "memory");
+        };
+        int raw = look_up(0), cur_keys = keys, raw_next = look_up(8);
+        int cur = checked(raw, cur_keys), next = checked(raw_next, keys);
+        raw = look_up(16);
+        int raw_keys = keys;
+        fetch(0, 0, cur);
+        if (ok && n_blocks > 1) fetch(1, 0, cur);
         if (!ok) break;
-        blk_base += n_blocks;
+        // the Q tile, for which the item in front has to be done with its own
+        if (lane == 0) {
+          ok = mbar_wait(&tm.q_empty, (items_seen & 1) ^ 1, abort_flag, a.status);
+          if (ok) {
+            mbar_expect_tx(&tm.q_full, copies * G_::HALVES * p.heads * p.tile_seqs * 128);
+            for (int k = 0; k < copies; ++k)
+              for (int h = 0; h < G_::HALVES; ++h)
+                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                                 smem_u32(q_smem + h * 16384 + k * 8192)),
+                             "l"(reinterpret_cast<uint64_t>(&p.tm_q)), "r"(smem_u32(&tm.q_full)), "r"(h * 64), "r"(it.head0), "r"(it.seq0)
+                             : "memory");
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        for (int j = 0; j < n_blocks && ok; ++j) {
+          if ((j & 7) == 0 && j > 0) {
+            cur = next;
+            next = checked(raw, raw_keys);
+            raw = look_up(j + 16);
+            raw_keys = keys;
+          }
+          fetch(j, 1, cur);
+          if (ok && j + 2 < n_blocks) fetch(j + 2, 0, (j + 2) >> 3 == j >> 3 ? cur : next);
+        }
+        __syncwarp();
+        ++items_seen;
+        g += n_blocks;
+        if (++rs == 2) { rs = 0; rph ^= 1; }
+      }
+    } else if (warp == 9 || warp == 11) {
+      // ============================================================= products ==
+      if (lane == 0) {
+        constexpr uint32_t idesc_s = idesc_16<F16>(128, SA_KEYS);
+        constexpr uint32_t idesc_pv = idesc_16<F16>(128, DH) | (1u << 16);   // B (= V) is MN-major
+        const uint64_t q_desc = umma_desc_kmajor_sw128(smem_u32(q_smem));
+        const uint64_t k_desc0 = umma_desc_kmajor_sw128(smem_u32(k_smem));
+        const uint64_t v_desc0 = umma_desc_mnmajor_sw128(smem_u32(v_smem), 8192, 1024);
+        const uint32_t s_base = tmem + team * SA_TEAM_TMEM, d_o = s_base + G_::O0;
+        auto pv_block = [&](uint32_t b, bool first) -> bool {
+          const uint32_t buf = b & 1, ph = (b >> 1) & 1;
+          if (!mbar_wait(&tm.v_full[buf], ph, abort_flag, a.status) || !mbar_wait(&tm.p_full[buf], ph, abort_flag, a.status)) return false;
+          fence_proxy_async();                           // (V came by ordinary copies)
+          tc_fence_after_sync();
+          const uint64_t vdesc = v_desc0 + uint64_t(buf * (G_::KV_BYTES >> 4));
+#pragma unroll
+          for (int pg = 0; pg < 4; ++pg)                 // 16 keys (one page) per MMA: 8 columns of P
+            umma_ts(d_o, s_base + buf * SA_KEYS + 8 * pg, vdesc + uint64_t(pg * (2048 >> 4)), idesc_pv, pg != 0 || !first ? 1u : 0u);
+          umma_commit(&tm.o_full[buf]);                  // (which frees the V slot, too)
+          return true;
+        };
+        bool ok = true;
+        while (ok) {
+          if (!mbar_wait(&tm.ring_full[rs], rph, abort_flag, a.status)) break;
+          const int valid = tm.ring[rs].valid, n_blocks = tm.ring[rs].n_blocks;
+          mbar_arrive(&tm.ring_empty[rs]);
+          if (++rs == 2) { rs = 0; rph ^= 1; }
+          if (!valid) break;
+          if (!mbar_wait(&tm.q_full, items_seen & 1, abort_flag, a.status)) break;
+          ++items_seen;
+          for (int j = 0; j < n_blocks && ok; ++j) {
+            const uint32_t b = g + j, buf = b & 1;
+            ok = mbar_wait(&tm.k_full[buf], (b >> 1) & 1, abort_flag, a.status);
+            if (!ok) break;
+            fence_proxy_async();                         // (K came by ordinary copies)
+            tc_fence_after_sync();
+            const uint64_t kdesc = k_desc0 + uint64_t(buf * (G_::KV_BYTES >> 4));
+#pragma unroll
+            for (int ks = 0; ks < DH / 16; ++ks)
+              umma_bf16(s_base + buf * SA_KEYS, q_desc + uint64_t((ks >> 2) * (16384 >> 4) + 2 * (ks & 3)),
+                        kdesc + uint64_t((ks >> 2) * (8192 >> 4) + 2 * (ks & 3)), idesc_s, ks != 0);
+            umma_commit(&tm.s_full[buf]);                // (which frees the K slot, too)
+            if (j > 0) ok = pv_block(b - 1, j == 1);     // overlaps the softmax of block j
+          }
+          if (ok) ok = pv_block(g + n_blocks - 1, n_blocks == 1);
+          g += n_blocks;
+        }
+      }
+    } else {
+      // ============================================================== softmax ==
+      const ScoreScale& sc = p.score;
+      const int row_in = copies == 2 ? r & 63 : r, i_seq = row_in / p.heads, h = row_in - i_seq * p.heads;      // (rows of a box have room for p.heads each)
+      const int n_chunks = copies == 2 ? 1 : 2, half = copies == 2 && r >= 64 ? 1 : 0;     // 32 keys at a time: how many times, and the first
+      for (;;) {
+        bool ok = __all_sync(0xffffffffu, mbar_wait(&tm.ring_full[rs], rph, abort_flag, a.status));
+        if (!ok) break;
+        const Item& it = tm.ring[rs];
+        if (!it.valid) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tm.ring_empty[rs]);
+          if (++rs == 2) { rs = 0; rph ^= 1; }
+          break;
+        }
+        const int n_blocks = it.n_blocks, block0 = it.block0, shared_blocks = it.shared_blocks;
+        const bool row_valid = i_seq < it.n_seq && h < it.heads;
+        const int kv = row_valid ? it.kv[i_seq] : 0, shared_keys = kv > 0 ? it.shared_pages * HS_PAGE_SIZE : 0;
+        // the row sees the first shared_keys of the shared blocks' keys, and lo .. hi - 1 of the others'
+        const int lo = row_valid ? it.begin[i_seq] * HS_PAGE_SIZE : 0, hi = lo + kv - shared_keys;
+        const float slope = MOD && a.slopes && row_valid ? a.slopes[it.head0 + h] * 1.4426950408889634f : 0.f;
+        m_ref = -INFINITY;
+        l_run = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < n_blocks; ++j) {
+          const uint32_t b = g + j, buf = b & 1, ph = (b >> 1) & 1;
+          const int block = block0 + j;
+          const bool common = block < shared_blocks;
+          const int key0 = (common ? block : block - shared_blocks) * SA_KEYS + half * 32;          // the thread's first key
+          // bits of the keys seen, 32 and 32
+          uint32_t seen[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            seen[c] = common ? first_bits(shared_keys - key0 - 32 * c) : first_bits(hi - key0 - 32 * c) & ~first_bits(lo - key0 - 32 * c);
+          if (n_chunks == 1) seen[1] = 0;
+          ok = __all_sync(0xffffffffu, mbar_wait(&tm.s_full[buf], ph, abort_flag, a.status));
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t s_col = t_lane + buf * SA_KEYS;
+          if (__any_sync(0xffffffffu, (seen[0] | seen[1]) != 0)) {
+            const bool masked = __any_sync(0xffffffffu, seen[0] != 0xffffffffu || (n_chunks == 2 && seen[1] != 0xffffffffu));
+            auto mask = [&](int c, uint32_t to) {
+              const uint32_t bits = c ? seen[1] : seen[0];
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!(bits & (1u << e))) sreg[e] = to;
+            };
+            auto reduce = [&](auto op) {                 // eight chains
+              float x[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(sreg[e]);
+#pragma unroll
+              for (int e = 8; e < 32; ++e) x[e & 7] = op(x[e & 7], __uint_as_float(sreg[e]));
+              return op(op(op(x[0], x[1]), op(x[2], x[3])), op(op(x[4], x[5]), op(x[6], x[7])));
+            };
+            auto largest = [&]() { return reduce([](float x, float y) { return fmaxf(x, y); }); };
+            auto smallest = [&]() { return reduce([](float x, float y) { return fminf(x, y); }); };
+            // Raw scores.  Capped ones that are not seen are NaN, which maxima and minima pass over and whose weight is made 0 behind the exponential.
+            auto load = [&](int c, bool with_mask) {
+              tmem_ld32(s_col + (half + c) * 32, sreg);
+              tmem_ld_wait();
+              if (with_mask && masked) mask(c, MOD ? 0x7fffffffu : 0xff800000u);
+            };
+            // While the warp's scores allow a polynomial for the cap, that of the largest score is the largest one, and the reference is part of its last
+            // multiply-add.  A bias, or the cap beyond, has to be worked out before the maximum is known, and once more behind it.
+            float mx = -INFINITY, least = INFINITY;
+            int degree = 0;
+            bool direct = !MOD;
+            if (!MOD || sc.out != 0.f) {
+#pragma unroll 1
+              for (int c = n_chunks - 1; c >= 0; --c) {
+                load(c, true);
+                mx = fmaxf(mx, largest());
+                if (MOD) least = fminf(least, smallest());
+              }
+              if (MOD) {
+                const float u = (seen[0] | seen[1]) != 0 ? fmaxf(mx * mx, least * least) : 0.f;
+                // one vote: the worst row's polynomial (6: degree three, 4: five, 0: none)
+                const unsigned vote = __reduce_and_sync(0xffffffffu, u <= sc.limit3 ? 6u : u <= sc.limit5 ? 4u : 0u);
+                degree = vote == 6 ? 3 : vote == 4 ? 5 : 0;
+                direct = degree != 0 && a.slopes == nullptr;
+                if (direct && mx > -INFINITY) {
+                  float unused;
+                  if (degree == 3) split(odd_poly(f2(mx, mx), sc.c3, f2(0.f, 0.f)), mx, unused);
+                  else split(odd_poly(f2(mx, mx), sc.c5, f2(0.f, 0.f)), mx, unused);
+                }
+              }
+            }
+            auto finish = [&](int c) {                   // scores with cap and bias, in log2 units
+              load(c, false);
+              // the row is at position kv - 1, element e of the chunk at kv - 1 - (base - e)
+              const float base = float(kv - 1 - (common ? key0 : shared_keys + key0 - lo) - 32 * c);
+              const F2 base2 = f2(-slope * base, -slope * base), slope2 = f2(slope, slope), in2 = f2(sc.in, sc.in);
+              auto all = [&](auto score) {               // score(pair of raw scores, what to add)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  float y0, y1;
+                  split(score(f2(__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1])), fma2(slope2, f2(float(e), float(e + 1)), base2)), y0, y1);
+                  sreg[e] = __float_as_uint(y0);
+                  sreg[e + 1] = __float_as_uint(y1);
+                }
+              };
+              if (sc.out == 0.f) all([&](F2 s, F2 plus) { return fma2(s, in2, plus); });
+              else if (degree != 0) all([&](F2 s, F2 plus) { return odd_poly(s, sc.c5, plus); });
+              else {
+                all([&](F2 s, F2 plus) {
+                  float s0, s1;
+                  split(s, s0, s1);
+                  return fma2(f2(tanh_any(s0 * sc.in), tanh_any(s1 * sc.in)), f2(sc.out, sc.out), plus);
+                });
+              }
+              if (masked) mask(c, 0xff800000u);          // -infinity
+            };
+            if (MOD && !direct) {
+              mx = -INFINITY;
+#pragma unroll 1
+              for (int c = n_chunks - 1; c >= 0; --c) {
+                finish(c);
+                mx = fmaxf(mx, largest());
+              }
+            }
+            // the reference maximum moves only when the block's maximum is far above it
+            const float unit = MOD ? 1.f : sc.in;
+            float alpha = 1.f;
+            const bool move = mx > -INFINITY && (m_ref == -INFINITY || (mx - m_ref) * unit > kRefSlack);
+            if (move) {
+              alpha = m_ref == -INFINITY ? 0.f : fast_exp2((m_ref - mx) * unit);
+              m_ref = mx;
+            }
+            const bool rescale = j > 0 && __any_sync(0xffffffffu, move);
+            const float neg_ms = m_ref == -INFINITY ? 0.f : -m_ref * unit;
+            const F2 neg2 = f2(neg_ms, neg_ms), unit2 = f2(unit, unit);
+            F2 sums[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll 1
+            for (int c = 0; c < n_chunks; ++c) {
+              if (c > 0) {
+                if (MOD && !direct) finish(c);
+                else load(c, true);
+              }
+              // log2 of the weights, eight pairs step by step, so that the pairs' steps overlap; P over S: column e of row r = keys 2 e, 2 e + 1
+              uint32_t pk[16];
+              auto weights = [&](auto score) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 16) {
+                  F2 x[8];
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) x[i] = f2(__uint_as_float(sreg[e + 2 * i]), __uint_as_float(sreg[e + 2 * i + 1]));
+                  score(x);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    float y0, y1;
+                    split(x[i], y0, y1);
+                    y0 = fast_exp2(y0);
+                    y1 = fast_exp2(y1);
+                    if (MOD) {                           // (NaN: not seen)
+                      y0 = fmaxf(y0, 0.f);
+                      y1 = fmaxf(y1, 0.f);
+                    }
+                    sums[i & 3] = add2(sums[i & 3], f2(y0, y1));
+                    // (at most 2^kRefSlack, rounded once for the product with v in 16 bits; the sums keep fp32)
+                    pk[e / 2 + i] = pack_16<F16>(y0, y1);
+                  }
+                }
+              };
+              auto poly = [&](F2(&x)[8], const auto& k, int n) {
+                F2 u[8], q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = mul2(x[i], x[i]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[i] = f2(k[n - 1], k[n - 1]);
+#pragma unroll
+                for (int d = n - 2; d >= 0; --d)
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) q[i] = fma2(q[i], u[i], f2(k[d], k[d]));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = fma2(q[i], x[i], neg2);
+              };
+              if (!MOD || !direct) {
+                weights([&](F2(&x)[8]) {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) x[i] = fma2(x[i], unit2, neg2);
+                });
+              } else if (degree == 3) {
+                weights([&](F2(&x)[8]) { poly(x, sc.c3, 4); });
+              } else {
+                weights([&](F2(&x)[8]) { poly(x, sc.c5, 6); });
+              }
+              tmem_st16(s_col + (half + c) * 16, pk);
+            }
+            float sum_a, sum_b;
+            split(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), sum_a, sum_b);
+            l_run = l_run * alpha + (sum_a + sum_b);
+            if (copies == 2) {                           // the other copy's keys
+              uint32_t none[16] = {};
+              tmem_st16(s_col + (half ^ 1) * 16, none);
+            }
+            if (rescale) {
+              // O must be at rest: the P V product of the previous block has completed (the next cannot be issued before this team hands over P)
+              ok = __all_sync(0xffffffffu, mbar_wait(&tm.o_full[(b - 1) & 1], ((b - 1) >> 1) & 1, abort_flag, a.status));
+              if (!ok) break;
+              tc_fence_after_sync();
+#pragma unroll 1
+              for (int c = 0; c < DH; c += 32) {
+                tmem_ld32(t_lane + G_::O0 + c, sreg);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sreg[e] = __float_as_uint(__uint_as_float(sreg[e]) * alpha);
+                tmem_st32(t_lane + G_::O0 + c, sreg);
+              }
+            }
+          } else {
+            uint32_t none[16] = {};
+            tmem_st16(s_col, none);
+            tmem_st16(s_col + 16, none);
+          }
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tm.p_full[buf]);
+        }
+        if (!ok) break;
+        // ------------------------------------------------------------ the item's end
+        g += n_blocks;
+        ok = __all_sync(0xffffffffu, mbar_wait(&tm.o_full[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag, a.status));
+        if (!ok) break;
+        tc_fence_after_sync();
+        if (!it.middle) {
+          float f;
+          const float2 total = row_total(f, ok);
+          if (!ok || !deliver(it, total, f, [](int, float(&)[32]) {})) break;
+          if (it.parts > 1) {
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) arrived(it, 1);
+          }
+        }
+        tc_fence_before_sync();
+        fence_proxy_async();                             // (Q's place was written)
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&tm.q_empty);
+          mbar_arrive(&tm.ring_empty[rs]);
+        }
+        if (++rs == 2) { rs = 0; rph ^= 1; }
       }
     }
-  } else {
-    // ================================================================ softmax ==
-    const int t = warp >> 2;                             // stream of this warp group
-    const int r = tid & 127;                             // row of the tile = TMEM lane
-    const uint32_t lane_base = uint32_t((warp & 3) * 32) << 16;
-    const uint32_t s_col = t * 128, o_col = G_::O0 + t * DH;
-    const ScoreScale& sc = p.score;
-    uint32_t g = 0;                                      // blocks this stream has processed, over all items
-    for (;;) {
-      bool ok = mbar_wait(&bar->ring_full[rs], rph, abort_flag, a.status);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      const Item& it = ring[rs];
-      if (!it.valid) break;
-      const int n_blocks = it.n_blocks, block0 = it.block0, shared_blocks = it.shared_blocks, heads = it.heads, parts = it.parts, slot = it.slot, number = it.number;
-      const int i_seq = r / p.heads, h = r - i_seq * p.heads;        // (rows of a box have room for p.heads each)
-      const bool row_valid = i_seq < it.n_seq && h < heads;
-      const int kv = row_valid ? it.kv[i_seq] : 0, shared_keys = kv > 0 ? it.shared_pages * HS_PAGE_SIZE : 0;
-      // the row sees the first shared_keys of the shared blocks' keys, and lo .. hi - 1 of the others'
-      const int lo = row_valid ? it.begin[i_seq] * HS_PAGE_SIZE : 0, hi = lo + kv - shared_keys;
-      const int head = it.head0 + h;
-      const int64_t row = it.seq0 + i_seq;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bar->ring_empty[rs]);
-      if (++rs == 2) { rs = 0; rph ^= 1; }
-      const bool warp_valid = __any_sync(0xffffffffu, row_valid);
-      const float slope = MOD && a.slopes && row_valid ? a.slopes[head] * 1.4426950408889634f : 0.f;
-
-      float m_ref = -INFINITY, l_run = 0.f;              // (MOD: in log2 units; else of the raw scores, whose scale is positive)
-      uint32_t sreg[32], sreg2[32];
-      for (int j = t; j < n_blocks; j += 2, ++g) {
-        const uint32_t buf = g & 1, bph = (g >> 1) & 1;
-        const int block = block0 + j;
-        const bool common = block < shared_blocks;
-        const int key0 = (common ? block : block - shared_blocks) * SA_KEYS;
-        uint32_t seen1, seen2;                           // bit e: key key0 + e, key0 + 32 + e
-        if (common) {
-          seen1 = first_bits(shared_keys - key0);
-          seen2 = first_bits(shared_keys - 32 - key0);
-        } else {
-          seen1 = first_bits(hi - key0) & ~first_bits(lo - key0);
-          seen2 = first_bits(hi - 32 - key0) & ~first_bits(lo - 32 - key0);
-        }
-        ok = mbar_wait(&bar->s_full[t][buf], bph, abort_flag, a.status);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after_sync();
-        uint32_t pk[32];
-        if (__any_sync(0xffffffffu, (seen1 | seen2) != 0)) {
-          tmem_ld32(tmem + lane_base + s_col + buf * SA_KEYS, sreg);
-          tmem_ld32(tmem + lane_base + s_col + buf * SA_KEYS + 32, sreg2);
-          tmem_ld_wait();
-          const bool masked = (seen1 & seen2) != 0xffffffffu;
-          auto mask = [&](uint32_t to) {
+    // -------------------------------------------------------------- the share's end
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (*abort_flag) break;
+    const int mid = xm < x1 && xm > x0 ? number_at(xm) : 0;
+    if (xm > x0 && middle_of(share, mid)) {
+      // The tile in the middle: the second team's rows go through its own Q, K and V, which are idle.  The item is the teams' last one, in the ring's slot in front
+      // of the last.
+      float2 total = make_float2(-INFINITY, 0.f);
+      float f = 1.f;
+      bool ok = true;
+      if (warp < 8) total = row_total(f, ok);
+      if (warp >= 4 && warp < 8) {
+        // (the copies meet in Q, the sum goes behind it)
+        float4* dst = reinterpret_cast<float4*>(smem + G_::TEAM_BYTES + (copies == 2 ? G_::Q_BYTES : 0));
+        ok = each_columns(f, [&](int c, float(&x)[32]) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              if (!(seen1 & (1u << e))) sreg[e] = to;
-              if (!(seen2 & (1u << e))) sreg2[e] = to;
-            }
-          };
-          auto largest = [&]() {                         // four chains
-            float mx[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx[e] = fmaxf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e]));
-#pragma unroll
-            for (int e = 4; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e])));
-            return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-          };
-          auto smallest = [&]() {
-            float mn[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mn[e] = fminf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e]));
-#pragma unroll
-            for (int e = 4; e < 32; ++e) mn[e & 3] = fminf(mn[e & 3], fminf(__uint_as_float(sreg[e]), __uint_as_float(sreg2[e])));
-            return fminf(fminf(mn[0], mn[1]), fminf(mn[2], mn[3]));
-          };
-          if (MOD) {
-            int degree = 0;
-            if (sc.out != 0.f) {
-              if (masked) mask(0u);                      // (what is not seen must not decide which polynomial the others take)
-              const float top = largest(), low = smallest(), u = fmaxf(top * top, low * low);
-              // one vote: the worst row's polynomial (6: degree three, 4: five, 0: none)
-              const unsigned vote = __reduce_and_sync(0xffffffffu, u <= sc.limit3 ? 6u : u <= sc.limit5 ? 4u : 0u);
-              degree = vote == 6 ? 3 : vote == 4 ? 5 : 0;
-            }
-            // the row is at position kv - 1, key e of the block at p - (base - e)
-            const float base = float(kv - 1 - (common ? key0 : shared_keys + key0 - lo));
-            const F2 base2 = f2(-slope * base, -slope * base), slope2 = f2(slope, slope), in2 = f2(sc.in, sc.in);
-            auto finish = [&](auto score) {              // score(pair of raw scores, what to add)
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                float x0, x1;
-                const F2 p1 = fma2(slope2, f2(float(e), float(e + 1)), base2), p2 = fma2(slope2, f2(float(e + 32), float(e + 33)), base2);
-                split(score(f2(__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1])), p1), x0, x1);
-                sreg[e] = __float_as_uint(x0);
-                sreg[e + 1] = __float_as_uint(x1);
-                split(score(f2(__uint_as_float(sreg2[e]), __uint_as_float(sreg2[e + 1])), p2), x0, x1);
-                sreg2[e] = __float_as_uint(x0);
-                sreg2[e + 1] = __float_as_uint(x1);
-              }
-            };
-            if (degree == 3) finish([&](F2 s, F2 plus) { return odd_poly(s, sc.c3, plus); });
-            else if (degree == 5) finish([&](F2 s, F2 plus) { return odd_poly(s, sc.c5, plus); });
-            else if (sc.out == 0.f) finish([&](F2 s, F2 plus) { return fma2(s, in2, plus); });
-            else {
-              finish([&](F2 s, F2 plus) {
-                float s0, s1;
-                split(s, s0, s1);
-                return fma2(f2(tanh_any(s0 * sc.in), tanh_any(s1 * sc.in)), f2(sc.out, sc.out), plus);
-              });
-            }
-          }
-          if (masked) mask(0xff800000u);                 // -infinity
-          const float mx = largest();
-          // the reference maximum moves only when the block's maximum is far above it
-          const float unit = MOD ? 1.f : sc.in;
-          float alpha = 1.f;
-          const bool move = mx > -INFINITY && (m_ref == -INFINITY || (mx - m_ref) * unit > kRefSlack);
-          if (move) {
-            alpha = m_ref == -INFINITY ? 0.f : fast_exp2((m_ref - mx) * unit);
-            m_ref = mx;
-          }
-          const bool rescale = j >= 2 && __any_sync(0xffffffffu, move);
-          const float neg_ms = m_ref == -INFINITY ? 0.f : -m_ref * unit;
-          const F2 neg2 = f2(neg_ms, neg_ms), unit2 = f2(unit, unit);
-          F2 sums[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
-          auto weights = [&](auto score) {               // score(pair of raw or finished scores) = log2 of their weights
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              float x0, x1, y0, y1;
-              split(score(f2(__uint_as_float(sreg[e]), __uint_as_float(sreg[e + 1]))), x0, x1);
-              split(score(f2(__uint_as_float(sreg2[e]), __uint_as_float(sreg2[e + 1]))), y0, y1);
-              x0 = fast_exp2(x0);
-              x1 = fast_exp2(x1);
-              y0 = fast_exp2(y0);
-              y1 = fast_exp2(y1);
-              sums[0] = add2(sums[0], f2(x0, x1));
-              sums[1] = add2(sums[1], f2(y0, y1));
-              // (at most 2^kRefSlack, rounded once for the product with v in 16 bits; the sums keep fp32)
-              pk[e >> 1] = pack_16<F16>(x0, x1);
-              pk[16 + (e >> 1)] = pack_16<F16>(y0, y1);
-            }
-          };
-          if (!MOD) weights([&](F2 s) { return fma2(s, unit2, neg2); });
-          else weights([&](F2 s) { return add2(s, neg2); });
-          float sum_a, sum_b;
-          split(add2(sums[0], sums[1]), sum_a, sum_b);
-          l_run = l_run * alpha + (sum_a + sum_b);
-          if (rescale) {
-            // O must be at rest: the stream's P V product of its previous block has completed (the next cannot be issued
-            // before this warp group hands over P)
-            ok = mbar_wait(&bar->o_full[t][(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag, a.status);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            tc_fence_after_sync();
-#pragma unroll
-            for (int c = 0; c < DH / 32; ++c) {
-              tmem_ld32(tmem + lane_base + o_col + c * 32, sreg);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) sreg[e] = __float_as_uint(__uint_as_float(sreg[e]) * alpha);
-              tmem_st32(tmem + lane_base + o_col + c * 32, sreg);
-            }
-            tmem_st_wait();
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) pk[e] = 0;
-        }
-        // P over the first 32 columns of the S buffer just read: column c of row r = keys 2 c, 2 c + 1
-        tmem_st32(tmem + lane_base + s_col + buf * SA_KEYS, pk);
-        // V rows of keys that no row sees may hold anything and must not meet the weight 0
-        {
-          const uint32_t gb = blk_base + j, s = gb % SA_STAGES;
-          const bool w = mbar_wait(&bar->v_full[s], (gb / SA_STAGES) & 1, abort_flag, a.status);
-          if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
-          const int4 keys = *reinterpret_cast<const int4*>(bar->v_keys[s]);
-          if ((keys.x & keys.y & keys.z & keys.w) != HS_PAGE_SIZE) {
-            uint8_t* vst = v_smem + s * G_::KV_BYTES;
-            for (int idx = r; idx < SA_KEYS * G_::HALVES * 8; idx += 128) {
-              const int u = idx & 7, half = (idx >> 3) % G_::HALVES, k = (idx >> 3) / G_::HALVES, page = k >> 4;
-              if ((k & 15) < (page == 0 ? keys.x : page == 1 ? keys.y : page == 2 ? keys.z : keys.w)) continue;
-              *reinterpret_cast<uint4*>(vst + half * 8192 + page * 2048 + (k & 15) * 128 + (u << 4)) = make_uint4(0, 0, 0, 0);
-            }
-            fence_proxy_async();
-          }
-        }
-        tmem_st_wait();
-        tc_fence_before_sync();
-        mbar_arrive(&bar->p_full[t][buf]);
+          for (int u = 0; u < 8; ++u) dst[(c / 4 + u) * copy_rows + r] = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+        });
+        if (r < copy_rows) tm.ml[r] = total;             // (both copies have read theirs)
       }
-      if (!ok) break;
-      // -------------------------------------------------------------- the item's end
-      // Both streams' last products, their (reference, sum) by row; then each half of the warps has half of the coordinates.
-      if (t < n_blocks) {
-        ok = mbar_wait(&bar->o_full[t][(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag, a.status);
-        if (!__all_sync(0xffffffffu, ok)) break;
+      __syncthreads();
+      if (warp < 4 && ok) {
+        const Item& it = tm.ring[rs];
+        const float4* src = reinterpret_cast<const float4*>(smem + G_::TEAM_BYTES + (copies == 2 ? G_::Q_BYTES : 0));
+        const float2 other = reinterpret_cast<Team*>(smem + G_::TEAMS)[1].ml[copies == 2 ? r & 63 : r];
+        const float top = fmaxf(total.x, other.x), zero = top == -INFINITY ? 0.f : top, f0 = fast_exp2(total.x - zero), f1 = fast_exp2(other.x - zero);
+        ok = deliver(it, make_float2(top, fmaf(total.y, f0, other.y * f1)), f * f0, [&](int c, float(&x)[32]) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float4 y = src[(c / 4 + u) * copy_rows + r];
+            x[4 * u] = fmaf(y.x, f1, x[4 * u]);
+            x[4 * u + 1] = fmaf(y.y, f1, x[4 * u + 1]);
+            x[4 * u + 2] = fmaf(y.z, f1, x[4 * u + 2]);
+            x[4 * u + 3] = fmaf(y.w, f1, x[4 * u + 3]);
+          }
+        });
+        if (it.parts > 1) __threadfence();
+        fence_proxy_async();
       }
-      const float m_log2 = m_ref == -INFINITY ? -INFINITY : MOD ? m_ref : __fmul_rn(m_ref, sc.in);
-      ml[t][r] = make_float2(m_log2, l_run);
+      if (warp >= 4 && warp < 8) fence_proxy_async();
       tc_fence_before_sync();
-      mbar_arrive(&bar->end_full);
-      ok = mbar_wait(&bar->end_full, items_seen & 1, abort_flag, a.status);
-      if (!__all_sync(0xffffffffu, ok)) break;
+      __syncthreads();
       tc_fence_after_sync();
-      const float2 other = ml[t ^ 1][r];
-      const float top = fmaxf(m_log2, other.x), zero = top == -INFINITY ? 0.f : top;
-      const float f_mine = fast_exp2(m_log2 - zero), f_other = fast_exp2(other.x - zero);      // (0 for a stream in which the row has seen nothing)
-      const float l = t == 0 ? fmaf(l_run, f_mine, other.y * f_other) : fmaf(other.y, f_other, l_run * f_mine);
-      const float f0 = t == 0 ? f_mine : f_other, f1 = n_blocks > 1 ? (t == 0 ? f_other : f_mine) : 0.f;
-      if (warp_valid) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH;
-        RowsPart<DH>& part = reinterpret_cast<RowsPart<DH>*>(static_cast<char*>(a.workspace) + kWsScratch)[slot];
-#pragma unroll
-        for (int c = 0; c < DH / 64; ++c) {
-          const int col = t * (DH / 2) + c * 32;
-          tmem_ld32(tmem + lane_base + G_::O0 + col, sreg);
-          tmem_ld32(tmem + lane_base + G_::O0 + DH + col, sreg2);
-          tmem_ld_wait();
-          float x[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            x[e] = __uint_as_float(sreg[e]) * f0;
-            if (n_blocks > 1) x[e] = fmaf(__uint_as_float(sreg2[e]), f1, x[e]);         // (else the odd stream's O is not this item's)
-          }
-          if (row_valid) {
-            if (parts == 1) {
-              uint32_t w[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) w[e] = pack_16<F16>(x[2 * e] * inv, x[2 * e + 1] * inv);
-#pragma unroll
-              for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4*>(dst + col + u * 8) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
-            } else {
-#pragma unroll
-              for (int u = 0; u < 8; ++u) __stcg(&part.o[col / 4 + u][r], make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]));
-            }
-          }
-        }
-        if (row_valid && t == 0) {
-          if (parts > 1) __stcg(&part.ml[r], make_float2(top, l));
-          else if (a.lse) a.lse[row * a.n_q_heads + head] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
-        }
-      }
-      if (parts > 1) __threadfence();
-      tc_fence_before_sync();
-      mbar_arrive(&bar->end_read);
-      ok = mbar_wait(&bar->end_read, items_seen & 1, abort_flag, a.status);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      ++items_seen;
-      if (parts > 1 && tid == 0) {
+      if (*abort_flag) break;
+      if (tid == 0 && tm.ring[rs].parts > 1) {
         __threadfence();
-        int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + first_share(number);
-        if (atomicAdd(done, 1) == parts - 1) {
-          *done = 0;                                     // ready for the next call
-          joins[bar->n_joins++] = number;
-        }
+        arrived(tm.ring[rs], 4);
       }
-      blk_base += n_blocks;
     }
   }
 
@@ -797,74 +989,104 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   __threadfence();
 #pragma unroll 1
   for (int i = 0; i < n_joins; ++i) {
-    const int number = joins[i], place = place_of(number), end = place + cost_of(number), f = first_share(number);
+    const int number = bar->joins[i], place = place_of(number), blocks = blocks_of(number), end = place + blocks + SA_ITEM_COST, f = first_share(place);
     const int t_ = number / units, unit = number - t_ * units, g = find_last(plan.tile, n_groups, t_);
     const int s0 = int(plan.group[g]) + (t_ - int(plan.tile[g])) * p.tile_seqs, n = min(int(plan.group[g + 1]) - s0, p.tile_seqs);
     const int hk = unit / p.chunks, heads_all = a.n_q_heads / a.n_kv_heads, in_head = (unit - hk * p.chunks) * p.heads, heads = min(heads_all - in_head, p.heads);
-    // the slots of the parts, in order (ring and K / V tiles are idle: the list goes there)
+    // The slots of the parts, in order, and what each row's parts weigh (Q, K and V are idle: both lie there), [part][row]; then sums of the parts.
     int* slots = reinterpret_cast<int*>(smem);
+    float* weight = reinterpret_cast<float*>(smem + 1024);
     __syncthreads();
-    if (tid == 0) {
+    if (warp == 0) {
       int parts = 0;
-      for (int k = f; k < plan.shares && share_begin(k) < end; ++k) {
-        const int from = k == f ? 0 : cut_block(number, share_begin(k));
-        const int to = share_begin(k + 1) < end ? cut_block(number, share_begin(k + 1)) : cost_of(number) - SA_ITEM_COST;
-        if (from < to) slots[1 + parts++] = 2 * k + (place < share_begin(k) ? 0 : 1);
+      for (int k0 = f; k0 < plan.shares && share_begin(k0) < end; k0 += 32) {
+        const int k = k0 + lane;
+        bool has = false;
+        if (k < plan.shares && share_begin(k) < end) {
+          const int from = k == f ? 0 : cut_block(place, blocks, share_begin(k));
+          has = from < (share_begin(k + 1) < end ? cut_block(place, blocks, share_begin(k + 1)) : blocks);
+        }
+        const unsigned who = __ballot_sync(0xffffffffu, has);
+        if (has) slots[1 + parts + __popc(who & ((1u << lane) - 1u))] = 2 * k + (place < share_begin(k) ? 0 : 1);
+        parts += __popc(who);
       }
-      slots[0] = parts;
+      if (lane == 0) slots[0] = parts;
     }
     __syncthreads();
     const int parts = slots[0], n_rows = n * p.heads;
     const RowsPart<DH>* rows_parts = reinterpret_cast<const RowsPart<DH>*>(static_cast<const char*>(a.workspace) + kWsScratch);
-    // a thread has a row and eight of its coordinates at a time; eight parts are on their way at a time
-#pragma unroll 1
-    for (int x = tid; x < n_rows * (DH / 8); x += SA_THREADS) {
-      const int c = x / n_rows, r = x - c * n_rows, i_seq = r / p.heads, h = r - i_seq * p.heads;
+    for (int r = tid; r < n_rows; r += SA_THREADS) {
+      const int i_seq = r / p.heads, h = r - i_seq * p.heads;
       if (h >= heads) continue;
       float top = -INFINITY, l = 0.f;
-      float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 1
       for (int k0 = 0; k0 < parts; k0 += 4) {
         float2 q[4];
-        float4 v[2][4];
         float next = top;
 #pragma unroll
+        for (int u = 0; u < 4; ++u) q[u] = k0 + u < parts ? __ldcg(&rows_parts[slots[1 + k0 + u]].ml[r]) : make_float2(-INFINITY, 0.f);
+#pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const bool there = k0 + u < parts;
-          const RowsPart<DH>& from = rows_parts[slots[1 + min(k0 + u, parts - 1)]];
-          q[u] = there ? __ldcg(&from.ml[r]) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) v[e][u] = __ldcg(&from.o[2 * c + e][r]);
+          next = fmaxf(next, q[u].x);
+          if (k0 + u < parts) weight[(k0 + u) * SA_ROWS + r] = q[u].x;
         }
+        const float zero = next == -INFINITY ? 0.f : next;
+        l *= fast_exp2(top - zero);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) next = fmaxf(next, q[u].x);
-        const float zero = next == -INFINITY ? 0.f : next, f0 = fast_exp2(top - zero);
+        for (int u = 0; u < 4; ++u) l = fmaf(fast_exp2(q[u].x - zero), q[u].y, l);
         top = next;
-        l *= f0;
+      }
+      const float zero = top == -INFINITY ? 0.f : top, inv = l == 0.f ? 0.f : 1.f / l;
+      for (int k = 0; k < parts; ++k) weight[k * SA_ROWS + r] = fast_exp2(weight[k * SA_ROWS + r] - zero) * inv;
+      if (a.lse) a.lse[int64_t(s0 + i_seq) * a.n_q_heads + hk * heads_all + in_head + h] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
+    }
+    __syncthreads();
+    // a thread has eight coordinates of two rows at a time, four parts of each on their way
+    const int n_pieces = n_rows * (DH / 8);
+#pragma unroll 1
+    for (int x0 = tid; x0 < n_pieces; x0 += 2 * SA_THREADS) {
+      float4 o[2][2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          o[e].x *= f0; o[e].y *= f0; o[e].z *= f0; o[e].w *= f0;
+      for (int y = 0; y < 2; ++y) o[y][0] = o[y][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int k0 = 0; k0 < parts; k0 += 4) {
+        float4 v[2][4][2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int x = min(x0 + y * SA_THREADS, n_pieces - 1), c = x / n_rows, r = x - c * n_rows;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (k0 + u >= parts) continue;
+            const RowsPart<DH>& from = rows_parts[slots[1 + k0 + u]];
+            v[y][u][0] = __ldcg(&from.o[2 * c][r]);
+            v[y][u][1] = __ldcg(&from.o[2 * c + 1][r]);
+          }
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float w = fast_exp2(q[u].x - zero);      // (0 for a part that is not there; its outputs are another part's)
-          l = fmaf(w, q[u].y, l);
+        for (int y = 0; y < 2; ++y) {
+          const int x = min(x0 + y * SA_THREADS, n_pieces - 1), r = x % n_rows;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            o[e].x = fmaf(w, v[e][u].x, o[e].x);
-            o[e].y = fmaf(w, v[e][u].y, o[e].y);
-            o[e].z = fmaf(w, v[e][u].z, o[e].z);
-            o[e].w = fmaf(w, v[e][u].w, o[e].w);
+          for (int u = 0; u < 4; ++u) {
+            if (k0 + u >= parts) continue;
+            const float w = weight[(k0 + u) * SA_ROWS + r];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              o[y][e].x = fmaf(w, v[y][u][e].x, o[y][e].x);
+              o[y][e].y = fmaf(w, v[y][u][e].y, o[y][e].y);
+              o[y][e].z = fmaf(w, v[y][u][e].z, o[y][e].z);
+              o[y][e].w = fmaf(w, v[y][u][e].w, o[y][e].w);
+            }
           }
         }
       }
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int64_t row = s0 + i_seq;
-      const int head = hk * heads_all + in_head + h;
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH + c * 8) =
-          make_uint4(pack_16<F16>(o[0].x * inv, o[0].y * inv), pack_16<F16>(o[0].z * inv, o[0].w * inv), pack_16<F16>(o[1].x * inv, o[1].y * inv),
-                     pack_16<F16>(o[1].z * inv, o[1].w * inv));
-      if (c == 0 && a.lse) a.lse[row * a.n_q_heads + head] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int x = x0 + y * SA_THREADS, c = x / n_rows, r = x - c * n_rows, i_seq = r / p.heads, h = r - i_seq * p.heads;
+        if (x >= n_pieces || h >= heads) continue;
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + int64_t(s0 + i_seq) * a.o_stride + (hk * heads_all + in_head + h) * DH + c * 8) =
+            make_uint4(pack_16<F16>(o[y][0].x, o[y][0].y), pack_16<F16>(o[y][0].z, o[y][0].w), pack_16<F16>(o[y][1].x, o[y][1].y),
+                       pack_16<F16>(o[y][1].z, o[y][1].w));
+      }
     }
   }
 }
@@ -884,8 +1106,15 @@ SharedKernel pick(int dh, bool f16, bool mod) { return dh == 128 ? pick<128>(f16
 
 }  // namespace
 
-int shared_attention_tile_heads(int n_q_heads, int n_kv_heads) { return std::min(n_q_heads / n_kv_heads, SA_ROWS); }
-int shared_attention_tile_seqs(int n_q_heads, int n_kv_heads) { return SA_ROWS / shared_attention_tile_heads(n_q_heads, n_kv_heads); }
+// Groups whose rows are 64 or fewer on average stand in the matrix twice.
+SharedTile shared_attention_tile(const hs_shared_attention_t& a) {
+  SharedTile t;
+  const int heads = a.n_q_heads / a.n_kv_heads, seqs = (a.n_seqs + a.n_groups - 1) / a.n_groups;
+  t.copies = int64_t(heads) * seqs <= SA_ROWS / 2 ? 2 : 1;
+  t.heads = std::min(heads, SA_ROWS);
+  t.seqs = SA_ROWS / t.copies / t.heads;
+  return t;
+}
 
 cudaError_t shared_attention_set_attributes() {
   for (int i = 0; i < 8; ++i) {
@@ -896,16 +1125,16 @@ cudaError_t shared_attention_set_attributes() {
   return cudaSuccess;
 }
 
-cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtensorMap& tm_kv, const CUtensorMap& tm_q, int sm_count, int sm_budget,
-                                    cudaStream_t stream) {
+cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtensorMap& tm_q, int sm_count, int sm_budget, cudaStream_t stream) {
   SharedParams p{};
-  p.tm_kv = tm_kv;
   p.tm_q = tm_q;
   p.a = a;
   p.score = score_scale(a.scale, a.cap);
-  p.heads = shared_attention_tile_heads(a.n_q_heads, a.n_kv_heads);
+  const SharedTile tile = shared_attention_tile(a);
+  p.heads = tile.heads;
   p.chunks = (a.n_q_heads / a.n_kv_heads + p.heads - 1) / p.heads;
-  p.tile_seqs = shared_attention_tile_seqs(a.n_q_heads, a.n_kv_heads);
+  p.tile_seqs = tile.seqs;
+  p.copies = tile.copies;
   p.shares = share_count(sm_count);
   // Without a cap and slopes the kernel masks and compares raw scores and multiplies by the scale in the exponent: right for a positive scale only.  The other
   // instantiation scales first.

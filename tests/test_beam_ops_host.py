@@ -96,8 +96,8 @@ REFUSED = {
                               (dict(n_q_heads=2048, q_stride=1 << 18, o_stride=1 << 18), SHAPE), (dict(cap=-1.0), INVALID), (dict(cap=NAN), INVALID), (dict(cap=INF), INVALID),
                               (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(q_stride=252), INVALID), (dict(o_stride=260), INVALID), (dict(q=P + 8), INVALID),
                               (dict(kv_pool=P + 64), INVALID), (dict(type=0), INVALID), (dict(layer=2), INVALID), (dict(layer=-1), INVALID), (dict(workspace=P + 64), INVALID),
-                              (dict(group_begin=0), INVALID), (dict(shared_len=0), INVALID), (dict(n_seqs=4097), SHAPE), (dict(n_seqs=4096, max_pages_per_seq=16385), SHAPE),
-                              (dict(n_seqs=4096, max_pages_per_seq=16384, n_q_heads=16, q_stride=1024, o_stride=1024), SHAPE),
+                              (dict(group_begin=0), INVALID), (dict(shared_len=0), INVALID), (dict(n_seqs=2049), SHAPE), (dict(n_seqs=2048, max_pages_per_seq=32769), SHAPE),
+                              (dict(n_seqs=2048, max_pages_per_seq=32768, n_q_heads=16, q_stride=1024, o_stride=1024), SHAPE),
                               (dict(num_pages=1 << 25, n_layers=64), SHAPE)],
 }
 
