@@ -4,7 +4,7 @@
 //   tile      sequences of one group that follow one another, all query heads of one KV head: up to 128 rows of a matrix, sequence after sequence.  Where groups
 //             are small (a rule on the call's shape) a tile is 64 rows, which stand in the matrix twice: each copy's softmax has half of a block's keys.
 //   keys      the tile's keys are one line of blocks of 64: the group's shared pages, read once for all rows, then the pages of each sequence's own keys, one sequence
-//             behind the other.  A row sees the shared keys and a run of the others; what it does not see is masked, and a warp whose 32 rows see nothing
+//             behind the other, a block of the first half of the rows and one of the second half in turn: they are different warps' work, which overlaps.  A row sees the shared keys and a run of the others; what it does not see is masked, and a warp whose 32 rows see nothing
 //             of a block gives it the weight 0 and goes on.  (The products with rows that see nothing cost little: a block's two products take a third of
 //             the time that its 32 KB take to come.)
 //   teams     two to a thread block, each with a running softmax of its own: a warp that fetches, one that issues S = Q K^T into tensor memory and O += P V, four with one
@@ -20,6 +20,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_tiles.cuh"
 
@@ -38,6 +39,7 @@ struct SharedParams {
   hs_shared_attention_t a;
   ScoreScale score;
   int heads, chunks;                                     // query heads of a tile; groups of them per KV head
+  int half_seqs;                                         // of them, the first half: those that begin in the first half of the rows
   int tile_seqs, copies;                                 // sequences of a tile; how often its rows stand in the matrix: 1 or 2
   int shares;                                            // at most
 };
@@ -59,9 +61,16 @@ struct Item {
   int block0, n_blocks;                                  // of the tile's line
   int parts, slot;                                       // parts of the tile (1: not cut), and where this one goes
   int middle;                                            // the other team has a part of this part
-  int number, unused;                                    // of the tile and its head, in the line
+  int first_b, pages_a, pages_b;                         // own keys: the first sequence of the second half; pages of either half
+  int number;                                   // of the tile and its head, in the line
   int begin[SA_ROWS + 1];                                // own pages in front of each sequence's
   int kv[SA_ROWS];                                       // keys of each sequence
+  // Block `own` of the own keys: which half it is of (its return value), and its number there; a number behind the half's last page is a block without pages.
+  __device__ __forceinline__ int half_of(int own, int& block) const {
+    const int a = (pages_a + 3) / 4, b = (pages_b + 3) / 4, both = 2 * min(a, b);
+    block = own < both ? own >> 1 : own - min(a, b);
+    return own < both ? own & 1 : a < b ? 1 : 0;
+  }
 };
 struct alignas(16) Team {
   uint64_t q_full, q_empty, k_full[2], v_full[2], s_full[2], p_full[2], o_full[2];
@@ -94,6 +103,17 @@ static_assert(sizeof(RowsPart<128>) <= SharedGeom<128>::TEAM_BYTES && sizeof(Row
 static_assert(1024 + kMaxShares * SA_ROWS * 4 <= SharedGeom<64>::TEAMS, "weights of a join");
 static_assert(kWsSharedQueue + kMaxShares * 4 <= kWsScratch && SA_MAX_SEQS < 65536, "one word per share");
 
+// The largest and the smallest of three (numbers rather than NaN).
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+__device__ __forceinline__ float min3(float x, float y, float z) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
 // 32 lanes x 16 consecutive 32-bit columns, registers -> tensor memory.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -157,7 +177,8 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   Block* bar = reinterpret_cast<Block*>(smem + G_::BLOCK);
   volatile int* abort_flag = &bar->abort_flag;
   const hs_shared_attention_t& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = int(threadIdx.x);
+  // (the warp's number by a shuffle, so that the compiler knows it is the same in all lanes: descriptors then stay in uniform registers)
+  const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31, tid = int(threadIdx.x);
   // Warps 0 .. 3 and 4 .. 7 are the teams' softmax warps (of tensor memory lanes 32 (warp % 4) on), 8 and 10 fetch, 9 and 11 issue the products.
   const int team = warp < 8 ? warp >> 2 : (warp - 8) >> 1;
   Team& tm = reinterpret_cast<Team*>(smem + G_::TEAMS)[team];
@@ -262,11 +283,13 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       atomicAdd(&cost[int(tile[g]) + (s - int(group[g])) / p.tile_seqs], (keys + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE - shared[g]);
     });
     __syncthreads();
-    // (at least one block, so that rows that see no key take the same way)
+    // (at least one block, so that rows that see no key take the same way, too)
     const int all = running_sums(plan.tiles, bar->warp_sum,
                                  [&](int t) {
-                                   const int common = shared[t < n_groups && tile[t] == t && tile[t + 1] > t ? t : find_last(tile, n_groups, t)];
-                                   return max((common + 3) / 4 + (cost[t] + 3) / 4, 1) + SA_ITEM_COST;
+                                   const int g = t < n_groups && tile[t] == t && tile[t + 1] > t ? t : find_last(tile, n_groups, t);
+                                   // (with sequences in both halves there may be one block more)
+                                   const int two = int(group[g + 1]) - int(group[g]) - (t - int(tile[g])) * p.tile_seqs > p.half_seqs ? 1 : 0;
+                                   return max((shared[g] + 3) / 4 + (cost[t] + 3) / 4 + two, 1) + SA_ITEM_COST;
                                  },
                                  [&](int t, int sum) { cost[t] = sum; });
     if (tid == 0) cost[plan.tiles] = all;
@@ -325,6 +348,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     return parts;
   };
 
+  auto warp_wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag, a.status)) != 0; };
   int rs = 0;
   uint32_t rph = 0;                                      // item ring slot / phase
   uint32_t items_seen = 0;
@@ -535,26 +559,34 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
             it.middle = middle_of(share, number);
             it.number = number;
             it.begin[n] = sum;
+            it.first_b = min(p.half_seqs, n);
+          }
+          __syncwarp();
+          if (lane == 0) {
+            it.pages_a = it.begin[it.first_b];
+            it.pages_b = sum - it.pages_a;
           }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&tm.ring_full[rs]);
         const int n_seq = it.n_seq, n_blocks = it.n_blocks, block0 = it.block0, shared_pages = it.shared_pages, shared_blocks = it.shared_blocks;
-        const int own_pages = it.begin[n_seq];
         // Lane l looks up page l % 4 of block j0 + l / 4: its id and how many of its keys are seen (0: there is no such page).
         int keys = 0;
         auto look_up = [&](int j0) {
           const int j = j0 + (lane >> 2);
           keys = 0;
           if (j >= n_blocks) return 0;
-          int u = (block0 + j) * 4 + (lane & 3);
           if (block0 + j < shared_blocks) {
+            const int u = (block0 + j) * 4 + (lane & 3);
             if (u >= shared_pages) return 0;
             keys = HS_PAGE_SIZE;
             return a.block_tables[int64_t(it.table) * a.max_pages_per_seq + u];
           }
-          u -= shared_blocks * 4;
-          if (u >= own_pages) return 0;
+          int block;
+          const int second = it.half_of(block0 + j - shared_blocks, block);
+          int u = block * 4 + (lane & 3);
+          if (u >= (second ? it.pages_b : it.pages_a)) return 0;
+          u += second ? it.pages_a : 0;
           const int k = find_last(it.begin, n_seq, u), page = shared_pages + u - it.begin[k];
           keys = min(it.kv[k] - page * HS_PAGE_SIZE, HS_PAGE_SIZE);
           return a.block_tables[int64_t(it.seq0 + k) * a.max_pages_per_seq + page];
@@ -567,21 +599,50 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
           }
           return n > 0 ? (n << 26) | id : 0;
         };
-        // K or V of block j, whose pages are in `pages`
         const char* pool = static_cast<const char*>(a.kv_pool) + (int64_t(a.layer * 2) * a.num_pages * a.n_kv_heads + it.hk) * (HS_PAGE_SIZE * DH * 2) + lane * 16;
-        auto fetch = [&](int j, int kv, int pages) {
+        // The pages of eight blocks: K's, V's where K is ahead of them, and the ids that are on their way for the next eight.
+        int k_pages = look_up(0), v_pages = 0, k_eight = 0;
+        k_pages = checked(k_pages, keys);
+        int raw = look_up(8), raw_keys = keys;
+        // K of blocks 0 and 1, then V of a block and K of the one behind the next in turn.
+#pragma unroll 1
+        for (int e = -2; ok && e < 2 * n_blocks; ++e) {
+          const int kv = e >= 0 && (e & 1) == 0 ? 1 : 0, j = e < 0 ? e + 2 : kv ? e >> 1 : (e >> 1) + 2;
+          // the Q tile, for which the item in front has to be done with its own, behind the first two K blocks
+          if (e == 0) {
+            ok = warp_wait(&tm.q_empty, (items_seen & 1) ^ 1);
+            if (ok && lane == 0) {
+              mbar_expect_tx(&tm.q_full, copies * G_::HALVES * p.heads * p.tile_seqs * 128);
+#pragma unroll 1
+              for (int k = 0; k < copies; ++k)
+#pragma unroll 1
+                for (int h = 0; h < G_::HALVES; ++h)
+                  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                                   smem_u32(q_smem + h * 16384 + k * 8192)),
+                               "l"(reinterpret_cast<uint64_t>(&p.tm_q)), "r"(smem_u32(&tm.q_full)), "r"(h * 64), "r"(it.head0), "r"(it.seq0)
+                               : "memory");
+            }
+            if (!ok) break;
+          }
+          if (j >= n_blocks) continue;
+          if (!kv && (j & 7) == 0 && j > 0) {
+            v_pages = k_pages;
+            k_pages = checked(raw, raw_keys);
+            k_eight = j >> 3;
+            raw = look_up(j + 8);
+            raw_keys = keys;
+          }
           const uint32_t b = g + j, buf = b & 1;
           // a slot is free when the products with what it held are done
-          if (b >= 2) {
-            ok = __all_sync(0xffffffffu, mbar_wait(kv ? &tm.o_full[buf] : &tm.s_full[buf], ((b - 2) >> 1) & 1, abort_flag, a.status));
-            if (!ok) return;
-          }
+          if (b >= 2) ok = warp_wait(kv ? &tm.o_full[buf] : &tm.s_full[buf], ((b - 2) >> 1) & 1);
+          if (!ok) break;
           const uint32_t dst = smem_u32((kv ? v_smem : k_smem) + buf * G_::KV_BYTES) + to;
           const char* src_kv = pool + kv * int64_t(a.num_pages) * page_bytes;
-#pragma unroll
+          const int pages = j >> 3 == k_eight ? k_pages : v_pages;
+#pragma unroll 1
           for (int w = 0; w < 4; ++w) {
             const int word = __shfl_sync(0xffffffffu, pages, (j & 7) * 4 + w), n = word >> 26;
-            if (n == 0 && !kv) continue;                 // (scores of no key; V has to be finite everywhere)
+            if (n == 0 && !kv) continue;                 // (scores that no row looks at; V has to be finite everywhere)
             const char* src = src_kv + int64_t(word & ((1 << 26) - 1)) * page_bytes;
 #pragma unroll
             for (int c = 0; c < G_::COPIES; ++c)
@@ -590,37 +651,6 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
                            : "memory");
           }
           asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(kv ? &tm.v_full[buf] : &tm.k_full[buf])) : "memory");
-        };
-        int raw = look_up(0), cur_keys = keys, raw_next = look_up(8);
-        int cur = checked(raw, cur_keys), next = checked(raw_next, keys);
-        raw = look_up(16);
-        int raw_keys = keys;
-        fetch(0, 0, cur);
-        if (ok && n_blocks > 1) fetch(1, 0, cur);
-        if (!ok) break;
-        // the Q tile, for which the item in front has to be done with its own
-        if (lane == 0) {
-          ok = mbar_wait(&tm.q_empty, (items_seen & 1) ^ 1, abort_flag, a.status);
-          if (ok) {
-            mbar_expect_tx(&tm.q_full, copies * G_::HALVES * p.heads * p.tile_seqs * 128);
-            for (int k = 0; k < copies; ++k)
-              for (int h = 0; h < G_::HALVES; ++h)
-                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-                                 smem_u32(q_smem + h * 16384 + k * 8192)),
-                             "l"(reinterpret_cast<uint64_t>(&p.tm_q)), "r"(smem_u32(&tm.q_full)), "r"(h * 64), "r"(it.head0), "r"(it.seq0)
-                             : "memory");
-          }
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        for (int j = 0; j < n_blocks && ok; ++j) {
-          if ((j & 7) == 0 && j > 0) {
-            cur = next;
-            next = checked(raw, raw_keys);
-            raw = look_up(j + 16);
-            raw_keys = keys;
-          }
-          fetch(j, 1, cur);
-          if (ok && j + 2 < n_blocks) fetch(j + 2, 0, (j + 2) >> 3 == j >> 3 ? cur : next);
         }
         __syncwarp();
         ++items_seen;
@@ -629,51 +659,60 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       }
     } else if (warp == 9 || warp == 11) {
       // ============================================================= products ==
-      if (lane == 0) {
-        constexpr uint32_t idesc_s = idesc_16<F16>(128, SA_KEYS);
-        constexpr uint32_t idesc_pv = idesc_16<F16>(128, DH) | (1u << 16);   // B (= V) is MN-major
-        const uint64_t q_desc = umma_desc_kmajor_sw128(smem_u32(q_smem));
-        const uint64_t k_desc0 = umma_desc_kmajor_sw128(smem_u32(k_smem));
-        const uint64_t v_desc0 = umma_desc_mnmajor_sw128(smem_u32(v_smem), 8192, 1024);
-        const uint32_t s_base = tmem + team * SA_TEAM_TMEM, d_o = s_base + G_::O0;
-        auto pv_block = [&](uint32_t b, bool first) -> bool {
-          const uint32_t buf = b & 1, ph = (b >> 1) & 1;
-          if (!mbar_wait(&tm.v_full[buf], ph, abort_flag, a.status) || !mbar_wait(&tm.p_full[buf], ph, abort_flag, a.status)) return false;
-          fence_proxy_async();                           // (V came by ordinary copies)
-          tc_fence_after_sync();
-          const uint64_t vdesc = v_desc0 + uint64_t(buf * (G_::KV_BYTES >> 4));
-#pragma unroll
-          for (int pg = 0; pg < 4; ++pg)                 // 16 keys (one page) per MMA: 8 columns of P
-            umma_ts(d_o, s_base + buf * SA_KEYS + 8 * pg, vdesc + uint64_t(pg * (2048 >> 4)), idesc_pv, pg != 0 || !first ? 1u : 0u);
-          umma_commit(&tm.o_full[buf]);                  // (which frees the V slot, too)
-          return true;
-        };
-        bool ok = true;
-        while (ok) {
-          if (!mbar_wait(&tm.ring_full[rs], rph, abort_flag, a.status)) break;
-          const int valid = tm.ring[rs].valid, n_blocks = tm.ring[rs].n_blocks;
-          mbar_arrive(&tm.ring_empty[rs]);
-          if (++rs == 2) { rs = 0; rph ^= 1; }
-          if (!valid) break;
-          if (!mbar_wait(&tm.q_full, items_seen & 1, abort_flag, a.status)) break;
-          ++items_seen;
-          for (int j = 0; j < n_blocks && ok; ++j) {
+      // (the whole warp goes through the loop, and one lane issues: a thread by itself took 77 cycles for each product, to bring its descriptor to uniform registers)
+      constexpr uint32_t idesc_s = idesc_16<F16>(128, SA_KEYS);
+      constexpr uint32_t idesc_pv = idesc_16<F16>(128, DH) | (1u << 16);     // B (= V) is MN-major
+      const uint64_t q_desc = umma_desc_kmajor_sw128(smem_u32(q_smem));
+      const uint64_t k_desc0 = umma_desc_kmajor_sw128(smem_u32(k_smem));
+      const uint64_t v_desc0 = umma_desc_mnmajor_sw128(smem_u32(v_smem), 8192, 1024);
+      const uint32_t s_base = tmem + team * SA_TEAM_TMEM, d_o = s_base + G_::O0;
+      bool ok = true;
+#pragma unroll 1
+      while (ok) {
+        ok = warp_wait(&tm.ring_full[rs], rph);
+        if (!ok) break;
+        const int valid = __shfl_sync(0xffffffffu, tm.ring[rs].valid, 0), n_blocks = __shfl_sync(0xffffffffu, tm.ring[rs].n_blocks, 0);
+        if (lane == 0) mbar_arrive(&tm.ring_empty[rs]);
+        if (++rs == 2) { rs = 0; rph ^= 1; }
+        if (!valid) break;
+        ok = warp_wait(&tm.q_full, items_seen & 1);
+        ++items_seen;
+        // S of block j, then P V of block j - 1, which overlaps the softmax of block j
+#pragma unroll 1
+        for (int j = 0; j <= n_blocks && ok; ++j) {
+          if (j < n_blocks) {
             const uint32_t b = g + j, buf = b & 1;
-            ok = mbar_wait(&tm.k_full[buf], (b >> 1) & 1, abort_flag, a.status);
+            ok = warp_wait(&tm.k_full[buf], (b >> 1) & 1);
             if (!ok) break;
             fence_proxy_async();                         // (K came by ordinary copies)
             tc_fence_after_sync();
             const uint64_t kdesc = k_desc0 + uint64_t(buf * (G_::KV_BYTES >> 4));
+            if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < DH / 16; ++ks)
-              umma_bf16(s_base + buf * SA_KEYS, q_desc + uint64_t((ks >> 2) * (16384 >> 4) + 2 * (ks & 3)),
-                        kdesc + uint64_t((ks >> 2) * (8192 >> 4) + 2 * (ks & 3)), idesc_s, ks != 0);
-            umma_commit(&tm.s_full[buf]);                // (which frees the K slot, too)
-            if (j > 0) ok = pv_block(b - 1, j == 1);     // overlaps the softmax of block j
+              for (int ks = 0; ks < DH / 16; ++ks)
+                umma_bf16(s_base + buf * SA_KEYS, q_desc + uint64_t((ks >> 2) * (16384 >> 4) + 2 * (ks & 3)),
+                          kdesc + uint64_t((ks >> 2) * (8192 >> 4) + 2 * (ks & 3)), idesc_s, ks != 0);
+              umma_commit(&tm.s_full[buf]);              // (which frees the K slot, too)
+            }
+            __syncwarp();
           }
-          if (ok) ok = pv_block(g + n_blocks - 1, n_blocks == 1);
-          g += n_blocks;
+          if (j > 0) {
+            const uint32_t b = g + j - 1, buf = b & 1, ph = (b >> 1) & 1;
+            ok = warp_wait(&tm.v_full[buf], ph) && warp_wait(&tm.p_full[buf], ph);
+            if (!ok) break;
+            fence_proxy_async();                         // (V came by ordinary copies)
+            tc_fence_after_sync();
+            const uint64_t vdesc = v_desc0 + uint64_t(buf * (G_::KV_BYTES >> 4));
+            if (elect_one()) {
+#pragma unroll
+              for (int pg = 0; pg < 4; ++pg)             // 16 keys (one page) per MMA: 8 columns of P; the item's first block overwrites O
+                umma_ts(d_o, s_base + buf * SA_KEYS + 8 * pg, vdesc + uint64_t(pg * (2048 >> 4)), idesc_pv, pg != 0 || j != 1 ? 1u : 0u);
+              umma_commit(&tm.o_full[buf]);              // (which frees the V slot, too)
+            }
+            __syncwarp();
+          }
         }
+        g += n_blocks;
       }
     } else {
       // ============================================================== softmax ==
@@ -693,8 +732,9 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
         const int n_blocks = it.n_blocks, block0 = it.block0, shared_blocks = it.shared_blocks;
         const bool row_valid = i_seq < it.n_seq && h < it.heads;
         const int kv = row_valid ? it.kv[i_seq] : 0, shared_keys = kv > 0 ? it.shared_pages * HS_PAGE_SIZE : 0;
-        // the row sees the first shared_keys of the shared blocks' keys, and lo .. hi - 1 of the others'
-        const int lo = row_valid ? it.begin[i_seq] * HS_PAGE_SIZE : 0, hi = lo + kv - shared_keys;
+        // the row sees the first shared_keys of the shared blocks' keys, and lo .. hi - 1 of its half's others
+        const int my_half = i_seq >= it.first_b ? 1 : 0;
+        const int lo = row_valid ? (it.begin[i_seq] - (my_half ? it.pages_a : 0)) * HS_PAGE_SIZE : 0, hi = lo + kv - shared_keys;
         const float slope = MOD && a.slopes && row_valid ? a.slopes[it.head0 + h] * 1.4426950408889634f : 0.f;
         m_ref = -INFINITY;
         l_run = 0.f;
@@ -703,63 +743,78 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
           const uint32_t b = g + j, buf = b & 1, ph = (b >> 1) & 1;
           const int block = block0 + j;
           const bool common = block < shared_blocks;
-          const int key0 = (common ? block : block - shared_blocks) * SA_KEYS + half * 32;          // the thread's first key
+          int in_half = block;
+          const bool mine = common || it.half_of(block - shared_blocks, in_half) == my_half;
+          const int key0 = in_half * SA_KEYS + half * 32;          // the thread's first key
           // bits of the keys seen, 32 and 32
           uint32_t seen[2];
 #pragma unroll
           for (int c = 0; c < 2; ++c)
-            seen[c] = common ? first_bits(shared_keys - key0 - 32 * c) : first_bits(hi - key0 - 32 * c) & ~first_bits(lo - key0 - 32 * c);
+            seen[c] = !mine ? 0u : common ? first_bits(shared_keys - key0 - 32 * c) : first_bits(hi - key0 - 32 * c) & ~first_bits(lo - key0 - 32 * c);
           if (n_chunks == 1) seen[1] = 0;
           ok = __all_sync(0xffffffffu, mbar_wait(&tm.s_full[buf], ph, abort_flag, a.status));
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t s_col = t_lane + buf * SA_KEYS;
           if (__any_sync(0xffffffffu, (seen[0] | seen[1]) != 0)) {
-            const bool masked = __any_sync(0xffffffffu, seen[0] != 0xffffffffu || (n_chunks == 2 && seen[1] != 0xffffffffu));
+            // A row sees all of a page's keys or none, but for a sequence's last page: only a warp that meets one of those masks key by key.
+            auto page_seen = [&](int c, int q) { return ((c ? seen[1] : seen[0]) >> (16 * q) & 0xffffu) != 0; };
+            auto in_part = [](uint32_t w) { return ((w & 0xffffu) != 0 && (w & 0xffffu) != 0xffffu) || ((w >> 16) != 0 && (w >> 16) != 0xffffu); };
+            const bool partial = __any_sync(0xffffffffu, in_part(seen[0]) || in_part(seen[1]));
             auto mask = [&](int c, uint32_t to) {
               const uint32_t bits = c ? seen[1] : seen[0];
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!(bits & (1u << e))) sreg[e] = to;
+              for (int k = 0; k < 32; ++k)
+                if (!(bits & (1u << k))) sreg[k] = to;
             };
-            auto reduce = [&](auto op) {                 // eight chains
-              float x[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(sreg[e]);
-#pragma unroll
-              for (int e = 8; e < 32; ++e) x[e & 7] = op(x[e & 7], __uint_as_float(sreg[e]));
-              return op(op(op(x[0], x[1]), op(x[2], x[3])), op(op(x[4], x[5]), op(x[6], x[7])));
-            };
-            auto largest = [&]() { return reduce([](float x, float y) { return fmaxf(x, y); }); };
-            auto smallest = [&]() { return reduce([](float x, float y) { return fminf(x, y); }); };
-            // Raw scores.  Capped ones that are not seen are NaN, which maxima and minima pass over and whose weight is made 0 behind the exponential.
+            // Raw scores.  Capped ones that are not seen are NaN, which maxima and minima pass over.
             auto load = [&](int c, bool with_mask) {
               tmem_ld32(s_col + (half + c) * 32, sreg);
               tmem_ld_wait();
-              if (with_mask && masked) mask(c, MOD ? 0x7fffffffu : 0xff800000u);
+              if (with_mask && partial) mask(c, MOD ? 0x7fffffffu : 0xff800000u);
             };
+            // The largest (or smallest) of the pages that are seen, in two chains each with three operands at a time.
+            auto over_pages = [&](int c, float none, auto op) {
+              float x[2];
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                auto at = [&](int k) { return __uint_as_float(sreg[16 * q + k]); };
+                float y = op(at(0), at(2), at(4)), z = op(at(1), at(3), at(5));
+#pragma unroll
+                for (int k = 6; k < 14; k += 4) {
+                  y = op(y, at(k), at(k + 2));
+                  z = op(z, at(k + 1), at(k + 3));
+                }
+                y = op(y, at(14), at(15));
+                x[q] = page_seen(c, q) ? op(y, z, z) : none;
+              }
+              return op(x[0], x[1], x[1]);
+            };
+            auto largest = [&](int c) { return over_pages(c, -INFINITY, [](float x, float y, float z) { return max3(x, y, z); }); };
+            auto smallest = [&](int c) { return over_pages(c, INFINITY, [](float x, float y, float z) { return min3(x, y, z); }); };
             // While the warp's scores allow a polynomial for the cap, that of the largest score is the largest one, and the reference is part of its last
-            // multiply-add.  A bias, or the cap beyond, has to be worked out before the maximum is known, and once more behind it.
-            float mx = -INFINITY, least = INFINITY;
+            // multiply-add.  A bias, a mask key by key, or the cap beyond, has to be worked out before the maximum is known, and once more behind it.
+            float mx = -INFINITY;
             int degree = 0;
             bool direct = !MOD;
             if (!MOD || sc.out != 0.f) {
+              float least = INFINITY;
 #pragma unroll 1
               for (int c = n_chunks - 1; c >= 0; --c) {
                 load(c, true);
-                mx = fmaxf(mx, largest());
-                if (MOD) least = fminf(least, smallest());
+                mx = fmaxf(mx, largest(c));
+                if (MOD) least = fminf(least, smallest(c));
               }
               if (MOD) {
-                const float u = (seen[0] | seen[1]) != 0 ? fmaxf(mx * mx, least * least) : 0.f;
+                const float u = mx > -INFINITY ? fmaxf(mx * mx, least * least) : 0.f;
                 // one vote: the worst row's polynomial (6: degree three, 4: five, 0: none)
                 const unsigned vote = __reduce_and_sync(0xffffffffu, u <= sc.limit3 ? 6u : u <= sc.limit5 ? 4u : 0u);
                 degree = vote == 6 ? 3 : vote == 4 ? 5 : 0;
-                direct = degree != 0 && a.slopes == nullptr;
+                direct = degree != 0 && a.slopes == nullptr && !partial;
                 if (direct && mx > -INFINITY) {
-                  float unused;
-                  if (degree == 3) split(odd_poly(f2(mx, mx), sc.c3, f2(0.f, 0.f)), mx, unused);
-                  else split(odd_poly(f2(mx, mx), sc.c5, f2(0.f, 0.f)), mx, unused);
+                  const float v = mx * mx;
+                  mx *= degree == 3 ? fmaf(fmaf(fmaf(sc.c3[3], v, sc.c3[2]), v, sc.c3[1]), v, sc.c3[0])
+                                    : fmaf(fmaf(fmaf(fmaf(fmaf(sc.c5[5], v, sc.c5[4]), v, sc.c5[3]), v, sc.c5[2]), v, sc.c5[1]), v, sc.c5[0]);
                 }
               }
             }
@@ -778,7 +833,8 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
                 }
               };
               if (sc.out == 0.f) all([&](F2 s, F2 plus) { return fma2(s, in2, plus); });
-              else if (degree != 0) all([&](F2 s, F2 plus) { return odd_poly(s, sc.c5, plus); });
+              else if (degree == 3) all([&](F2 s, F2 plus) { return odd_poly(s, sc.c3, plus); });
+              else if (degree == 5) all([&](F2 s, F2 plus) { return odd_poly(s, sc.c5, plus); });
               else {
                 all([&](F2 s, F2 plus) {
                   float s0, s1;
@@ -786,14 +842,14 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
                   return fma2(f2(tanh_any(s0 * sc.in), tanh_any(s1 * sc.in)), f2(sc.out, sc.out), plus);
                 });
               }
-              if (masked) mask(c, 0xff800000u);          // -infinity
+              if (partial) mask(c, 0xff800000u);         // -infinity
             };
             if (MOD && !direct) {
               mx = -INFINITY;
 #pragma unroll 1
               for (int c = n_chunks - 1; c >= 0; --c) {
                 finish(c);
-                mx = fmaxf(mx, largest());
+                mx = fmaxf(mx, largest(c));
               }
             }
             // the reference maximum moves only when the block's maximum is far above it
@@ -807,21 +863,21 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
             const bool rescale = j > 0 && __any_sync(0xffffffffu, move);
             const float neg_ms = m_ref == -INFINITY ? 0.f : -m_ref * unit;
             const F2 neg2 = f2(neg_ms, neg_ms), unit2 = f2(unit, unit);
-            F2 sums[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+            float sum = 0.f;
 #pragma unroll 1
             for (int c = 0; c < n_chunks; ++c) {
               if (c > 0) {
                 if (MOD && !direct) finish(c);
                 else load(c, true);
               }
-              // log2 of the weights, eight pairs step by step, so that the pairs' steps overlap; P over S: column e of row r = keys 2 e, 2 e + 1
+              // log2 of the weights, a page's eight pairs step by step, so that the pairs' steps overlap; P over S: column e of row r = keys 2 e, 2 e + 1
               uint32_t pk[16];
               auto weights = [&](auto score) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 16) {
-                  F2 x[8];
+                for (int q = 0; q < 2; ++q) {
+                  F2 x[8], sums[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) x[i] = f2(__uint_as_float(sreg[e + 2 * i]), __uint_as_float(sreg[e + 2 * i + 1]));
+                  for (int i = 0; i < 8; ++i) x[i] = f2(__uint_as_float(sreg[16 * q + 2 * i]), __uint_as_float(sreg[16 * q + 2 * i + 1]));
                   score(x);
 #pragma unroll
                   for (int i = 0; i < 8; ++i) {
@@ -829,17 +885,17 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
                     split(x[i], y0, y1);
                     y0 = fast_exp2(y0);
                     y1 = fast_exp2(y1);
-                    if (MOD) {                           // (NaN: not seen)
-                      y0 = fmaxf(y0, 0.f);
-                      y1 = fmaxf(y1, 0.f);
-                    }
-                    sums[i & 3] = add2(sums[i & 3], f2(y0, y1));
+                    sums[i & 1] = add2(sums[i & 1], f2(y0, y1));
                     // (at most 2^kRefSlack, rounded once for the product with v in 16 bits; the sums keep fp32)
-                    pk[e / 2 + i] = pack_16<F16>(y0, y1);
+                    const uint32_t word = pack_16<F16>(y0, y1);
+                    pk[8 * q + i] = page_seen(c, q) ? word : 0u;
                   }
+                  float sum_a, sum_b;
+                  split(add2(sums[0], sums[1]), sum_a, sum_b);
+                  sum += page_seen(c, q) ? sum_a + sum_b : 0.f;
                 }
               };
-              auto poly = [&](F2(&x)[8], const auto& k, int n) {
+              auto poly = [&](F2(&x)[8], const auto& k, auto n) {
                 F2 u[8], q[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) u[i] = mul2(x[i], x[i]);
@@ -858,15 +914,13 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
                   for (int i = 0; i < 8; ++i) x[i] = fma2(x[i], unit2, neg2);
                 });
               } else if (degree == 3) {
-                weights([&](F2(&x)[8]) { poly(x, sc.c3, 4); });
+                weights([&](F2(&x)[8]) { poly(x, sc.c3, std::integral_constant<int, 4>()); });
               } else {
-                weights([&](F2(&x)[8]) { poly(x, sc.c5, 6); });
+                weights([&](F2(&x)[8]) { poly(x, sc.c5, std::integral_constant<int, 6>()); });
               }
               tmem_st16(s_col + (half + c) * 16, pk);
             }
-            float sum_a, sum_b;
-            split(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), sum_a, sum_b);
-            l_run = l_run * alpha + (sum_a + sum_b);
+            l_run = l_run * alpha + sum;
             if (copies == 2) {                           // the other copy's keys
               uint32_t none[16] = {};
               tmem_st16(s_col + (half ^ 1) * 16, none);
@@ -1041,52 +1095,47 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       if (a.lse) a.lse[int64_t(s0 + i_seq) * a.n_q_heads + hk * heads_all + in_head + h] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
     }
     __syncthreads();
-    // a thread has eight coordinates of two rows at a time, four parts of each on their way
+    // A thread has eight coordinates each of all its rows at once, and a part's are asked for together: it is one SM's way to the L2 that bounds it.
+    constexpr int PIECES = (SA_ROWS * (DH / 8) + SA_THREADS - 1) / SA_THREADS;
     const int n_pieces = n_rows * (DH / 8);
+    float4 o[PIECES][2];
+    int at[PIECES];                                      // row, and the place of its coordinates in a part
+#pragma unroll
+    for (int y = 0; y < PIECES; ++y) {
+      const int x = min(tid + y * SA_THREADS, n_pieces - 1), c = x / n_rows;
+      at[y] = 2 * c * SA_ROWS + x - c * n_rows;
+      o[y][0] = o[y][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
 #pragma unroll 1
-    for (int x0 = tid; x0 < n_pieces; x0 += 2 * SA_THREADS) {
-      float4 o[2][2];
+    for (int k = 0; k < parts; ++k) {
+      const RowsPart<DH>& from = rows_parts[slots[1 + k]];
+      float4 v[PIECES][2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) o[y][0] = o[y][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-      for (int k0 = 0; k0 < parts; k0 += 4) {
-        float4 v[2][4][2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int x = min(x0 + y * SA_THREADS, n_pieces - 1), c = x / n_rows, r = x - c * n_rows;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (k0 + u >= parts) continue;
-            const RowsPart<DH>& from = rows_parts[slots[1 + k0 + u]];
-            v[y][u][0] = __ldcg(&from.o[2 * c][r]);
-            v[y][u][1] = __ldcg(&from.o[2 * c + 1][r]);
-          }
-        }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int x = min(x0 + y * SA_THREADS, n_pieces - 1), r = x % n_rows;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (k0 + u >= parts) continue;
-            const float w = weight[(k0 + u) * SA_ROWS + r];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              o[y][e].x = fmaf(w, v[y][u][e].x, o[y][e].x);
-              o[y][e].y = fmaf(w, v[y][u][e].y, o[y][e].y);
-              o[y][e].z = fmaf(w, v[y][u][e].z, o[y][e].z);
-              o[y][e].w = fmaf(w, v[y][u][e].w, o[y][e].w);
-            }
-          }
-        }
+      for (int y = 0; y < PIECES; ++y) {
+        if (y * SA_THREADS >= n_pieces) continue;
+        v[y][0] = __ldcg(&from.o[0][0] + at[y]);
+        v[y][1] = __ldcg(&from.o[0][0] + at[y] + SA_ROWS);
       }
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int x = x0 + y * SA_THREADS, c = x / n_rows, r = x - c * n_rows, i_seq = r / p.heads, h = r - i_seq * p.heads;
-        if (x >= n_pieces || h >= heads) continue;
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + int64_t(s0 + i_seq) * a.o_stride + (hk * heads_all + in_head + h) * DH + c * 8) =
-            make_uint4(pack_16<F16>(o[y][0].x, o[y][0].y), pack_16<F16>(o[y][0].z, o[y][0].w), pack_16<F16>(o[y][1].x, o[y][1].y),
-                       pack_16<F16>(o[y][1].z, o[y][1].w));
+      for (int y = 0; y < PIECES; ++y) {
+        if (y * SA_THREADS >= n_pieces) continue;
+        const float w = weight[k * SA_ROWS + at[y] % SA_ROWS];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          o[y][e].x = fmaf(w, v[y][e].x, o[y][e].x);
+          o[y][e].y = fmaf(w, v[y][e].y, o[y][e].y);
+          o[y][e].z = fmaf(w, v[y][e].z, o[y][e].z);
+          o[y][e].w = fmaf(w, v[y][e].w, o[y][e].w);
+        }
       }
+    }
+#pragma unroll
+    for (int y = 0; y < PIECES; ++y) {
+      const int r = at[y] % SA_ROWS, c = at[y] / (2 * SA_ROWS), i_seq = r / p.heads, h = r - i_seq * p.heads;
+      if (tid + y * SA_THREADS >= n_pieces || h >= heads) continue;
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + int64_t(s0 + i_seq) * a.o_stride + (hk * heads_all + in_head + h) * DH + c * 8) =
+          make_uint4(pack_16<F16>(o[y][0].x, o[y][0].y), pack_16<F16>(o[y][0].z, o[y][0].w), pack_16<F16>(o[y][1].x, o[y][1].y),
+                     pack_16<F16>(o[y][1].z, o[y][1].w));
     }
   }
 }
@@ -1134,6 +1183,7 @@ cudaError_t launch_shared_attention(const hs_shared_attention_t& a, const CUtens
   p.heads = tile.heads;
   p.chunks = (a.n_q_heads / a.n_kv_heads + p.heads - 1) / p.heads;
   p.tile_seqs = tile.seqs;
+  p.half_seqs = (SA_ROWS / tile.copies / 2 + tile.heads - 1) / tile.heads;
   p.copies = tile.copies;
   p.shares = share_count(sm_count);
   // Without a cap and slopes the kernel masks and compares raw scores and multiplies by the scale in the exponent: right for a positive scale only.  The other
