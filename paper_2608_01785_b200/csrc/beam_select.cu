@@ -3,16 +3,16 @@
 //   row b of a request     L_b = log sum_v exp(scale x_v),   its n_out largest x_v
 //   request                the n_out largest  weight_b (S_b + scale x_v - L_b)  of all its beams' largest
 //
-// Work.  An item is a row or one of its equal parts.  Four teams of eight warps share a block, each with an item of its own from a queue, so that one team's
-// beginning and end hide behind the others' streams.  A thread reads four 16-byte pieces of a tile while it works on the last tile's, and keeps
+// Work.  An item is a row or one of its equal parts.  Four teams of four warps share a block, each with an item of its own from a queue, so that one team's
+// beginning and end hide behind the others' streams.  A thread reads eight 16-byte pieces of a tile while it works on the last tile's, and keeps
 //   M, s        a whole number M near the maximum in log2 units, and s = sum 2^(k x - M), k = scale log2(e): references are changed and joined by exact
 //               powers of two.  k is the sum of two fp32 numbers, and a tile's sum is added with its rounding error kept, so that log s is good to about 1e-7.
 //               (A part whose largest logit is 2^20 of those units from zero, as in a row masked with its type's lowest number from end to end, is
 //               summed a second time with that logit as its reference.)
-//   best, tile  its largest logit, and the first tile that has it.
-// At an item's end the n_out-th largest of 64 groups of four threads' (best, tile) bounds its n_out largest logits from below: only threads whose
-// own pair reaches it can hold one, a few of 256, and the team looks through their pieces once more (the L2 has them), lists what reaches the bound and
-// ranks the list.  The main loop carries no list and no test per element for it.
+//   best, tile  its largest logit, and the first tile that has it; second, the largest of its other tiles.
+// At an item's end the n_out-th largest of 64 groups of two threads' (best, tile) bounds its n_out largest logits from below: only threads whose
+// own pair reaches it can hold one, a few of 128, and the team looks through that tile's pieces once more (the L2 has them; through all of a thread's, where its second
+// reaches the bound, too), lists what reaches the bound and ranks the list.  The main loop carries no list and no test per element for it.
 // The team that delivers a request's last item makes the choice: L_b from the parts, candidates' scores in 64 bits, the same bound, list and ranks.
 #include <algorithm>
 
@@ -21,19 +21,18 @@
 namespace hs {
 namespace {
 
-constexpr int BS_TEAMS = 4, BS_TEAM = 256, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
-constexpr int BS_PIECES = 4, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
+constexpr int BS_TEAMS = 4, BS_TEAM = 128, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
+constexpr int BS_PIECES = 8, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
 constexpr int BS_LIST = 512;                                             // candidates that a team ranks at a time
+constexpr int BS_ITEM_COST = 3;                                          // tiles
 constexpr int BS_MAX_PARTS = 64;                                         // of a row
 constexpr float BS_FAR = 1048576.f;                                      // log2 units from zero beyond which references are logits
 constexpr float BS_SLACK = 16.f;                                         // log2 units that a logit may lie above its thread's reference
 
 using Key = unsigned long long;
 
-struct SelectPart {                                      // of a row, in the workspace
-  double s;                                              // sum of 2^(k (x - ref) - m)
-  float m, ref;
-  int bad, unused;                                       // bad: the part holds NaN or +infinity
+struct alignas(16) SelectPart {                          // of a row, in the workspace
+  float s_hi, s_lo, m, ref;                              // s_hi + s_lo: sum of 2^(k (x - ref) - m); m is NaN where the part holds NaN or +infinity
   Key keys[HS_MAX_BEAMS];                                // falling; 0: none
 };
 struct SelectParams {
@@ -51,7 +50,7 @@ struct alignas(16) SelectTeam {
   float m[BS_WARPS], top[BS_WARPS], base[HS_MAX_BEAMS], weight[HS_MAX_BEAMS], ref[HS_MAX_BEAMS];
   int state[HS_MAX_BEAMS];                               // of a beam: 0: no continuation, 1: in use, 2: done
   Key bound;
-  int flagged[BS_WARPS][32];
+  int2 flagged[BS_WARPS][32];                            // threads, and the tile that is to be looked at
   int n_list, bad, next, last;
 };
 
@@ -105,6 +104,25 @@ struct Piece {
   }
 };
 
+// The piece that begins with element e0 of a row whose elements are mis .. end - 1, one by one.
+template <int TYPE>
+__device__ __noinline__ uint4 edge_piece(const char* base, int e0, int mis, int end) {
+  constexpr int kPer = Piece<TYPE>::kPer;
+  constexpr uint32_t none = TYPE == HS_TYPE_F32 ? 0xff800000u : TYPE == HS_TYPE_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+  uint32_t w[4] = {none, none, none, none};
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (e0 + i < mis || e0 + i >= end) continue;
+    if constexpr (kPer == 4) {
+      w[i] = reinterpret_cast<const uint32_t*>(base)[e0 + i];
+    } else {
+      const uint32_t h = reinterpret_cast<const uint16_t*>(base)[e0 + i];
+      w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | h << 16 : (w[i / 2] & 0xffff0000u) | h;
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A row as 16-byte pieces, counted from the boundary at or below its beginning: the row is elements mis .. end - 1 of them.
 template <int TYPE>
 struct Row {
@@ -127,38 +145,40 @@ struct Row {
   __device__ __forceinline__ uint4 any(int piece) const {
     const int e0 = piece * P::kPer;
     if (e0 >= mis && e0 + P::kPer <= end) return whole(piece);
-    constexpr uint32_t none = TYPE == HS_TYPE_F32 ? 0xff800000u : TYPE == HS_TYPE_BF16 ? 0xff80u : 0xfc00u;
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = P::kSize == 4 ? none : none | none << 16;
-#pragma unroll
-    for (int i = 0; i < P::kPer; ++i) {
-      if (e0 + i < mis || e0 + i >= end) continue;
-      if constexpr (P::kSize == 4) {
-        w[i] = reinterpret_cast<const uint32_t*>(base)[e0 + i];
-      } else {
-        const uint32_t h = reinterpret_cast<const uint16_t*>(base)[e0 + i];
-        w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | h << 16 : (w[i / 2] & 0xffff0000u) | h;
-      }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    constexpr uint32_t none = TYPE == HS_TYPE_F32 ? 0xff800000u : TYPE == HS_TYPE_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+    if (e0 >= end || e0 + P::kPer <= mis) return make_uint4(none, none, none, none);
+    return edge_piece<TYPE>(base, e0, mis, end);
   }
 };
 
-// The n-th largest of 64 groups' keys (each the largest of four threads'), by the team's first warp; 0 where fewer groups have one.
+// A warp's part of sum 2^(k (x - ref)) over tiles tile0 .. tile1 - 1, in every lane.
+template <int TYPE>
+__device__ __noinline__ float far_sum(const Row<TYPE>& r, int tile0, int tile1, float ref, float k, int tid) {
+  float v = 0.f;
+#pragma unroll 1
+  for (int i = tile0 * BS_PIECES; i < tile1 * BS_PIECES; ++i) {
+    float x[Piece<TYPE>::kPer];
+    Piece<TYPE>::get(r.any(i * BS_TEAM + tid), x);
+#pragma unroll
+    for (int e = 0; e < Piece<TYPE>::kPer; ++e) v += exp2f((x[e] - ref) * k);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The n-th largest of 64 groups' keys (each the larger of two threads'), by the team's first warp; 0 where fewer groups have one.
 __device__ __forceinline__ void find_bound(SelectTeam& t, int n, int lane) {
   Key g[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    g[h] = t.best[4 * h][lane];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) g[h] = max(g[h], t.best[4 * h + w][lane]);
+    g[h] = max(t.best[2 * h][lane], t.best[2 * h + 1][lane]);
     t.group[32 * h + lane] = g[h];
   }
   if (lane == 0) t.bound = 0;
   __syncwarp();
   int above[2] = {0, 0};
-#pragma unroll 8
+#pragma unroll 4
   for (int j = 0; j < 64; j += 2) {
     const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&t.group[j]);
 #pragma unroll
@@ -186,7 +206,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
   SelectPart* parts = reinterpret_cast<SelectPart*>(static_cast<char*>(a.workspace) + kWsScratch);
   griddep_wait();
 
-  int item = int(blockIdx.x) * BS_TEAMS + team;
+  int item = team * int(gridDim.x) + int(blockIdx.x);    // (the first items on different SMs)
   while (item < p.items) {
     const int row = item / p.parts, part_i = item - row * p.parts;
     const bool ended = a.done != nullptr && a.done[row] != 0;
@@ -200,7 +220,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       const Row<TYPE> r(a, row);
       const int tiles = r.tiles(), tile0 = int(int64_t(tiles) * part_i / p.parts), tile1 = int(int64_t(tiles) * (part_i + 1) / p.parts);
       // ------------------------------------------------------------------ the stream
-      float m = -INFINITY, s = 0.f, lost = 0.f, best = -INFINITY;
+      float m = -INFINITY, s = 0.f, lost = 0.f, best = -INFINITY, second = -INFINITY;
       int best_tile = 0, bad = 0;
       auto inside = [&](int tile) {                      // every piece of the tile lies in the row
         return tile * BS_TILE_PIECES * P::kPer >= r.mis && (tile + 1) * BS_TILE_PIECES * P::kPer <= r.end;
@@ -226,6 +246,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
 #pragma unroll
         for (int i = 1; i < BS_PIECES; ++i) top = max_nan(top, P::largest(w[i]));
         if (!(top < INFINITY)) bad = 1;
+        second = fmaxf(second, fminf(top, best));
         if (top > best) {
           best = top;
           best_tile = tile;
@@ -285,20 +306,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       team_sync();
       if (top > -INFINITY && top < INFINITY && !(fabsf(top * p.k_hi) < BS_FAR)) {
         ref = top;
-        float v = 0.f;
-#pragma unroll 1
-        for (int tile = tile0; tile < tile1; ++tile) {
-          load(tile, next);
-#pragma unroll
-          for (int i = 0; i < BS_PIECES; ++i) {
-            float x[P::kPer];
-            P::get(next[i], x);
-#pragma unroll
-            for (int e = 0; e < P::kPer; ++e) v += exp2f((x[e] - ref) * p.k_hi);
-          }
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        const float v = far_sum(r, tile0, tile1, ref, p.k_hi, tid);
         if (lane == 0) {
           t.m[warp] = 0.f;
           t.sum[warp] = double(v);
@@ -311,36 +319,44 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         const float least_x = logit_of(least);
         const int least_tile = by_tile && least ? int(0xffffffffu - unsigned(least)) : 0;
         const bool look = mine != 0 && (by_tile ? mine >= least : best >= least_x);
-        const unsigned who = __ballot_sync(0xffffffffu, look);
-        if (look) t.flagged[warp][__popc(who & ((1u << lane) - 1u))] = tid;
-        __syncwarp();
-        const int per = (tile1 - tile0) * BS_PIECES, total = __popc(who) * per;
-        for (int at = 0; at < total; at += 128) {
-          uint4 w[4];
-          int piece[4];
+        // pass 0: threads of whose tiles one can hold something; pass 1: the others
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+          const unsigned who = __ballot_sync(0xffffffffu, look && (by_tile && least != 0 && second < least_x) == (pass == 0));
+          if (who == 0) continue;
+          if (who >> lane & 1u) t.flagged[warp][__popc(who & ((1u << lane) - 1u))] = make_int2(tid, pass == 0 ? best_tile : tile0);
+          __syncwarp();
+          const int per = pass == 0 ? BS_PIECES : (tile1 - tile0) * BS_PIECES, total = __popc(who) * per;
+#pragma unroll 1
+          for (int at = 0; at < total; at += 128) {
+            uint4 w[4];
+            int piece[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int i = at + 32 * u + lane, f = i / per, q = i - f * per;
-            piece[u] = i < total ? (tile0 + q / BS_PIECES) * BS_TILE_PIECES + (q % BS_PIECES) * BS_TEAM + t.flagged[warp][f] : -1;
-            if (piece[u] >= 0) w[u] = r.any(piece[u]);
-          }
+            for (int u = 0; u < 4; ++u) {
+              const int i = at + 32 * u + lane, f = min(i, total - 1) / per, q = i - f * per;
+              const int2 of = t.flagged[warp][f];
+              piece[u] = i < total ? (of.y + q / BS_PIECES) * BS_TILE_PIECES + (q % BS_PIECES) * BS_TEAM + of.x : -1;
+              if (piece[u] >= 0) w[u] = r.any(piece[u]);
+            }
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (piece[u] < 0) continue;
-            if (least != 0 && !(P::largest(w[u]) >= least_x)) continue;
-            float x[P::kPer];
-            P::get(w[u], x);
-            const int tile = piece[u] / BS_TILE_PIECES;
+            for (int u = 0; u < 4; ++u) {
+              if (piece[u] < 0) continue;
+              if (least != 0 && !(P::largest(w[u]) >= least_x)) continue;
+              float x[P::kPer];
+              P::get(w[u], x);
+              const int tile = piece[u] / BS_TILE_PIECES;
 #pragma unroll
-            for (int e = 0; e < P::kPer; ++e) {
-              const Key key = token_key(x[e], piece[u] * P::kPer + e - r.mis);
-              const bool in = x[e] > -INFINITY && (least == 0 || (by_tile ? x[e] > least_x || (x[e] == least_x && tile <= least_tile) : key >= least));
-              if (in) {
-                const int n = atomicAdd(&t.n_list, 1);
-                if (n < BS_LIST) t.list[n] = key;
+              for (int e = 0; e < P::kPer; ++e) {
+                const Key key = token_key(x[e], piece[u] * P::kPer + e - r.mis);
+                const bool in = x[e] > -INFINITY && (least == 0 || (by_tile ? x[e] > least_x || (x[e] == least_x && tile <= least_tile) : key >= least));
+                if (in) {
+                  const int n = atomicAdd(&t.n_list, 1);
+                  if (n < BS_LIST) t.list[n] = key;
+                }
               }
             }
           }
+          __syncwarp();
         }
         team_sync();
         const int n = t.n_list;
@@ -371,10 +387,8 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         double sum = 0.0;
         for (int w = 0; w < BS_WARPS; ++w)
           if (t.m[w] > -INFINITY) sum += t.sum[w] * double(exp2f(t.m[w] - top));
-        part.m = top;
-        part.ref = ref;
-        part.s = sum;
-        part.bad = t.bad;
+        const float hi = float(sum);
+        *reinterpret_cast<float4*>(&part) = make_float4(hi, float(sum - double(hi)), t.bad ? NAN : top, ref);
       }
     }
     __threadfence();
@@ -397,20 +411,24 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         double far = -INFINITY, s = 0.0;
         float m = -INFINITY, ref = 0.f;
         int bad = 0;
-        if (!over) {
-          for (int i = lane; i < p.parts; i += 32) {
-            const SelectPart& q = parts[size_t(row0 + b) * p.parts + i];
-            const float qm = __ldcg(&q.m), qr = __ldcg(&q.ref);
-            bad |= __ldcg(&q.bad);
-            if (qm > -INFINITY && p.k * double(qr) + double(qm) > far) {
-              far = p.k * double(qr) + double(qm);
-              m = qm;
-              ref = qr;
-            }
+        float4 q[BS_MAX_PARTS / 32];
+#pragma unroll
+        for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {
+          const int i = lane + 32 * u;
+          q[u] = !over && i < p.parts ? __ldcg(reinterpret_cast<const float4*>(&parts[size_t(row0 + b) * p.parts + i])) : make_float4(0.f, 0.f, -INFINITY, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {
+          bad |= q[u].z != q[u].z;
+          const double f = p.k * double(q[u].w) + double(q[u].z);
+          if (f > far) {
+            far = f;
+            m = q[u].z;
+            ref = q[u].w;
           }
         }
         bad = __any_sync(0xffffffffu, bad);
-#pragma unroll
+#pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) {
           const double of = __shfl_xor_sync(0xffffffffu, far, o);
           const float om = __shfl_xor_sync(0xffffffffu, m, o), other = __shfl_xor_sync(0xffffffffu, ref, o);
@@ -420,14 +438,11 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
             ref = other;
           }
         }
-        if (!over) {
-          for (int i = lane; i < p.parts; i += 32) {
-            const SelectPart& q = parts[size_t(row0 + b) * p.parts + i];
-            const float qm = __ldcg(&q.m);
-            if (qm > -INFINITY) s += __ldcg(&q.s) * exp2(p.k * (double(__ldcg(&q.ref)) - double(ref)) + (double(qm) - double(m)));
-          }
-        }
 #pragma unroll
+        for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {    // (references of parts near zero are whole numbers: their powers are exact)
+          if (q[u].z > -INFINITY) s += (double(q[u].x) + double(q[u].y)) * double(exp2f(float(p.k * (double(q[u].w) - double(ref)) + (double(q[u].z) - double(m)))));
+        }
+#pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (lane == 0) {
           const double lse = (double(m) + log2(s)) * 0.69314718055994530942;         // and scale ref
@@ -442,47 +457,51 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       team_sync();
       // Candidate c: beam, part and place in the part's keys.
       const int per_beam = p.parts * n_out, n_cand = a.n_beams * per_beam;
-      auto candidate = [&](int c, Key& rank, Key& flat, float& score) {
+      auto candidate = [&](int c) {                      // its rank key, 0: none; where it goes on from and what it is are asked for only when it is chosen
         const int b = c / per_beam, i = c - b * per_beam;
-        rank = 0;
-        double s;
+        double s = -INFINITY;
         if (t.state[b] == 2) {
-          if (i > 0) return;
-          s = double(t.base[b]);
-          flat = (Key(b) << 32) | unsigned(a.end_token);
+          if (i == 0) s = double(t.base[b]);
         } else {
           const Key k = t.state[b] == 1 ? __ldcg(&parts[size_t(row0 + b) * p.parts + i / n_out].keys[i % n_out]) : 0;
-          if (k == 0) return;
-          s = double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]);
-          flat = (Key(b) << 32) | unsigned(token_of(k));
+          if (k != 0) s = double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]);
         }
         const double ranked = double(t.weight[b]) * s;
-        if (!(ranked > -INFINITY)) return;
-        rank = order_of(ranked);
-        score = float(s);
+        return ranked > -INFINITY ? order_of(ranked) : Key(0);
       };
+      auto describe = [&](int c, Key& flat, float& score) {
+        const int b = c / per_beam, i = c - b * per_beam;
+        if (t.state[b] == 2) {
+          flat = (Key(b) << 32) | unsigned(a.end_token);
+          score = t.base[b];
+        } else {
+          const Key k = __ldcg(&parts[size_t(row0 + b) * p.parts + i / n_out].keys[i % n_out]);
+          flat = (Key(b) << 32) | unsigned(token_of(k));
+          score = float(double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]));
+        }
+      };
+      // Every part's keys fall.  With d = n_out / parts (up), each part's d-th key and the n_out / d-th largest (up) of those, there are n_out candidates from that one up: a
+      // bound.  What reaches it is found key by key; where there are many parts, in each from its first key on until one does not.
+      const int n_lists = a.n_beams * p.parts, depth = (n_out + n_lists - 1) / n_lists;
       Key top = 0;
-      for (int c = tid; c < n_cand; c += BS_TEAM) {
-        Key rank, flat;
-        float score;
-        candidate(c, rank, flat, score);
-        top = max(top, rank);
-      }
+#pragma unroll 1
+      for (int l = tid; l < n_lists; l += BS_TEAM) top = max(top, candidate(l * n_out + depth - 1));
       t.best[warp][lane] = top;
       team_sync();
-      if (warp == 0) find_bound(t, n_out, lane);
+      if (warp == 0) find_bound(t, (n_out + depth - 1) / depth, lane);
       team_sync();
       const Key least = t.bound;
-      for (int c = tid; c < n_cand; c += BS_TEAM) {
-        Key rank, flat;
-        float score;
-        candidate(c, rank, flat, score);
-        if (rank == 0 || rank < least) continue;
-        const int n = atomicAdd(&t.n_list, 1);
-        if (n < BS_LIST) {
+      const int run = n_cand <= 4 * BS_TEAM ? 1 : n_out;
+#pragma unroll 1
+      for (int c = tid * run; c < n_cand; c += BS_TEAM * run) {
+#pragma unroll 1
+        for (int k = 0; k < run; ++k) {
+          const Key rank = candidate(c + k);
+          if (rank == 0 || rank < least) break;
+          const int n = atomicAdd(&t.n_list, 1);
+          if (n >= BS_LIST) break;
           t.list[n] = rank;
-          t.flat[n] = flat;
-          t.score[n] = score;
+          describe(c + k, t.flat[n], t.score[n]);
         }
       }
       team_sync();
@@ -494,11 +513,14 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         for (; found < n_out; ++found) {
           Key rank_b = 0, flat_b = ~0ull;
           float score_b = 0.f;
+#pragma unroll 1
           for (int c = tid; c < n_cand; c += BS_TEAM) {
-            Key rank, flat;
+            const Key rank = candidate(c);
+            if (rank == 0 || rank > last_rank || rank < rank_b) continue;
+            Key flat;
             float score;
-            candidate(c, rank, flat, score);
-            if (rank == 0 || !(rank < last_rank || (rank == last_rank && flat > last_flat))) continue;
+            describe(c, flat, score);
+            if (rank == last_rank && flat <= last_flat) continue;
             if (rank > rank_b || (rank == rank_b && flat < flat_b)) {
               rank_b = rank;
               flat_b = flat;
@@ -598,21 +620,21 @@ cudaError_t launch_beam_select(const hs_beam_select_t& a, int sm_count, int sm_b
   if (double(p.k_hi) > k) p.k_hi = std::nextafterf(p.k_hi, 0.f);
   // (above zero, so that -infinity stays -infinity under both)
   p.k_lo = std::max(float(k - double(p.k_hi)), 1e-37f);
-  // Rows are cut into equal parts so that the teams' rounds are even and short; a round costs its tiles and about two more for the item's end.
+  // Rows are cut into equal parts so that the teams' rounds are even and short; a round costs its tiles and about BS_ITEM_COST more for the item's end.
   const int64_t rows = int64_t(a.n_requests) * a.n_beams;
   const int per = a.type == HS_TYPE_F32 ? 4 : 8, tiles = (a.vocab + per - 1 + BS_TILE_PIECES * per - 1) / (BS_TILE_PIECES * per);
   const int64_t teams = int64_t(share_count(sm_count)) * BS_TEAMS;
   int64_t least = -1;
   p.parts = 1;
   for (int parts = 1; parts <= std::min(tiles, BS_MAX_PARTS) && rows * parts <= std::max(rows, 4 * teams); ++parts) {
-    const int64_t cost = (rows * parts + teams - 1) / teams * ((tiles + parts - 1) / parts + 2);
+    const int64_t cost = (rows * parts + teams - 1) / teams * ((tiles + parts - 1) / parts + BS_ITEM_COST);
     if (least < 0 || cost < least) {
       least = cost;
       p.parts = parts;
     }
   }
   p.items = int(rows * p.parts);
-  const int grid = int(std::min<int64_t>(sm_budget, (p.items + BS_TEAMS - 1) / BS_TEAMS));
+  const int grid = int(std::min<int64_t>(sm_budget, p.items));
   return launch_step_kernel(pick(a.type), grid, BS_THREADS, kSelectSmem, stream, true, p);
 }
 
