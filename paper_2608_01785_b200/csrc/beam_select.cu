@@ -42,8 +42,9 @@ struct SelectParams {
   float k_hi, k_lo;                                      // k rounded towards zero, and what that leaves out (above zero)
 };
 struct alignas(16) SelectTeam {
-  Key best[BS_WARPS][32];
+  Key best[BS_TEAM];
   Key group[64];
+  int rank[64];
   Key list[BS_LIST], flat[BS_LIST];
   float score[BS_LIST];
   double sum[BS_WARPS], lse[HS_MAX_BEAMS];
@@ -167,29 +168,28 @@ __device__ __noinline__ float far_sum(const Row<TYPE>& r, int tile0, int tile1, 
   return v;
 }
 
-// The n-th largest of 64 groups' keys (each the larger of two threads'), by the team's first warp; 0 where fewer groups have one.
-__device__ __forceinline__ void find_bound(SelectTeam& t, int n, int lane) {
-  Key g[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    g[h] = max(t.best[2 * h][lane], t.best[2 * h + 1][lane]);
-    t.group[32 * h + lane] = g[h];
-  }
-  if (lane == 0) t.bound = 0;
-  __syncwarp();
-  int above[2] = {0, 0};
+// The n-th largest of 64 groups' keys (each the larger of two threads'), or 0 where fewer groups have one: t.bound, behind the next team_sync.  Called by the whole team
+// with a key of each thread.  A thread compares one group with half of the others.
+template <typename F>
+__device__ __forceinline__ void find_bound(SelectTeam& t, Key mine, int n, int tid, F team_sync) {
+  t.best[tid] = mine;
+  if (tid < 64) t.rank[tid] = 0;
+  if (tid == 0) t.bound = 0;
+  team_sync();
+  const int i = tid & 63, half = tid >> 6;
+  const Key g = max(t.best[i], t.best[i + 64]);
+  if (half == 0) t.group[i] = g;
+  team_sync();
+  int above = 0;
 #pragma unroll 4
-  for (int j = 0; j < 64; j += 2) {
+  for (int j = 32 * half; j < 32 * half + 32; j += 2) {
     const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&t.group[j]);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      above[h] += o.x > g[h] || (o.x == g[h] && j < 32 * h + lane) ? 1 : 0;
-      above[h] += o.y > g[h] || (o.y == g[h] && j + 1 < 32 * h + lane) ? 1 : 0;
-    }
+    above += o.x > g || (o.x == g && j < i) ? 1 : 0;
+    above += o.y > g || (o.y == g && j + 1 < i) ? 1 : 0;
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    if (above[h] == n - 1) t.bound = g[h];
+  atomicAdd(&t.rank[i], above);
+  team_sync();
+  if (half == 0 && t.rank[i] == n - 1) t.bound = g;
 }
 
 template <int TYPE>
@@ -206,16 +206,19 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
   SelectPart* parts = reinterpret_cast<SelectPart*>(static_cast<char*>(a.workspace) + kWsScratch);
   griddep_wait();
 
+  // Whether an item was a request's last one is known a while after its end: the choice is made behind the item that comes next.
   int item = team * int(gridDim.x) + int(blockIdx.x);    // (the first items on different SMs)
-  while (item < p.items) {
-    const int row = item / p.parts, part_i = item - row * p.parts;
-    const bool ended = a.done != nullptr && a.done[row] != 0;
+  if (tid == 0) t.last = -1;
+#pragma unroll 1
+  for (bool more = item < p.items; ; more = item < p.items) {
+    const int row = more ? item / p.parts : 0, part_i = item - row * p.parts;
+    const bool ended = !more || (a.done != nullptr && a.done[row] != 0);
     if (tid == 0) {
-      t.next = int(gridDim.x) * BS_TEAMS + atomicAdd(queue, 1);
+      if (more) t.next = int(gridDim.x) * BS_TEAMS + atomicAdd(queue, 1);
       t.n_list = 0;
       t.bad = 0;
     }
-    SelectPart& part = parts[item];
+    SelectPart& part = parts[more ? item : 0];
     if (!ended) {
       const Row<TYPE> r(a, row);
       const int tiles = r.tiles(), tile0 = int(int64_t(tiles) * part_i / p.parts), tile1 = int(int64_t(tiles) * (part_i + 1) / p.parts);
@@ -296,10 +299,8 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         }
       }
       const Key mine = best > -INFINITY ? (Key(order_of(best)) << 32) | (0xffffffffu - unsigned(best_tile)) : 0ull;
-      t.best[warp][lane] = mine;
-      team_sync();
+      find_bound(t, mine, n_out, tid, team_sync);
       if (bad) t.bad = 1;
-      if (warp == 0) find_bound(t, n_out, lane);
       float top = t.top[0], ref = 0.f;
 #pragma unroll
       for (int w = 1; w < BS_WARPS; ++w) top = fmaxf(top, t.top[w]);
@@ -391,18 +392,24 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         *reinterpret_cast<float4*>(&part) = make_float4(hi, float(sum - double(hi)), t.bad ? NAN : top, ref);
       }
     }
-    __threadfence();
     team_sync();
-    const int request = row / a.n_beams;
+    const int request = t.last, next = t.next;           // (of the item before, and the one behind this)
+    team_sync();
     if (tid == 0) {
-      const int all = a.n_beams * p.parts;
-      t.last = atomicAdd(done_words + request, 1) == all - 1;
-      if (t.last) done_words[request] = 0;               // ready for the next call
+      t.last = -1;
       t.n_list = 0;
+      if (more) {
+        __threadfence();                                 // (of the whole team's part, which the barrier has brought here)
+        const int mine = row / a.n_beams, all = a.n_beams * p.parts;
+        if (atomicAdd(done_words + mine, 1) == all - 1) {
+          done_words[mine] = 0;                          // ready for the next call
+          t.last = mine;
+        }
+      }
     }
-    team_sync();
-    if (t.last) {
+    if (request >= 0) {
       // -------------------------------------------------------------------- the request's choice
+      team_sync();
       __threadfence();
       const int row0 = request * a.n_beams;
       for (int b = warp; b < a.n_beams; b += BS_WARPS) {
@@ -486,9 +493,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       Key top = 0;
 #pragma unroll 1
       for (int l = tid; l < n_lists; l += BS_TEAM) top = max(top, candidate(l * n_out + depth - 1));
-      t.best[warp][lane] = top;
-      team_sync();
-      if (warp == 0) find_bound(t, (n_out + depth - 1) / depth, lane);
+      find_bound(t, top, (n_out + depth - 1) / depth, tid, team_sync);
       team_sync();
       const Key least = t.bound;
       const int run = n_cand <= 4 * BS_TEAM ? 1 : n_out;
@@ -575,9 +580,13 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         put(above, t.score[i], row0 + b, token, t.state[b] == 2 || token == a.end_token ? 1 : 0);
       }
       if (tid >= n && tid < n_out) put(tid, -INFINITY, -1, -1, 0);
+      team_sync();                                       // (everybody has read what the next item writes over)
     }
-    item = t.next;
-    team_sync();                                         // (everybody has read what the next item writes over)
+    if (!more) {
+      team_sync();
+      if (request < 0 && t.last < 0) break;
+    }
+    if (more) item = next;
   }
   __syncthreads();
   // the last block to leave puts the queue back to zero
