@@ -22,37 +22,61 @@ namespace hs {
 namespace {
 
 constexpr int SP_THREADS = 1024, SP_PER_THREAD = HS_DEVICE_MAX_SEQS / SP_THREADS;
-constexpr int SP_COLUMNS = 8, SP_RUN = 32;               // columns of a block's slice; rows whose counts are added up before they go to memory
-constexpr int SP_FORK_SMEM = HS_DEVICE_MAX_SEQS * (4 * 4 + SP_COLUMNS * 4);
+constexpr int SP_COLUMNS = 8;                            // columns of a block's slice
+constexpr int SP_FORK_SMEM = HS_DEVICE_MAX_SEQS * (6 * 4 + SP_COLUMNS * 4);
 static_assert(SP_FORK_SMEM <= 227 * 1024, "fits one SM");
 static_assert(HS_BEAMS_MAX_PAGES % 32 == 0 && HS_COMPACT_MAX_PAGES <= HS_BEAMS_MAX_PAGES, "a bit per page");
 
 __device__ __forceinline__ unsigned* page_bits(void* workspace) { return reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kWsPageBits); }
 __device__ __forceinline__ int owned_pages(int ctx) { return (ctx + HS_PAGE_SIZE - 1) / HS_PAGE_SIZE; }
 
+// Where a block has column c of its slice of row i: a column of 32 rows and all columns of four rows both touch every bank once.
+__device__ __forceinline__ int entry_of(int i, int c) { return i * SP_COLUMNS + (c ^ (i >> 2 & (SP_COLUMNS - 1))); }
+
 __global__ void __launch_bounds__(SP_THREADS, 1) fork_pages_kernel(const hs_fork_pages_t a) {
   extern __shared__ int smem[];
   __shared__ unsigned long long warp_sums[32];
-  __shared__ int most;
+  __shared__ int most, ended;
   griddep_wait();
-  const int n = a.n_rows, tid = threadIdx.x;
+  const int n = a.n_rows, tid = threadIdx.x, lane = tid & 31, width = a.max_pages_per_seq;
   int* ctx = smem;                                       // [n] each, as they were
-  int* children = smem + n;
-  int* first = smem + 2 * n;                             // successor
-  int* place = smem + 3 * n;                             // of the row's copy among the copies, -1: none
-  int* slice = smem + 4 * n;                             // [n][SP_COLUMNS]
+  int* parent = smem + n;
+  int* children = smem + 2 * n;
+  int* first = smem + 3 * n;                             // successor
+  int* place = smem + 4 * n;                             // of the row's copy among the copies, -1: none
+  int* target = smem + 5 * n;                            // and its page
+  int* slice = smem + 6 * n;                             // [n][SP_COLUMNS]
+  // Everything that needs no other answer is asked for at once: counts, lengths, parents, and the first columns whether rows own them or not.
+  auto load_slice = [&](int c0) {
+#pragma unroll 4
+    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
+      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS;
+      slice[entry_of(i, x % SP_COLUMNS)] = c < width ? a.block_tables[int64_t(i) * width + c] : -1;
+    }
+  };
+  const int free_count = *a.free_count;
+  int lengths[SP_PER_THREAD], parents[SP_PER_THREAD];
+#pragma unroll
+  for (int u = 0; u < SP_PER_THREAD; ++u) {
+    const int i = tid + u * SP_THREADS;
+    lengths[u] = i < n ? a.ctx_len[i] : 0;
+    parents[u] = i < n ? a.parent[i] : -1;
+  }
+  load_slice(int(blockIdx.x) * SP_COLUMNS);
   if (tid == 0) most = 0;
   for (int i = tid; i < n; i += SP_THREADS) {
     children[i] = 0;
     first[i] = n;
   }
   __syncthreads();
-  const int free_count = *a.free_count;
   int wrong = 0;
-  for (int i = tid; i < n; i += SP_THREADS) {
-    const int c = a.ctx_len[i], p = a.parent[i];
-    if (c < 0 || c > row_tokens(a.max_pages_per_seq) || p < -1 || p >= n) wrong = 1;
+#pragma unroll
+  for (int u = 0; u < SP_PER_THREAD; ++u) {
+    const int i = tid + u * SP_THREADS, c = lengths[u], p = parents[u];
+    if (i >= n) continue;
+    if (c < 0 || c > row_tokens(width) || p < -1 || p >= n) wrong = 1;
     ctx[i] = c;
+    parent[i] = p;
     if (p >= 0 && p < n) {
       atomicAdd(&children[p], 1);
       atomicMin(&first[p], i);
@@ -66,20 +90,12 @@ __global__ void __launch_bounds__(SP_THREADS, 1) fork_pages_kernel(const hs_fork
     for (int u = 0; u < SP_PER_THREAD; ++u) {
       const int i = tid * SP_PER_THREAD + u;
       if (i >= n) continue;
-      const int p = a.parent[i];
+      const int p = parent[i];
       place[i] = p >= 0 && ctx[p] % HS_PAGE_SIZE != 0 && first[p] != i ? 0 : -1;
       mine += place[i] == 0 ? 1 : 0;
     }
   }
   unsigned long long at = block_scan(mine, warp_sums, n_copies);
-  if (!wrong) {
-#pragma unroll
-    for (int u = 0; u < SP_PER_THREAD; ++u) {
-      const int i = tid * SP_PER_THREAD + u;
-      if (i < n && place[i] == 0) place[i] = int(at++);
-    }
-  }
-  __syncthreads();
   const int error = wrong || free_count < 0 || free_count > a.num_pages ? kErrInvalidArg : int(n_copies) > free_count ? kErrOutOfPages : 0;
   if (error) {
     for (int i = int(blockIdx.x) * SP_THREADS + tid; i < n; i += int(gridDim.x) * SP_THREADS) {
@@ -89,96 +105,130 @@ __global__ void __launch_bounds__(SP_THREADS, 1) fork_pages_kernel(const hs_fork
     if (blockIdx.x == 0 && tid == 0) atomicExch(a.status, error);
     return;
   }
-  if (blockIdx.x == 0) {
-    for (int i = tid; i < n; i += SP_THREADS) {
-      if (place[i] >= 0) continue;
+#pragma unroll
+  for (int u = 0; u < SP_PER_THREAD; ++u) {
+    const int i = tid * SP_PER_THREAD + u;
+    if (i >= n) continue;
+    if (place[i] == 0) {
+      target[i] = a.free_list[free_count - 1 - int(at)];
+      place[i] = int(at++);
+    } else if (blockIdx.x == 0) {
       a.copy_src[i] = a.copy_dst[i] = -1;
       a.copy_len[i] = 0;
     }
   }
 
   unsigned* bits = page_bits(a.workspace);
-  int* words = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsTables);        // blocks that are done; whether a page was freed
+  int* word = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsTables);         // blocks that are done, and in its upper half those that freed a page
   bool bad_page = false, freed = false;
   auto inside = [&](int page) { return page >= 0 && page < a.num_pages; };
   for (int c0 = int(blockIdx.x) * SP_COLUMNS; c0 < most; c0 += int(gridDim.x) * SP_COLUMNS) {
-    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
-      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS;
-      slice[x] = c < owned_pages(ctx[i]) ? a.block_tables[int64_t(i) * a.max_pages_per_seq + c] : -1;
-    }
+    if (c0 >= int(gridDim.x) * SP_COLUMNS) load_slice(c0);
+    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS)               // (a thread's own entries)
+      if (c0 + x % SP_COLUMNS >= owned_pages(ctx[x / SP_COLUMNS])) slice[entry_of(x / SP_COLUMNS, x % SP_COLUMNS)] = -1;
     __syncthreads();
-    // holders that full pages gain and lose; a last page that is not full is lost by a row that nobody continues
-    auto change = [&](int i, int c) { return c < ctx[i] / HS_PAGE_SIZE ? children[i] - 1 : children[i] == 0 ? -1 : 0; };
-    for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
-      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS;
-      if (c >= owned_pages(ctx[i])) continue;
-      const int page = slice[x];
-      if (!inside(page)) {
-        bad_page = true;
-        continue;
+    // A warp takes a column of 32 rows; the first of neighbours with the same page adds for all of them: a difference of running sums.
+    // (Four of them at a time, so that the counts' answers are waited for once.)
+    for (int x0 = tid >> 5; x0 < (n + 31) / 32 * SP_COLUMNS; x0 += 4 * (SP_THREADS / 32)) {
+      int pages[4], by[4], was[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int x = x0 + u * (SP_THREADS / 32), i = x / SP_COLUMNS * 32 + lane, c = c0 + x % SP_COLUMNS;
+        const bool owned = i < n && c < owned_pages(ctx[i]);
+        const int page = i < n ? slice[entry_of(i, x % SP_COLUMNS)] : -1;             // (entries that a row does not own are -1 here)
+        bad_page |= owned && !inside(page);
+        // holders that full pages gain and lose; a last page that is not full is lost by a row that nobody continues
+        int sum = !owned ? 0 : c < ctx[i] / HS_PAGE_SIZE ? children[i] - 1 : children[i] == 0 ? -1 : 0;
+        const int mine = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          sum += lane >= o ? y : 0;
+        }
+        const int before = __shfl_up_sync(0xffffffffu, page, 1);
+        const bool leads = lane == 0 || page != before;
+        const unsigned behind = __ballot_sync(0xffffffffu, leads) & (0xfffffffeu << lane);
+        const int run = __shfl_sync(0xffffffffu, sum, behind ? __ffs(behind) - 2 : 31) - (sum - mine);
+        pages[u] = page;
+        by[u] = leads && inside(page) ? run : 0;
       }
-      auto same = [&](int j) { return slice[j * SP_COLUMNS + x % SP_COLUMNS] == page; };
-      if (i % SP_RUN != 0 && same(i - 1)) continue;      // (entries that a row does not own are -1 here)
-      int by = change(i, c);
-      for (int j = i + 1; j < n && j % SP_RUN != 0 && same(j); ++j) by += change(j, c);
-      if (by == 0) continue;
-      const int was = atomicAdd(&a.shares[page], by);
-      if (was >= 0 && was + by < 0) {
-        atomicOr(&bits[page >> 5], 1u << (page & 31));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) was[u] = by[u] != 0 ? atomicAdd(&a.shares[pages[u]], by[u]) : -1;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (was[u] < 0 || was[u] + by[u] >= 0) continue;
+        atomicOr(&bits[pages[u] >> 5], 1u << (pages[u] & 31));
         freed = true;
       }
     }
     for (int x = tid; x < n * SP_COLUMNS; x += SP_THREADS) {
-      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS, p = a.parent[i];
-      int32_t* entry = a.block_tables + int64_t(i) * a.max_pages_per_seq + c;
+      const int i = x / SP_COLUMNS, c = c0 + x % SP_COLUMNS, p = parent[i];
+      int32_t* entry = a.block_tables + int64_t(i) * width + c;
       if (p < 0 || c >= owned_pages(ctx[p])) {
         if (c < owned_pages(ctx[i])) *entry = -1;
         continue;
       }
-      int page = slice[p * SP_COLUMNS + x % SP_COLUMNS];
+      int page = slice[entry_of(p, x % SP_COLUMNS)];
       if (place[i] >= 0 && c == ctx[p] / HS_PAGE_SIZE) {
         const int from = page;
-        page = a.free_list[free_count - 1 - place[i]];
+        page = target[i];
         const bool ok = inside(from) && inside(page);
         bad_page |= !ok;
         a.copy_src[i] = ok ? from : -1;
         a.copy_dst[i] = ok ? page : -1;
         a.copy_len[i] = ok ? ctx[p] % HS_PAGE_SIZE : 0;
       }
-      *entry = page;
+      if (page != slice[entry_of(i, x % SP_COLUMNS)] || page == -1) *entry = page;
     }
     __syncthreads();
   }
   if (bad_page) atomicExch(a.status, kErrBadBlockTable);
-  if (freed) atomicExch(words + 1, 1);
-  if (!last_block(words)) return;
+  const int any = __syncthreads_or(freed);
+  if (tid == 0) {
+    __threadfence();
+    const int now = atomicAdd(word, any ? 0x10001 : 1) + (any ? 0x10001 : 1);
+    ended = (now & 0xffff) == int(gridDim.x) ? now : 0;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!ended) return;
   for (int i = tid; i < n; i += SP_THREADS) {
-    const int p = a.parent[i];
+    const int p = parent[i];
     a.ctx_len[i] = p >= 0 ? ctx[p] : 0;
   }
   int top = free_count - int(n_copies);
-  if (__ldcg(words + 1) != 0) {
-    // freed pages in rising order, a run of words a thread
-    const int n_words = (a.num_pages + 31) / 32, per = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per, n_words), w1 = min(w0 + per, n_words);
-    unsigned long long count = 0, total = 0;
-    for (int w = w0; w < w1; ++w) count += __popc(__ldcg(bits + w));
-    __syncthreads();                                     // (warp_sums)
-    int to = top + int(block_scan(count, warp_sums, total));
-    for (int w = w0; w < w1; ++w) {
-      unsigned left = __ldcg(bits + w);
-      if (left == 0) continue;
-      bits[w] = 0;                                       // ready for the next call
-      for (; left; left &= left - 1) {
-        const int page = w * 32 + __ffs(left) - 1;
-        a.shares[page] = 0;
-        if (to < a.num_pages) a.free_list[to] = page;
-        ++to;
+  if (ended >> 16) {
+    // freed pages in rising order, four words a thread
+    const int n_words = (a.num_pages + 31) / 32;
+    uint4* words = reinterpret_cast<uint4*>(bits);
+    for (int w0 = 0; w0 < n_words; w0 += 4 * SP_THREADS) {
+      const int at = w0 / 4 + tid;
+      const uint4 q = 4 * at < n_words ? __ldcg(words + at) : make_uint4(0, 0, 0, 0);
+      const unsigned long long count = __popc(q.x) + __popc(q.y) + __popc(q.z) + __popc(q.w);
+      unsigned long long total;
+      int to = top + int(block_scan(count, warp_sums, total));
+      if (count > 0) {
+        words[at] = make_uint4(0, 0, 0, 0);              // ready for the next call
+        const unsigned left4[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          for (unsigned left = left4[e]; left; left &= left - 1) {
+            const int page = (4 * at + e) * 32 + __ffs(left) - 1;
+            a.shares[page] = 0;
+            if (to < a.num_pages) a.free_list[to] = page;
+            ++to;
+          }
+        }
       }
+      top += int(total);
+      __syncthreads();                                   // (warp_sums)
     }
-    top = min(top + int(total), a.num_pages);
-    if (tid == 0) words[1] = 0;
+    top = min(top, a.num_pages);
   }
-  if (tid == 0) *a.free_count = top;
+  if (tid == 0) {
+    *a.free_count = top;
+    *word = 0;                                           // ready for the next call
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------ copies
@@ -259,23 +309,27 @@ __global__ void __launch_bounds__(SP_THREADS, 1) compact_number_kernel(const hs_
   block_scan(before, warp_sums, before);
   if (tid == 0) all = before;
   __syncthreads();
-  const int per = (b1 - b0 + SP_THREADS - 1) / SP_THREADS, w0 = min(b0 + tid * per, b1), w1 = min(w0 + per, b1);
+  // a warp a run of words, a lane a page of each
+  const int lane = tid & 31, per = (b1 - b0 + 31) / 32, w0 = min(b0 + (tid >> 5) * per, b1), w1 = min(w0 + per, b1);
   unsigned long long mine = 0, total = 0;
-  int free_high = 0;
-  for (int w = w0; w < w1; ++w) mine += counts(__ldcg(bits + w), w);
-  unsigned long long at = all + block_scan(mine, warp_sums, total);
+  for (int w = w0 + lane; w < w1; w += 32) mine += counts(__ldcg(bits + w), w);
+  const unsigned long long at = __shfl_sync(0xffffffffu, all + block_scan(mine, warp_sums, total), 0);
   int low = int(at >> 32), number = int(unsigned(at));
   int *targets = targets_of(a), *numbers = numbers_of(a), *sources = sources_of(a);
+  const unsigned in_front = (1u << lane) - 1u;
+#pragma unroll 2
   for (int w = w0; w < w1; ++w) {
-    const unsigned free = __ldcg(bits + w);
-    for (unsigned left = free & below(w); left; left &= left - 1) targets[low++] = w * 32 + __ffs(left) - 1;
-    for (unsigned left = ~below(w) & exists(w); left; left &= left - 1) {
-      const int bit = __ffs(left) - 1, page = w * 32 + bit;
-      const bool used = !(free >> bit & 1u);
-      free_high += used ? 0 : 1;
-      numbers[page - keep] = used ? number : -1;
-      if (used) sources[number++] = page;
+    const unsigned free = __ldcg(bits + w), free_low = free & below(w), high = ~below(w) & exists(w), used = high & ~free;
+    const int page = w * 32 + lane;
+    if (free_low >> lane & 1u) targets[low + __popc(free_low & in_front)] = page;
+    if (high >> lane & 1u) {
+      const int n = number + __popc(used & in_front);
+      const bool moves = used >> lane & 1u;
+      numbers[page - keep] = moves ? n : -1;
+      if (moves) sources[n] = page;
     }
+    low += __popc(free_low);
+    number += __popc(used);
   }
   Compaction* plan = plan_of(a);
   if (int(blockIdx.x) == (n_words - 1) / per_block && tid == 0) {
@@ -346,7 +400,7 @@ cudaError_t shared_pages_set_attributes() {
 }
 
 cudaError_t launch_fork_pages(const hs_fork_pages_t& a, int sm_budget, cudaStream_t stream) {
-  const int smem = std::max(a.n_rows * (4 * 4 + SP_COLUMNS * 4), kMinSmemBytes);
+  const int smem = std::max(a.n_rows * (6 * 4 + SP_COLUMNS * 4), kMinSmemBytes);
   return launch_step_kernel(fork_pages_kernel, grid_for(a.max_pages_per_seq, SP_COLUMNS, sm_budget), SP_THREADS, smem, stream, true, a);
 }
 
