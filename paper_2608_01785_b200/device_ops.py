@@ -18,6 +18,7 @@ WORKSPACE_BYTES = 32 << 20
 MAX_SEQS = 4096
 MAX_ALTERNATIVES = 32
 MAX_BEAMS = 32
+MAX_SHARED_SEQS = 2048
 PAGE = 16
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = range(4)
 EXPORTS = ("hs_op_step_tables", "hs_op_release_pages", "hs_op_rope_table", "hs_op_rope_cache", "hs_op_paged_attention", "hs_op_token_logprobs")
