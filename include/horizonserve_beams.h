@@ -38,6 +38,7 @@ extern "C" {
  * continuation, itself:  s = S_b,  v = end_token.  Continuations are ranked by weight[r][b] s (by s without weights), the largest first,
  * ties to the lower beam and then to the lower token, and the first n_out of them are written:
  *     out_score = s,   out_parent = r n_beams + b,   out_token = v,   out_done = whether the beam was done or v is end_token
+ * A weight that is not above zero gives its beam no continuation, with the status INVALID_ARG; a call of such weights is done otherwise.
  * A weighted score of -infinity or NaN is no continuation: tokens and beams at -infinity are left out, and so is a beam whose row holds NaN or +infinity or
  * nothing above -infinity.  Where there are fewer than n_out, the rest have score -infinity, parent and token -1 and done 0.
  * lse[r n_beams + b] = L (0 for a beam that is done, whose logits are not read; NaN where the row holds NaN or +infinity).
@@ -54,7 +55,7 @@ typedef struct {
   int64_t row_stride;
   const float *scores;                /* device [n_requests, n_beams] */
   const int32_t *done;                /* device [n_requests, n_beams], or NULL */
-  const float *weight;                /* device [n_requests, n_beams], or NULL */
+  const float *weight;                /* device [n_requests, n_beams], above zero, or NULL */
   float scale;                        /* > 0: the inverse temperature */
   float *out_score;                   /* device [n_requests, n_out] */
   int32_t *out_parent, *out_token;    /* device [n_requests, n_out] */

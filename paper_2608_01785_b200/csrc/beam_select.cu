@@ -9,10 +9,10 @@
 //               powers of two.  k is the sum of two fp32 numbers, and a tile's sum is added with its rounding error kept, so that log s is good to about 1e-7.
 //               (A part whose largest logit is 2^20 of those units from zero, as in a row masked with its type's lowest number from end to end, is
 //               summed a second time with that logit as its reference.)
-//   best, tile  its largest logit, and the first tile that has it; second, the largest of its other tiles.
+//   best, tile  its largest logit, and the first tile that has it; second, with its tile, the largest of its other tiles, third of those that are left.
 // At an item's end the n_out-th largest of 64 groups of two threads' (best, tile) bounds its n_out largest logits from below: only threads whose
-// own pair reaches it can hold one, a few of 128, and the team looks through that tile's pieces once more (the L2 has them; through all of a thread's, where its second
-// reaches the bound, too), lists what reaches the bound and ranks the list.  The main loop carries no list and no test per element for it.
+// own pair reaches it can hold one, a few of 128, and the team looks through that tile's pieces once more, or through the first two tiles', or, where third reaches the bound
+// as well, all of a thread's (the L2 has them); it lists what reaches the bound and ranks the list.  The main loop carries no list and no test per element for it.
 // The team that delivers a request's last item makes the choice: L_b from the parts, candidates' scores in 64 bits, the same bound, list and ranks.
 #include <algorithm>
 
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int BS_TEAMS = 4, BS_TEAM = 128, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
 constexpr int BS_PIECES = 8, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
+constexpr int BS_AHEAD = 2;                                              // tiles that are on their way to L2 before they are loaded
 constexpr int BS_LIST = 512;                                             // candidates that a team ranks at a time
 constexpr int BS_ITEM_COST = 3;                                          // tiles
 constexpr int BS_MAX_PARTS = 64;                                         // of a row
@@ -38,6 +39,7 @@ struct alignas(16) SelectPart {                          // of a row, in the wor
 struct SelectParams {
   hs_beam_select_t a;
   int parts, items;                                      // of a row; of all rows
+  int lanes;                                             // the power of two from parts on, at most 32
   double k;                                              // scale log2(e)
   float k_hi, k_lo;                                      // k rounded towards zero, and what that leaves out (above zero)
 };
@@ -51,7 +53,7 @@ struct alignas(16) SelectTeam {
   float m[BS_WARPS], top[BS_WARPS], base[HS_MAX_BEAMS], weight[HS_MAX_BEAMS], ref[HS_MAX_BEAMS];
   int state[HS_MAX_BEAMS];                               // of a beam: 0: no continuation, 1: in use, 2: done
   Key bound;
-  int2 flagged[BS_WARPS][32];                            // threads, and the tile that is to be looked at
+  int2 flagged[BS_WARPS][64];                            // threads, and a tile that is to be looked at
   int n_list, bad, next, last;
 };
 
@@ -142,6 +144,11 @@ struct Row {
     asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(base + int64_t(piece) * 16));
     return v;
   }
+  // A tile's way from memory to L2, a line a thread.
+  __device__ __forceinline__ void ahead(int tile, int tid) const {
+    const int piece = tile * BS_TILE_PIECES + tid * (BS_TILE_PIECES / BS_TEAM);
+    if (piece * P::kPer < end) asm volatile("prefetch.global.L2 [%0];" ::"l"(base + int64_t(piece) * 16));
+  }
   // Any piece: what lies outside the row is -infinity.
   __device__ __forceinline__ uint4 any(int piece) const {
     const int e0 = piece * P::kPer;
@@ -223,8 +230,8 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       const Row<TYPE> r(a, row);
       const int tiles = r.tiles(), tile0 = int(int64_t(tiles) * part_i / p.parts), tile1 = int(int64_t(tiles) * (part_i + 1) / p.parts);
       // ------------------------------------------------------------------ the stream
-      float m = -INFINITY, s = 0.f, lost = 0.f, best = -INFINITY, second = -INFINITY;
-      int best_tile = 0, bad = 0;
+      float m = -INFINITY, s = 0.f, lost = 0.f, best = -INFINITY, second = -INFINITY, third = -INFINITY;   // (of the tiles' largest)
+      int best_tile = 0, second_tile = 0, bad = 0;
       auto inside = [&](int tile) {                      // every piece of the tile lies in the row
         return tile * BS_TILE_PIECES * P::kPer >= r.mis && (tile + 1) * BS_TILE_PIECES * P::kPer <= r.end;
       };
@@ -240,16 +247,26 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       uint4 next[BS_PIECES];
       if (tile0 < tile1) load(tile0, next);
 #pragma unroll 1
+      for (int tile = tile0 + 1; tile < min(tile0 + BS_AHEAD, tile1); ++tile) r.ahead(tile, tid);
+#pragma unroll 1
       for (int tile = tile0; tile < tile1; ++tile) {
         uint4 w[BS_PIECES];
 #pragma unroll
         for (int i = 0; i < BS_PIECES; ++i) w[i] = next[i];
         if (tile + 1 < tile1) load(tile + 1, next);
+        if (tile + BS_AHEAD < tile1) r.ahead(tile + BS_AHEAD, tid);
         float top = P::largest(w[0]);
 #pragma unroll
         for (int i = 1; i < BS_PIECES; ++i) top = max_nan(top, P::largest(w[i]));
         if (!(top < INFINITY)) bad = 1;
-        second = fmaxf(second, fminf(top, best));
+        if (top > second) {
+          third = second;
+          const bool first = top > best;
+          second = first ? best : top;
+          second_tile = first ? best_tile : tile;
+        } else {
+          third = fmaxf(third, top);
+        }
         if (top > best) {
           best = top;
           best_tile = tile;
@@ -320,14 +337,17 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         const float least_x = logit_of(least);
         const int least_tile = by_tile && least ? int(0xffffffffu - unsigned(least)) : 0;
         const bool look = mine != 0 && (by_tile ? mine >= least : best >= least_x);
-        // pass 0: threads of whose tiles one can hold something; pass 1: the others
+        // pass 0: one or two tiles of the threads that have no more to show; pass 1: all of the others'
+        const int tiles_of = !look ? 0 : least == 0 ? 3 : second < least_x ? 1 : third < least_x ? 2 : 3;
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
-          const unsigned who = __ballot_sync(0xffffffffu, look && (by_tile && least != 0 && second < least_x) == (pass == 0));
+          const unsigned who = __ballot_sync(0xffffffffu, pass == 0 ? tiles_of == 1 || tiles_of == 2 : tiles_of == 3);
+          const unsigned twice = pass == 0 ? __ballot_sync(0xffffffffu, tiles_of == 2) : 0u;
           if (who == 0) continue;
           if (who >> lane & 1u) t.flagged[warp][__popc(who & ((1u << lane) - 1u))] = make_int2(tid, pass == 0 ? best_tile : tile0);
+          if (twice >> lane & 1u) t.flagged[warp][__popc(who) + __popc(twice & ((1u << lane) - 1u))] = make_int2(tid, second_tile);
           __syncwarp();
-          const int per = pass == 0 ? BS_PIECES : (tile1 - tile0) * BS_PIECES, total = __popc(who) * per;
+          const int per = pass == 0 ? BS_PIECES : (tile1 - tile0) * BS_PIECES, total = (__popc(who) + __popc(twice)) * per;
 #pragma unroll 1
           for (int at = 0; at < total; at += 128) {
             uint4 w[4];
@@ -404,112 +424,179 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         if (atomicAdd(done_words + mine, 1) == all - 1) {
           done_words[mine] = 0;                          // ready for the next call
           t.last = mine;
+          __threadfence();                               // (of the others' parts, for the whole team behind the next barrier)
         }
       }
     }
     if (request >= 0) {
       // -------------------------------------------------------------------- the request's choice
-      team_sync();
-      __threadfence();
-      const int row0 = request * a.n_beams;
-      for (int b = warp; b < a.n_beams; b += BS_WARPS) {
-        const bool over = a.done != nullptr && a.done[row0 + b] != 0;
-        // (parts of a row may have different references: how far they are apart is worked out in 64 bits)
-        double far = -INFINITY, s = 0.0;
+      // Candidates: every part's keys, largest first, a list each.  The first keys that a thread looks at are on their way while the beams' sums are put together.
+      const int row0 = request * a.n_beams, n_lists = a.n_beams * p.parts, n_cand = n_lists * n_out, depth = (n_out + n_lists - 1) / n_lists;
+      const SelectPart* lists = parts + size_t(row0) * p.parts;
+      const bool few = n_cand <= BS_TEAM;                // all of them go into the list
+      Key early[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int l = few ? tid / n_out : tid + u * BS_TEAM, k = few ? tid - l * n_out : depth - 1;
+        early[u] = l < n_lists && (!few || u == 0) ? __ldcg(&lists[l].keys[k]) : 0;
+      }
+      // p.lanes lanes a beam: the powers of two of its parts
+#pragma unroll 1
+      for (int b0 = 0; b0 < a.n_beams; b0 += BS_TEAM / p.lanes) {
+        const int b = b0 + tid / p.lanes, at = tid & (p.lanes - 1);
+        const bool valid = b < a.n_beams, over = !valid || (a.done != nullptr && a.done[row0 + b] != 0);
+        const float base = valid ? a.scores[row0 + b] : 0.f, weight = valid && a.weight ? a.weight[row0 + b] : 1.f;
+        double s = 0.0;
         float m = -INFINITY, ref = 0.f;
-        int bad = 0;
+        int bad = 0, distant = 0;
         float4 q[BS_MAX_PARTS / 32];
 #pragma unroll
         for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {
-          const int i = lane + 32 * u;
-          q[u] = !over && i < p.parts ? __ldcg(reinterpret_cast<const float4*>(&parts[size_t(row0 + b) * p.parts + i])) : make_float4(0.f, 0.f, -INFINITY, 0.f);
+          const int i = at + 32 * u;
+          q[u] = !over && i < p.parts ? __ldcg(reinterpret_cast<const float4*>(&lists[b * p.parts + i])) : make_float4(0.f, 0.f, -INFINITY, 0.f);
         }
 #pragma unroll
         for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {
-          bad |= q[u].z != q[u].z;
-          const double f = p.k * double(q[u].w) + double(q[u].z);
-          if (f > far) {
-            far = f;
-            m = q[u].z;
-            ref = q[u].w;
-          }
+          bad |= q[u].z != q[u].z ? 1 : 0;
+          distant |= q[u].w != 0.f ? 1 : 0;
+          m = fmaxf(m, q[u].z);
         }
-        bad = __any_sync(0xffffffffu, bad);
-#pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) {
-          const double of = __shfl_xor_sync(0xffffffffu, far, o);
-          const float om = __shfl_xor_sync(0xffffffffu, m, o), other = __shfl_xor_sync(0xffffffffu, ref, o);
-          if (of > far || (of == far && (om > m || (om == m && other > ref)))) {
-            far = of;
-            m = om;
-            ref = other;
+        if (__any_sync(0xffffffffu, distant)) {
+          // (parts of a row may have different references: how far they are apart is worked out in 64 bits)
+          double far = -INFINITY;
+          m = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {
+            const double f = p.k * double(q[u].w) + double(q[u].z);
+            if (f > far) {
+              far = f;
+              m = q[u].z;
+              ref = q[u].w;
+            }
           }
+#pragma unroll 1
+          for (int o = p.lanes >> 1; o > 0; o >>= 1) {
+            const double of = __shfl_xor_sync(0xffffffffu, far, o);
+            const float om = __shfl_xor_sync(0xffffffffu, m, o), other = __shfl_xor_sync(0xffffffffu, ref, o);
+            if (of > far || (of == far && (om > m || (om == m && other > ref)))) {
+              far = of;
+              m = om;
+              ref = other;
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int o = p.lanes >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         }
 #pragma unroll
         for (int u = 0; u < BS_MAX_PARTS / 32; ++u) {    // (references of parts near zero are whole numbers: their powers are exact)
           if (q[u].z > -INFINITY) s += (double(q[u].x) + double(q[u].y)) * double(exp2f(float(p.k * (double(q[u].w) - double(ref)) + (double(q[u].z) - double(m)))));
         }
 #pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0) {
+        for (int o = p.lanes >> 1; o > 0; o >>= 1) {
+          s += __shfl_xor_sync(0xffffffffu, s, o);
+          bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+        }
+        if (at == 0 && valid) {
           const double lse = (double(m) + log2(s)) * 0.69314718055994530942;         // and scale ref
           t.lse[b] = lse;
           t.ref[b] = ref;
-          t.base[b] = a.scores[row0 + b];
-          t.weight[b] = a.weight ? a.weight[row0 + b] : 1.f;
-          t.state[b] = over ? 2 : bad || m == -INFINITY ? 0 : 1;
+          t.base[b] = base;
+          t.weight[b] = weight;
+          t.state[b] = !(weight > 0.f) ? 0 : over ? 2 : bad || m == -INFINITY ? 0 : 1;
           if (a.lse) a.lse[row0 + b] = over ? 0.f : bad ? NAN : m == -INFINITY ? -INFINITY : float(double(a.scale) * double(ref) + lse);
+          if (!(weight > 0.f)) atomicExch(a.status, kErrInvalidArg);
         }
       }
       team_sync();
-      // Candidate c: beam, part and place in the part's keys.
-      const int per_beam = p.parts * n_out, n_cand = a.n_beams * per_beam;
-      auto candidate = [&](int c) {                      // its rank key, 0: none; where it goes on from and what it is are asked for only when it is chosen
-        const int b = c / per_beam, i = c - b * per_beam;
-        double s = -INFINITY;
+      // A key of beam b: its score, and its rank (0: none).  A beam that is done has one, the first of its first list.
+      auto rank_of = [&](int b, bool first, Key k, double& score) {
+        score = -INFINITY;
         if (t.state[b] == 2) {
-          if (i == 0) s = double(t.base[b]);
-        } else {
-          const Key k = t.state[b] == 1 ? __ldcg(&parts[size_t(row0 + b) * p.parts + i / n_out].keys[i % n_out]) : 0;
-          if (k != 0) s = double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]);
+          if (first) score = double(t.base[b]);
+        } else if (t.state[b] == 1 && k != 0) {
+          score = double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]);
         }
-        const double ranked = double(t.weight[b]) * s;
-        return ranked > -INFINITY ? order_of(ranked) : Key(0);
+        const double ranked = double(t.weight[b]) * score;
+        return score > -INFINITY && ranked > -INFINITY ? order_of(ranked) : Key(0);
       };
-      auto describe = [&](int c, Key& flat, float& score) {
-        const int b = c / per_beam, i = c - b * per_beam;
-        if (t.state[b] == 2) {
-          flat = (Key(b) << 32) | unsigned(a.end_token);
-          score = t.base[b];
-        } else {
-          const Key k = __ldcg(&parts[size_t(row0 + b) * p.parts + i / n_out].keys[i % n_out]);
-          flat = (Key(b) << 32) | unsigned(token_of(k));
-          score = float(double(t.base[b]) + (double(a.scale) * (double(logit_of(k)) - double(t.ref[b])) - t.lse[b]));
+      auto append = [&](int b, Key rank, Key k, double score) {
+        const int n = atomicAdd(&t.n_list, 1);
+        if (n >= BS_LIST) return;
+        t.list[n] = rank;
+        t.flat[n] = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
+        t.score[n] = float(score);
+      };
+      auto candidate = [&](int c, Key& flat, float& score) {             // candidate c of all: its rank, beam and token, and score
+        const int l = c / n_out, b = l / p.parts;
+        const Key k = t.state[b] == 2 ? 0 : __ldcg(&lists[l].keys[c - l * n_out]);
+        double s;
+        const Key rank = rank_of(b, c == b * p.parts * n_out, k, s);
+        flat = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
+        score = float(s);
+        return rank;
+      };
+      if (few) {
+        const int b = min(tid / n_out / p.parts, a.n_beams - 1);
+        double score;
+        const Key rank = tid < n_cand ? rank_of(b, tid == b * p.parts * n_out, early[0], score) : 0;
+        if (rank != 0) append(b, rank, early[0], score);
+        team_sync();
+      } else {
+        // Every part's keys fall.  With d = n_out / lists (up), each list's d-th key and the n_out / d-th largest (up) of those, there are n_out candidates from that one up:
+        // a bound.
+        Key top = 0, of[2];
+        double score;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int l = tid + u * BS_TEAM, b = min(l / p.parts, a.n_beams - 1);
+          of[u] = l < n_lists ? rank_of(b, l == b * p.parts && depth == 1, early[u], score) : 0;
+          top = max(top, of[u]);
         }
-      };
-      // Every part's keys fall.  With d = n_out / parts (up), each part's d-th key and the n_out / d-th largest (up) of those, there are n_out candidates from that one up: a
-      // bound.  What reaches it is found key by key; where there are many parts, in each from its first key on until one does not.
-      const int n_lists = a.n_beams * p.parts, depth = (n_out + n_lists - 1) / n_lists;
-      Key top = 0;
 #pragma unroll 1
-      for (int l = tid; l < n_lists; l += BS_TEAM) top = max(top, candidate(l * n_out + depth - 1));
-      find_bound(t, top, (n_out + depth - 1) / depth, tid, team_sync);
-      team_sync();
-      const Key least = t.bound;
-      const int run = n_cand <= 4 * BS_TEAM ? 1 : n_out;
+        for (int l = tid + 2 * BS_TEAM; l < n_lists; l += BS_TEAM) top = max(top, rank_of(l / p.parts, l % p.parts == 0 && depth == 1, __ldcg(&lists[l].keys[depth - 1]), score));
+        find_bound(t, top, (n_out + depth - 1) / depth, tid, team_sync);
+        team_sync();
+        Key least = t.bound;
+        for (;;) {
+          // What reaches it: in each list from its first key on until one does not.
 #pragma unroll 1
-      for (int c = tid * run; c < n_cand; c += BS_TEAM * run) {
+          for (int u = 0, l = tid; l < n_lists; ++u, l += BS_TEAM) {
+            if (depth == 1 && u < 2 && (u == 0 ? of[0] : of[1]) < max(least, Key(1))) continue;
+            const int b = l / p.parts;
+            if (t.state[b] != 1) {
+              const Key rank = rank_of(b, l == b * p.parts, 0, score);
+              if (rank != 0 && rank >= least) append(b, rank, 0, score);
+              continue;
+            }
+            bool on = true;
 #pragma unroll 1
-        for (int k = 0; k < run; ++k) {
-          const Key rank = candidate(c + k);
-          if (rank == 0 || rank < least) break;
-          const int n = atomicAdd(&t.n_list, 1);
-          if (n >= BS_LIST) break;
-          t.list[n] = rank;
-          describe(c + k, t.flat[n], t.score[n]);
+            for (int k0 = 0; on && k0 < n_out; k0 += 4) {
+              Key keys[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) keys[e] = k0 + e < n_out ? __ldcg(&lists[l].keys[k0 + e]) : 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (!on) break;
+                const Key rank = rank_of(b, false, keys[e], score);
+                on = rank != 0 && rank >= least;
+                if (on) append(b, rank, keys[e], score);
+              }
+            }
+          }
+          team_sync();
+          if (t.n_list <= BS_LIST) break;
+          // The list has run over.  The n_out-th largest of 64 groups of the ranks that it holds is a bound that fewer reach, unless they are all alike.
+          Key mine = 0;
+          for (int i = tid; i < BS_LIST; i += BS_TEAM) mine = max(mine, t.list[i]);
+          find_bound(t, mine, n_out, tid, team_sync);
+          team_sync();
+          if (t.bound <= least) break;
+          least = t.bound;
+          if (tid == 0) t.n_list = 0;
+          team_sync();
         }
       }
-      team_sync();
       int n = t.n_list;
       if (n > BS_LIST) {
         // More ties than the list holds: one continuation after the other, each the best behind the last.
@@ -520,11 +607,10 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
           float score_b = 0.f;
 #pragma unroll 1
           for (int c = tid; c < n_cand; c += BS_TEAM) {
-            const Key rank = candidate(c);
-            if (rank == 0 || rank > last_rank || rank < rank_b) continue;
             Key flat;
             float score;
-            describe(c, flat, score);
+            const Key rank = candidate(c, flat, score);
+            if (rank == 0 || rank > last_rank || rank < rank_b) continue;
             if (rank == last_rank && flat <= last_flat) continue;
             if (rank > rank_b || (rank == rank_b && flat < flat_b)) {
               rank_b = rank;
@@ -574,6 +660,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       for (int i = tid; i < n; i += BS_TEAM) {
         const Key k = t.list[i], f = t.flat[i];
         int above = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) above += t.list[j] > k || (t.list[j] == k && t.flat[j] < f) ? 1 : 0;
         if (above >= n_out) continue;
         const int b = int(f >> 32), token = int(unsigned(f));
@@ -643,6 +730,7 @@ cudaError_t launch_beam_select(const hs_beam_select_t& a, int sm_count, int sm_b
     }
   }
   p.items = int(rows * p.parts);
+  for (p.lanes = 1; p.lanes < std::min(p.parts, 32); p.lanes *= 2) {}
   const int grid = int(std::min<int64_t>(sm_budget, p.items));
   return launch_step_kernel(pick(a.type), grid, BS_THREADS, kSelectSmem, stream, true, p);
 }

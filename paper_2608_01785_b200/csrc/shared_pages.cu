@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(CP_THREADS, 1) copy_pages_kernel(const hs_copy
   griddep_wait();
   // A warp's heads follow one another in steps of the grid: neighbouring warps have neighbouring heads of a page.
   for (unsigned x = blockIdx.x * (CP_THREADS / 32) + (threadIdx.x >> 5); x < unsigned(n); x += unsigned(stride)) {
-    const int rest = int(x) / a.n_kv_heads, head = int(x) - rest * a.n_kv_heads, i = rest / (2 * a.n_layers), layer = rest - i * 2 * a.n_layers;
+    const int rest = int(x) / a.n_kv_heads, head = int(x) - rest * a.n_kv_heads, layer = rest / a.n_copies, i = rest - layer * a.n_copies;
     const int src = a.src[i], dst = a.dst[i], tokens = a.length ? a.length[i] : HS_PAGE_SIZE;
     if (src == -1 || dst == -1) continue;
     if (src < 0 || src >= a.num_pages || dst < 0 || dst >= a.num_pages || tokens < 0 || tokens > HS_PAGE_SIZE) {
@@ -258,10 +258,10 @@ __global__ void __launch_bounds__(CP_THREADS, 1) copy_pages_kernel(const hs_copy
       uint4 v[CP_UNROLL];
 #pragma unroll
       for (int u = 0; u < CP_UNROLL; ++u)
-        if (at + 32 * u + lane < count) v[u] = __ldcs(from + at + 32 * u + lane);
+        if (at + 32 * u + lane < count) v[u] = from[at + 32 * u + lane];
 #pragma unroll
       for (int u = 0; u < CP_UNROLL; ++u)
-        if (at + 32 * u + lane < count) __stcs(to + at + 32 * u + lane, v[u]);
+        if (at + 32 * u + lane < count) to[at + 32 * u + lane] = v[u];
     }
   }
 }

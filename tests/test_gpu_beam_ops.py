@@ -350,6 +350,34 @@ def test_more_ties_than_the_lists_hold(ws, status):
     check_select(x, np.zeros((1, 1), dtype=np.float32), 32, ws, status, exact_order=True)
 
 
+@pytest.mark.parametrize("b,vocab", [(8, 16000), (8, 152064), (32, 4097), (2, 152064), (3, 30000)])
+@pytest.mark.parametrize("last", [0.0, -20.0, -1e4])
+def test_a_beam_behind_all_others(b, vocab, last, ws, status):
+    """A bound that holds for every part's first keys says little where one beam is far behind: most candidates of the others reach it."""
+    scores = np.full((2, b), -1.0, dtype=np.float32) - 0.001 * np.arange(b, dtype=np.float32)
+    scores[0, -1] += last
+    scores[1, 0] += last
+    check_select(logits(torch.Generator().manual_seed(b), 2 * b, vocab, torch.float32), scores, 32, ws, status, scale=0.8)
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("bad", [0.0, -0.5, NAN])
+def test_a_weight_that_is_not_above_zero_gives_no_continuation(bad, ws, status):
+    scores = np.zeros((2, 3), dtype=np.float32)
+    weight, plain = np.ones((2, 3), dtype=np.float32), scores.copy()
+    weight[1, 1], plain[1, 1] = bad, -INF
+    x = logits(torch.Generator().manual_seed(8), 6, 3000, torch.bfloat16)
+    done = np.array([[0, 0, 0], [0, 1, 0]], dtype=np.int32)
+    for over in (None, done):
+        status.zero_()
+        got = run_select(x.to(DEV), scores, 5, ws, status, weight=weight, done=over)
+        assert int(status) == STATUS["INVALID_ARG"]
+        status.zero_()
+        want = run_select(x.to(DEV), plain, 5, ws, status, done=over)
+        assert int(status) == 0 and all(torch.equal(a, b) for a, b in zip(got[:4], want[:4]))
+    status.zero_()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("scale", [1.0, 0.3])
 def test_masked_logits(dtype, scale, ws, status):
