@@ -398,6 +398,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       for (int i = tid; i < n; i += BS_TEAM) {
         const Key k = t.list[i];
         int above = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) above += t.list[j] > k ? 1 : 0;
         if (above < n_out) part.keys[above] = k;
       }
@@ -559,19 +560,21 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         team_sync();
         Key least = t.bound;
         for (;;) {
-          // What reaches it: in each list from its first key on until one does not.
+          // What reaches it: in each list from its first key on until one does not.  A thread takes a list, or, where there are fewer lists than threads, four keys of one.
+          const int quarters = n_lists > BS_TEAM ? 1 : (n_out + 3) / 4;
 #pragma unroll 1
-          for (int u = 0, l = tid; l < n_lists; ++u, l += BS_TEAM) {
-            if (depth == 1 && u < 2 && (u == 0 ? of[0] : of[1]) < max(least, Key(1))) continue;
-            const int b = l / p.parts;
+          for (int u = 0, x = tid; x < n_lists * quarters; ++u, x += BS_TEAM) {
+            if (depth == 1 && quarters == 1 && u < 2 && (u == 0 ? of[0] : of[1]) < max(least, Key(1))) continue;
+            const int l = x / quarters, b = l / p.parts;
+            int k0 = 4 * (x - l * quarters);
             if (t.state[b] != 1) {
-              const Key rank = rank_of(b, l == b * p.parts, 0, score);
+              const Key rank = rank_of(b, l == b * p.parts && k0 == 0, 0, score);
               if (rank != 0 && rank >= least) append(b, rank, 0, score);
               continue;
             }
             bool on = true;
 #pragma unroll 1
-            for (int k0 = 0; on && k0 < n_out; k0 += 4) {
+            do {
               Key keys[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) keys[e] = k0 + e < n_out ? __ldcg(&lists[l].keys[k0 + e]) : 0;
@@ -582,7 +585,8 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
                 on = rank != 0 && rank >= least;
                 if (on) append(b, rank, keys[e], score);
               }
-            }
+              k0 += 4;
+            } while (on && quarters == 1 && k0 < n_out);
           }
           team_sync();
           if (t.n_list <= BS_LIST) break;
@@ -661,7 +665,10 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         const Key k = t.list[i], f = t.flat[i];
         int above = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) above += t.list[j] > k || (t.list[j] == k && t.flat[j] < f) ? 1 : 0;
+        for (int j = 0; j < n; ++j) {                    // (both numbers are read in any case: no answer is waited for before the next is asked for)
+          const Key r = t.list[j], g = t.flat[j];
+          above += int(r > k) | (int(r == k) & int(g < f));
+        }
         if (above >= n_out) continue;
         const int b = int(f >> 32), token = int(unsigned(f));
         put(above, t.score[i], row0 + b, token, t.state[b] == 2 || token == a.end_token ? 1 : 0);
