@@ -81,6 +81,7 @@ struct alignas(16) Team {
 struct alignas(16) Block {
   uint32_t tmem_base;
   int abort_flag, n_joins;
+  int middle[2];                                         // whether the teams' last item is the same, in shares of either parity
   int warp_sum[SA_THREADS / 32];
   int joins[kMaxShares];                                 // tiles that this block joins
 };
@@ -369,9 +370,10 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     end_phase ^= 1;
     return ok;
   };
+  auto row_reference = [&]() { return m_ref == -INFINITY ? -INFINITY : MOD ? m_ref : __fmul_rn(m_ref, p.score.in); };          // in log2 units
   // (reference, sum) of the thread's row over its copies; f: what the thread's own outputs count
   auto row_total = [&](float& f, bool& ok) {
-    const float m_log2 = m_ref == -INFINITY ? -INFINITY : MOD ? m_ref : __fmul_rn(m_ref, p.score.in);
+    const float m_log2 = row_reference();
     f = 1.f;
     ok = true;
     if (copies == 1) return make_float2(m_log2, l_run);
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     return ok;
   };
   // Finished rows, or a part of them in the workspace.
-  auto deliver = [&](const Item& it, float2 total, float f, auto more) {
+  auto deliver = [&](const Item& it, float2 total, float f) {
     const int row_in = copies == 2 ? r & 63 : r, i_seq = row_in / p.heads, h = row_in - i_seq * p.heads;
     const bool mine = r < copy_rows && i_seq < it.n_seq && h < it.heads;
     const int64_t row = it.seq0 + i_seq;
@@ -435,7 +437,6 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       else if (a.lse) a.lse[row * a.n_q_heads + head] = total.y == 0.f ? -INFINITY : kLn2 * (total.x + log2f(total.y));
     }
     return each_columns(f, [&](int c, float(&x)[32]) {
-      more(c, x);
       if (!mine) return;
       if (whole) {
 #pragma unroll
@@ -458,8 +459,9 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   };
 
 #pragma unroll 1
-  for (int share = plan.tiles > 0 ? int(blockIdx.x) : plan.shares; share < plan.shares; share += int(gridDim.x)) {
+  for (int share = plan.tiles > 0 ? int(blockIdx.x) : plan.shares, turn = 0; share < plan.shares; share += int(gridDim.x), ++turn) {
     const int x0 = share_begin(share), x1 = share_begin(share + 1), xm = x0 + (x1 - x0) / 2;
+    int middle = 0;                                      // softmax: of the last item
     if (warp == 8 || warp == 10) {
       // ============================================================ fetching ==
       // Items from this team's half of the share, the first team's in rising order, the second's in falling order, so that both come to the middle last.
@@ -955,10 +957,11 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
         ok = __all_sync(0xffffffffu, mbar_wait(&tm.o_full[(g - 1) & 1], ((g - 1) >> 1) & 1, abort_flag, a.status));
         if (!ok) break;
         tc_fence_after_sync();
-        if (!it.middle) {
+        middle = it.middle;
+        if (!middle) {
           float f;
           const float2 total = row_total(f, ok);
-          if (!ok || !deliver(it, total, f, [](int, float(&)[32]) {})) break;
+          if (!ok || !deliver(it, total, f)) break;
           if (it.parts > 1) {
             __threadfence();
             __syncwarp();
@@ -976,55 +979,92 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       }
     }
     // -------------------------------------------------------------- the share's end
+    if (tid == 0) bar->middle[turn & 1] = middle;
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     if (*abort_flag) break;
-    const int mid = xm < x1 && xm > x0 ? number_at(xm) : 0;
-    if (xm > x0 && middle_of(share, mid)) {
-      // The tile in the middle: the second team's rows go through its own Q, K and V, which are idle.  The item is the teams' last one, in the ring's slot in front
-      // of the last.
-      float2 total = make_float2(-INFINITY, 0.f);
-      float f = 1.f;
-      bool ok = true;
-      if (warp < 8) total = row_total(f, ok);
-      if (warp >= 4 && warp < 8) {
-        // (the copies meet in Q, the sum goes behind it)
-        float4* dst = reinterpret_cast<float4*>(smem + G_::TEAM_BYTES + (copies == 2 ? G_::Q_BYTES : 0));
-        ok = each_columns(f, [&](int c, float(&x)[32]) {
+    if (bar->middle[turn & 1]) {
+      // The tile in the middle, the last item of both teams, in the ring's slot in front of the last.  All rows of both go through their own Q, K and V, which are idle,
+      // [columns / 4][128 rows]; then a thread has some columns of one row, and adds up its two or four places.
+      const Item& it = tm.ring[rs];
+      if (warp < 8) {
+        float4* dst = reinterpret_cast<float4*>(q_smem);
+        tm.ml[r] = make_float2(row_reference(), l_run);
+#pragma unroll 1
+        for (int c = 0; c < DH; c += 32) {
+          tmem_ld32(t_lane + G_::O0 + c, sreg);
+          tmem_ld_wait();
 #pragma unroll
-          for (int u = 0; u < 8; ++u) dst[(c / 4 + u) * copy_rows + r] = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
-        });
-        if (r < copy_rows) tm.ml[r] = total;             // (both copies have read theirs)
+          for (int u = 0; u < 8; ++u)
+            dst[(c / 4 + u) * SA_ROWS + r] = make_float4(__uint_as_float(sreg[4 * u]), __uint_as_float(sreg[4 * u + 1]), __uint_as_float(sreg[4 * u + 2]),
+                                                         __uint_as_float(sreg[4 * u + 3]));
+        }
       }
       __syncthreads();
-      if (warp < 4 && ok) {
-        const Item& it = tm.ring[rs];
-        const float4* src = reinterpret_cast<const float4*>(smem + G_::TEAM_BYTES + (copies == 2 ? G_::Q_BYTES : 0));
-        const float2 other = reinterpret_cast<Team*>(smem + G_::TEAMS)[1].ml[copies == 2 ? r & 63 : r];
-        const float top = fmaxf(total.x, other.x), zero = top == -INFINITY ? 0.f : top, f0 = fast_exp2(total.x - zero), f1 = fast_exp2(other.x - zero);
-        ok = deliver(it, make_float2(top, fmaf(total.y, f0, other.y * f1)), f * f0, [&](int c, float(&x)[32]) {
+      if (warp < 8) {
+        const int row_in = tid & (copy_rows - 1), i_seq = row_in / p.heads, h = row_in - i_seq * p.heads, columns = DH * copy_rows / 256, c0 = tid / copy_rows * columns;
+        if (i_seq < it.n_seq && h < it.heads) {
+          const float4* src[4];
+          float w[4], top = -INFINITY, l = 0.f;
+          float2 x[4];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float4 y = src[(c / 4 + u) * copy_rows + r];
-            x[4 * u] = fmaf(y.x, f1, x[4 * u]);
-            x[4 * u + 1] = fmaf(y.y, f1, x[4 * u + 1]);
-            x[4 * u + 2] = fmaf(y.z, f1, x[4 * u + 2]);
-            x[4 * u + 3] = fmaf(y.w, f1, x[4 * u + 3]);
+          for (int q = 0; q < 4; ++q) {                  // (team q % 2, copy q / 2)
+            src[q] = reinterpret_cast<const float4*>(smem + (q & 1) * G_::TEAM_BYTES) + (row_in + (q >> 1) * copy_rows) % SA_ROWS;
+            x[q] = q < 2 * copies ? reinterpret_cast<const Team*>(smem + G_::TEAMS)[q & 1].ml[(row_in + (q >> 1) * copy_rows) % SA_ROWS] : make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, x[q].x);
           }
-        });
-        if (it.parts > 1) __threadfence();
-        fence_proxy_async();
+          const float zero = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            w[q] = fast_exp2(x[q].x - zero);
+            l = fmaf(x[q].y, w[q], l);
+          }
+          const bool whole = it.parts == 1;
+          const int64_t row = it.seq0 + i_seq;
+          const int head = it.head0 + h;
+          RowsPart<DH>& part = reinterpret_cast<RowsPart<DH>*>(static_cast<char*>(a.workspace) + kWsScratch)[it.slot];
+          uint16_t* dst = static_cast<uint16_t*>(a.o) + row * a.o_stride + head * DH;
+          if (c0 == 0) {
+            if (!whole) __stcg(&part.ml[row_in], make_float2(top, l));
+            else if (a.lse) a.lse[row * a.n_q_heads + head] = l == 0.f ? -INFINITY : kLn2 * (top + log2f(l));
+          }
+          const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[q] *= inv;
+#pragma unroll 1
+          for (int c = c0; c < c0 + columns; c += 8) {
+            float4 y[2] = {};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (q >= 2 * copies) continue;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float4 v = src[q][(c / 4 + e) * SA_ROWS];
+                y[e].x = fmaf(v.x, w[q], y[e].x);
+                y[e].y = fmaf(v.y, w[q], y[e].y);
+                y[e].z = fmaf(v.z, w[q], y[e].z);
+                y[e].w = fmaf(v.w, w[q], y[e].w);
+              }
+            }
+            if (whole) {
+              *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_16<F16>(y[0].x, y[0].y), pack_16<F16>(y[0].z, y[0].w), pack_16<F16>(y[1].x, y[1].y),
+                                                              pack_16<F16>(y[1].z, y[1].w));
+            } else {
+              __stcg(&part.o[c / 4][row_in], y[0]);
+              __stcg(&part.o[c / 4 + 1][row_in], y[1]);
+            }
+          }
+        }
+        fence_proxy_async();                             // (Q's place was written)
       }
-      if (warp >= 4 && warp < 8) fence_proxy_async();
       tc_fence_before_sync();
       __syncthreads();
       tc_fence_after_sync();
-      if (*abort_flag) break;
-      if (tid == 0 && tm.ring[rs].parts > 1) {
-        __threadfence();
-        arrived(tm.ring[rs], 4);
+      if (tid == 0 && it.parts > 1) {
+        __threadfence();                                 // (of both teams' part, which the barrier has brought here)
+        arrived(it, 4);
       }
     }
   }
