@@ -13,7 +13,12 @@
 // At an item's end the n_out-th largest of 64 groups of two threads' (best, tile) bounds its n_out largest logits from below: only threads whose
 // own pair reaches it can hold one, a few of 128, and the team looks through that tile's pieces once more, or through the first two tiles', or, where third reaches the bound
 // as well, all of a thread's (the L2 has them); it lists what reaches the bound and ranks the list.  The main loop carries no list and no test per element for it.
-// The team that delivers a request's last item makes the choice: L_b from the parts, candidates' scores in 64 bits, the same bound, list and ranks.
+// The team that delivers a request's last item makes the choice: L_b from the parts, candidates' scores in 64 bits, the same bound, list and ranks.  A list that runs over gives a
+// better bound, until only candidates that are all alike are left, which are taken one by one.  It comes behind the team's next item, while the others work on.
+//
+// 64 requests of 8 beams over 152,064 bf16 logits: 42 us.  The stream ends after 26 of them on average and 30 at most (5.2 TB/s; the exponentials alone would take 20), the items' ends, of 4 us
+// each, follow at once where rows are not cut, and a choice takes 4.  Cutting rows in two for a second round that hides the ends costs more than it hides (60 us).  One request of 4 beams: 13.0 us,
+// of which the stream is 2: launch, an item's end (2.5), its delivery (2) and the choice (5) are round trips and code that runs once.
 #include <algorithm>
 
 #include "paged_scores.cuh"

@@ -4,19 +4,23 @@
 //   tile      sequences of one group that follow one another, all query heads of one KV head: up to 128 rows of a matrix, sequence after sequence.  Where groups
 //             are small (a rule on the call's shape) a tile is 64 rows, which stand in the matrix twice: each copy's softmax has half of a block's keys.
 //   keys      the tile's keys are one line of blocks of 64: the group's shared pages, read once for all rows, then the pages of each sequence's own keys, one sequence
-//             behind the other, a block of the first half of the rows and one of the second half in turn: they are different warps' work, which overlaps.  A row sees the shared keys and a run of the others; what it does not see is masked, and a warp whose 32 rows see nothing
-//             of a block gives it the weight 0 and goes on.  (The products with rows that see nothing cost little: a block's two products take a third of
+//             behind the other, a block of the first half of the rows and one of the second half in turn: they are different warps' work, which overlaps.  A row sees the
+//             shared keys and a run of the others; what it does not see is masked, and a warp whose 32 rows see nothing of a block gives it the weight 0 and goes on.  (The products with rows that see nothing cost little: a block's two products take a third of
 //             the time that its 32 KB take to come.)
 //   teams     two to a thread block, each with a running softmax of its own: a warp that fetches, one that issues S = Q K^T into tensor memory and O += P V, four with one
 //             thread per row.  K and V come by 16-byte asynchronous copies: a page's 4 KB are too small a box for the tensor copies, 16 of which a block took
 //             1400 cycles.  V rows that no row sees are filled with zeros by the copy.
 //   shares    all tiles' lines, one after the other, are cut into equal shares, about one per SM of the device, wherever the cut falls, and each share into halves for
-//             the teams.  Both teams come last to the tile in the middle, which is added up over them there.  A tile that is cut between shares leaves its
+//             the teams.  Both teams come last to the tile in the middle: their rows meet in shared memory, where all eight warps add them up.  A tile that is cut between shares leaves its
 //             parts in the workspace; the block that delivers the last one joins them, in order.  Where the cuts lie depends on the lengths and the device,
 //             never on the budget, and a block takes one share after the other.
 //
 // Every block plans for itself, from the lengths, in shared memory.  The softmax works through a block 32 keys at a time in rolled loops, as it is few warps' instructions
 // that have to be fetched: unrolled over 64 keys with all its variants the same work took twice as long.
+//
+// 64 groups of 8 sequences behind 512 .. 2,048 shared keys, 28 heads on 4 of 128, capped: 87 us against a floor of 44 for the bytes; 256 sequences behind 8,191 shared keys with up
+// to 1,024 own ones: 123 against 47.  The softmax warps bound the shared keys (1,000 cycles a block of 64 keys for two teams), a row's exponentials and the way of P; own keys
+// keep one or two warps of four busy (2,000 cycles).  Plan and first pages are 6 us of a call, the ends and joins of cut tiles 8 to 10.  One group of 4 behind 500 keys: 21 us, all latency.
 #include <math.h>
 
 #include <algorithm>
