@@ -15,8 +15,8 @@
 // streaming loads and stores it was 108.
 //
 // Compact.  Bits of the free pages; running sums of the bits number the free pages below the bound and the used ones above it; then tables, counts, stack and
-// copy list from those numbers.  Three small kernels, one after the other: each needs the whole of the one in front.  1,000 pages 7.8 us, 200,000 pages 13.4 us, which is their
-// launches and a few round trips each.
+// copy list from those numbers.  Three small kernels, one after the other: each needs the whole of the one in front.  200,000 pages 13.4 us, which is their launches and a few
+// round trips each.  A small pool is one block's work, in shared memory: 1,000 pages 5 us.
 #include <algorithm>
 
 #include "block_scan.cuh"
@@ -28,6 +28,8 @@ namespace {
 
 constexpr int SP_THREADS = 1024, SP_PER_THREAD = HS_DEVICE_MAX_SEQS / SP_THREADS;
 constexpr int SP_COLUMNS = 8;                            // columns of a block's slice
+constexpr int SP_SMALL_PAGES = 8192, SP_SMALL_WORK = 12288;              // pages that one block compacts at most, and with the entries of tables
+constexpr int SP_SMALL_SMEM = 3 * SP_SMALL_PAGES * 4;
 constexpr int SP_FORK_SMEM = HS_DEVICE_MAX_SEQS * (6 * 4 + SP_COLUMNS * 4);
 static_assert(SP_FORK_SMEM <= 227 * 1024, "fits one SM");
 static_assert(HS_BEAMS_MAX_PAGES % 32 == 0 && HS_COMPACT_MAX_PAGES <= HS_BEAMS_MAX_PAGES, "a bit per page");
@@ -282,49 +284,37 @@ __device__ __forceinline__ int* numbers_of(const hs_compact_pages_t& a) { return
 __device__ __forceinline__ int* sources_of(const hs_compact_pages_t& a) { return targets_of(a) + a.num_pages; }     // [num_pages - n_keep]
 static_assert(256 + size_t(HS_COMPACT_MAX_PAGES) * 2 * sizeof(int) <= kWsScratchBytes, "three lists of pages");
 
-__global__ void __launch_bounds__(SP_THREADS, 1) compact_mark_kernel(const hs_compact_pages_t a) {
-  griddep_wait();
-  const int count = *a.free_count, first = int(blockIdx.x) * SP_THREADS + threadIdx.x, stride = int(gridDim.x) * SP_THREADS;
-  Compaction* plan = plan_of(a);
-  unsigned* bits = page_bits(a.workspace);
-  const int n = count < 0 || count > a.num_pages ? 0 : count;
+// The bits of the free pages, from the stack.
+__device__ __forceinline__ void mark_free(const hs_compact_pages_t& a, int free_count, unsigned* bits, int first, int stride) {
+  const int n = free_count < 0 || free_count > a.num_pages ? 0 : free_count;
+#pragma unroll 4
   for (int i = first; i < n; i += stride) {
     const int page = a.free_list[i];
     if (page >= 0 && page < a.num_pages) atomicOr(&bits[page >> 5], 1u << (page & 31));
   }
-  if (first == 0) plan->wrong = 0;
 }
 
-// Numbers the pages: a block its share of the words, behind the sums of all words in front of it.
-__global__ void __launch_bounds__(SP_THREADS, 1) compact_number_kernel(const hs_compact_pages_t a) {
-  __shared__ unsigned long long warp_sums[32];
-  __shared__ unsigned long long all;
-  griddep_wait();
-  const int tid = threadIdx.x, n_words = (a.num_pages + 31) / 32, keep = a.n_keep;
-  const unsigned* bits = page_bits(a.workspace);
-  const int per_block = (n_words + int(gridDim.x) - 1) / int(gridDim.x), b0 = min(int(blockIdx.x) * per_block, n_words), b1 = min(b0 + per_block, n_words);
-  // free pages below the bound (upper half) and used ones from it up
+// Numbers the pages of words b0 .. b1 - 1 by the whole block: counts of free pages below the bound (upper half) and used ones from it up, those in front of b0 in `before`.
+// Returns the counts behind b1 - 1.  LOAD reads a word of the bits.
+template <typename F>
+__device__ __forceinline__ unsigned long long number_pages(const hs_compact_pages_t& a, F load, int b0, int b1, unsigned long long before, unsigned long long* warp_sums, int* targets,
+                                                           int* numbers, int* sources) {
+  const int tid = threadIdx.x, keep = a.n_keep;
   auto below = [&](int w) { return keep <= w * 32 ? 0u : keep >= w * 32 + 32 ? ~0u : (1u << (keep - w * 32)) - 1u; };
   auto exists = [&](int w) { return a.num_pages >= w * 32 + 32 ? ~0u : (1u << (a.num_pages - w * 32)) - 1u; };
-  auto counts = [&](unsigned free, int w) {
-    return (static_cast<unsigned long long>(__popc(free & below(w))) << 32) + __popc(~free & ~below(w) & exists(w));
-  };
-  unsigned long long before = 0;
-  for (int w = tid; w < b0; w += SP_THREADS) before += counts(__ldcg(bits + w), w);
-  block_scan(before, warp_sums, before);
-  if (tid == 0) all = before;
-  __syncthreads();
   // a warp a run of words, a lane a page of each
   const int lane = tid & 31, per = (b1 - b0 + 31) / 32, w0 = min(b0 + (tid >> 5) * per, b1), w1 = min(w0 + per, b1);
   unsigned long long mine = 0, total = 0;
-  for (int w = w0 + lane; w < w1; w += 32) mine += counts(__ldcg(bits + w), w);
-  const unsigned long long at = __shfl_sync(0xffffffffu, all + block_scan(mine, warp_sums, total), 0);
+  for (int w = w0 + lane; w < w1; w += 32) {
+    const unsigned free = load(w);
+    mine += (static_cast<unsigned long long>(__popc(free & below(w))) << 32) + __popc(~free & ~below(w) & exists(w));
+  }
+  const unsigned long long at = __shfl_sync(0xffffffffu, before + block_scan(mine, warp_sums, total), 0);
   int low = int(at >> 32), number = int(unsigned(at));
-  int *targets = targets_of(a), *numbers = numbers_of(a), *sources = sources_of(a);
   const unsigned in_front = (1u << lane) - 1u;
 #pragma unroll 2
   for (int w = w0; w < w1; ++w) {
-    const unsigned free = __ldcg(bits + w), free_low = free & below(w), high = ~below(w) & exists(w), used = high & ~free;
+    const unsigned free = load(w), free_low = free & below(w), high = ~below(w) & exists(w), used = high & ~free;
     const int page = w * 32 + lane;
     if (free_low >> lane & 1u) targets[low + __popc(free_low & in_front)] = page;
     if (high >> lane & 1u) {
@@ -336,27 +326,19 @@ __global__ void __launch_bounds__(SP_THREADS, 1) compact_number_kernel(const hs_
     low += __popc(free_low);
     number += __popc(used);
   }
-  Compaction* plan = plan_of(a);
-  if (int(blockIdx.x) == (n_words - 1) / per_block && tid == 0) {
-    const unsigned long long end = all + total;
-    plan->moves = int(unsigned(end));
-    plan->low = int(end >> 32);
-    plan->free_pages = int(end >> 32) + (a.num_pages - keep - int(unsigned(end)));
-  }
-  // lengths that no row can have
-  int wrong = 0;
-  for (int i = int(blockIdx.x) * SP_THREADS + tid; i < a.n_rows; i += int(gridDim.x) * SP_THREADS) wrong |= a.ctx_len[i] < 0 || a.ctx_len[i] > row_tokens(a.max_pages_per_seq);
-  if (wrong) atomicExch(&plan->wrong, 1);
+  return before + total;
 }
 
-__global__ void __launch_bounds__(SP_THREADS, 1) compact_move_kernel(const hs_compact_pages_t a) {
-  griddep_wait();
-  const Compaction plan = *plan_of(a);
-  const int *targets = targets_of(a), *numbers = numbers_of(a), *sources = sources_of(a);
-  const int first = int(blockIdx.x) * SP_THREADS + threadIdx.x, stride = int(gridDim.x) * SP_THREADS, keep = a.n_keep;
-  unsigned* bits = page_bits(a.workspace);
-  for (int w = first; w < (a.num_pages + 31) / 32; w += stride) bits[w] = 0;           // ready for the next call
-  const int error = plan.wrong || plan.free_pages != *a.free_count || plan.moves > a.max_copies ? kErrInvalidArg : plan.moves > plan.low ? kErrOutOfPages : 0;
+__device__ __forceinline__ Compaction compaction_of(const hs_compact_pages_t& a, unsigned long long end, int wrong) {
+  const int moves = int(unsigned(end)), low = int(end >> 32);
+  return Compaction{moves, low, low + (a.num_pages - a.n_keep - moves), wrong};
+}
+
+// Copy list, counts, stack and tables, by threads first, first + stride, ...
+__device__ __forceinline__ void move_pages(const hs_compact_pages_t& a, const Compaction& plan, int free_count, const int* targets, const int* numbers, const int* sources, int first,
+                                           int stride) {
+  const int keep = a.n_keep;
+  const int error = plan.wrong || plan.free_pages != free_count || plan.moves > a.max_copies ? kErrInvalidArg : plan.moves > plan.low ? kErrOutOfPages : 0;
   const int moves = error ? 0 : plan.moves;
   for (int k = first; k < a.max_copies; k += stride) {
     a.copy_src[k] = k < moves ? sources[k] : -1;
@@ -373,23 +355,102 @@ __global__ void __launch_bounds__(SP_THREADS, 1) compact_move_kernel(const hs_co
   // the highest free page at the bottom of the stack
   const int low = plan.low - moves, high = a.num_pages - keep;
   for (int k = first; k < low + high; k += stride) a.free_list[low + high - 1 - k] = k < low ? targets[moves + k] : keep + k - low;
-  // a warp a row's run of entries
+  // a warp a row's run of entries, four of them at a time, whose loads do not wait for one another
   const int lane = threadIdx.x & 31, width = (a.max_pages_per_seq + 31) / 32;
+  const int64_t runs = int64_t(a.n_rows) * width;
   bool bad_page = false;
-  for (int64_t x = first >> 5; x < int64_t(a.n_rows) * width; x += stride >> 5) {
-    const int row = int(x / width), c = int(x - int64_t(row) * width) * 32 + lane;
-    if (c >= owned_pages(a.ctx_len[row])) continue;
-    int32_t* entry = a.block_tables + int64_t(row) * a.max_pages_per_seq + c;
-    const int page = *entry;
-    if (page < 0 || page >= a.num_pages) {
-      bad_page = true;
-    } else if (page >= keep) {
-      const int k = numbers[page - keep];
-      if (k >= 0) *entry = targets[k];
-      else bad_page = true;
+  for (int64_t x0 = first >> 5; x0 < runs; x0 += 4 * (stride >> 5)) {
+    int32_t* entry[4];
+    int page[4], owned[4], c[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t x = x0 + u * (stride >> 5);
+      const int row = int(min(x, runs - 1) / width);
+      c[u] = int(x - int64_t(row) * width) * 32 + lane;
+      entry[u] = a.block_tables + int64_t(row) * a.max_pages_per_seq + c[u];
+      const bool there = x < runs && c[u] < a.max_pages_per_seq;
+      page[u] = there ? *entry[u] : 0;
+      owned[u] = there ? owned_pages(a.ctx_len[row]) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (c[u] >= owned[u]) continue;
+      if (page[u] < 0 || page[u] >= a.num_pages) {
+        bad_page = true;
+      } else if (page[u] >= keep) {
+        const int k = numbers[page[u] - keep];
+        if (k >= 0) *entry[u] = targets[k];
+        else bad_page = true;
+      }
     }
   }
   if (bad_page) atomicExch(a.status, kErrBadBlockTable);
+}
+
+__device__ __forceinline__ int wrong_length(const hs_compact_pages_t& a, int first, int stride) {
+  int wrong = 0;
+  for (int i = first; i < a.n_rows; i += stride) wrong |= a.ctx_len[i] < 0 || a.ctx_len[i] > row_tokens(a.max_pages_per_seq);
+  return wrong;
+}
+
+// All of it in one block, bits and lists in shared memory.
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_small_kernel(const hs_compact_pages_t a) {
+  extern __shared__ int smem[];
+  __shared__ unsigned long long warp_sums[32];
+  __shared__ unsigned bits[(SP_SMALL_PAGES + 31) / 32];
+  const int tid = threadIdx.x;
+  int *targets = smem, *numbers = smem + SP_SMALL_PAGES, *sources = smem + 2 * SP_SMALL_PAGES;
+  for (int w = tid; w < (SP_SMALL_PAGES + 31) / 32; w += SP_THREADS) bits[w] = 0;
+  griddep_wait();
+  const int free_count = *a.free_count;
+  const int wrong = __syncthreads_or(wrong_length(a, tid, SP_THREADS));
+  mark_free(a, free_count, bits, tid, SP_THREADS);
+  __syncthreads();
+  const unsigned long long end = number_pages(a, [&](int w) { return bits[w]; }, 0, (a.num_pages + 31) / 32, 0, warp_sums, targets, numbers, sources);
+  __syncthreads();
+  move_pages(a, compaction_of(a, end, wrong), free_count, targets, numbers, sources, tid, SP_THREADS);
+}
+
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_mark_kernel(const hs_compact_pages_t a) {
+  griddep_wait();
+  const int first = int(blockIdx.x) * SP_THREADS + threadIdx.x;
+  mark_free(a, *a.free_count, page_bits(a.workspace), first, int(gridDim.x) * SP_THREADS);
+  if (first == 0) plan_of(a)->wrong = 0;
+}
+
+// Numbers the pages: a block its share of the words, behind the sums of all words in front of it.
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_number_kernel(const hs_compact_pages_t a) {
+  __shared__ unsigned long long warp_sums[32];
+  griddep_wait();
+  const int tid = threadIdx.x, n_words = (a.num_pages + 31) / 32, keep = a.n_keep;
+  const unsigned* bits = page_bits(a.workspace);
+  const int per_block = (n_words + int(gridDim.x) - 1) / int(gridDim.x), b0 = min(int(blockIdx.x) * per_block, n_words), b1 = min(b0 + per_block, n_words);
+  // (a word in front is below the bound, or from it up, or the one that has it: counts() of number_pages)
+  unsigned long long mine = 0, before = 0;
+  for (int w = tid; w < b0; w += SP_THREADS) {
+    const unsigned free = __ldcg(bits + w), low = keep <= w * 32 ? 0u : keep >= w * 32 + 32 ? ~0u : (1u << (keep - w * 32)) - 1u;
+    mine += (static_cast<unsigned long long>(__popc(free & low)) << 32) + __popc(~free & ~low);          // (no word in front is the pool's last)
+  }
+  block_scan(mine, warp_sums, before);
+  __syncthreads();                                       // (warp_sums)
+  const unsigned long long end =
+      number_pages(a, [&](int w) { return __ldcg(bits + w); }, b0, b1, before, warp_sums, targets_of(a), numbers_of(a), sources_of(a));
+  Compaction* plan = plan_of(a);
+  if (int(blockIdx.x) == (n_words - 1) / per_block && tid == 0) {
+    const Compaction c = compaction_of(a, end, 0);
+    plan->moves = c.moves;
+    plan->low = c.low;
+    plan->free_pages = c.free_pages;
+  }
+  if (wrong_length(a, int(blockIdx.x) * SP_THREADS + tid, int(gridDim.x) * SP_THREADS)) atomicExch(&plan->wrong, 1);
+}
+
+__global__ void __launch_bounds__(SP_THREADS, 1) compact_move_kernel(const hs_compact_pages_t a) {
+  griddep_wait();
+  const int first = int(blockIdx.x) * SP_THREADS + threadIdx.x, stride = int(gridDim.x) * SP_THREADS;
+  unsigned* bits = page_bits(a.workspace);
+  for (int w = first; w < (a.num_pages + 31) / 32; w += stride) bits[w] = 0;           // ready for the next call
+  move_pages(a, *plan_of(a), *a.free_count, targets_of(a), numbers_of(a), sources_of(a), first, stride);
 }
 
 int grid_for(int64_t work, int64_t per_block, int sm_budget) { return int(std::max<int64_t>(1, std::min<int64_t>((work + per_block - 1) / per_block, sm_budget))); }
@@ -399,6 +460,7 @@ int grid_for(int64_t work, int64_t per_block, int sm_budget) { return int(std::m
 cudaError_t shared_pages_set_attributes() {
   cudaError_t e = set_kernel_smem(fork_pages_kernel, std::max(SP_FORK_SMEM, kMinSmemBytes));
   if (e == cudaSuccess) e = set_kernel_smem(copy_pages_kernel, kMinSmemBytes);
+  if (e == cudaSuccess) e = set_kernel_smem(compact_small_kernel, std::max(SP_SMALL_SMEM, kMinSmemBytes));
   if (e == cudaSuccess) e = set_kernel_smem(compact_mark_kernel, kMinSmemBytes);
   if (e == cudaSuccess) e = set_kernel_smem(compact_number_kernel, kMinSmemBytes);
   return e == cudaSuccess ? set_kernel_smem(compact_move_kernel, kMinSmemBytes) : e;
@@ -415,6 +477,10 @@ cudaError_t launch_copy_pages(const hs_copy_pages_t& a, int sm_budget, cudaStrea
 }
 
 cudaError_t launch_compact_pages(const hs_compact_pages_t& a, int sm_budget, cudaStream_t stream) {
+  // One launch of one block, or three of many: 1,000 pages with 1,024 entries 5.3 us for 8 to 12, 4,000 with 7,680 8.6 for 9 to 12, 8,000 with 9,216 10.9 for 9.7.
+  const int64_t all_entries = int64_t(a.n_rows) * ((a.max_pages_per_seq + 31) / 32 * 32);
+  if (a.num_pages <= SP_SMALL_PAGES && a.num_pages + all_entries <= SP_SMALL_WORK && a.max_copies <= SP_SMALL_PAGES)
+    return launch_step_kernel(compact_small_kernel, 1, SP_THREADS, std::max(SP_SMALL_SMEM, kMinSmemBytes), stream, true, a);
   cudaError_t e = launch_step_kernel(compact_mark_kernel, grid_for(a.num_pages, SP_THREADS, sm_budget), SP_THREADS, kMinSmemBytes, stream, true, a);
   if (e == cudaSuccess) e = launch_step_kernel(compact_number_kernel, grid_for(a.num_pages, 32 * 64, sm_budget), SP_THREADS, kMinSmemBytes, stream, true, a);
   if (e != cudaSuccess) return e;

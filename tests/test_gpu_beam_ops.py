@@ -180,11 +180,17 @@ def test_compact_pages(n, beams, most, spare, ws, status):
     assert int(status) == 0
 
 
+@pytest.mark.parametrize("n,beams,most,spare", [(2, 3, 400, 8150), (2, 3, 400, 8300), (40, 8, 600, 5000), (300, 1, 900, 30000), (8, 8, 2000, 70001)])
+def test_compact_pages_of_larger_pools(n, beams, most, spare, ws, status):
+    test_compact_pages(n, beams, most, spare, ws, status)
+
+
 @pytest.mark.parametrize("what", ["too many moves", "out of pages", "negative length", "length beyond the row", "free count", "a page twice", "a page outside", "bad entry", "a free entry"])
-def test_compaction_that_cannot_be_done(what, ws, status):
+@pytest.mark.parametrize("spare", [40, 20000])
+def test_compaction_that_cannot_be_done(what, spare, ws, status):
     rng = np.random.default_rng(9)
-    ctx, tables, shares, free, num_pages = ref.shared_rows(rng, 3, 2, [100, 40, 64], 40)
-    keep, copies, count = num_pages - 20, 20, len(free)
+    ctx, tables, shares, free, num_pages = ref.shared_rows(rng, 3, 2, [100, 40, 64], spare)
+    keep, copies, count = num_pages - spare // 2, 20, len(free)
     if what == "too many moves":
         copies = sum(p not in free for p in range(keep, num_pages)) - 1
     elif what == "out of pages":
