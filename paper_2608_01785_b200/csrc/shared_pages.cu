@@ -8,7 +8,7 @@
 // them, so no block waits for another; the last one to end sweeps the bits of freed pages, in order, onto the stack.  Rows that share a page in a column
 // are neighbours as a rule (beams of a request): a warp adds up their counts first, mostly to zero, which spares the atomics on a prompt's pages.
 // Latency bounds it: launch, one round trip for lengths, parents and table entries together, one for the counts, one for the blocks that are done, one for the
-// freed pages' bits.  16 rows of 49 pages 7.6 us, 512 rows of 258 pages 11.5 us.
+// freed pages' bits.  16 rows of 49 pages 7.3 us, 512 rows of 258 pages 11.5 us.
 //
 // Copy.  A warp takes one head of one page and layer, K or V, at a time: up to 16 rows that follow one another, eight 16-byte pieces a lane on their way.  The pages of a
 // layer follow one another, so that what is being copied lies together.  HBM bounds it: 300 whole pages of 28 layers (550 MB read and written) 104 us, 5.3 TB/s; with
@@ -141,6 +141,8 @@ __global__ void __launch_bounds__(SP_THREADS, 1) fork_pages_kernel(const hs_fork
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int x = x0 + u * (SP_THREADS / 32), i = x / SP_COLUMNS * 32 + lane, c = c0 + x % SP_COLUMNS;
+        by[u] = pages[u] = 0;
+        if (x / SP_COLUMNS * 32 >= n) continue;          // (the same for the whole warp)
         const bool owned = i < n && c < owned_pages(ctx[i]);
         const int page = i < n ? slice[entry_of(i, x % SP_COLUMNS)] : -1;             // (entries that a row does not own are -1 here)
         bad_page |= owned && !inside(page);
