@@ -1,0 +1,149 @@
+"""The operators of horizonserve_beams.h at the ends of their arguments: offsets past 32 bits, the largest pools, the most rows, two calls that share a stream and
+a workspace."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_01785_b200 import device_ops as ops
+from tests import beam_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def i32(values):
+    return torch.tensor(np.asarray(values, dtype=np.int32), device=DEV)
+
+
+@pytest.fixture(scope="module")
+def ws():
+    return ops.workspace(DEV)
+
+
+@pytest.fixture()
+def status():
+    return torch.zeros(1, dtype=torch.int32, device=DEV)
+
+
+def test_a_cache_of_more_than_four_gigabytes(ws, status):
+    """The last pages of the last layer give what the same pages of a small cache give, bit for bit."""
+    rng, layers, pages, hkv, dim = np.random.default_rng(1), 4, 20000, 8, 128
+    big = torch.empty(layers, 2, pages, hkv, 16, dim, dtype=torch.bfloat16, device=DEV)
+    assert big.numel() * 2 > 1 << 32
+    tables, used = ref.grouped_tables(rng, [(100, [5, 40]), (33, [1, 20, 3])], 12)
+    small = torch.randn(1, 2, used, hkv, 16, dim, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    first = pages - used
+    big[-1, :, first:] = small[0]
+    kv, q = i32([105, 140, 34, 53, 36]), torch.randn(5, 16, dim, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    out = []
+    for pool, offset in ((small, 0), (big, first)):
+        o = torch.empty_like(q)
+        ops.shared_attention(q, pool, pool.shape[0] - 1, i32(np.where(tables >= 0, tables + offset, -1)), kv, i32([0, 2, 5]), i32([100, 33]), o, ws, status)
+        out.append(o)
+    assert torch.equal(*out) and int(status) == 0
+    # copies among them
+    big[:, :, first:] = small
+    src, dst = list(range(0, used - 1, 2)), list(range(1, used, 2))
+    n = min(len(src), len(dst))
+    ops.copy_pages(big, i32([first + p for p in src[:n]]), i32([first + p for p in dst[:n]]), status)
+    want = small[0].clone()
+    want[:, dst[:n]] = small[0][:, src[:n]]
+    for layer in range(layers):
+        assert torch.equal(big[layer, :, first:], want)
+    assert int(status) == 0
+
+
+def test_logits_whose_rows_are_far_apart(ws, status):
+    rows, vocab, stride = 6, 30001, 450_000_001
+    x = torch.randn(rows, vocab, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).bfloat16()
+    far = torch.empty(stride * (rows - 1) + vocab, dtype=torch.bfloat16, device=DEV)
+    view = far.as_strided((rows, vocab), (stride, 1))
+    view.copy_(x)
+    out = []
+    for logits in (x, view):
+        s = torch.zeros(2, 3, device=DEV)
+        o = [torch.empty(2, 8, device=DEV), *(torch.empty(2, 8, dtype=torch.int32, device=DEV) for _ in range(2))]
+        lse = torch.empty(rows, device=DEV)
+        ops.beam_select(logits, s, *o, ws, status, lse=lse)
+        out.append([*o, lse])
+    for a, b in zip(*out):                                # (rows begin at other places of a tile: sums are rounded elsewhere)
+        assert torch.equal(a, b) if a.dtype == torch.int32 else float((a - b).abs().max()) <= 1e-5
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("n,beams", [(1, 8), (512, 8), (128, 32)])
+def test_rows_of_the_largest_pool_fork_as_those_of_a_small_one(n, beams, ws, status):
+    rng = np.random.default_rng(n)
+    ctx, tables, shares, free, num = ref.shared_rows(rng, n, beams, [int(x) for x in rng.integers(0, 90, n)], n * beams + 9)
+    parent = [int(r * beams + rng.integers(0, beams)) if rng.random() < 0.95 else -1 for r in range(n) for _ in range(beams)]
+    most, out = 1 << 24, []
+    for pages in (num, most):
+        at = pages - num
+        t = [i32(parent), i32(ctx), i32(np.where(tables >= 0, tables + at, -1)), torch.zeros(pages, dtype=torch.int32, device=DEV),
+             torch.full((pages,), -5, dtype=torch.int32, device=DEV), i32([len(free)]), *(torch.empty(n * beams, dtype=torch.int32, device=DEV) for _ in range(3))]
+        t[3][at:] = i32(shares)
+        t[4][:len(free)] = i32(free) + at
+        ops.fork_pages(*t, ws, status)
+        count = int(t[5])
+        back = lambda x: torch.where(x >= 0, x - at, x)  # noqa: E731
+        assert int(t[3][:at].abs().sum()) == 0 and bool((t[4][num:] == -5).all())
+        out.append([t[1], back(t[2]), t[3][at:], back(t[4][:count]), t[5], back(t[6]), back(t[7]), t[8]])
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert int(status) == 0 and not bool(ws[-(2 << 20):].any()) and not bool(ws[:64 << 10].any())
+
+
+@pytest.mark.parametrize("pages", [1 << 21, (1 << 21) - 37])
+def test_the_largest_pool_that_is_compacted(pages, ws, status):
+    rng, rows, width = np.random.default_rng(pages), 4096, 300
+    name = rng.permutation(pages)
+    ctx = rng.integers(0, width * 16 + 1, rows)
+    owned = -(-ctx // 16)
+    tables = np.full((rows, width), -1, dtype=np.int64)
+    mine = np.arange(width)[None] < owned[:, None]
+    tables[mine] = name[:int(owned.sum())]
+    used = np.zeros(pages, dtype=bool)
+    used[tables[mine]] = True
+    free, keep = rng.permutation(np.nonzero(~used)[0]), int(pages * 0.7)
+    shares = np.where(used, rng.integers(0, 5, pages), 0)
+    src, dst = np.nonzero(used[keep:])[0] + keep, np.nonzero(~used[:keep])[0]
+    moves = len(src)
+    assert 0 < moves < len(dst)
+    to = np.arange(pages)
+    to[src] = dst[:moves]
+    t = [i32(ctx), i32(tables), i32(shares), i32(np.concatenate([free, np.full(pages - len(free), -5)])), i32([len(free)]),
+         *(torch.empty(pages - keep, dtype=torch.int32, device=DEV) for _ in range(2))]
+    ops.compact_pages(keep, *t, ws, status)
+    got = [x.cpu().numpy() for x in t]
+    assert int(status) == 0
+    assert np.array_equal(got[5], np.concatenate([src, np.full(pages - keep - moves, -1)])) and np.array_equal(got[6][:moves], dst[:moves])
+    assert np.array_equal(got[1], np.where(mine, to[tables.clip(0)], -1))
+    want = shares.copy()
+    want[dst[:moves]], want[src] = shares[src], 0
+    assert np.array_equal(got[2], want)
+    rest = np.concatenate([dst[moves:], np.arange(keep, pages)])[::-1]
+    assert np.array_equal(got[3][:len(rest)], rest) and bool((got[3][len(rest):] == -5).all()) and int(got[4][0]) == len(rest)
+    assert not bool(ws[-(2 << 20):].any())
+
+
+def test_calls_behind_one_another_share_a_workspace(ws, status):
+    """Selections of different shapes, attention, forks and compactions on one stream without a pause give what each gives by itself."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    shapes = [(64, 8, 20000, 8), (1, 32, 152064, 32), (4096, 1, 33, 2), (3, 5, 7001, 5)]
+    xs = [torch.randn(n * b, v, generator=g, device=DEV) for n, b, v, _ in shapes]
+
+    def select(i):
+        n, b, _, k = shapes[i]
+        o = [torch.empty(n, k, device=DEV), *(torch.empty(n, k, dtype=torch.int32, device=DEV) for _ in range(2))]
+        ops.beam_select(xs[i], torch.zeros(n, b, device=DEV), *o, ws, status)
+        return o
+
+    alone = []
+    for i in range(4):
+        alone.append(select(i))
+        torch.cuda.synchronize()
+    for _ in range(3):
+        together = [select(i) for i in (0, 1, 2, 3, 2, 1, 0)]
+        for got, i in zip(together, (0, 1, 2, 3, 2, 1, 0)):
+            assert all(torch.equal(a, b) for a, b in zip(got, alone[i]))
+    assert int(status) == 0
