@@ -23,6 +23,7 @@ from . import binding as B
 from . import device_ops as ops
 
 HEAD_ROWS = 128                       # rows that one hs_head_step samples from
+COPIES = 16384                        # pages that one copy_pages moves: any number of layers and heads fits
 
 
 @dataclass(frozen=True)
@@ -323,7 +324,8 @@ class BeamLoop(DeviceLoop):
         src, dst = (torch.empty(num_pages - n_keep, dtype=torch.int32, device=self.device) for _ in range(2))
         status = torch.zeros_like(self.status)
         ops.compact_pages(n_keep, self.ctx_len, self.tables, self.shares, self.free_list, self.free_count, src, dst, self.workspace, status, sm_budget=self.budget)
-        ops.copy_pages(self.pool, src, dst, status, sm_budget=self.budget)
+        for i in range(0, num_pages - n_keep, COPIES):
+            ops.copy_pages(self.pool, src[i:i + COPIES], dst[i:i + COPIES], status, sm_budget=self.budget)
         if int(status) != 0:
             raise B.HsError(int(status), "compact_pages")
         self.graph = None

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_2608_01785_b200 import binding as B
+from paper_2608_01785_b200 import device_loop
 from paper_2608_01785_b200 import device_ops as ops
 from paper_2608_01785_b200.device_loop import BeamLoop, LoopDims, make_weights
 from tests import beam_ref as R
@@ -170,7 +171,9 @@ def test_the_beams_are_those_of_the_definition(plain, beams, end_token, penalty)
     loop.close()
 
 
-def test_a_request_ends_while_others_go_on_in_a_smaller_pool(plain):
+@pytest.mark.parametrize("copies", [16384, 3])
+def test_a_request_ends_while_others_go_on_in_a_smaller_pool(plain, copies, monkeypatch):
+    monkeypatch.setattr(device_loop, "COPIES", copies)     # (pages that move at a time)
     p = prompts(20, 3, 40)
     loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 3, 3, 60, 80, sum(map(len, p)), 30)
     loop.prefill(p)
