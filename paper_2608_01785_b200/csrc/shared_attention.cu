@@ -20,7 +20,7 @@
 //
 // 64 groups of 8 sequences behind 512 .. 2,048 shared keys, 28 heads on 4 of 128, capped: 87 us against a floor of 44 for the bytes; 256 sequences behind 8,191 shared keys with up
 // to 1,024 own ones: 123 against 47.  The softmax warps bound the shared keys (1,000 cycles a block of 64 keys for two teams), a row's exponentials and the way of P; own keys
-// keep one or two warps of four busy (2,000 cycles).  Plan and first pages are 6 us of a call, the ends and joins of cut tiles 8 to 10.  One group of 4 behind 500 keys: 21 us, all latency.
+// keep one or two warps of four busy (2,000 cycles).  Plan and first pages are 6 us of a call, the ends and joins of cut tiles 8 to 10.  One group of 4 behind 500 keys: 19.5 us, all latency.
 #include <math.h>
 
 #include <algorithm>
@@ -34,7 +34,7 @@ namespace {
 constexpr int SA_THREADS = 384, SA_KEYS = 64, SA_ROWS = 128, SA_MAX_SEQS = HS_SHARED_MAX_SEQS;
 constexpr int SA_TMEM = 512, SA_TEAM_TMEM = 256;         // columns: of a team, S (two buffers of 64, P over their first 32) and O
 constexpr int SA_ITEM_COST = 3;                          // blocks that take as long as a tile's beginning and end
-constexpr int SA_MIN_SHARE = 6, SA_MIN_PART = 2;         // blocks, with the tiles' costs; blocks of a part
+constexpr int SA_MIN_SHARE = 4, SA_MIN_PART = 1;         // blocks, with the tiles' costs; blocks of a part
 constexpr float kRefSlack = 8.f;                         // log2 units by which a row's running maximum may exceed its reference
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -304,7 +304,10 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     plan.group = group;
     plan.tile = tile;
     plan.line = all * units;
-    plan.shares = max(1, min(p.shares, plan.line / SA_MIN_SHARE));
+    // Small calls: a share's blocks come one after the other, and so do the parts that a join reads, so the shares grow with the root of the tiles' lengths.  Measured, with 6 blocks
+    // or more for every length: 4 sequences behind 500 keys 21.2 us (19.5 so), one behind 32,000 with one KV head 55.6 (40.1), 8 behind 16,000 with two 41.9 (33.7).
+    const int least = max(SA_MIN_SHARE, int(sqrtf(float(all) / float(max(plan.tiles, 1)))));
+    plan.shares = max(1, min(p.shares, plan.line / least));
     plan.base = plan.line / plan.shares;
     plan.more = plan.line - plan.base * plan.shares;
   }

@@ -530,7 +530,11 @@ def test_sequences_outside_the_groups_are_left_alone(ws, status):
     c = attention_case(9, [(40, [3, 4]), (40, [5, 6, 7]), (0, [9])], 8, 2, 64, torch.float16)
     whole, whole_lse = run_attention(c, ws, status)
     o, lse = run_attention(c, ws, status, begin=[2, 2, 5], shared=[40, 40])
-    assert torch.equal(o[2:5], whole[2:5]) and torch.equal(lse[2:5], whole_lse[2:5])
+    # Where tiles are cut follows from the lengths of all of a call's sequences, so the two calls may join other parts.  Each is within (2 u + 5e-4) max |v| of the exact
+    # outputs, u = 2^-11, and 3e-4 of the exact lse (check_attention), so they are within twice that of one another.
+    v = c["pool"][1, 1].float()
+    assert float((o[2:5].float() - whole[2:5].float()).abs().max()) <= 2 * (2 * 2.0 ** -11 + 5e-4) * float(v[~v.isnan()].abs().max())
+    assert float((lse[2:5] - whole_lse[2:5]).abs().max()) <= 6e-4
     for rest in (slice(0, 2), slice(5, 6)):
         assert bool((o[rest] == 77.0).all()) and bool((lse[rest] == 55.0).all())
     o, _ = run_attention(c, ws, status, begin=[3, 3, 3], shared=[1, 1])
