@@ -28,7 +28,7 @@ namespace {
 
 constexpr int BS_TEAMS = 4, BS_TEAM = 128, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
 constexpr int BS_PIECES = 8, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
-constexpr int BS_AHEAD = 2;                                              // tiles that are on their way to L2 before they are loaded
+constexpr int BS_AHEAD = 2;                                              // tiles that are on their way to L2 before they are loaded (fp32 rows 45 -> 42 us; 4: 43, 8: 48)
 constexpr int BS_LIST = 512;                                             // candidates that a team ranks at a time
 constexpr int BS_ITEM_COST = 3;                                          // tiles
 constexpr int BS_MAX_PARTS = 64;                                         // of a row
