@@ -456,12 +456,12 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       }
     });
   };
-  // A part has arrived, by one of its four warps (n = 1) or all of it (n = 4).
-  auto arrived = [&](const Item& it, int n) {
-    int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + first_share(place_of(it.number));
-    if (atomicAdd(done, n) == 4 * it.parts - n) {
+  // A part of an item with so many has arrived, by one of its four warps (n = 1) or all of it (n = 4).
+  auto arrived = [&](int number, int parts, int n) {
+    int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + first_share(place_of(number));
+    if (atomicAdd(done, n) == 4 * parts - n) {
       *done = 0;                                         // ready for the next call
-      bar->joins[atomicAdd(&bar->n_joins, 1)] = it.number;
+      bar->joins[atomicAdd(&bar->n_joins, 1)] = number;
     }
   };
 
@@ -972,7 +972,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
           if (it.parts > 1) {
             __threadfence();
             __syncwarp();
-            if (lane == 0) arrived(it, 1);
+            if (lane == 0) arrived(it.number, it.parts, 1);
           }
         }
         tc_fence_before_sync();
@@ -996,6 +996,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       // The tile in the middle, the last item of both teams, in the ring's slot in front of the last.  All rows of both go through their own Q, K and V, which are idle,
       // [columns / 4][128 rows]; then a thread has some columns of one row, and adds up its two or four places.
       const Item& it = tm.ring[rs];
+      const int parts = it.parts, number = it.number;    // (the slot is given back: behind the last barrier here the next share's first item goes into it)
       if (warp < 8) {
         float4* dst = reinterpret_cast<float4*>(q_smem);
         tm.ml[r] = make_float2(row_reference(), l_run);
@@ -1028,7 +1029,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
             w[q] = fast_exp2(x[q].x - zero);
             l = fmaf(x[q].y, w[q], l);
           }
-          const bool whole = it.parts == 1;
+          const bool whole = parts == 1;
           const int64_t row = it.seq0 + i_seq;
           const int head = it.head0 + h;
           RowsPart<DH>& part = reinterpret_cast<RowsPart<DH>*>(static_cast<char*>(a.workspace) + kWsScratch)[it.slot];
@@ -1069,9 +1070,9 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       tc_fence_before_sync();
       __syncthreads();
       tc_fence_after_sync();
-      if (tid == 0 && it.parts > 1) {
+      if (tid == 0 && parts > 1) {
         __threadfence();                                 // (of both teams' part, which the barrier has brought here)
-        arrived(it, 4);
+        arrived(number, parts, 4);
       }
     }
   }

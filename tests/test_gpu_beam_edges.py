@@ -147,3 +147,28 @@ def test_calls_behind_one_another_share_a_workspace(ws, status):
         for got, i in zip(together, (0, 1, 2, 3, 2, 1, 0)):
             assert all(torch.equal(a, b) for a, b in zip(got, alone[i]))
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("groups,hq,hkv,dim,cap", [([(4000, [30] * 36)], 28, 4, 128, 0.0), ([(900, [5, 60, 17, 1]), (2000, [64] * 9), (16, [300, 40])] * 3, 16, 4, 64, 30.0),
+                                                    ([(8000, [40, 1])], 4, 1, 128, 0.0), ([(1500 + 61 * g, [9 + g] * 8) for g in range(12)], 14, 2, 128, 50.0)])
+def test_shared_attention_of_cut_tiles_time_after_time(groups, hq, hkv, dim, cap, ws, status):
+    """Tiles cut between many shares, which one block or a few take one behind the other: every call leaves the bits and the control words of the first."""
+    rng, g = np.random.default_rng(6), torch.Generator(device=DEV).manual_seed(6)
+    kv = [s + n for s, own in groups for n in own]
+    tables, pages = ref.grouped_tables(rng, groups, max(map(ref.pages, kv)) + 1)
+    q = torch.randn(len(kv), hq, dim, generator=g, device=DEV).bfloat16()
+    pool = torch.randn(1, 2, pages, hkv, 16, dim, generator=g, device=DEV).bfloat16()
+    arguments = [pool, 0, i32(tables), i32(kv), i32(np.cumsum([0] + [len(own) for _, own in groups])), i32([s for s, _ in groups])]
+
+    def call(budget):
+        o, lse = torch.full_like(q, 77.0), torch.full((len(kv), hq), 55.0, device=DEV)
+        ops.shared_attention(q, *arguments, o, ws, status, lse=lse, cap=cap, sm_budget=budget)
+        return torch.cat([o.view(torch.int16).flatten().int(), lse.view(torch.int32).flatten()])
+
+    first = call(None)
+    for budget in (1, 2, 5, 9, 37, 74, 147):
+        wrong = torch.zeros(1, dtype=torch.int64, device=DEV)
+        for _ in range(200):
+            wrong += (call(budget) != first).sum() + (ws[:64 << 10] != 0).sum()
+        assert int(wrong) == 0, f"budget {budget}"
+    assert int(status) == 0
