@@ -272,10 +272,17 @@ class BeamLoop(DeviceLoop):
         self.q_len.copy_(ok & (self.steps < self.max_tokens) & (self.ctx_len > 0) & (self.done.flatten() == 0))
 
     def prefill(self, prompts: Sequence[Sequence[int]]) -> None:
-        """Runs all prompts as one chunk, each in the first row of its request, and begins the beams with its n_beams most likely tokens.  Prompts that do not fit leave a
-        status and no beams."""
+        """Begins a run: all prompts as one chunk, each in the first row of its request, then the beams with its n_beams most likely tokens.  Prompts that do not fit leave a
+        status and no beams.  What a run before has left is forgotten; all of its requests have to be finished."""
         b, lens, n = self._prompt_buffers, [len(p) for p in prompts], self.n_requests
         assert len(lens) == n and min(lens) >= 1 and sum(lens) <= b["tokens"].numel()
+        if bool((self.ctx_len != 0).any()):
+            raise RuntimeError("requests of a run before still hold tokens: finish them first")
+        for t in (self.steps, self.length, self.done, self.q_len):
+            t.zero_()
+        self.scores.fill_(-math.inf)
+        for t in (self.past_parent, self.past_token):
+            t.fill_(-1)
         lengths = torch.tensor(lens, dtype=torch.int32, device=self.device)
         q_len = torch.zeros_like(self.q_len)
         q_len[::self.n_beams] = lengths

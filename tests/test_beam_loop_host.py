@@ -257,3 +257,44 @@ def test_a_pool_of_no_size_is_refused(plain, n_keep):
     loop.shrink(60)
     assert loop.pool.shape[2] == 60
     loop.close()
+
+
+@pytest.mark.parametrize("steps", [3, 9])
+@pytest.mark.parametrize("penalty", [0.0, 0.9])
+def test_a_second_run_begins_like_the_first(plain, steps, penalty):
+    """Requests that were ended leave nothing to those that are prefilled behind them, fewer steps than max_tokens or more."""
+    first, second = prompts(20, 3), [p[::-1] for p in prompts(35, 18)]
+    loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 2, 3, 60, 64, 60, 8, end_token=7, length_penalty=penalty)
+    loop.prefill(first)
+    for _ in range(steps):
+        loop.step()
+    loop.finish(torch.ones(2, dtype=torch.int32))
+    assert int(loop.free_count) == 60
+    for p in (second, first):
+        loop.prefill(p)
+        for step in range(1, 9):
+            check_pages(loop)
+            for r, got in enumerate(loop.hypotheses()):
+                same(got, search(p[r], 3, step, 7, penalty))
+            loop.step()
+        assert int(loop.status) == 0 and int(loop.steps) == 8
+        loop.finish(torch.ones(2, dtype=torch.int32))
+    loop.close()
+
+
+def test_a_run_is_not_begun_over_another(plain):
+    p = prompts(20, 3)
+    loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 2, 3, 60, 64, 60, 8)
+    loop.prefill(p)
+    loop.step()
+    before = loop.hypotheses()
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="finish"):
+            loop.prefill(p)
+        assert loop.hypotheses() == before
+        check_pages(loop)
+        loop.finish(torch.tensor([0, 1], dtype=torch.int32))
+        before = [before[0], []]
+    loop.step()
+    same(loop.hypotheses()[0], search(p[0], 3, 3))
+    loop.close()

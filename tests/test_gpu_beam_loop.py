@@ -166,3 +166,29 @@ def test_command_runs(capsys):
     device_loop.main(["--requests", "3", "--tokens", "20", "--beams", "4"])
     out = capsys.readouterr().out
     assert "requests of 4 beams" in out and "pages free again" in out
+
+
+def test_a_second_run_is_that_of_a_new_loop():
+    """The captured step goes on with other prompts, behind a run that had come to its last token."""
+    dims, w, prompts = make()
+    others = [p[::-1] for p in prompts[::-1]]
+    used, new = (BeamLoop(dims, w, 5, 3, 90, 160, sum(map(len, prompts)), 10, length_penalty=0.5) for _ in range(2))
+    used.prefill(prompts)
+    for _ in range(12):
+        used.step()
+    used.finish(torch.ones(5, dtype=torch.int32, device="cuda"))
+    assert int(used.free_count) == 90
+    for loop in (used, new):
+        loop.prefill(others)
+        for _ in range(9):
+            loop.step()
+        torch.cuda.synchronize()
+        assert int(loop.status) == 0 and int(loop.steps) == 10
+        check_pages(loop)
+    assert used.hypotheses() == new.hypotheses()
+    for name in ("ctx_len", "scores", "done", "length", "past_parent", "past_token", "q_len", "steps"):
+        assert torch.equal(getattr(used, name), getattr(new, name)), name
+    with pytest.raises(RuntimeError, match="finish"):
+        used.prefill(others)
+    for loop in (used, new):
+        loop.close()
