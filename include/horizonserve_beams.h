@@ -42,8 +42,8 @@ extern "C" {
  * A weighted score of -infinity or NaN is no continuation: tokens and beams at -infinity are left out, and so is a beam whose row holds NaN or +infinity or
  * nothing above -infinity.  Where there are fewer than n_out, the rest have score -infinity, parent and token -1 and done 0.
  * lse[r n_beams + b] = L (0 for a beam that is done, whose logits are not read; NaN where the row holds NaN or +infinity).
- * Logits of any row stride and alignment of their type.  Exponentials and their sums in fp32, what is ranked in 64 bits from there on, so the order is that of scores
- * about 1e-7 from the exact ones; equal logits of a beam are ranked by their tokens.
+ * Logits of any row stride and alignment of their type.  Exponentials in fp32, sums of a few of them too, and what is ranked in 64 bits from there on: L is within 2.5e-6 of
+ * the exact one (1e-7 as a rule), and the order is that of scores as near as that; equal logits of a beam are ranked by their tokens.
  * Outputs overlap no inputs.  n_requests 1 .. HS_DEVICE_MAX_SEQS, n_requests * n_beams at most 65536.
  */
 typedef struct {

@@ -6,7 +6,7 @@
 // Work.  An item is a row or one of its equal parts.  Four teams of four warps share a block, each with an item of its own from a queue, so that one team's
 // beginning and end hide behind the others' streams.  A thread reads eight 16-byte pieces of a tile while it works on the last tile's, and keeps
 //   M, s        a whole number M near the maximum in log2 units, and s = sum 2^(k x - M), k = scale log2(e): references are changed and joined by exact
-//               powers of two.  k is the sum of two fp32 numbers, and a tile's sum is added with its rounding error kept, so that log s is good to about 1e-7.
+//               powers of two.  k is the sum of two fp32 numbers, and a tile's sum is added with its rounding error kept, so that log s is good to 2.5e-6 at worst and 1e-7 as a rule.
 //               (A part whose largest logit is 2^20 of those units from zero, as in a row masked with its type's lowest number from end to end, is
 //               summed a second time with that logit as its reference.)
 //   best, tile  its largest logit, and the first tile that has it; second, with its tile, the largest of its other tiles, third of those that are left.
@@ -164,16 +164,25 @@ struct Row {
   }
 };
 
-// A warp's part of sum 2^(k (x - ref)) over tiles tile0 .. tile1 - 1, in every lane.
+// A warp's part of sum 2^(k (x - ref)) over tiles tile0 .. tile1 - 1, in every lane.  (x - ref is exact where it counts: 32 of k's log2 units are far less than half of
+// ref.  A thread adds up to 16 numbers one after the other; from there on the sum is held in 64 bits, as equal addends are rounded to the same side every time.)
 template <int TYPE>
-__device__ __noinline__ float far_sum(const Row<TYPE>& r, int tile0, int tile1, float ref, float k, int tid) {
-  float v = 0.f;
+__device__ __noinline__ double far_sum(const Row<TYPE>& r, int tile0, int tile1, float ref, float k_hi, float k_lo, int tid) {
+  double v = 0.0;
 #pragma unroll 1
-  for (int i = tile0 * BS_PIECES; i < tile1 * BS_PIECES; ++i) {
-    float x[Piece<TYPE>::kPer];
-    Piece<TYPE>::get(r.any(i * BS_TEAM + tid), x);
+  for (int tile = tile0; tile < tile1; ++tile) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int i = tile * BS_PIECES; i < (tile + 1) * BS_PIECES; ++i) {
+      float x[Piece<TYPE>::kPer];
+      Piece<TYPE>::get(r.any(i * BS_TEAM + tid), x);
 #pragma unroll
-    for (int e = 0; e < Piece<TYPE>::kPer; ++e) v += exp2f((x[e] - ref) * k);
+      for (int e = 0; e < Piece<TYPE>::kPer; ++e) {
+        const float d = x[e] - ref;
+        sum[e & 3] += exp2f(fmaf(d, k_hi, d * k_lo));
+      }
+    }
+    v += double((sum[0] + sum[1]) + (sum[2] + sum[3]));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -329,10 +338,10 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
       team_sync();
       if (top > -INFINITY && top < INFINITY && !(fabsf(top * p.k_hi) < BS_FAR)) {
         ref = top;
-        const float v = far_sum(r, tile0, tile1, ref, p.k_hi, tid);
+        const double v = far_sum(r, tile0, tile1, ref, p.k_hi, p.k_lo, tid);
         if (lane == 0) {
           t.m[warp] = 0.f;
-          t.sum[warp] = double(v);
+          t.sum[warp] = v;
         }
       }
       // ------------------------------------------------------------------ what reaches it

@@ -613,3 +613,20 @@ def test_on_other_streams_and_in_a_graph(ws, status):
             assert torch.equal(a.view(torch.int16) if a.dtype != torch.int32 else a, b.view(torch.int16) if b.dtype != torch.int32 else b)
         captured["x"].copy_(captured["x"].roll(i + 1, 0))
     assert int(status) == 0 and control_words_are_zero(other_ws)
+
+
+@pytest.mark.parametrize("offset", [5e6, -5e6, 1e8])
+@pytest.mark.parametrize("scale", [1.0, 0.8, 0.3, 3.7])
+@pytest.mark.parametrize("below", [(0, 1), (0, 1, 2), (0, 9, 9, 9, 9, 9, 9), (0, 3, 5, 11, 17)])
+def test_many_logits_far_from_zero(offset, scale, below, ws, status):
+    """Whole rows (one for each team of threads of the device, so that none is cut) of few different logits, whose distances are small multiples of their type's step there: equal numbers are added up, so
+    what each addition rounds away has one sign."""
+    rows, vocab, step = 4 * ops.sm_count(0), 152064, float(np.spacing(np.float32(abs(offset))))
+    away = step * torch.tensor(below, dtype=torch.float64)[torch.arange(vocab) % len(below)]
+    x = (offset - away).float()
+    assert bool((x.double() == offset - away).all())
+    score, parent, token, over, _ = run_select(x.to(DEV).expand(rows, vocab).contiguous(), np.zeros((rows, 1), dtype=np.float32), 8, ws, status, scale=scale)
+    assert torch.equal(token, torch.nonzero(x == offset)[:8, 0].int().to(DEV).expand(rows, 8)) and torch.equal(parent, torch.arange(rows, device=DEV).int()[:, None].expand(rows, 8))
+    # log sum is off by 2.5e-6 at most (check_select), as a thread adds up at most 16 numbers before the sum goes on in more bits, and a score is rounded once
+    want = -math.log(float(torch.exp(-float(np.float32(scale)) * away).sum()))
+    assert float((score.double() - want).abs().max()) <= 2.5e-6 + 2.0 ** -24 * abs(want) and int(status) == 0
