@@ -20,6 +20,7 @@
 // each, follow at once where rows are not cut, and a choice takes 4.  Cutting rows in two for a second round that hides the ends costs more than it hides (60 us).  One request of 4 beams: 13.0 us,
 // of which the stream is 2: launch, an item's end (2.5), its delivery (2) and the choice (5) are round trips and code that runs once.
 #include <algorithm>
+#include <limits>
 
 #include "paged_scores.cuh"
 
@@ -735,8 +736,8 @@ cudaError_t launch_beam_select(const hs_beam_select_t& a, int sm_count, int sm_b
   const double k = p.k = double(a.scale) * 1.4426950408889634074;
   p.k_hi = float(k);
   if (double(p.k_hi) > k) p.k_hi = std::nextafterf(p.k_hi, 0.f);
-  // (above zero, so that -infinity stays -infinity under both)
-  p.k_lo = std::max(float(k - double(p.k_hi)), 1e-37f);
+  // (above zero, so that -infinity stays -infinity under both; by no more than the smallest number, as logits may be large where the scale is small)
+  p.k_lo = std::max(float(k - double(p.k_hi)), std::numeric_limits<float>::denorm_min());
   // Rows are cut into equal parts so that the teams' rounds are even and short; a round costs its tiles and about BS_ITEM_COST more for the item's end.
   const int64_t rows = int64_t(a.n_requests) * a.n_beams;
   const int per = a.type == HS_TYPE_F32 ? 4 : 8, tiles = (a.vocab + per - 1 + BS_TILE_PIECES * per - 1) / (BS_TILE_PIECES * per);

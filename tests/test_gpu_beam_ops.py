@@ -630,3 +630,13 @@ def test_many_logits_far_from_zero(offset, scale, below, ws, status):
     # log sum is off by 2.5e-6 at most (check_select), as a thread adds up at most 16 numbers before the sum goes on in more bits, and a score is rounded once
     want = -math.log(float(torch.exp(-float(np.float32(scale)) * away).sum()))
     assert float((score.double() - want).abs().max()) <= 2.5e-6 + 2.0 ** -24 * abs(want) and int(status) == 0
+
+
+@pytest.mark.parametrize("scale,largest", [(1e-30, 2e31), (1e-36, 1e37), (1e-37, 2e38), (3e-38, 3e38), (1e-40, 3e38)])
+@pytest.mark.parametrize("vocab", [7, 5000])
+def test_small_scales_of_large_logits(scale, largest, vocab, ws, status):
+    x = (largest / 4 * torch.randn(6, vocab, generator=torch.Generator().manual_seed(vocab))).clamp(-largest, largest)
+    x[1, ::3] = -INF
+    x[2, :] = largest
+    check_select(x, beam_scores(np.random.default_rng(2), 3, 2), 5, ws, status, scale=scale)
+    assert int(status) == 0
