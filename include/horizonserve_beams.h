@@ -41,6 +41,7 @@ extern "C" {
  * A weight that is not above zero gives its beam no continuation, with the status INVALID_ARG; a call of such weights is done otherwise.
  * A weighted score of -infinity or NaN is no continuation: tokens and beams at -infinity are left out, and so is a beam whose row holds NaN or +infinity or
  * nothing above -infinity.  Where there are fewer than n_out, the rest have score -infinity, parent and token -1 and done 0.
+ * A finite score or L that fp32 does not hold is written as its largest number of that sign.
  * lse[r n_beams + b] = L (0 for a beam that is done, whose logits are not read; NaN where the row holds NaN or +infinity).
  * Logits of any row stride and alignment of their type.  Exponentials in fp32, sums of a few of them too, and what is ranked in 64 bits from there on: L is within 2.5e-6 of
  * the exact one (1e-7 as a rule), and the order is that of scores as near as that; equal logits of a beam are ranked by their tokens.

@@ -19,6 +19,8 @@
 // 64 requests of 8 beams over 152,064 bf16 logits: 42 us.  The stream ends after 26 of them on average and 30 at most (5.2 TB/s; the exponentials alone would take 20), the items' ends, of 4 us
 // each, follow at once where rows are not cut, and a choice takes 4.  Cutting rows in two for a second round that hides the ends costs more than it hides (60 us).  One request of 4 beams: 13.0 us,
 // of which the stream is 2: launch, an item's end (2.5), its delivery (2) and the choice (5) are round trips and code that runs once.
+#include <float.h>
+
 #include <algorithm>
 #include <limits>
 
@@ -77,6 +79,12 @@ __device__ __forceinline__ Key order_of(double x) {
 __device__ __forceinline__ Key token_key(float x, int v) { return (Key(order_of(x)) << 32) | (0xffffffffu - unsigned(v)); }
 __device__ __forceinline__ int token_of(Key k) { return int(0xffffffffu - unsigned(k)); }
 __device__ __forceinline__ float logit_of(Key k) { return float_of(uint32_t(k >> 32)); }
+
+// In fp32, where a finite number beyond its range is held to its largest: a score of -infinity means no continuation.
+__device__ __forceinline__ float held(double x) {
+  const float f = float(x);
+  return fabsf(f) < INFINITY || fabs(x) == double(INFINITY) || x != x ? f : copysignf(FLT_MAX, f);
+}
 
 // The kPer logits of a 16-byte piece.
 template <int TYPE>
@@ -520,7 +528,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
           t.base[b] = base;
           t.weight[b] = weight;
           t.state[b] = !(weight > 0.f) ? 0 : over ? 2 : bad || m == -INFINITY ? 0 : 1;
-          if (a.lse) a.lse[row0 + b] = over ? 0.f : bad ? NAN : m == -INFINITY ? -INFINITY : float(double(a.scale) * double(ref) + lse);
+          if (a.lse) a.lse[row0 + b] = over ? 0.f : bad ? NAN : m == -INFINITY ? -INFINITY : held(double(a.scale) * double(ref) + lse);
           if (!(weight > 0.f)) atomicExch(a.status, kErrInvalidArg);
         }
       }
@@ -541,7 +549,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         if (n >= BS_LIST) return;
         t.list[n] = rank;
         t.flat[n] = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
-        t.score[n] = float(score);
+        t.score[n] = held(score);
       };
       auto candidate = [&](int c, Key& flat, float& score) {             // candidate c of all: its rank, beam and token, and score
         const int l = c / n_out, b = l / p.parts;
@@ -549,7 +557,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         double s;
         const Key rank = rank_of(b, c == b * p.parts * n_out, k, s);
         flat = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
-        score = float(s);
+        score = held(s);
         return rank;
       };
       if (few) {

@@ -640,3 +640,20 @@ def test_small_scales_of_large_logits(scale, largest, vocab, ws, status):
     x[2, :] = largest
     check_select(x, beam_scores(np.random.default_rng(2), 3, 2), 5, ws, status, scale=scale)
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_scores_beyond_fp32_are_held_to_its_largest_number(weighted, ws, status):
+    """Masked with the type's lowest value, sharpened, few tokens left: the continuations behind those have scores, though none that fp32 holds."""
+    most, x = float(torch.finfo(torch.float32).max), torch.full((4, 900), torch.finfo(torch.float32).min)
+    x[:, 5], x[:, 7], x[2] = 1.0, 2.0, most
+    scores = np.array([[-1.0, -2.0], [-3.0, -most]], dtype=np.float32)
+    weight = np.full((2, 2), 0.25, dtype=np.float32) if weighted else None
+    score, parent, token, _, lse = run_select(x.to(DEV), scores, 6, ws, status, weight=weight, scale=2.0)
+    want, _ = ref.select(x.double().numpy(), scores, None, weight, 6, -1, 2.0)
+    assert [(int(p), int(t)) for p, t in zip(parent.flatten(), token.flatten())] == [(2 * r + i, v) for r in range(2) for _, i, v, _, _ in want[r]]
+    exact = torch.tensor([[s for _, _, _, s, _ in w] for w in want], dtype=torch.float64)
+    assert float(exact.min()) < -most
+    held = exact.clamp(-most, most)
+    assert bool(((score.cpu().double() - held).abs() <= 2.5e-6 + 2.0 ** -24 * held.abs()).all()) and bool(score.isfinite().all())
+    assert float(lse[2]) == most and int(status) == 0     # (2 * most and the logarithm of 900)
