@@ -36,7 +36,7 @@ extern "C" {
  * Request r has beams b in 0 .. n_beams - 1 with accumulated log probability S_b = scores[r][b] and the logit row x = logits[r n_beams + b].
  * A beam that is not done continues with every token v,  s = S_b + scale x_v - L,  L = log sum_v exp(scale x_v);  one that is done (done != 0) has one
  * continuation, itself:  s = S_b,  v = end_token.  Continuations are ranked by weight[r][b] s (by s without weights), the largest first,
- * ties to the lower beam and then to the lower token, and the first n_out of them are written:
+ * ties to the lower beam, then to the larger logit (a score far from zero swallows their differences) and then to the lower token, and the first n_out of them are written:
  *     out_score = s,   out_parent = r n_beams + b,   out_token = v,   out_done = whether the beam was done or v is end_token
  * A weight that is not above zero gives its beam no continuation, with the status INVALID_ARG; a call of such weights is done otherwise.
  * A weighted score of -infinity or NaN is no continuation: tokens and beams at -infinity are left out, and so is a beam whose row holds NaN or +infinity or

@@ -56,6 +56,7 @@ struct alignas(16) SelectTeam {
   Key group[64];
   int rank[64];
   Key list[BS_LIST], flat[BS_LIST];
+  int token[BS_LIST];
   float score[BS_LIST];
   double sum[BS_WARPS], lse[HS_MAX_BEAMS];
   float m[BS_WARPS], top[BS_WARPS], base[HS_MAX_BEAMS], weight[HS_MAX_BEAMS], ref[HS_MAX_BEAMS];
@@ -77,6 +78,12 @@ __device__ __forceinline__ Key order_of(double x) {
 }
 // The larger logit is the larger key, and of equal ones the lower token.
 __device__ __forceinline__ Key token_key(float x, int v) { return (Key(order_of(x)) << 32) | (0xffffffffu - unsigned(v)); }
+// Candidates of equal rank: the lower beam first, then the larger logit (next to a score that is far from zero the logits' differences vanish in 64 bits, too), then
+// the lower place among the beam's candidates, which is the lower token.
+constexpr int BS_PLACE_BITS = 11;
+__device__ __forceinline__ Key tie_key(int b, Key k, int place) { return (Key(b) << (32 + BS_PLACE_BITS)) | (Key(~uint32_t(k >> 32)) << BS_PLACE_BITS) | unsigned(place); }
+__device__ __forceinline__ int beam_of(Key flat) { return int(flat >> (32 + BS_PLACE_BITS)); }
+__device__ __forceinline__ int place_of(Key flat) { return int(flat) & ((1 << BS_PLACE_BITS) - 1); }
 __device__ __forceinline__ int token_of(Key k) { return int(0xffffffffu - unsigned(k)); }
 __device__ __forceinline__ float logit_of(Key k) { return float_of(uint32_t(k >> 32)); }
 
@@ -544,27 +551,29 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         const double ranked = double(t.weight[b]) * score;
         return score > -INFINITY && ranked > -INFINITY ? order_of(ranked) : Key(0);
       };
-      auto append = [&](int b, Key rank, Key k, double score) {
+      const int per_beam = p.parts * n_out;              // candidates
+      auto append = [&](int b, Key rank, Key k, int c, double score) {
         const int n = atomicAdd(&t.n_list, 1);
         if (n >= BS_LIST) return;
         t.list[n] = rank;
-        t.flat[n] = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
+        t.flat[n] = tie_key(b, k, c - b * per_beam);
+        t.token[n] = t.state[b] == 2 ? a.end_token : token_of(k);
         t.score[n] = held(score);
       };
-      auto candidate = [&](int c, Key& flat, float& score) {             // candidate c of all: its rank, beam and token, and score
+      auto candidate = [&](int c, Key& flat, float& score) {             // candidate c of all: its rank, its place among those of equal rank, and score
         const int l = c / n_out, b = l / p.parts;
         const Key k = t.state[b] == 2 ? 0 : __ldcg(&lists[l].keys[c - l * n_out]);
         double s;
-        const Key rank = rank_of(b, c == b * p.parts * n_out, k, s);
-        flat = (Key(b) << 32) | unsigned(t.state[b] == 2 ? a.end_token : token_of(k));
+        const Key rank = rank_of(b, c == b * per_beam, k, s);
+        flat = tie_key(b, k, c - b * per_beam);
         score = held(s);
         return rank;
       };
       if (few) {
         const int b = min(tid / n_out / p.parts, a.n_beams - 1);
         double score;
-        const Key rank = tid < n_cand ? rank_of(b, tid == b * p.parts * n_out, early[0], score) : 0;
-        if (rank != 0) append(b, rank, early[0], score);
+        const Key k = t.state[b] == 2 ? 0 : early[0], rank = tid < n_cand ? rank_of(b, tid == b * per_beam, k, score) : 0;
+        if (rank != 0) append(b, rank, k, tid, score);
         team_sync();
       } else {
         // Every part's keys fall.  With d = n_out / lists (up), each list's d-th key and the n_out / d-th largest (up) of those, there are n_out candidates from that one up:
@@ -592,7 +601,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
             int k0 = 4 * (x - l * quarters);
             if (t.state[b] != 1) {
               const Key rank = rank_of(b, l == b * p.parts && k0 == 0, 0, score);
-              if (rank != 0 && rank >= least) append(b, rank, 0, score);
+              if (rank != 0 && rank >= least) append(b, rank, 0, l * n_out, score);
               continue;
             }
             bool on = true;
@@ -606,7 +615,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
                 if (!on) break;
                 const Key rank = rank_of(b, false, keys[e], score);
                 on = rank != 0 && rank >= least;
-                if (on) append(b, rank, keys[e], score);
+                if (on) append(b, rank, keys[e], l * n_out + k0 + e, score);
               }
               k0 += 4;
             } while (on && quarters == 1 && k0 < n_out);
@@ -671,8 +680,11 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
         }
         if (tid < found) {
           t.list[tid] = t.list[BS_TEAM + tid];
-          t.flat[tid] = t.flat[BS_TEAM + tid];
+          const Key f = t.flat[BS_TEAM + tid];
+          const int b = beam_of(f), c = place_of(f), in_list = c / n_out;
+          t.flat[tid] = f;
           t.score[tid] = t.score[BS_TEAM + tid];
+          t.token[tid] = t.state[b] == 2 ? a.end_token : token_of(__ldcg(&lists[b * p.parts + in_list].keys[c - in_list * n_out]));
         }
         n = found;
         team_sync();
@@ -693,7 +705,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
           above += int(r > k) | (int(r == k) & int(g < f));
         }
         if (above >= n_out) continue;
-        const int b = int(f >> 32), token = int(unsigned(f));
+        const int b = beam_of(f), token = t.token[i];
         put(above, t.score[i], row0 + b, token, t.state[b] == 2 || token == a.end_token ? 1 : 0);
       }
       if (tid >= n && tid < n_out) put(tid, -INFINITY, -1, -1, 0);
@@ -718,6 +730,7 @@ __global__ void __launch_bounds__(BS_THREADS, 1) beam_select_kernel(const __grid
 
 constexpr int kSelectSmem = BS_TEAMS * int(sizeof(SelectTeam)) > kMinSmemBytes ? BS_TEAMS * int(sizeof(SelectTeam)) : kMinSmemBytes;
 static_assert(sizeof(SelectTeam) % 16 == 0 && kSelectSmem <= 227 * 1024, "fits one SM");
+static_assert(BS_MAX_PARTS * HS_MAX_BEAMS <= 1 << BS_PLACE_BITS, "a beam's candidates");
 static_assert(BS_LIST >= BS_TEAM + HS_MAX_BEAMS, "the list's upper half holds the continuations");
 constexpr int64_t kMaxRows = 65536;
 static_assert(kMaxRows * sizeof(SelectPart) <= kWsScratchBytes, "a part per row");

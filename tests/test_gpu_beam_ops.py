@@ -657,3 +657,25 @@ def test_scores_beyond_fp32_are_held_to_its_largest_number(weighted, ws, status)
     held = exact.clamp(-most, most)
     assert bool(((score.cpu().double() - held).abs() <= 2.5e-6 + 2.0 ** -24 * held.abs()).all()) and bool(score.isfinite().all())
     assert float(lse[2]) == most and int(status) == 0     # (2 * most and the logarithm of 900)
+
+
+@pytest.mark.parametrize("b,vocab,n_out", [(1, 152064, 8), (4, 152064, 8), (32, 152064, 32), (3, 50, 5), (8, 9000, 32), (2, 40, 32)])
+@pytest.mark.parametrize("start", [-1e30, float(np.finfo(np.float32).min), 1e30])
+def test_beams_so_far_away_that_their_continuations_tie(b, vocab, n_out, start, ws, status):
+    """A score next to which differences of logits vanish, in 64 bits too: the order is that of the exact scores, beam by beam and from the largest logit down."""
+    x = logits(torch.Generator().manual_seed(vocab), 2 * b, vocab, torch.float32)
+    x[:, 3] = x.amax(1)                                   # (a logit that a row has twice: the lower token first)
+    scores = np.full((2, b), start, dtype=np.float32)
+    scores[1, -1] *= 2.0 if start == -1e30 else 0.5       # (one beam of the second request is behind the others or in front of them)
+    over = np.zeros((2, b), dtype=np.int32)
+    over[0, b // 2] = int(b > 2)
+    score, parent, token, _, _ = run_select(x.to(DEV), scores, n_out, ws, status, done=over, end=5)
+    order = torch.sort(x.double(), dim=1, descending=True, stable=True).indices
+    for r in range(2):
+        want = []
+        for i in sorted(range(b), key=lambda i: -float(scores[r, i])):
+            want += [(r * b + i, 5)] if over[r, i] else [(r * b + i, int(v)) for v in order[r * b + i][:n_out]]
+        got = list(zip(parent[r].tolist(), token[r].tolist()))
+        assert got[:len(want)] == want[:n_out] and set(got[len(want):]) <= {(-1, -1)}
+        assert all(s == scores[r, p - r * b] for s, p in zip(score[r].cpu().numpy(), parent[r].tolist()) if p >= 0)
+    assert int(status) == 0
