@@ -214,6 +214,8 @@ class BeamLoop(DeviceLoop):
             raise ValueError(f"n_requests: 1 .. {ops.MAX_SHARED_SEQS} rows of all beams are possible")
         if max_tokens < 1:
             raise ValueError("max_tokens: at least 1")
+        if not (math.isfinite(length_penalty) and abs(length_penalty) * math.log(max_tokens + 1) <= 87.0):     # (fp32 holds e^-87 .. e^87; steps behind max_tokens rank, too)
+            raise ValueError("length_penalty: max_tokens + 1 to that power, and its inverse, have to be fp32 numbers")
         if dims.window != 0:
             raise ValueError("window: beams attend to all keys")
         super().__init__(dims, weights, n_requests * n_beams, num_pages, max_positions, max_prompt_tokens, n_top=1, sm_budget=sm_budget)

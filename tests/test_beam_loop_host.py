@@ -298,3 +298,22 @@ def test_a_run_is_not_begun_over_another(plain):
     loop.step()
     same(loop.hypotheses()[0], search(p[0], 3, 3))
     loop.close()
+
+
+@pytest.mark.parametrize("penalty,tokens", [(40.0, 10), (-40.0, 10), (13.0, 1000), (-13.0, 1000), (math.nan, 4), (math.inf, 1), (-math.inf, 4), (200.0, 1)])
+def test_a_length_penalty_whose_weights_leave_fp32_is_refused(plain, penalty, tokens):
+    """Weights of 0 would end every beam, and infinite ones too."""
+    with pytest.raises(ValueError, match="length_penalty"):
+        Loop(DIMS, make_weights(DIMS, device="cpu"), 1, 2, 60, 64, 8, tokens, length_penalty=penalty)
+
+
+@pytest.mark.parametrize("penalty", [30.0, -30.0])
+def test_the_largest_length_penalties(plain, penalty):
+    p = prompts(3)
+    loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 1, 3, 60, 64, 8, 15, end_token=7, length_penalty=penalty)
+    loop.prefill(p)
+    for _ in range(14):
+        loop.step()
+    assert int(loop.status) == 0 and int(loop.steps) == 15
+    same(loop.hypotheses()[0], search(p[0], 3, 15, 7, penalty))
+    loop.close()
