@@ -324,22 +324,25 @@ class BeamLoop(DeviceLoop):
 
     def shrink(self, n_keep: int) -> None:
         """Makes the pool n_keep pages large: pages behind move below, and the memory of the rest is given back.  Raises HsError, and changes nothing, where there is no
-        room.  The next step is captured anew."""
+        room or a block table names a page that is not a row's to have.  The next step is captured anew.  Both pools exist until the smaller one is filled: a layer's pages follow
+        one another, so that the upper end is no end of the memory."""
         num_pages = self.shares.numel()
         if not 1 <= n_keep <= num_pages:
             raise ValueError(f"n_keep: 1 .. {num_pages} are possible")
         if n_keep == num_pages:
             return
         src, dst = (torch.empty(num_pages - n_keep, dtype=torch.int32, device=self.device) for _ in range(2))
-        status = torch.zeros_like(self.status)
-        ops.compact_pages(n_keep, self.ctx_len, self.tables, self.shares, self.free_list, self.free_count, src, dst, self.workspace, status, sm_budget=self.budget)
-        for i in range(0, num_pages - n_keep, COPIES):
-            ops.copy_pages(self.pool, src[i:i + COPIES], dst[i:i + COPIES], status, sm_budget=self.budget)
+        status, (tables, shares, free_list) = torch.zeros_like(self.status), (t.clone() for t in (self.tables, self.shares, self.free_list))
+        ops.compact_pages(n_keep, self.ctx_len, tables, shares, free_list, self.free_count, src, dst, self.workspace, status, sm_budget=self.budget)
         if int(status) != 0:
             raise B.HsError(int(status), "compact_pages")
+        pool = self.pool.new_empty(*self.pool.shape[:2], n_keep, *self.pool.shape[3:])
+        for i in range(0, num_pages - n_keep, COPIES):    # (to pages that are free: nothing has changed until the tables do)
+            ops.copy_pages(self.pool, src[i:i + COPIES], dst[i:i + COPIES], status, sm_budget=self.budget)
+        pool.copy_(self.pool[:, :, :n_keep])
         self.graph = None
-        self.pool, self.shares = self.pool[:, :, :n_keep].clone(), self.shares[:n_keep].clone()
-        self.free_list = self.free_list[num_pages - n_keep:].clone()
+        self.pool, self.shares, self.free_list = pool, shares[:n_keep].clone(), free_list[num_pages - n_keep:].clone()
+        self.tables.copy_(tables)
         self.free_count.sub_(num_pages - n_keep)
 
     def hypotheses(self):

@@ -317,3 +317,32 @@ def test_the_largest_length_penalties(plain, penalty):
     assert int(loop.status) == 0 and int(loop.steps) == 15
     same(loop.hypotheses()[0], search(p[0], 3, 15, 7, penalty))
     loop.close()
+
+
+@pytest.mark.parametrize("keep,entry", [(40, 999), (40, -5), (5, None), (40, "free")])
+def test_a_pool_that_cannot_shrink_changes_nothing(plain, monkeypatch, keep, entry):
+    """No room, or a block table entry that is no page of the pool or a free one."""
+    monkeypatch.setitem(STATUS, "BAD_BLOCK_TABLE", B.HS_ERR_BAD_BLOCK_TABLE)
+    p = prompts(20, 3, 40)
+    loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 3, 3, 60, 80, sum(map(len, p)), 30)
+    # (pages from the pool's upper end, so that some have to move)
+    loop.free_list.copy_(loop.free_list.flip(0))
+    loop.prefill(p)
+    for _ in range(5):
+        loop.step()
+    right = int(loop.tables[0, 0])
+    if entry is not None:
+        loop.tables[0, 0] = int(loop.free_list[:int(loop.free_count)].max()) if entry == "free" else entry
+    names = ("ctx_len", "tables", "free_list", "free_count", "shares", "scores", "q_len", "status")
+    before, pool, found = {k: getattr(loop, k).clone() for k in names}, loop.pool, loop.hypotheses()
+    with pytest.raises(B.HsError):
+        loop.shrink(keep)
+    assert loop.pool is pool and all(torch.equal(getattr(loop, k), before[k]) for k in names) and loop.hypotheses() == found
+    loop.tables[0, 0] = right
+    loop.shrink(40)
+    check_pages(loop)
+    for _ in range(5):
+        loop.step()
+    for r in range(3):
+        same(loop.hypotheses()[r], search(p[r], 3, 11))
+    loop.close()
