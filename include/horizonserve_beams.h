@@ -4,7 +4,8 @@
  *
  * Rows of block tables may share pages here.  shares[page] counts the holders of a page beyond the first, 0 for a page of one row and for a
  * free one, so hs_op_step_tables, whose new pages have one holder, needs no change.  A page that is not full has one holder: the
- * rows that append to it never meet.
+ * rows that append to it never meet.  Rows that share pages are ended by hs_op_fork_pages (parent -1).  hs_op_release_pages knows no holders and gives all pages of
+ * a row to the stack, those of rows that go on and those that another row gives back among them: it is for rows whose pages have one holder each.
  *     hs_op_beam_select       the best continuations of every request over its beams and the vocabulary
  *     hs_op_fork_pages        rows continue other rows: shared pages counted, partly filled ones listed to be copied, dropped ones freed
  *     hs_op_copy_pages        the keys and values of listed pages, in every layer
@@ -29,8 +30,8 @@ extern "C" {
 
 #define HS_MAX_BEAMS 32           /* beams of a request, and continuations that a call gives it */
 #define HS_BEAMS_MAX_PAGES (1 << 24)   /* pages of a pool in hs_op_fork_pages */
+#define HS_COMPACT_MAX_PAGES (1 << 21) /* pages of a pool in hs_op_compact_pages */
 #define HS_SHARED_MAX_SEQS 2048        /* sequences of a call of hs_op_shared_attention */
-#define HS_COMPACT_MAX_PAGES (1 << 21) /* and in hs_op_compact_pages */
 
 /*
  * Request r has beams b in 0 .. n_beams - 1 with accumulated log probability S_b = scores[r][b] and the logit row x = logits[r n_beams + b].
@@ -148,7 +149,8 @@ hs_status_t hs_op_compact_pages(const hs_compact_pages_t *a, int32_t sm_budget, 
  * differ there, the result is that of the pages read.  A sequence outside all groups is not computed, its rows are left as they were; one without keys gives o = 0, lse = -infinity.
  * Scores, maxima, sums and o are held in fp32; the softmax weights are rounded to the cache's type for the product with v, before they are divided by their
  * sum.  What the cache holds behind a sequence's keys may be anything.  All keys have a finite v: an infinity or NaN there may reach the other sequences of the group.
- * Work is planned on the device from the lengths, divided along the keys, and joined in an order that does not depend on the budget.
+ * Work is planned on the device from the lengths, divided along the keys, and joined in an order that does not depend on the budget.  Where it is divided depends on the
+ * lengths of all sequences of the call: next to others, a sequence's o and lse may differ in the last bits, within the roundings above.
  * Status INVALID_ARG: group_begin that falls or leaves 0 .. n_seqs, a negative shared_len; nothing is computed.  Status BAD_BLOCK_TABLE: a page id outside
  * the pool, or a kv_len that is negative or beyond the block table row (or 2^31 - 64); nothing outside the pool is read, and the rows of the group are not defined.
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 1024; scale and cap as in hs_op_paged_attention.  q and o rows 16-byte aligned, strides multiples

@@ -81,6 +81,7 @@ hs_status_t hs_op_step_tables(const hs_step_tables_t *a, int32_t sm_budget, void
 /*
  * Gives the pages of finished requests back: request s with done[s] != 0 pushes its ceil(ctx_len[s] / 16) pages onto the stack,
  * the last page first, requests in order (the order of hs_kv_free); their block table entries become -1 and ctx_len[s] becomes 0.
+ * No page of theirs is another row's, too: rows that share pages are ended by hs_op_fork_pages (horizonserve_beams.h).
  * The lengths, the block tables and the stack stay as they were (entries of free_list behind the stack's top apart), with the status
  *     INVALID_ARG      a negative length or one beyond the block table row, or more pages than the stack has room for
  *     BAD_BLOCK_TABLE  one of the pages is outside 0 .. num_pages - 1

@@ -60,7 +60,7 @@ def step_tables(ctx_len, q_len, free_list, free_count, block_tables, kv_len, tok
 
 
 def release_pages(done, ctx_len, block_tables, free_list, free_count, workspace, status, sm_budget: Optional[int] = None) -> None:
-    """Gives the pages of the requests with done != 0 back to the stack (hs_op_release_pages)."""
+    """Gives the pages of the requests with done != 0 back to the stack (hs_op_release_pages).  Rows that share pages are ended by fork_pages."""
     st = (_binding or _load()).release_pages(done, ctx_len, block_tables, free_list, free_count, workspace, status, sm_budget)
     if st:
         raise B.HsError(st, "hs_op_release_pages")
