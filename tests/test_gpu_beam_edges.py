@@ -172,3 +172,75 @@ def test_shared_attention_of_cut_tiles_time_after_time(groups, hq, hkv, dim, cap
             wrong += (call(budget) != first).sum() + (ws[:64 << 10] != 0).sum()
         assert int(wrong) == 0, f"budget {budget}"
     assert int(status) == 0
+
+
+def test_all_operators_behind_one_another_share_a_workspace(ws, status):
+    """Attention of cut tiles, forks that free pages, compactions by three launches, selections of cut rows, copies: in mixed order on one stream and workspace, without a
+    pause and at several budgets, each gives what it gives by itself."""
+    rng, g = np.random.default_rng(7), torch.Generator(device=DEV).manual_seed(7)
+
+    def selection(n, b, vocab, k):
+        x = torch.randn(n * b, vocab, generator=g, device=DEV).bfloat16()
+
+        def call(budget):
+            out = [torch.empty(n, k, device=DEV), *(torch.empty(n, k, dtype=torch.int32, device=DEV) for _ in range(2))]
+            ops.beam_select(x, torch.zeros(n, b, device=DEV), *out, ws, status, sm_budget=budget)
+            return out
+        return call
+
+    def attention(groups, hq, hkv, dim):
+        kv = [s + n for s, own in groups for n in own]
+        tables, pages = ref.grouped_tables(rng, groups, max(map(ref.pages, kv)) + 1)
+        q = torch.randn(len(kv), hq, dim, generator=g, device=DEV).bfloat16()
+        pool = torch.randn(1, 2, pages, hkv, 16, dim, generator=g, device=DEV).bfloat16()
+        rest = [i32(tables), i32(kv), i32(np.cumsum([0] + [len(own) for _, own in groups])), i32([s for s, _ in groups])]
+
+        def call(budget):
+            o, lse = torch.empty_like(q), torch.empty(len(kv), hq, device=DEV)
+            ops.shared_attention(q, pool, 0, *rest, o, ws, status, lse=lse, sm_budget=budget)
+            return [o, lse]
+        return call
+
+    def fork(n, beams, most):
+        ctx, tables, shares, free, num = ref.shared_rows(rng, n, beams, [int(x) for x in rng.integers(20, most, n)], n * beams + 9)
+        parent = [-1 if rng.random() < 0.3 else i // beams * beams + int(rng.integers(beams)) for i in range(n * beams)]
+        given = [i32(x) for x in (parent, ctx, tables, shares, free + [0] * (num - len(free)), [len(free)])]
+
+        def call(budget):
+            out = [t.clone() for t in given] + [torch.empty(n * beams, dtype=torch.int32, device=DEV) for _ in range(3)]
+            ops.fork_pages(*out, ws, status, sm_budget=budget)
+            return out
+        return call
+
+    def compaction(spare):
+        ctx, tables, shares, free, num = ref.shared_rows(rng, 20, 4, [int(x) for x in rng.integers(0, 700, 20)], spare)
+        given = [i32(x) for x in (ctx, tables, shares, free + [0] * (num - len(free)), [len(free)])]
+
+        def call(budget):
+            out = [t.clone() for t in given] + [torch.empty(spare // 2, dtype=torch.int32, device=DEV) for _ in range(2)]
+            ops.compact_pages(num - spare // 2, *out, ws, status, sm_budget=budget)
+            return out
+        return call
+
+    def copies():
+        pool, order = torch.randn(2, 2, 101, 2, 16, 64, generator=g, device=DEV).bfloat16(), rng.permutation(101)
+        src, dst = i32(order[:50]), i32(order[50:100])
+
+        def call(budget):
+            out = pool.clone()
+            ops.copy_pages(out, src, dst, status, sm_budget=budget)
+            return [out]
+        return call
+
+    calls = [selection(64, 8, 20000, 8), selection(1, 32, 152064, 32), selection(3, 5, 7001, 5), attention([(3000, [30] * 20)], 28, 4, 128),
+             attention([(900, [5, 60]), (40, [300, 1, 7])] * 4, 16, 4, 64), fork(40, 8, 300), fork(3, 2, 60), compaction(30000), compaction(9000), compaction(60), copies()]
+    alone = []
+    for call in calls:
+        alone.append([t.clone() for t in call(None)])
+        torch.cuda.synchronize()
+    for budget in (None, 1, 20):
+        order = np.concatenate([rng.permutation(len(calls)) for _ in range(6)])
+        together = [(i, calls[i](budget)) for i in order]
+        for i, got in together:
+            assert all(torch.equal(a, b) for a, b in zip(got, alone[i])), (budget, i)
+    assert int(status) == 0 and not bool(ws[:64 << 10].any()) and not bool(ws[-(2 << 20):].any())
