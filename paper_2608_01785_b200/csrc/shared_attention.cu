@@ -85,6 +85,7 @@ struct alignas(16) Team {
 struct alignas(16) Block {
   uint32_t tmem_base;
   int abort_flag, n_joins;
+  int again;                                             // a row that this block has delivered is infinite or NaN
   int middle[2];                                         // whether the teams' last item is the same, in shares of either parity
   int warp_sum[SA_THREADS / 32];
   int joins[kMaxShares];                                 // tiles that this block joins
@@ -170,9 +171,145 @@ __device__ __forceinline__ int find_last(const T* begin, int n, int x) {
 struct Plan {
   const int *cost, *shared;                              // [tiles + 1], [groups]
   const uint16_t *group, *tile;                          // [groups + 1]: first sequence, first tile
-  int tiles, line, shares;
+  int tiles, line, shares, units;                        // units: KV heads, or chunks of their query heads
   int base, more;                                        // of the line for a share; shares with one more, the first ones
+  // An item's number is tile * units + unit; its place in the line is the sum of the costs in front of it.
+  __device__ __forceinline__ int blocks_of(int number) const { return cost[number / units + 1] - cost[number / units] - SA_ITEM_COST; }
+  __device__ __forceinline__ int place_of(int number) const {
+    const int t = number / units;
+    return cost[t] * units + (number - t * units) * (cost[t + 1] - cost[t]);
+  }
+  __device__ __forceinline__ int share_begin(int k) const { return base * k + min(k, more); }
+  __device__ __forceinline__ int number_at(int x) const {           // of the item that has place x of the line
+    const int t = find_last(cost, tiles, x / units);
+    return t * units + (x - cost[t] * units) / (cost[t + 1] - cost[t]);
+  }
+  // The block of an item in front of which the cut at place x falls; not so near an end that a part would be too short.
+  __device__ __forceinline__ int cut_block(int place, int blocks, int x) const {
+    const int b = x - place - SA_ITEM_COST;
+    return b < SA_MIN_PART ? 0 : b > blocks - SA_MIN_PART ? blocks : b;
+  }
+  __device__ __forceinline__ int first_share(int x) const {         // the share that has place x
+    const int x_more = more * (base + 1);
+    return x < x_more ? x / (base + 1) : more + (x - x_more) / base;
+  }
 };
+
+// The sum of a row's 32 coordinates.
+__device__ __forceinline__ float sum_of(const float (&x)[32]) {
+  F2 y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = add2(f2(x[4 * e], x[4 * e + 1]), f2(x[4 * e + 2], x[4 * e + 3]));
+#pragma unroll
+  for (int n = 4; n > 0; n >>= 1)
+#pragma unroll
+    for (int e = 0; e < n; ++e) y[e] = add2(y[e], y[e + n]);
+  float a, b;
+  split(y[0], a, b);
+  return a + b;
+}
+// o of one row by itself, by a warp: a lane a key, then DH / 32 of the row's coordinates.  (For rows next to a sequence whose v is infinite or NaN at some key.)
+template <int DH, bool F16>
+__device__ __noinline__ void row_alone(const SharedParams& p, int seq, int head, int table, int shared_pages) {
+  const hs_shared_attention_t& a = p.a;
+  constexpr int PER = DH / 32;
+  const int lane = threadIdx.x & 31, kv = min(max(a.kv_len[seq], 0), row_tokens(a.max_pages_per_seq)), hk = head / (a.n_q_heads / a.n_kv_heads);
+  const uint16_t *q = static_cast<const uint16_t*>(a.q) + seq * a.q_stride + head * DH, *pool = static_cast<const uint16_t*>(a.kv_pool);
+  const int64_t to_v = int64_t(a.num_pages) * a.n_kv_heads * (HS_PAGE_SIZE * DH);
+  const float slope = a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
+  auto pair = [](uint32_t w) {
+    if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  };
+  float m = -INFINITY, l = 0.f, o[PER] = {};
+#pragma unroll 1
+  for (int j0 = 0; j0 < kv; j0 += 32) {
+    const int j = j0 + lane, page = j / HS_PAGE_SIZE;
+    int64_t at = -1;                                     // of the key in the pool; a page outside has none
+    float x = -INFINITY;
+    if (j < kv) {
+      const int id = a.block_tables[int64_t(page < shared_pages ? table : seq) * a.max_pages_per_seq + page];
+      if (id >= 0 && id < a.num_pages) at = ((int64_t(a.layer * 2) * a.num_pages + id) * a.n_kv_heads + hk) * (HS_PAGE_SIZE * DH) + (j % HS_PAGE_SIZE) * DH;
+    }
+    if (at >= 0) {
+      float dot = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < DH; c += 8) {
+        const uint4 qw = *reinterpret_cast<const uint4*>(q + c), kw = *reinterpret_cast<const uint4*>(pool + at + c);
+        const uint32_t qs[4] = {qw.x, qw.y, qw.z, qw.w}, ks[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 u = pair(qs[e]), v = pair(ks[e]);
+          dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+        }
+      }
+      x = fmaf(-slope, float(kv - 1 - j), p.score.out == 0.f ? dot * p.score.in : tanh_any(dot * p.score.in) * p.score.out);
+    }
+    float top = fmaxf(m, x);
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+    const float zero = top == -INFINITY ? 0.f : top, f = fast_exp2(m - zero), w = fast_exp2(x - zero);
+    float sum = w;
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+    m = top;
+    l = fmaf(l, f, sum);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] *= f;
+#pragma unroll 4
+    for (int t = 0; t < min(32, kv - j0); ++t) {
+      const int64_t of = __shfl_sync(0xffffffffu, at, t);
+      const float wt = __shfl_sync(0xffffffffu, w, t);
+      if (of < 0) continue;
+#pragma unroll
+      for (int e = 0; e < PER; e += 2) {
+        const float2 v = pair(*reinterpret_cast<const uint32_t*>(pool + to_v + of + lane * PER + e));
+        o[e] = fmaf(wt, v.x, o[e]);
+        o[e + 1] = fmaf(wt, v.y, o[e + 1]);
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o) + seq * a.o_stride + head * DH + lane * PER);
+#pragma unroll
+  for (int e = 0; e < PER; e += 2) dst[e / 2] = pack_16<F16>(o[e] * inv, o[e + 1] * inv);
+}
+
+// The weight 0 of a key that a row does not see gives NaN where its v is infinite or NaN.  A block that has finished such a row looks through the tiles that it has finished: rows with
+// an output that is no number are worked out once more, each by itself.  Those that see such a v keep what it gives.
+template <int DH, bool F16>
+__device__ __noinline__ void finished_again(const SharedParams& p, const Plan plan, const int* joins, int n_joins) {
+  const hs_shared_attention_t& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads_all = a.n_q_heads / a.n_kv_heads;
+  auto tile_again = [&](int number) {
+    const int t = number / plan.units, unit = number - t * plan.units, g = find_last(plan.tile, a.n_groups, t), g_end = plan.group[g + 1];
+    const int s0 = int(plan.group[g]) + (t - int(plan.tile[g])) * p.tile_seqs, n = min(g_end - s0, p.tile_seqs);
+    const int hk = unit / p.chunks, in_head = (unit - hk * p.chunks) * p.heads, heads = min(heads_all - in_head, p.heads);
+    int table = plan.group[g];                           // (one of the group's has keys, where there are shared pages)
+    while (plan.shared[g] > 0 && table < g_end - 1 && a.kv_len[table] <= 0) ++table;
+#pragma unroll 1
+    for (int i = warp; i < n * heads; i += SA_THREADS / 32) {
+      const int seq = s0 + i / heads, head = hk * heads_all + in_head + i % heads;
+      const uint16_t* row = static_cast<const uint16_t*>(a.o) + seq * a.o_stride + head * DH;
+      constexpr int kExponent = F16 ? 0x7c00 : 0x7f80;
+      bool bad = false;
+      for (int c = lane; c < DH; c += 32) bad |= (row[c] & kExponent) == kExponent;
+      if (__any_sync(0xffffffffu, bad)) row_alone<DH, F16>(p, seq, head, table, plan.shared[g]);
+    }
+  };
+#pragma unroll 1
+  for (int share = int(blockIdx.x); share < plan.shares; share += int(gridDim.x)) {
+    const int x0 = plan.share_begin(share), x1 = plan.share_begin(share + 1), last = plan.number_at(x1 - 1);
+#pragma unroll 1
+    for (int number = plan.number_at(x0); number <= last; ++number) {
+      const int place = plan.place_of(number), blocks = plan.blocks_of(number);
+      const int from = place < x0 ? plan.cut_block(place, blocks, x0) : 0, to = place + blocks + SA_ITEM_COST > x1 ? plan.cut_block(place, blocks, x1) : blocks;
+      if (from == 0 && to == blocks) tile_again(number);
+    }
+  }
+#pragma unroll 1
+  for (int i = 0; i < n_joins; ++i) tile_again(joins[i]);
+}
 
 template <int DH, bool F16, bool MOD>
 __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const __grid_constant__ SharedParams p) {
@@ -212,6 +349,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
   if (tid == 0) {
     bar->abort_flag = 0;
     bar->n_joins = 0;
+    bar->again = 0;
     tma_prefetch_desc(&p.tm_q);
   }
   if (warp == 9) {
@@ -303,6 +441,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     plan.shared = shared;
     plan.group = group;
     plan.tile = tile;
+    plan.units = units;
     plan.line = all * units;
     // Small calls: a share's blocks come one after the other, and so do the parts that a join reads, so the shares grow with the root of the tiles' lengths.  Measured, with 6 blocks
     // or more for every length: 4 sequences behind 500 keys 21.2 us (19.5 so), one behind 32,000 with one KV head 55.6 (40.1), 8 behind 16,000 with two 41.9 (33.7).
@@ -311,45 +450,25 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     plan.base = plan.line / plan.shares;
     plan.more = plan.line - plan.base * plan.shares;
   }
-  // An item's number is tile * units + unit; its place in the line is the sum of the costs in front of it.
-  auto blocks_of = [&](int number) { return plan.cost[number / units + 1] - plan.cost[number / units] - SA_ITEM_COST; };
-  auto place_of = [&](int number) {
-    const int t = number / units;
-    return plan.cost[t] * units + (number - t * units) * (plan.cost[t + 1] - plan.cost[t]);
-  };
-  auto share_begin = [&](int k) { return plan.base * k + min(k, plan.more); };
-  auto number_at = [&](int x) {                          // of the item that has place x of the line
-    const int t = find_last(plan.cost, plan.tiles, x / units);
-    return t * units + (x - plan.cost[t] * units) / (plan.cost[t + 1] - plan.cost[t]);
-  };
-  // The block of an item in front of which the cut at place x falls; not so near an end that a part would be too short.
-  auto cut_block = [&](int place, int blocks, int x) {
-    const int b = x - place - SA_ITEM_COST;
-    return b < SA_MIN_PART ? 0 : b > blocks - SA_MIN_PART ? blocks : b;
-  };
-  auto first_share = [&](int x) {                        // the share that has place x
-    const int x_more = plan.more * (plan.base + 1);
-    return x < x_more ? x / (plan.base + 1) : plan.more + (x - x_more) / plan.base;
-  };
   // Whether both teams have blocks of the item in their share.
   auto middle_of = [&](int share, int number) {
-    const int x0 = share_begin(share), x1 = share_begin(share + 1), xm = x0 + (x1 - x0) / 2, place = place_of(number), blocks = blocks_of(number);
+    const int x0 = plan.share_begin(share), x1 = plan.share_begin(share + 1), xm = x0 + (x1 - x0) / 2, place = plan.place_of(number), blocks = plan.blocks_of(number);
     const int end = place + blocks + SA_ITEM_COST;
     if (place >= xm || end <= xm) return 0;
-    const int from = place < x0 ? cut_block(place, blocks, x0) : 0, at = cut_block(place, blocks, xm), to = end > x1 ? cut_block(place, blocks, x1) : blocks;
+    const int from = place < x0 ? plan.cut_block(place, blocks, x0) : 0, at = plan.cut_block(place, blocks, xm), to = end > x1 ? plan.cut_block(place, blocks, x1) : blocks;
     return from < at && at < to ? 1 : 0;
   };
 
   // The shares' parts of an item: block ranges between the cuts that fall into it; how many there are (a warp asks).
   auto count_parts = [&](int number, int place, int blocks) {
-    const int end = place + blocks + SA_ITEM_COST, f = first_share(place);
+    const int end = place + blocks + SA_ITEM_COST, f = plan.first_share(place);
     int parts = 0;
-    for (int k0 = f; k0 < plan.shares && share_begin(k0) < end; k0 += 32) {
+    for (int k0 = f; k0 < plan.shares && plan.share_begin(k0) < end; k0 += 32) {
       const int k = k0 + lane;
       bool has = false;
-      if (k < plan.shares && share_begin(k) < end) {
-        const int from = k == f ? 0 : cut_block(place, blocks, share_begin(k));
-        has = from < (share_begin(k + 1) < end ? cut_block(place, blocks, share_begin(k + 1)) : blocks);
+      if (k < plan.shares && plan.share_begin(k) < end) {
+        const int from = k == f ? 0 : plan.cut_block(place, blocks, plan.share_begin(k));
+        has = from < (plan.share_begin(k + 1) < end ? plan.cut_block(place, blocks, plan.share_begin(k + 1)) : blocks);
       }
       parts += __popc(__ballot_sync(0xffffffffu, has));
     }
@@ -443,9 +562,11 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       if (!whole) __stcg(&part.ml[r], total);
       else if (a.lse) a.lse[row * a.n_q_heads + head] = total.y == 0.f ? -INFINITY : kLn2 * (total.x + log2f(total.y));
     }
-    return each_columns(f, [&](int c, float(&x)[32]) {
+    float none = 0.f;                                    // NaN where an output is infinite or NaN
+    const bool ok = each_columns(f, [&](int c, float(&x)[32]) {
       if (!mine) return;
       if (whole) {
+        none = fmaf(sum_of(x), 0.f, none);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           *reinterpret_cast<uint4*>(dst + c + u * 8) = make_uint4(pack_16<F16>(x[8 * u] * inv, x[8 * u + 1] * inv), pack_16<F16>(x[8 * u + 2] * inv, x[8 * u + 3] * inv),
@@ -455,10 +576,12 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
         for (int u = 0; u < 8; ++u) __stcg(&part.o[c / 4 + u][r], make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]));
       }
     });
+    if (none != 0.f) bar->again = 1;
+    return ok;
   };
   // A part of an item with so many has arrived, by one of its four warps (n = 1) or all of it (n = 4).
   auto arrived = [&](int number, int parts, int n) {
-    int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + first_share(place_of(number));
+    int* done = reinterpret_cast<int*>(static_cast<char*>(a.workspace) + kWsSharedQueue) + plan.first_share(plan.place_of(number));
     if (atomicAdd(done, n) == 4 * parts - n) {
       *done = 0;                                         // ready for the next call
       bar->joins[atomicAdd(&bar->n_joins, 1)] = number;
@@ -467,7 +590,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
 
 #pragma unroll 1
   for (int share = plan.tiles > 0 ? int(blockIdx.x) : plan.shares, turn = 0; share < plan.shares; share += int(gridDim.x), ++turn) {
-    const int x0 = share_begin(share), x1 = share_begin(share + 1), xm = x0 + (x1 - x0) / 2;
+    const int x0 = plan.share_begin(share), x1 = plan.share_begin(share + 1), xm = x0 + (x1 - x0) / 2;
     int middle = 0;                                      // softmax: of the last item
     if (warp == 8 || warp == 10) {
       // ============================================================ fetching ==
@@ -479,7 +602,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
       const int64_t page_bytes = int64_t(a.n_kv_heads) * (HS_PAGE_SIZE * DH * 2);
       const uint32_t to = uint32_t((chunk >> 3) * 8192 + key * 128 + (((chunk & 7) ^ key) << 4));
       const int xa = team == 0 ? x0 : xm, xb = team == 0 ? xm : x1;
-      const int first = xa < xb ? number_at(xa) : 0, last = xa < xb ? number_at(xb - 1) : -1;
+      const int first = xa < xb ? plan.number_at(xa) : 0, last = xa < xb ? plan.number_at(xb - 1) : -1;
       bool ok = true;
       int t_cached = -1;                                 // the tile whose sequences are in the ring's other slot
       for (int i = 0; ok; ++i) {
@@ -492,8 +615,8 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
           unit = number - t * units;
           blocks = plan.cost[t + 1] - plan.cost[t] - SA_ITEM_COST;
           place = plan.cost[t] * units + unit * (blocks + SA_ITEM_COST);
-          b0 = place < xa ? cut_block(place, blocks, xa) : 0;
-          b1 = place + blocks + SA_ITEM_COST > xb ? cut_block(place, blocks, xb) : blocks;
+          b0 = place < xa ? plan.cut_block(place, blocks, xa) : 0;
+          b1 = place + blocks + SA_ITEM_COST > xb ? plan.cut_block(place, blocks, xb) : blocks;
           some = b0 < b1;
         }
         --i;
@@ -1041,6 +1164,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
           const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
           for (int q = 0; q < 4; ++q) w[q] *= inv;
+          float none = 0.f;
 #pragma unroll 1
           for (int c = c0; c < c0 + columns; c += 8) {
             float4 y[2] = {};
@@ -1057,6 +1181,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
               }
             }
             if (whole) {
+              none = fmaf((y[0].x + y[0].y) + (y[0].z + y[0].w) + ((y[1].x + y[1].y) + (y[1].z + y[1].w)), 0.f, none);
               *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_16<F16>(y[0].x, y[0].y), pack_16<F16>(y[0].z, y[0].w), pack_16<F16>(y[1].x, y[1].y),
                                                               pack_16<F16>(y[1].z, y[1].w));
             } else {
@@ -1064,6 +1189,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
               __stcg(&part.o[c / 4 + 1][row_in], y[1]);
             }
           }
+          if (none != 0.f) bar->again = 1;
         }
         fence_proxy_async();                             // (Q's place was written)
       }
@@ -1087,11 +1213,10 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     tmem_dealloc(tmem, SA_TMEM);
   }
   const int n_joins = bar->n_joins;
-  if (n_joins == 0) return;
-  __threadfence();
+  if (n_joins > 0) __threadfence();
 #pragma unroll 1
   for (int i = 0; i < n_joins; ++i) {
-    const int number = bar->joins[i], place = place_of(number), blocks = blocks_of(number), end = place + blocks + SA_ITEM_COST, f = first_share(place);
+    const int number = bar->joins[i], place = plan.place_of(number), blocks = plan.blocks_of(number), end = place + blocks + SA_ITEM_COST, f = plan.first_share(place);
     const int t_ = number / units, unit = number - t_ * units, g = find_last(plan.tile, n_groups, t_);
     const int s0 = int(plan.group[g]) + (t_ - int(plan.tile[g])) * p.tile_seqs, n = min(int(plan.group[g + 1]) - s0, p.tile_seqs);
     const int hk = unit / p.chunks, heads_all = a.n_q_heads / a.n_kv_heads, in_head = (unit - hk * p.chunks) * p.heads, heads = min(heads_all - in_head, p.heads);
@@ -1101,15 +1226,15 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     __syncthreads();
     if (warp == 0) {
       int parts = 0;
-      for (int k0 = f; k0 < plan.shares && share_begin(k0) < end; k0 += 32) {
+      for (int k0 = f; k0 < plan.shares && plan.share_begin(k0) < end; k0 += 32) {
         const int k = k0 + lane;
         bool has = false;
-        if (k < plan.shares && share_begin(k) < end) {
-          const int from = k == f ? 0 : cut_block(place, blocks, share_begin(k));
-          has = from < (share_begin(k + 1) < end ? cut_block(place, blocks, share_begin(k + 1)) : blocks);
+        if (k < plan.shares && plan.share_begin(k) < end) {
+          const int from = k == f ? 0 : plan.cut_block(place, blocks, plan.share_begin(k));
+          has = from < (plan.share_begin(k + 1) < end ? plan.cut_block(place, blocks, plan.share_begin(k + 1)) : blocks);
         }
         const unsigned who = __ballot_sync(0xffffffffu, has);
-        if (has) slots[1 + parts + __popc(who & ((1u << lane) - 1u))] = 2 * k + (place < share_begin(k) ? 0 : 1);
+        if (has) slots[1 + parts + __popc(who & ((1u << lane) - 1u))] = 2 * k + (place < plan.share_begin(k) ? 0 : 1);
         parts += __popc(who);
       }
       if (lane == 0) slots[0] = parts;
@@ -1181,11 +1306,15 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     for (int y = 0; y < PIECES; ++y) {
       const int r = at[y] % SA_ROWS, c = at[y] / (2 * SA_ROWS), i_seq = r / p.heads, h = r - i_seq * p.heads;
       if (tid + y * SA_THREADS >= n_pieces || h >= heads) continue;
+      if (((o[y][0].x + o[y][0].y) + (o[y][0].z + o[y][0].w) + ((o[y][1].x + o[y][1].y) + (o[y][1].z + o[y][1].w))) * 0.f != 0.f) bar->again = 1;
       *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + int64_t(s0 + i_seq) * a.o_stride + (hk * heads_all + in_head + h) * DH + c * 8) =
           make_uint4(pack_16<F16>(o[y][0].x, o[y][0].y), pack_16<F16>(o[y][0].z, o[y][0].w), pack_16<F16>(o[y][1].x, o[y][1].y),
                      pack_16<F16>(o[y][1].z, o[y][1].w));
     }
   }
+
+  if (n_joins > 0) __syncthreads();
+  if (bar->again) finished_again<DH, F16>(p, plan, bar->joins, n_joins);
 }
 
 template <int DH>

@@ -679,3 +679,38 @@ def test_beams_so_far_away_that_their_continuations_tie(b, vocab, n_out, start, 
         assert got[:len(want)] == want[:n_out] and set(got[len(want):]) <= {(-1, -1)}
         assert all(s == scores[r, p - r * b] for s, p in zip(score[r].cpu().numpy(), parent[r].tolist()) if p >= 0)
     assert int(status) == 0
+
+
+BAD_V = [("an own key", NAN), ("an own key", INF), ("a coordinate", -INF), ("a coordinate", NAN), ("two sequences", INF), ("a shared key", NAN), ("the last key", INF)]
+
+
+@pytest.mark.parametrize("what,bad", BAD_V)
+@pytest.mark.parametrize("groups,hq,hkv,dim,dtype,cap,bias", [
+    ([(40, [5, 9, 30]), (100, [1]), (130, [70, 4, 15, 16, 17]), (0, [7, 8])], 28, 4, 128, torch.bfloat16, 0.0, False),
+    ([(40, [5, 9, 30]), (100, [1]), (130, [70, 4, 15, 16, 17]), (0, [7, 8])], 16, 4, 64, torch.float16, 30.0, True),
+    ([(3000, [40, 9, 100])], 4, 1, 128, torch.float16, 0.0, False), ([(0, [0, 40, 9, 0])], 4, 1, 64, torch.bfloat16, 0.0, False), ([(900, [30] * 40)], 7, 1, 64, torch.bfloat16, 50.0, False),
+    ([(0, [700, 3, 64, 90]), (2000, [64] * 9)] * 3, 6, 2, 128, torch.bfloat16, 0.0, True), ([(60, [20, 40])], 150, 1, 64, torch.bfloat16, 0.0, False)])
+def test_a_v_that_is_no_number_stays_with_the_rows_that_see_it(what, bad, groups, hq, hkv, dim, dtype, cap, bias, ws, status):
+    """Infinities and NaN in v at keys of one sequence or two (one tile, tiles that two teams have, tiles cut between shares): the others are as the definition has them."""
+    c = attention_case(21, groups, hq, hkv, dim, dtype, cap, bias)
+    v = c["pool"][c["layer"], 1]
+    for s in range(1, min(3, len(c["kv"])) if what == "two sequences" else 2):
+        kv = c["kv"][s]
+        j = {"a shared key": min(20, kv - 1), "the last key": kv - 1}.get(what, max(kv - 2, 0))
+        at = v[int(c["tables"][s, j // 16]), :, j % 16]
+        at[..., 3 if what == "a coordinate" else slice(None)] = bad
+    o, lse = run_attention(c, ws, status)
+    want_o, want_lse = device_ref.attention(c["q"].double(), c["pool"][c["layer"]].double(), c["tables"], c["kv"], [1] * len(c["kv"]), None,
+                                            None if c["slopes"] is None else c["slopes"].double(), cap=c["cap"], scale=c["scale"])
+    whole, o64 = want_o.isfinite(), o.cpu().double()
+    assert (bool(whole.any()) or what == "a shared key") and not bool(whole.all())     # (a key that all rows share reaches all of them)
+    assert torch.equal(o64.isfinite(), whole) and torch.equal(o64.isnan(), want_o.isnan())
+    assert torch.equal(o64[o64.isinf()], want_o[want_o.isinf()])
+    u, most = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11, float(v.double()[v.isfinite()].abs().max())       # (bounds of check_attention)
+    assert float((o64 - want_o)[whole].abs().amax(dim=0) if bool(whole.any()) else 0.0) <= (2 * u + 5e-4) * most
+    some = want_lse > -INF
+    assert bool((lse.cpu()[~some] == -INF).all()) and float((lse.cpu().double() - want_lse)[some].abs().max()) <= 3e-4
+    for budget in (1, 9, 37):
+        o2, lse2 = run_attention(c, ws, status, budget, strided=False)
+        assert torch.equal(o2.view(torch.int16), o.view(torch.int16)) and torch.equal(lse2, lse), f"budget {budget}"
+    assert int(status) == 0
