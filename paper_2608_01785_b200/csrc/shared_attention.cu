@@ -35,6 +35,7 @@ constexpr int SA_THREADS = 384, SA_KEYS = 64, SA_ROWS = 128, SA_MAX_SEQS = HS_SH
 constexpr int SA_TMEM = 512, SA_TEAM_TMEM = 256;         // columns: of a team, S (two buffers of 64, P over their first 32) and O
 constexpr int SA_ITEM_COST = 3;                          // blocks that take as long as a tile's beginning and end
 constexpr int SA_MIN_SHARE = 4, SA_MIN_PART = 1;         // blocks, with the tiles' costs; blocks of a part
+constexpr int SA_ALONE = 4;                              // rows of a sequence that are worked out together where that has to be done by themselves
 constexpr float kRefSlack = 8.f;                         // log2 units by which a row's running maximum may exceed its reference
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -208,75 +209,114 @@ __device__ __forceinline__ float sum_of(const float (&x)[32]) {
   split(y[0], a, b);
   return a + b;
 }
-// o of one row by itself, by a warp: a lane a key, then DH / 32 of the row's coordinates.  (For rows next to a sequence whose v is infinite or NaN at some key.)
+// o of a sequence's rows by themselves, by a warp: query heads head .. head + n_heads - 1 (of one KV head, 4 at most), written where `which` has a bit.  32 keys at a time: DH / 8 lanes read
+// a key, 16 bytes each, and add up their products; the lane whose turn a key is keeps its scores, weights and place.
 template <int DH, bool F16>
-__device__ __noinline__ void row_alone(const SharedParams& p, int seq, int head, int table, int shared_pages) {
+__device__ __noinline__ void rows_alone(const SharedParams& p, int seq, int head, int n_heads, unsigned which, int table, int shared_pages) {
+  constexpr int H = SA_ALONE, LANES = DH / 8, KEYS = 32 / LANES;
   const hs_shared_attention_t& a = p.a;
-  constexpr int PER = DH / 32;
-  const int lane = threadIdx.x & 31, kv = min(max(a.kv_len[seq], 0), row_tokens(a.max_pages_per_seq)), hk = head / (a.n_q_heads / a.n_kv_heads);
-  const uint16_t *q = static_cast<const uint16_t*>(a.q) + seq * a.q_stride + head * DH, *pool = static_cast<const uint16_t*>(a.kv_pool);
+  const int lane = threadIdx.x & 31, pos = lane % LANES, sub = lane / LANES, lane0 = lane - pos;
+  const int kv = min(max(a.kv_len[seq], 0), row_tokens(a.max_pages_per_seq)), hk = head / (a.n_q_heads / a.n_kv_heads);
+  const uint16_t* pool = static_cast<const uint16_t*>(a.kv_pool) + ((int64_t(a.layer * 2) * a.num_pages) * a.n_kv_heads + hk) * (HS_PAGE_SIZE * DH) + pos * 8;
   const int64_t to_v = int64_t(a.num_pages) * a.n_kv_heads * (HS_PAGE_SIZE * DH);
-  const float slope = a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
-  auto pair = [](uint32_t w) {
-    if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
-    else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  auto unpack = [](const uint4& w, float (&x)[8]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float2 f;
+      if constexpr (F16) f = __half22float2(*reinterpret_cast<const __half2*>(&u[e]));
+      else f = make_float2(__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xffff0000u));
+      x[2 * e] = f.x;
+      x[2 * e + 1] = f.y;
+    }
   };
-  float m = -INFINITY, l = 0.f, o[PER] = {};
+  float q[H][8], o[H][8] = {}, m[H], l[H] = {}, slope[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    const int of = head + min(h, n_heads - 1);
+    unpack(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + seq * a.q_stride + of * DH + pos * 8), q[h]);
+    m[h] = -INFINITY;
+    slope[h] = a.slopes ? a.slopes[of] * 1.4426950408889634f : 0.f;
+  }
 #pragma unroll 1
   for (int j0 = 0; j0 < kv; j0 += 32) {
-    const int j = j0 + lane, page = j / HS_PAGE_SIZE;
-    int64_t at = -1;                                     // of the key in the pool; a page outside has none
-    float x = -INFINITY;
+    const int j = j0 + pos * KEYS + sub, page = j / HS_PAGE_SIZE;
+    int64_t at = -1;                                     // of the lane's key among those of the KV head; a page outside the pool has none
     if (j < kv) {
       const int id = a.block_tables[int64_t(page < shared_pages ? table : seq) * a.max_pages_per_seq + page];
-      if (id >= 0 && id < a.num_pages) at = ((int64_t(a.layer * 2) * a.num_pages + id) * a.n_kv_heads + hk) * (HS_PAGE_SIZE * DH) + (j % HS_PAGE_SIZE) * DH;
+      if (id >= 0 && id < a.num_pages) at = int64_t(id) * a.n_kv_heads * (HS_PAGE_SIZE * DH) + (j % HS_PAGE_SIZE) * DH;
     }
-    if (at >= 0) {
-      float dot = 0.f;
-#pragma unroll 4
-      for (int c = 0; c < DH; c += 8) {
-        const uint4 qw = *reinterpret_cast<const uint4*>(q + c), kw = *reinterpret_cast<const uint4*>(pool + at + c);
-        const uint32_t qs[4] = {qw.x, qw.y, qw.z, qw.w}, ks[4] = {kw.x, kw.y, kw.z, kw.w};
+    auto each_key = [&](const uint16_t* from, auto use) {          // use(lane of this group that has the key, its 8 coordinates); zeros for no key
+#pragma unroll 1
+      for (int i0 = 0; i0 < LANES; i0 += 8) {
+        uint4 w[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 u = pair(qs[e]), v = pair(ks[e]);
-          dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+        for (int u = 0; u < 8; ++u) {
+          const int64_t of = __shfl_sync(0xffffffffu, at, lane0 + i0 + u);
+          w[u] = of >= 0 ? *reinterpret_cast<const uint4*>(from + of) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          float x[8];
+          unpack(w[u], x);
+          use(i0 + u, x);
         }
       }
-      x = fmaf(-slope, float(kv - 1 - j), p.score.out == 0.f ? dot * p.score.in : tanh_any(dot * p.score.in) * p.score.out);
-    }
-    float top = fmaxf(m, x);
+    };
+    float w[H];
+    each_key(pool, [&](int i, float(&x)[8]) {
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
-    const float zero = top == -INFINITY ? 0.f : top, f = fast_exp2(m - zero), w = fast_exp2(x - zero);
-    float sum = w;
+      for (int h = 0; h < H; ++h) {
+        float dot = 0.f;
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
-    m = top;
-    l = fmaf(l, f, sum);
+        for (int e = 0; e < 8; ++e) dot = fmaf(q[h][e], x[e], dot);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] *= f;
-#pragma unroll 4
-    for (int t = 0; t < min(32, kv - j0); ++t) {
-      const int64_t of = __shfl_sync(0xffffffffu, at, t);
-      const float wt = __shfl_sync(0xffffffffu, w, t);
-      if (of < 0) continue;
-#pragma unroll
-      for (int e = 0; e < PER; e += 2) {
-        const float2 v = pair(*reinterpret_cast<const uint32_t*>(pool + to_v + of + lane * PER + e));
-        o[e] = fmaf(wt, v.x, o[e]);
-        o[e + 1] = fmaf(wt, v.y, o[e + 1]);
+        for (int n = LANES / 2; n > 0; n >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, n);
+        w[h] = pos == i ? dot : i == 0 ? 0.f : w[h];
       }
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o) + seq * a.o_stride + head * DH + lane * PER);
+    });
 #pragma unroll
-  for (int e = 0; e < PER; e += 2) dst[e / 2] = pack_16<F16>(o[e] * inv, o[e + 1] * inv);
+    for (int h = 0; h < H; ++h) {
+      const float y = p.score.out == 0.f ? w[h] * p.score.in : tanh_any(w[h] * p.score.in) * p.score.out;
+      const float x = at >= 0 ? fmaf(-slope[h], float(kv - 1 - j), y) : -INFINITY;
+      float top = fmaxf(m[h], x);
+#pragma unroll
+      for (int n = 16; n > 0; n >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, n));
+      const float zero = top == -INFINITY ? 0.f : top, f = fast_exp2(m[h] - zero);
+      m[h] = top;
+      w[h] = fast_exp2(x - zero);
+      l[h] = fmaf(l[h], f, w[h]);                        // (of the lane's keys)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[h][e] *= f;
+    }
+    each_key(pool + to_v, [&](int i, float(&x)[8]) {
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const float of = __shfl_sync(0xffffffffu, w[h], lane0 + i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[h][e] = fmaf(of, x[e], o[h][e]);
+      }
+    });
+  }
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], n);
+    const float inv = l[h] == 0.f ? 0.f : 1.f / l[h];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int n = 16; n >= LANES; n >>= 1) o[h][e] += __shfl_xor_sync(0xffffffffu, o[h][e], n);
+      o[h][e] *= inv;
+    }
+    if (sub == 0 && (which >> h & 1u))
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + seq * a.o_stride + (head + h) * DH + pos * 8) =
+          make_uint4(pack_16<F16>(o[h][0], o[h][1]), pack_16<F16>(o[h][2], o[h][3]), pack_16<F16>(o[h][4], o[h][5]), pack_16<F16>(o[h][6], o[h][7]));
+  }
 }
 
 // The weight 0 of a key that a row does not see gives NaN where its v is infinite or NaN.  A block that has finished such a row looks through the tiles that it has finished: rows with
-// an output that is no number are worked out once more, each by itself.  Those that see such a v keep what it gives.
+// an output that is no number are worked out once more, a sequence's by themselves.  Those that see such a v keep what it gives.
 template <int DH, bool F16>
 __device__ __noinline__ void finished_again(const SharedParams& p, const Plan plan, const int* joins, int n_joins) {
   const hs_shared_attention_t& a = p.a;
@@ -287,14 +327,19 @@ __device__ __noinline__ void finished_again(const SharedParams& p, const Plan pl
     const int hk = unit / p.chunks, in_head = (unit - hk * p.chunks) * p.heads, heads = min(heads_all - in_head, p.heads);
     int table = plan.group[g];                           // (one of the group's has keys, where there are shared pages)
     while (plan.shared[g] > 0 && table < g_end - 1 && a.kv_len[table] <= 0) ++table;
+    const int fours = (heads + SA_ALONE - 1) / SA_ALONE;
 #pragma unroll 1
-    for (int i = warp; i < n * heads; i += SA_THREADS / 32) {
-      const int seq = s0 + i / heads, head = hk * heads_all + in_head + i % heads;
-      const uint16_t* row = static_cast<const uint16_t*>(a.o) + seq * a.o_stride + head * DH;
+    for (int i = warp; i < n * fours; i += SA_THREADS / 32) {
+      const int seq = s0 + i / fours, in_tile = i % fours * SA_ALONE, head = hk * heads_all + in_head + in_tile, n_heads = min(heads - in_tile, SA_ALONE);
       constexpr int kExponent = F16 ? 0x7c00 : 0x7f80;
-      bool bad = false;
-      for (int c = lane; c < DH; c += 32) bad |= (row[c] & kExponent) == kExponent;
-      if (__any_sync(0xffffffffu, bad)) row_alone<DH, F16>(p, seq, head, table, plan.shared[g]);
+      unsigned which = 0;
+      for (int h = 0; h < n_heads; ++h) {
+        const uint16_t* row = static_cast<const uint16_t*>(a.o) + seq * a.o_stride + (head + h) * DH;
+        bool bad = false;
+        for (int c = lane; c < DH; c += 32) bad |= (row[c] & kExponent) == kExponent;
+        which |= __any_sync(0xffffffffu, bad) ? 1u << h : 0u;
+      }
+      if (which) rows_alone<DH, F16>(p, seq, head, n_heads, which, table, plan.shared[g]);
     }
   };
 #pragma unroll 1
