@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
         for (int u = 0; u < 8; ++u) __stcg(&part.o[c / 4 + u][r], make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]));
       }
     });
-    if (none != 0.f) bar->again = 1;
+    if (none != 0.f && total.y < INFINITY) bar->again = 1;          // (a row whose sum is NaN has a q or k that is)
     return ok;
   };
   // A part of an item with so many has arrived, by one of its four warps (n = 1) or all of it (n = 4).
@@ -1234,7 +1234,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
               __stcg(&part.o[c / 4 + 1][row_in], y[1]);
             }
           }
-          if (none != 0.f) bar->again = 1;
+          if (none != 0.f && l < INFINITY) bar->again = 1;
         }
         fence_proxy_async();                             // (Q's place was written)
       }
@@ -1351,7 +1351,7 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     for (int y = 0; y < PIECES; ++y) {
       const int r = at[y] % SA_ROWS, c = at[y] / (2 * SA_ROWS), i_seq = r / p.heads, h = r - i_seq * p.heads;
       if (tid + y * SA_THREADS >= n_pieces || h >= heads) continue;
-      if (((o[y][0].x + o[y][0].y) + (o[y][0].z + o[y][0].w) + ((o[y][1].x + o[y][1].y) + (o[y][1].z + o[y][1].w))) * 0.f != 0.f) bar->again = 1;
+      if (((o[y][0].x + o[y][0].y) + (o[y][0].z + o[y][0].w) + ((o[y][1].x + o[y][1].y) + (o[y][1].z + o[y][1].w))) * 0.f != 0.f && weight[r] == weight[r]) bar->again = 1;
       *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o) + int64_t(s0 + i_seq) * a.o_stride + (hk * heads_all + in_head + h) * DH + c * 8) =
           make_uint4(pack_16<F16>(o[y][0].x, o[y][0].y), pack_16<F16>(o[y][0].z, o[y][0].w), pack_16<F16>(o[y][1].x, o[y][1].y),
                      pack_16<F16>(o[y][1].z, o[y][1].w));
