@@ -150,6 +150,7 @@ hs_status_t hs_op_compact_pages(const hs_compact_pages_t *a, int32_t sm_budget, 
  * Scores, maxima, sums and o are held in fp32; the softmax weights are rounded to the cache's type for the product with v, before they are divided by their
  * sum.  What the cache holds behind a sequence's keys may be anything, and an infinity or NaN at a key reaches the rows that see it, and no others.  (Rows of one tile with a row that
  * sees an infinite or NaN v are worked out by themselves, with unrounded weights: such a call takes milliseconds behind a long prompt.)
+ * It pays where the sequences' keys and values, counted one by one, come to some 200 MB; below that hs_op_paged_attention, with max_q_len 1, takes down to half the time.
  * Work is planned on the device from the lengths, divided along the keys, and joined in an order that does not depend on the budget.  Where it is divided depends on the
  * lengths of all sequences of the call: next to others, a sequence's o and lse may differ in the last bits, within the roundings above.
  * Status INVALID_ARG: group_begin that falls or leaves 0 .. n_seqs, a negative shared_len; nothing is computed.  Status BAD_BLOCK_TABLE: a page id outside

@@ -17,7 +17,7 @@
 // better bound, until only candidates that are all alike are left, which are taken one by one.  It comes behind the team's next item, while the others work on.
 //
 // 64 requests of 8 beams over 152,064 bf16 logits: 42 us.  The stream ends after 26 of them on average and 30 at most (5.2 TB/s; the exponentials alone would take 20), the items' ends, of 4 us
-// each, follow at once where rows are not cut, and a choice takes 4.  Cutting rows in two for a second round that hides the ends costs more than it hides (60 us).  One request of 4 beams: 13.0 us,
+// each, follow at once where rows are not cut, and a choice takes 4.  Cutting rows in two for a second round that hides the ends costs more than it hides (60 us).  One request of 4 beams: 12.9 us,
 // of which the stream is 2: launch, an item's end (2.5), its delivery (2) and the choice (5) are round trips and code that runs once.
 #include <float.h>
 
@@ -31,7 +31,7 @@ namespace {
 
 constexpr int BS_TEAMS = 4, BS_TEAM = 128, BS_THREADS = BS_TEAMS * BS_TEAM, BS_WARPS = BS_TEAM / 32;
 constexpr int BS_PIECES = 8, BS_TILE_PIECES = BS_PIECES * BS_TEAM;       // 16-byte pieces of a tile: per thread, in all
-constexpr int BS_AHEAD = 2;                                              // tiles that are on their way to L2 before they are loaded (fp32 rows 45 -> 42 us; 4: 43, 8: 48)
+constexpr int BS_AHEAD = 2;                                              // tiles that are on their way to L2 before they are loaded (64 x 8 rows, bf16 and fp32: 43.0 and 66.1 us; none 44.6 and 73.3, four 43.7 and 71.5, eight 49.0 and 72.0)
 constexpr int BS_LIST = 512;                                             // candidates that a team ranks at a time
 constexpr int BS_ITEM_COST = 3;                                          // tiles
 constexpr int BS_MAX_PARTS = 64;                                         // of a row

@@ -18,9 +18,9 @@
 // Every block plans for itself, from the lengths, in shared memory.  The softmax works through a block 32 keys at a time in rolled loops, as it is few warps' instructions
 // that have to be fetched: unrolled over 64 keys with all its variants the same work took twice as long.
 //
-// 64 groups of 8 sequences behind 512 .. 2,048 shared keys, 28 heads on 4 of 128, capped: 87 us against a floor of 44 for the bytes; 256 sequences behind 8,191 shared keys with up
+// 64 groups of 8 sequences behind 512 .. 2,048 shared keys, 28 heads on 4 of 128, capped: 88 us against a floor of 44 for the bytes; 256 sequences behind 8,191 shared keys with up
 // to 1,024 own ones: 123 against 47.  The softmax warps bound the shared keys (1,000 cycles a block of 64 keys for two teams), a row's exponentials and the way of P; own keys
-// keep one or two warps of four busy (2,000 cycles).  Plan and first pages are 6 us of a call, the ends and joins of cut tiles 8 to 10.  One group of 4 behind 500 keys: 19.5 us, all latency.
+// keep one or two warps of four busy (2,000 cycles).  Plan and first pages are 6 us of a call, the ends and joins of cut tiles 8 to 10.  One group of 4 behind 500 keys: 18.8 us, all latency.
 #include <math.h>
 
 #include <algorithm>
@@ -488,8 +488,9 @@ __global__ void __launch_bounds__(SA_THREADS, 1) shared_attention_kernel(const _
     plan.tile = tile;
     plan.units = units;
     plan.line = all * units;
-    // Small calls: a share's blocks come one after the other, and so do the parts that a join reads, so the shares grow with the root of the tiles' lengths.  Measured, with 6 blocks
-    // or more for every length: 4 sequences behind 500 keys 21.2 us (19.5 so), one behind 32,000 with one KV head 55.6 (40.1), 8 behind 16,000 with two 41.9 (33.7).
+    // Small calls: a share's blocks come one after the other, and so do the parts that a join reads, so the shares grow with the root of the tiles' lengths.  Measured at head_dim 128
+    // with three sets of inputs in turn, against shares of 6 blocks and parts of 2 or more for every length: 4 sequences behind 500 keys, 28 heads on 4, 19.4 us for 21.3; one behind
+    // 32,000, 7 on one, 43.8 for 68.2; 8 behind 16,000, 14 on two, 34.1 for 43.3.
     const int least = max(SA_MIN_SHARE, int(sqrtf(float(all) / float(max(plan.tiles, 1)))));
     plan.shares = max(1, min(p.shares, plan.line / least));
     plan.base = plan.line / plan.shares;

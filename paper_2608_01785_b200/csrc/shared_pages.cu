@@ -8,14 +8,14 @@
 // them, so no block waits for another; the last one to end sweeps the bits of freed pages, in order, onto the stack.  Rows that share a page in a column
 // are neighbours as a rule (beams of a request): a warp adds up their counts first, mostly to zero, which spares the atomics on a prompt's pages.
 // Latency bounds it: launch, one round trip for lengths, parents and table entries together, one for the counts, one for the blocks that are done, one for the
-// freed pages' bits.  16 rows of 49 pages 7.3 us, 512 rows of 258 pages 11.5 us.
+// freed pages' bits.  16 rows of 49 pages 7.1 us, 512 rows of 258 pages 11.5 us.
 //
 // Copy.  A warp takes one head of one page and layer, K or V, at a time: up to 16 rows that follow one another, eight 16-byte pieces a lane on their way.  The pages of a
 // layer follow one another, so that what is being copied lies together.  HBM bounds it: 300 whole pages of 28 layers (550 MB read and written) 104 us, 5.3 TB/s; with
 // streaming loads and stores it was 108.
 //
 // Compact.  Bits of the free pages; running sums of the bits number the free pages below the bound and the used ones above it; then tables, counts, stack and
-// copy list from those numbers.  Three small kernels, one after the other: each needs the whole of the one in front.  200,000 pages 13.4 us, which is their launches and a few
+// copy list from those numbers.  Three small kernels, one after the other: each needs the whole of the one in front.  200,000 pages 13.3 us, which is their launches and a few
 // round trips each.  A small pool is one block's work, in shared memory: 1,000 pages 5 us.
 #include <algorithm>
 
