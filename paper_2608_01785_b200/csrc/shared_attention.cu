@@ -297,6 +297,16 @@ __device__ __noinline__ void rows_alone(const SharedParams& p, int seq, int head
         for (int e = 0; e < 8; ++e) o[h][e] = fmaf(of, x[e], o[h][e]);
       }
     });
+    // (nothing that follows changes rows that are NaN from end to end: those of a whole group, behind such a shared key)
+    bool over = true;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) over &= o[h][e] != o[h][e];
+    unsigned who = __ballot_sync(0xffffffffu, over);
+#pragma unroll
+    for (int n = 16; n >= LANES; n >>= 1) who |= who >> n;           // (the lanes that have the same coordinates of other keys)
+    if ((~who & ((1u << LANES) - 1u)) == 0) break;
   }
 #pragma unroll
   for (int h = 0; h < H; ++h) {
