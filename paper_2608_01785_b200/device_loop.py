@@ -275,11 +275,14 @@ class BeamLoop(DeviceLoop):
 
     def prefill(self, prompts: Sequence[Sequence[int]]) -> None:
         """Begins a run: all prompts as one chunk, each in the first row of its request, then the beams with its n_beams most likely tokens.  Prompts that do not fit leave a
-        status and no beams.  What a run before has left is forgotten; all of its requests have to be finished."""
+        status and no beams.  What a run before has left is forgotten; all of its requests have to be finished, and its status, if it left one, put
+        back to 0."""
         b, lens, n = self._prompt_buffers, [len(p) for p in prompts], self.n_requests
         assert len(lens) == n and min(lens) >= 1 and sum(lens) <= b["tokens"].numel()
         if bool((self.ctx_len != 0).any()):
             raise RuntimeError("requests of a run before still hold tokens: finish them first")
+        if int(self.status) != 0:
+            raise B.HsError(int(self.status), "a run before")
         for t in (self.steps, self.length, self.done, self.q_len):
             t.zero_()
         self.scores.fill_(-math.inf)

@@ -346,3 +346,21 @@ def test_a_pool_that_cannot_shrink_changes_nothing(plain, monkeypatch, keep, ent
     for r in range(3):
         same(loop.hypotheses()[r], search(p[r], 3, 11))
     loop.close()
+
+
+def test_a_run_is_not_begun_under_a_status(plain):
+    """A status that a step has left would keep every further one from doing anything."""
+    p = prompts(20, 40)
+    loop = Loop(DIMS, make_weights(DIMS, device="cpu"), 2, 3, 9, 64, 60, 30)
+    loop.prefill(p)
+    while int(loop.status) == 0:
+        loop.step()
+    loop.finish(torch.ones(2, dtype=torch.int32))
+    with pytest.raises(B.HsError):
+        loop.prefill(p)
+    assert int(loop.free_count) == 9 and loop.ctx_len.tolist() == [0] * 6
+    loop.status.zero_()
+    loop.prefill(p)
+    for r, got in enumerate(loop.hypotheses()):
+        same(got, search(p[r], 3, 1))
+    loop.close()
